@@ -37,7 +37,9 @@
  *    sequence-to-sequence workload, Sec. IV-A; hidden size cout, zero initial state, gates in
  *    the order input, forget, candidate, output): w is [4*cout][cin+cout], row q*cout + j =
  *    gate q of unit j, first the cin input weights, then the cout recurrent ones; b is
- *    [4*cout] (the sum of PyTorch's two bias vectors).
+ *    [4*cout] (the sum of PyTorch's two bias vectors).  Layer norm: w = gamma, b = beta.  Gated:
+ *    w is [2*cout][cin], the cout rows of the gate, to which the activation applies, before the
+ *    cout rows of the other projection; b is [2*cout].
  */
 #ifndef BAPIPE_STAGE_H
 #define BAPIPE_STAGE_H
@@ -71,13 +73,36 @@ typedef enum {
     BAPIPE_LINEAR = 6,       /* y = x W^T + b                                               */
     BAPIPE_SOFTMAX_XENT = 7, /* last layer only: p = softmax(z); loss from labels in bwd    */
     BAPIPE_AVGPOOL2D = 8,    /* mean of k x k windows, stride = k, pad = 0 (k = H: global)  */
-    BAPIPE_LSTM = 9          /* LSTM over the H axis of a (cin, T, 1) tensor -> (cout, T, 1) */
+    BAPIPE_LSTM = 9,         /* LSTM over the H axis of a (cin, T, 1) tensor -> (cout, T, 1) */
+    BAPIPE_LAYERNORM = 10,   /* over the channels of each position, biased variance         */
+    BAPIPE_GATED = 11,       /* act(x Wg^T + bg) * (x Wu^T + bu) at each position           */
+    BAPIPE_DROPOUT = 12      /* y = x / (1 - eps), or 0 with probability eps                */
 } bapipe_layer_kind_t;
+
+/* Activation of BAPIPE_GATED, in its descriptor's kh. */
+typedef enum {
+    BAPIPE_GATE_SIGMOID = 0, /* 1 / (1 + exp(-g))                                           */
+    BAPIPE_GATE_SILU = 1,    /* g / (1 + exp(-g))                                           */
+    BAPIPE_GATE_GELU = 2,    /* g (1 + erf(g / sqrt 2)) / 2                                 */
+    BAPIPE_GATE_RELU = 3     /* max(g, 0)                                                   */
+} bapipe_gate_t;
 
 /* One layer of the stage.  src0/src1: index of the producing layer in the list, -1 = the
  * stage input; producers must precede consumers.  fuse_relu applies max(.,0) to the output
  * of CONV2D / BATCHNORM2D / ADD / LINEAR.  cin/cout: channels (features for LINEAR;
- * BATCHNORM2D needs cin == cout == channels of its input). */
+ * BATCHNORM2D and LAYERNORM need cin == cout == channels of their input; GATED: channels of its
+ * input and of its output).  fuse_relu of LAYERNORM, GATED and DROPOUT must be 0.
+ *
+ * The layers of a transformer's feed-forward sublayer, x + DROPOUT(CONV2D 1x1(GATED(LAYERNORM(x)))),
+ * act on every position (n, h, w) by itself; sequences are (channels, T, 1) tensors as for LSTM.
+ * LAYERNORM: y = w (x - mean) / sqrt(var + eps) + b over the position's cin channels.
+ * GATED: cout units; projections and activation are one kernel.  Both projections are kept per
+ *   in-flight micro-batch, in the storage type; they need to be below 2 GiB.
+ * DROPOUT: eps is the probability of an element to be dropped, 0 <= eps < 1.  The mask is computed
+ *   where it is used and never stored.  Element e = ((n H + h) W + w) C + c of micro-batch m is
+ *   dropped if word e mod 4 of Philox4x32-10 is below 2^32 eps (rounded to nearest); key: the seed,
+ *   low word first; counter: e / 4, layer index + 65536 (stage_index - 1), m, number of the
+ *   mini-batch.  See bapipe_stage_set_dropout. */
 typedef struct {
     int32_t kind;
     int32_t cin, cout;
@@ -199,6 +224,15 @@ int bapipe_stage_backward_static(bapipe_stage_t *st, int mb_id, const void *dy_d
  * bookkeeping.  E_ORDER unless exactly M backwards have run since the last step. */
 int bapipe_stage_step(bapipe_stage_t *st, float lr);
 
+/* Seed of the masks of the stage's DROPOUT layers, and the number of the coming mini-batch, which
+ * every bapipe_stage_step counts up by one (modulo 2^32).  Both are 0 after create.  The same pair
+ * gives the same masks: a program that resumes sets the pair it stopped at; replicas that train on
+ * different data set different seeds.  Seed and number live in device memory, so that forward,
+ * backward and step captured into a graph draw new masks at every replay.  Enqueues on
+ * opts->hip_stream.  E_INVALID if the stage has no DROPOUT layer; E_ORDER unless between
+ * mini-batches (after create or step). */
+int bapipe_stage_set_dropout(bapipe_stage_t *st, uint64_t seed, uint32_t mini_batch);
+
 /* Per-layer profile (Sec. III-A "DNN profile"; Sec. III-B-2 asks for it per batch size, which
  * is the micro_batch the stage was created with).  Runs each layer's forward and backward
  * kernels in isolation on scratch data, `warmup` untimed then `iters` timed repetitions,
@@ -261,8 +295,8 @@ enum {
     BAPIPE_KC_CONV_WGRAD_MFMA = 1,  /* bf16 MFMA wgrad incl. its split-K reduction       */
     BAPIPE_KC_CONV_DIRECT = 2,      /* vector-ALU convolution (fp32 stages, odd channels) */
     BAPIPE_KC_POOL = 3,
-    BAPIPE_KC_BATCHNORM = 4,
-    BAPIPE_KC_ELEMENTWISE = 5,      /* ReLU, add, gradient copies, bias-gradient sums     */
+    BAPIPE_KC_BATCHNORM = 4,        /* and layer norm                                        */
+    BAPIPE_KC_ELEMENTWISE = 5,      /* ReLU, add, dropout, gradient copies, bias-gradient sums, gradients of GATED's projections */
     BAPIPE_KC_COUNT = 6
 };
 int bapipe_stage_kernel_timing(bapipe_stage_t *st, int kernel_class);

@@ -2,6 +2,7 @@
 
 TEST INFRASTRUCTURE ONLY.  Arrays are float64 numpy, activations NCHW."""
 import ctypes as ct
+import math
 import os
 
 import numpy as np
@@ -206,6 +207,86 @@ def linear_wgrad(x, dy, dw, db):
     Out = dy.shape[1]
     assert dw.shape == (Out, In)
     lib().orc_linear_wgrad(_p(x), _p(dy), _p(dw), _p(db), N, In, Out)
+
+
+# Layers that act on every position by itself; x [N][C][H][W]
+def layernorm_fwd(x, gamma, beta, eps):
+    """Returns y, xhat, 1/std (biased variance over the channels of a position)."""
+    x = _f64(x)
+    d = x - x.mean(axis=1, keepdims=True)
+    inv = 1.0 / np.sqrt((d * d).mean(axis=1, keepdims=True) + eps)
+    xhat = d * inv
+    return xhat * gamma[:, None, None] + beta[:, None, None], xhat, inv
+
+
+def layernorm_bwd(xhat, inv, dy, gamma, dgamma, dbeta):
+    """Returns dx; accumulates into dgamma, dbeta."""
+    dgamma += (dy * xhat).sum(axis=(0, 2, 3))
+    dbeta += dy.sum(axis=(0, 2, 3))
+    a = dy * gamma[:, None, None]
+    return inv * (a - a.mean(axis=1, keepdims=True) - xhat * (a * xhat).mean(axis=1, keepdims=True))
+
+
+_erf = np.vectorize(math.erf, otypes=[np.float64])
+
+
+def gate(act, g):
+    """act(g) and its derivative; act: 0 sigmoid, 1 SiLU, 2 GELU, 3 ReLU."""
+    if act == 3:
+        return np.maximum(g, 0.0), (g > 0).astype(np.float64)
+    if act == 2:
+        cdf = 0.5 * (1.0 + _erf(g / np.sqrt(2.0)))
+        return g * cdf, cdf + g * np.exp(-0.5 * g * g) / np.sqrt(2.0 * np.pi)
+    e = np.exp(-np.abs(g))
+    s = np.where(g < 0, e, 1.0) / (1.0 + e)
+    if act == 0:
+        return s, s * (1.0 - s)
+    return g * s, s + g * s * (1.0 - s)
+
+
+def gated_fwd(x, w, b, act):
+    """w [2*F][C], gate rows first.  Returns y [N][F][H][W] and the projections [N][2*F][H][W]."""
+    x = _f64(x)
+    both = np.tensordot(w, x, axes=([1], [1])).transpose(1, 0, 2, 3)
+    if b is not None:
+        both = both + b[:, None, None]
+    F = w.shape[0] // 2
+    return gate(act, both[:, :F])[0] * both[:, F:], both
+
+
+def gated_bwd(x, w, both, act, dy, dw, db, q=lambda a: a):
+    """Returns dx; accumulates into dw, db.  q rounds the gradients of the projections, which are stored."""
+    F = w.shape[0] // 2
+    a, da = gate(act, both[:, :F])
+    D = q(np.concatenate([dy * both[:, F:] * da, dy * a], axis=1))
+    dw += np.tensordot(D, x, axes=([0, 2, 3], [0, 2, 3]))
+    if db is not None:
+        db += D.sum(axis=(0, 2, 3))
+    return np.tensordot(D, w, axes=([1], [0])).transpose(0, 3, 1, 2)
+
+
+def philox4x32(counter, key):
+    """Ten rounds.  counter: uint32 array [..., 4], key: two numbers.  Returns uint32 [..., 4]."""
+    c = [counter[..., i].astype(np.uint64) for i in range(4)]
+    low, w32 = np.uint64(0xFFFFFFFF), np.uint64(32)
+    k = [int(key[0]), int(key[1])]
+    for _ in range(10):
+        a, b = np.uint64(0xD2511F53) * c[0], np.uint64(0xCD9E8D57) * c[2]
+        c = [(b >> w32) ^ c[1] ^ np.uint64(k[0]), b & low, (a >> w32) ^ c[3] ^ np.uint64(k[1]), a & low]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return np.stack(c, axis=-1).astype(np.uint32)
+
+
+def dropout_factor(shape, p, seed, layer, micro_batch, mini_batch):
+    """0 or 1/(1-p) per element of [N][C][H][W]; elements are numbered in NHWC order."""
+    N, C, H, W = shape
+    n, p = N * C * H * W, float(np.float32(p))
+    c = np.zeros(((n + 3) // 4, 4), np.uint32)
+    c[:, 0] = np.arange(len(c))
+    c[:, 1:] = layer, micro_batch, mini_batch
+    words = philox4x32(c, (seed & 0xFFFFFFFF, seed >> 32)).reshape(-1)[:n]
+    keep = words.astype(np.int64) >= min(int(np.floor(p * 2.0 ** 32 + 0.5)), 2 ** 32 - 1)
+    return (keep / (1.0 - p)).reshape(N, H, W, C).transpose(0, 3, 1, 2)
 
 
 def softmax_fwd(z):

@@ -13,7 +13,8 @@ input-gradient contribution in backward and their sum where a tensor feeds two l
 the working copy of conv/linear weight matrices.  Bias, gamma, beta, weight gradients,
 BN statistics, softmax and loss are never rounded.  Inside an LSTM layer the input projection
 of all steps and the pre-activation gradients are stored tensors too (rounded); the cell state
-and the recurrent sums are not.  storage="exact" rounds nothing.
+and the recurrent sums are not.  A gated layer's projections are rounded for the backward pass (its
+output is made of the unrounded ones), and so are their gradients.  storage="exact" rounds nothing.
 """
 import numpy as np
 
@@ -52,6 +53,7 @@ class OracleStage:
         self.trace = None          # set to {} to record, per (mb, layer), the masked output gradient and dx
         self.n_fwd = self.n_bwd = 0
         self.peak_in_flight = 0
+        self.dropout_seed = self.mini_batch = 0        # key and last counter word of the DROPOUT layers' masks
 
     # ---- schedule bookkeeping -------------------------------------------------------
     def _claim(self, mb):
@@ -112,6 +114,16 @@ class OracleStage:
                 y = q(y).reshape(a.shape[0], -1, 1, 1)
             elif k == C.LSTM:
                 y, extra = ops.lstm_fwd(a, q(self.w[i]), self.b[i], round16=self.storage == "bf16")
+            elif k == C.LAYERNORM:
+                y, xhat, inv = ops.layernorm_fwd(a, self.w[i], self.b[i], L["eps"])
+                y, extra = q(y), (xhat, inv)
+            elif k == C.GATED:
+                y, both = ops.gated_fwd(a, q(self.w[i]), self.b[i], L["kh"])
+                y, extra = q(y), q(both)
+            elif k == C.DROPOUT:
+                extra = ops.dropout_factor(a.shape, L["eps"], self.dropout_seed, i + 65536 * (self.stage["stage_index"] - 1), mb,
+                                           self.mini_batch)
+                y = q(a * extra)
             elif k == C.SOFTMAX_XENT:
                 y = ops.softmax_fwd(a.reshape(a.shape[0], -1)).reshape(a.shape)
             else:
@@ -191,6 +203,16 @@ class OracleStage:
                                   round16=self.storage == "bf16")
                 if wants:
                     give(L["src0"], dx)
+            elif k == C.LAYERNORM:
+                dx = ops.layernorm_bwd(*aux[i], g, self.w[i], self.dw[i], self.db[i])
+                if wants:
+                    give(L["src0"], dx)
+            elif k == C.GATED:
+                dx = ops.gated_bwd(a, q(self.w[i]), aux[i], L["kh"], g, self.dw[i], self.db[i], q)
+                if wants:
+                    give(L["src0"], dx)
+            elif k == C.DROPOUT:
+                give(L["src0"], g * aux[i])
             elif k == C.LINEAR:
                 a2 = a.reshape(a.shape[0], -1)
                 g2 = g.reshape(g.shape[0], -1)
@@ -213,6 +235,7 @@ class OracleStage:
                 ops.sgd_step(self.b[i], self.db[i], lr)
                 self.db[i][...] = 0.0
         self.n_fwd = self.n_bwd = 0
+        self.mini_batch = (self.mini_batch + 1) % 2 ** 32
 
     def pool_indices(self, mb, layer):
         return self.stash[mb][2][layer]

@@ -14,6 +14,9 @@ LIB_PATH = os.path.join(_HERE, "libbapipe_stage.so")
 
 OK, E_INVALID, E_SHAPE, E_ORDER, E_OOM, E_DEVICE, E_UNSUPPORTED = range(7)
 STATUS_NAMES = ["OK", "E_INVALID", "E_SHAPE", "E_ORDER", "E_OOM", "E_DEVICE", "E_UNSUPPORTED"]
+(CONV2D, RELU, MAXPOOL2D, BATCHNORM2D, ADD, FLATTEN, LINEAR, SOFTMAX_XENT, AVGPOOL2D, LSTM, LAYERNORM, GATED,
+ DROPOUT) = range(13)
+GATE_SIGMOID, GATE_SILU, GATE_GELU, GATE_RELU = range(4)
 FP32, BF16 = 0, 1
 NCHW, NHWC = 0, 1
 SCHED_1F1B, SCHED_1F1B_SO = 0, 1
@@ -22,7 +25,7 @@ STATIC_SCRATCH_BYTES = 64 << 20
 EXPORTS = [
     "bapipe_stage_create", "bapipe_stage_forward", "bapipe_stage_backward", "bapipe_stage_backward_static",
     "bapipe_stage_set_streams",
-    "bapipe_stage_step",
+    "bapipe_stage_step", "bapipe_stage_set_dropout",
     "bapipe_profile_layers", "bapipe_profile_sweep", "bapipe_stage_set_params", "bapipe_stage_get_params",
     "bapipe_stage_get_grads", "bapipe_stage_get_pool_indices", "bapipe_stage_get_loss",
     "bapipe_stage_stash_bytes", "bapipe_last_error", "bapipe_stage_destroy",
@@ -85,6 +88,7 @@ def load():
     lib.bapipe_stage_backward_static.argtypes = [vp, i32, vp, vp]
     lib.bapipe_stage_set_streams.argtypes = [vp, vp, vp]
     lib.bapipe_stage_step.argtypes = [vp, ct.c_float]
+    lib.bapipe_stage_set_dropout.argtypes = [vp, ct.c_uint64, ct.c_uint32]
     lib.bapipe_profile_layers.argtypes = [vp, i32, i32, ct.POINTER(LayerProfile), i32, ct.POINTER(i32)]
     fp = ct.POINTER(ct.c_float)
     lib.bapipe_stage_set_params.argtypes = [vp, i32, fp, fp]
@@ -182,6 +186,11 @@ def bapipe_stage_set_streams(h, backward_stream, wgrad_stream):
 
 def bapipe_stage_step(h, lr):
     _check(load().bapipe_stage_step(h, lr), h)
+
+
+def bapipe_stage_set_dropout(h, seed, mini_batch=0):
+    """Seed (taken modulo 2^64) of the DROPOUT layers' masks and number of the coming mini-batch (modulo 2^32)."""
+    _check(load().bapipe_stage_set_dropout(h, seed % (1 << 64), mini_batch % (1 << 32)), h)
 
 
 def bapipe_profile_layers(h, warmup, iters, n_layers):

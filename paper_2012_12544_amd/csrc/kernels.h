@@ -196,6 +196,32 @@ hipError_t bn_bwd(int dt, const void *x, const void *dy, const float *gamma, con
                   void *dx, float *dgamma, float *dbeta, GradEpi epi, int rows, int C,
                   void *workspace, hipStream_t s, int pre_chunks = 0);
 
+// ---- layer norm over the C channels of each of `rows` positions (kernels_layernorm.hip); stats: [2][rows] floats (mean, 1/std)
+size_t layernorm_workspace(int rows, int C);
+hipError_t layernorm_fwd(int dt, const void *x, const float *gamma, const float *beta, float eps, void *y, float *stats, int rows, int C,
+                         hipStream_t s);
+// dx may be NULL, or dy
+hipError_t layernorm_bwd(int dt, const void *x, const void *dy, const float *gamma, const float *stats, void *dx, float *dgamma, float *dbeta,
+                         GradEpi epi, int rows, int C, void *workspace, hipStream_t s);
+
+// ---- gated linear layer (kernels_gated.hip): h = act(x Wg^T + bg) (x Wu^T + bu), w [2F][C] with the gate rows first, bias [2F] or NULL
+// P [rows][2F] receives both projections in the storage type and, in gated_grad, the gradient of both, D
+enum { ACT_SIGMOID = 0, ACT_SILU = 1, ACT_GELU = 2, ACT_RELU = 3 };
+hipError_t gated_fwd(int dt, int act, const void *x, const void *w, const float *bias, void *P, void *h, int rows, int C, int F, hipStream_t s);
+hipError_t gated_grad(int dt, int act, const void *dh, void *P, int rows, int F, hipStream_t s);
+// dx = D W (wt: [C][2F]), dw += D^T x, db += column sums of D, of any sizes; even sizes of bf16 have conv_gather_mfma and conv_wgrad_mfma
+hipError_t gated_dgrad_direct(int dt, const void *D, const void *wt, void *dx, GradEpi epi, int rows, int C, int F, hipStream_t s);
+size_t gated_wgrad_direct_workspace(int rows, int C, int F);
+hipError_t gated_wgrad_direct(int dt, const void *x, const void *D, float *dw, float *db, int rows, int C, int F, void *workspace, hipStream_t s);
+
+// ---- dropout (kernels_dropout.hip): y[e] = word(e) >= 2^32 p ? x[e] / (1-p) : 0, or with the gradient epilogue the same of dy
+// state: three device words (seed low, seed high, number of the mini-batch), which the kernel reads
+constexpr int kDropoutState = 3;
+hipError_t dropout(int dt, const void *x, void *y, GradEpi epi, size_t n, float p, const uint32_t *state, uint32_t layer, uint32_t mb,
+                   hipStream_t s);
+hipError_t dropout_set(uint32_t *state, uint64_t seed, uint32_t mini_batch, hipStream_t s);
+hipError_t dropout_next(uint32_t *state, hipStream_t s);      // the next mini-batch
+
 // p = softmax(z) rows of K classes (float out), p2: a second destination
 hipError_t softmax_fwd(int dt, const void *z, float *p, int rows, int K, hipStream_t s, float *p2 = nullptr);
 // dz = scale*(p - onehot), loss[0] = -scale*sum_n log p[n,label]

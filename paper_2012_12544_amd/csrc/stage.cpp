@@ -14,6 +14,7 @@
 //   workspace split-K / column-reduction partials
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
@@ -91,6 +92,7 @@ struct Layer {
     // copy of h that the recurrent products read, the buffer shared by the input projection
     // (forward) and the pre-activation gradients (backward) and the cell-gradient carry
     size_t off_gates = 0, off_cells = 0, off_hs = 0, off_pd = 0, off_dcn = 0;
+    // GATED: the slot keeps both projections, whose gradients take their place (off_pd)
     bool groups = false;                 // its weight gradient may share a launch with others
     // LINEAR, a 1x1 convolution of 1x1 maps, and products that stream their filter (streams_filter), on the MFMA kernels: the copies that forward
     // and input gradient read are kept in panels (GatherConv::wt_panels).  LSTM: of its input block
@@ -156,6 +158,8 @@ struct bapipe_stage {
     int flushed = 0;                         // micro-batches whose deferred weight gradients are already in dw
     std::vector<SgdJob> updates;             // of all layers: an update allocates nothing
     float *losses = nullptr;                 // and, behind them, the tickets of conv_gather_mfma: of the handle's stream, of the backward stream
+    uint32_t *dropout_state = nullptr;       // behind those: seed and mini-batch number of the DROPOUT layers
+    bool has_dropout = false;
     unsigned *tickets = nullptr, *tickets_f = nullptr, *tickets_b = nullptr;      // as work: of the pass being enqueued, of either
     size_t params_bytes = 0, slot_bytes = 0, transient_bytes = 0, grads_bytes = 0, work_bytes = 0;
     size_t flush_bytes = 0;                  // workspace of flush_deferred, whatever part of a mini-batch it finds
@@ -260,9 +264,11 @@ hipError_t sync_streams(bapipe_stage *st)
 
 bool has_params(int kind)
 {
-    return kind == BAPIPE_CONV2D || kind == BAPIPE_LINEAR || kind == BAPIPE_BATCHNORM2D || kind == BAPIPE_LSTM;
+    return kind == BAPIPE_CONV2D || kind == BAPIPE_LINEAR || kind == BAPIPE_BATCHNORM2D || kind == BAPIPE_LSTM || kind == BAPIPE_LAYERNORM ||
+           kind == BAPIPE_GATED;
 }
-bool has_matrix(int kind) { return kind == BAPIPE_CONV2D || kind == BAPIPE_LINEAR || kind == BAPIPE_LSTM; }
+bool has_matrix(int kind) { return kind == BAPIPE_CONV2D || kind == BAPIPE_LINEAR || kind == BAPIPE_LSTM || kind == BAPIPE_GATED; }
+bool is_norm(int kind) { return kind == BAPIPE_BATCHNORM2D || kind == BAPIPE_LAYERNORM; }
 
 GatherConv fwd_geom(const bapipe_stage *st, const Layer &L)
 {
@@ -281,6 +287,13 @@ GatherConv fwd_geom(const bapipe_stage *st, const Layer &L)
     }
     g.Hi = A.H; g.Wi = A.W; g.Ci = A.Cp;
     g.Ho = O.H; g.Wo = O.W; g.Co = O.C;
+    if (L.d.kind == BAPIPE_GATED) {              // both projections at every position
+        g.Co = 2 * L.d.cout;
+        g.R = g.S = 1;
+        g.s_out = g.s_in = 1;
+        g.pad_h = g.pad_w = 0;
+        return g;
+    }
     g.R = L.d.kh; g.S = L.d.kw;
     g.s_out = L.d.stride; g.s_in = 1;
     g.pad_h = g.pad_w = L.d.pad;
@@ -348,6 +361,10 @@ void to_internal(const Layer &L, const float *src, float *dst)
         }
         return;
     }
+    if (L.d.kind == BAPIPE_GATED) {
+        memcpy(dst, src, sizeof(float) * L.w_elems);
+        return;
+    }
     if (L.d.kind == BAPIPE_LINEAR) {
         const int In = L.d.cin;
         if (!L.permute_in) {
@@ -380,6 +397,10 @@ void from_internal(const Layer &L, const float *src, float *dst)
             memcpy(dst + (size_t)k * (In + H), src + (size_t)k * In, sizeof(float) * In);
             memcpy(dst + (size_t)k * (In + H) + In, src + (size_t)G * In + (size_t)k * H, sizeof(float) * H);
         }
+        return;
+    }
+    if (L.d.kind == BAPIPE_GATED) {
+        memcpy(dst, src, sizeof(float) * L.w_elems);
         return;
     }
     if (L.d.kind == BAPIPE_LINEAR) {
@@ -415,6 +436,7 @@ hipError_t refresh_transposed(bapipe_stage *st, Layer &L)
         if (e != hipSuccess) return e;
         return make_dgrad_filter(st->dt, L.w + (size_t)G * In, (char *)L.w_t + (size_t)G * In * es, G, 1, 1, H, st->stream);
     }
+    if (L.d.kind == BAPIPE_GATED) return make_dgrad_filter(st->dt, L.w, L.w_t, 2 * L.d.cout, 1, 1, L.cin_p, st->stream);
     int R = L.d.kind == BAPIPE_LINEAR ? 1 : L.d.kh, S = L.d.kind == BAPIPE_LINEAR ? 1 : L.d.kw;
     return make_dgrad_filter(st->dt, L.w, L.w_t, L.d.cout, R, S, L.cin_p, st->stream, L.wt_panels);
 }
@@ -433,6 +455,10 @@ void update_jobs(const bapipe_stage *st, const Layer &L, std::vector<SgdJob> &jo
         const size_t at = (size_t)G * In, es = dt_size(st->dt);
         jobs.push_back({L.w, L.dw, L.w_work, L.w_t, b, L.db, G, 1, In, L.w_panels, L.wt_panels});
         jobs.push_back({L.w + at, L.dw + at, (char *)L.w_work + at * es, (char *)L.w_t + at * es, nullptr, nullptr, G, 1, H, false, false});
+        return;
+    }
+    if (L.d.kind == BAPIPE_GATED) {
+        jobs.push_back({L.w, L.dw, L.w_work, L.w_t, b, L.db, 2 * L.d.cout, 1, L.cin_p, false, false});
         return;
     }
     const int RS = L.d.kind == BAPIPE_LINEAR ? 1 : L.d.kh * L.d.kw;
@@ -593,6 +619,11 @@ const void *in_ptr(bapipe_stage *st, int t, const FwdCtx &c)
     return st->tptr(t, c.mbid);
 }
 
+// DROPOUT layers of different stages of a pipeline draw differently under one seed
+uint32_t dropout_layer(const bapipe_stage *st, int li) { return (uint32_t)li + 65536u * (uint32_t)(st->opts.stage_index - 1); }
+
+int rows_of(const bapipe_stage *st, const Tensor &T) { return st->mb * T.H * T.W; }
+
 int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
 {
     Layer &L = st->layers[li];
@@ -684,6 +715,28 @@ int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
     case BAPIPE_LSTM: {
         int rc = lstm_forward(st, L, a, o, c.mbid);
         if (rc != BAPIPE_OK) return rc;
+        break;
+    }
+    case BAPIPE_LAYERNORM: {
+        const Tensor &A = st->tensors[L.a];
+        const bool tp = st->tap_begin(BAPIPE_KC_BATCHNORM);
+        HIPCHK(layernorm_fwd(dt, a, L.w, L.bias, L.d.eps, o, (float *)(st->slot(c.mbid) + L.aux_off), rows_of(st, A), A.C, s));
+        st->tap_end(tp, 0.0, 2.0 * A.bytes());                                   // read x, write y
+        break;
+    }
+    case BAPIPE_GATED: {
+        const Tensor &A = st->tensors[L.a];
+        const GatherConv g = fwd_geom(st, L);
+        const bool tp = st->tap_begin(dt == DT_BF16 ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
+        HIPCHK(gated_fwd(dt, L.d.kh, a, L.w_work, L.bias, st->slot(c.mbid) + L.off_pd, o, rows_of(st, A), L.d.cin, L.d.cout, s));
+        st->tap_end(tp, conv_flop(g, L.d.cin), (double)A.bytes() + 3.0 * O.bytes() + (double)L.w_elems * dt_size(dt));
+        break;
+    }
+    case BAPIPE_DROPOUT: {
+        GradEpi none{nullptr, 0};
+        const bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
+        HIPCHK(dropout(dt, a, o, none, O.elems, L.d.eps, st->dropout_state, dropout_layer(st, li), c.mbid, s));
+        st->tap_end(tp, 0.0, 2.0 * O.bytes());
         break;
     }
     case BAPIPE_SOFTMAX_XENT:
@@ -923,6 +976,47 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
         if (rc != BAPIPE_OK) return rc;
         break;
     }
+    case BAPIPE_LAYERNORM: {
+        GradEpi e{nullptr, 0};
+        void *dx = nullptr;
+        if (a_grad) {
+            e = epi_for(st, L.a, c);
+            dx = grad_ptr(st, L.a, c);
+        }
+        const bool tp = st->tap_begin(BAPIPE_KC_BATCHNORM);
+        HIPCHK(layernorm_bwd(dt, st->tptr(L.a, c.mbid), grad_ptr(st, L.o, c), L.w, (const float *)(st->slot(c.mbid) + L.aux_off), dx, L.dw, L.db, e,
+                             rows_of(st, A), A.C, st->work, s));
+        st->tap_end(tp, 0.0, (double)A.bytes() * (2.0 + (dx ? 1.0 : 0.0) + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0)));
+        break;
+    }
+    case BAPIPE_GATED: {
+        void *D = st->slot(c.mbid) + L.off_pd;
+        const void *x = st->tptr(L.a, c.mbid);
+        const int rows = rows_of(st, A);
+        const double flop = conv_flop(fwd_geom(st, L), L.d.cin), wbytes = (double)L.w_elems;
+        bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
+        HIPCHK(gated_grad(dt, L.d.kh, grad_ptr(st, L.o, c), D, rows, L.d.cout, s));
+        st->tap_end(tp, 0.0, 5.0 * O.bytes());
+        const int direct = dt == DT_BF16 ? BAPIPE_KC_CONV_WGRAD_MFMA : BAPIPE_KC_CONV_DIRECT;
+        tp = st->tap_begin(direct);
+        HIPCHK(gated_wgrad_direct(dt, x, D, L.dw, L.db, rows, L.d.cin, L.d.cout, st->work, s));
+        st->tap_end(tp, flop, (double)A.bytes() + 2.0 * O.bytes() + 8.0 * wbytes);
+        if (a_grad) {
+            GradEpi e = epi_for(st, L.a, c);
+            tp = st->tap_begin(dt == DT_BF16 ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
+            HIPCHK(gated_dgrad_direct(dt, D, L.w_t, grad_ptr(st, L.a, c), e, rows, L.d.cin, L.d.cout, s));
+            st->tap_end(tp, flop, 2.0 * O.bytes() + wbytes * dt_size(dt) + (double)A.bytes() * (1.0 + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0)));
+        }
+        break;
+    }
+    case BAPIPE_DROPOUT:
+        if (a_grad) {
+            GradEpi e = epi_for(st, L.a, c);
+            const bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
+            HIPCHK(dropout(dt, grad_ptr(st, L.o, c), grad_ptr(st, L.a, c), e, O.elems, L.d.eps, st->dropout_state, dropout_layer(st, li), c.mbid, s));
+            st->tap_end(tp, 0.0, (double)O.bytes() * (2.0 + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0)));
+        }
+        break;
     case BAPIPE_SOFTMAX_XENT:
         if (a_grad) {
             c.written[A.root] = 1;
@@ -1131,6 +1225,34 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
             L.b_elems = d.has_bias ? (size_t)4 * d.cout : 0;
             break;
         }
+        case BAPIPE_LAYERNORM:
+            if (d.cin != A.C || d.cout != A.C) return create_fail(BAPIPE_E_SHAPE, "layer %d: layer norm over %d channels, input has %d", i, d.cin, A.C);
+            if (!(d.eps > 0.f) || d.eps > FLT_MAX) return create_fail(BAPIPE_E_INVALID, "layer %d: eps must be positive", i);
+            if (d.fuse_relu) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: layer norm has no fused ReLU", i);
+            O.C = A.C; O.H = A.H; O.W = A.W;
+            L.w_elems = A.C; L.b_elems = A.C;
+            break;
+        case BAPIPE_GATED:
+            if (d.cin <= 0 || d.cout <= 0 || d.cout > (1 << 29)) return create_fail(BAPIPE_E_INVALID, "layer %d: bad gated parameters", i);
+            if (d.kh < BAPIPE_GATE_SIGMOID || d.kh > BAPIPE_GATE_RELU) return create_fail(BAPIPE_E_INVALID, "layer %d: unknown activation %d", i, d.kh);
+            if (A.C != d.cin) return create_fail(BAPIPE_E_SHAPE, "layer %d: cin=%d but input has %d channels", i, d.cin, A.C);
+            if (d.fuse_relu) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: a gated layer has no fused ReLU", i);
+            if (A.Cp != A.C) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: gated input with padded channels", i);
+            if ((size_t)micro_batch * A.H * A.W * 2 * d.cout * es >= ((size_t)1 << 31))
+                return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: projections of 2 GiB or more per micro-batch", i);
+            O.C = d.cout; O.H = A.H; O.W = A.W;
+            L.cin_p = A.Cp;
+            L.w_elems = (size_t)2 * d.cout * d.cin;
+            L.b_elems = d.has_bias ? (size_t)2 * d.cout : 0;
+            break;
+        case BAPIPE_DROPOUT:
+            if (!(d.eps >= 0.f && d.eps < 1.f)) return create_fail(BAPIPE_E_INVALID, "layer %d: dropout needs 0 <= eps < 1, the share it drops", i);
+            if (d.fuse_relu) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: dropout has no fused ReLU", i);
+            if (n_layers > 65536 || opts->n_stages > 65536)      // both number the masks, in 16 bits each
+                return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: dropout among more than 65536 layers or stages", i);
+            O.C = A.C; O.H = A.H; O.W = A.W;
+            st->has_dropout = true;
+            break;
         case BAPIPE_RELU:
             O.C = A.C; O.H = A.H; O.W = A.W;
             break;
@@ -1230,7 +1352,7 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         const Layer &L = st->layers[i];
         Tensor &RA = st->tensors[root_of(L.a)];
         switch (L.d.kind) {
-        case BAPIPE_CONV2D: case BAPIPE_LINEAR: case BAPIPE_BATCHNORM2D: case BAPIPE_LSTM:
+        case BAPIPE_CONV2D: case BAPIPE_LINEAR: case BAPIPE_BATCHNORM2D: case BAPIPE_LSTM: case BAPIPE_LAYERNORM: case BAPIPE_GATED:
             RA.stashed = true;
             break;
         case BAPIPE_RELU: case BAPIPE_SOFTMAX_XENT:
@@ -1305,6 +1427,18 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         if (L.d.kind == BAPIPE_BATCHNORM2D) {
             L.aux_off = slot; L.aux_bytes = 2 * sizeof(float) * A.C; slot += align_up(L.aux_bytes);
             size_t w = bn_workspace(micro_batch * A.H * A.W, A.C);
+            work = w > work ? w : work;
+        }
+        if (L.d.kind == BAPIPE_LAYERNORM) {
+            const int rows = rows_of(st, A);
+            L.aux_off = slot; L.aux_bytes = 2 * sizeof(float) * (size_t)rows; slot += align_up(L.aux_bytes);
+            const size_t w = layernorm_workspace(rows, A.C);
+            work = w > work ? w : work;
+        }
+        if (L.d.kind == BAPIPE_GATED) {
+            const int rows = rows_of(st, A);
+            L.aux_off = L.off_pd = slot; L.aux_bytes = (size_t)rows * 2 * L.d.cout * es; slot += align_up(L.aux_bytes);
+            const size_t w = gated_wgrad_direct_workspace(rows, L.d.cin, L.d.cout);
             work = w > work ? w : work;
         }
         if (L.d.kind == BAPIPE_LSTM) {
@@ -1461,12 +1595,13 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
     st->grads = (char *)st->dev_alloc(st->grads_bytes);
     st->work = (char *)st->dev_alloc(st->flush_bytes);       // the handle's own; a pass on another stream or the static array needs work_bytes
     const size_t loss_words = align_up(sizeof(float) * n_micro) / sizeof(float);
-    st->losses = (float *)st->dev_alloc(sizeof(float) * (loss_words + 2 * kGatherTickets));
+    st->losses = (float *)st->dev_alloc(sizeof(float) * (loss_words + 2 * kGatherTickets + kDropoutState));
     if (defb) st->deferred = (char *)st->dev_alloc(defb);
     st->stream_f = st->stream;
     st->work_f = st->work;
     st->tickets = st->tickets_f = (unsigned *)(st->losses + loss_words);
     st->tickets_b = st->tickets_f + kGatherTickets;
+    st->dropout_state = (uint32_t *)(st->tickets_b + kGatherTickets);
     if (!st->params || !st->stash || !st->transient || !st->grads || !st->work || !st->losses || (defb && !st->deferred))
         return create_fail(BAPIPE_E_OOM, "device allocation failed (params %zu, stash %zu x %d, transient %zu, grads %zu, work %zu bytes)",
                            st->params_bytes, st->slot_bytes, st->depth, st->transient_bytes, st->grads_bytes, st->flush_bytes);
@@ -1490,14 +1625,14 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         L.w = (float *)(st->params + o_w[i]);
         L.dw = (float *)(st->params + o_dw[i]);
         if (L.b_elems) { L.bias = (float *)(st->params + o_b[i]); L.db = (float *)(st->params + o_db[i]); }
-        if (L.d.kind != BAPIPE_BATCHNORM2D) { L.w_work = st->params + o_ww[i]; L.w_t = st->params + o_wt[i]; }
+        if (has_matrix(L.d.kind)) { L.w_work = st->params + o_ww[i]; L.w_t = st->params + o_wt[i]; }
         update_jobs(st, L, st->updates);
     }
     // parameters start at zero (gamma at one); all of it through kernels on the stage's stream
     hipError_t e = fill_f32((float *)st->params, 0.f, st->params_bytes / 4, st->stream);
     for (int i = 0; i < n_layers && e == hipSuccess; ++i)
-        if (st->layers[i].d.kind == BAPIPE_BATCHNORM2D) e = fill_f32(st->layers[i].w, 1.f, st->layers[i].w_elems, st->stream);
-    if (e == hipSuccess) e = fill_f32(st->losses, 0.f, loss_words + 2 * kGatherTickets, st->stream);
+        if (is_norm(st->layers[i].d.kind)) e = fill_f32(st->layers[i].w, 1.f, st->layers[i].w_elems, st->stream);
+    if (e == hipSuccess) e = fill_f32(st->losses, 0.f, loss_words + 2 * kGatherTickets + kDropoutState, st->stream);
     if (e == hipSuccess) e = hipStreamSynchronize(st->stream);
     if (e != hipSuccess) return create_fail(BAPIPE_E_DEVICE, "initialisation: %s", hipGetErrorString(e));
     guard.s = nullptr;
@@ -1711,8 +1846,19 @@ int bapipe_stage_step(bapipe_stage_t *st, float lr)
         if (rc != BAPIPE_OK) return rc;
     }
     HIPCHK(sgd_update(st->dt, st->updates.data(), (int)st->updates.size(), lr, st->stream));
+    if (st->has_dropout) HIPCHK(dropout_next(st->dropout_state, st->stream));
     st->n_fwd = st->n_bwd = 0;
     st->flushed = 0;
+    return BAPIPE_OK;
+}
+
+int bapipe_stage_set_dropout(bapipe_stage_t *st, uint64_t seed, uint32_t mini_batch)
+{
+    if (!st) return BAPIPE_E_INVALID;
+    if (!st->has_dropout) return st->fail(BAPIPE_E_INVALID, "set_dropout: the stage has no DROPOUT layer");
+    if (st->n_fwd != 0 || st->n_bwd != 0)
+        return st->fail(BAPIPE_E_ORDER, "set_dropout: only between mini-batches (after create or step)");
+    HIPCHK(dropout_set(st->dropout_state, seed, mini_batch, st->stream));
     return BAPIPE_OK;
 }
 
@@ -1724,7 +1870,7 @@ int bapipe_stage_set_params(bapipe_stage_t *st, int layer, const float *w_host, 
     Layer &L = st->layers[layer];
     HIPCHK(sync_streams(st));
     if (w_host) {
-        if (L.d.kind == BAPIPE_BATCHNORM2D) {
+        if (is_norm(L.d.kind)) {
             HIPCHK(hipMemcpy(L.w, w_host, L.w_elems * 4, hipMemcpyHostToDevice));
         } else {
             std::vector<float> tmp(L.w_elems);
@@ -1754,7 +1900,7 @@ static int get_vectors(bapipe_stage_t *st, int layer, float *w_host, float *b_ho
     HIPCHK(sync_streams(st));
     if (w_host) {
         const float *src = grads ? L.dw : L.w;
-        if (L.d.kind == BAPIPE_BATCHNORM2D) {
+        if (is_norm(L.d.kind)) {
             HIPCHK(hipMemcpy(w_host, src, L.w_elems * 4, hipMemcpyDeviceToHost));
         } else {
             std::vector<float> tmp(L.w_elems);

@@ -11,9 +11,11 @@ A layer is a dict with the integer fields of the C descriptor:
 `src0`/`src1` name the producing layer (index in the list), -1 = stage input.
 """
 
-CONV2D, RELU, MAXPOOL2D, BATCHNORM2D, ADD, FLATTEN, LINEAR, SOFTMAX_XENT, AVGPOOL2D, LSTM = range(10)
+(CONV2D, RELU, MAXPOOL2D, BATCHNORM2D, ADD, FLATTEN, LINEAR, SOFTMAX_XENT, AVGPOOL2D, LSTM, LAYERNORM, GATED,
+ DROPOUT) = range(13)
 KIND_NAMES = ["conv2d", "relu", "maxpool2d", "batchnorm2d", "add", "flatten",
-              "linear", "softmax_xent", "avgpool2d", "lstm"]
+              "linear", "softmax_xent", "avgpool2d", "lstm", "layernorm", "gated", "dropout"]
+GATE_SIGMOID, GATE_SILU, GATE_GELU, GATE_RELU = range(4)
 
 FP32, BF16 = 0, 1
 SCHED_1F1B, SCHED_1F1B_SO = 0, 1
@@ -67,6 +69,18 @@ class _Builder:
     def lstm(self, cin, hidden, src=None):
         """LSTM over the H axis of a (cin, T, 1) tensor -> (hidden, T, 1); w [4*hidden][cin+hidden]."""
         return self.add(kind=LSTM, cin=cin, cout=hidden, has_bias=1, src0=src)
+
+    def layernorm(self, c, eps=1e-5, src=None):
+        return self.add(kind=LAYERNORM, cin=c, cout=c, has_bias=1, eps=eps, src0=src)
+
+    def gated(self, cin, units, act=GATE_SILU, bias=0, src=None):
+        """act(x Wg^T + bg) * (x Wu^T + bu) at every position; w [2*units][cin].  The descriptor's kh is the activation."""
+        i = self.add(kind=GATED, cin=cin, cout=units, has_bias=bias, src0=src)
+        self.layers[i]["kh"] = act
+        return i
+
+    def dropout(self, p, src=None):
+        return self.add(kind=DROPOUT, eps=p, src0=src)
 
     def xent(self, src=None):
         return self.add(kind=SOFTMAX_XENT, src0=src)
@@ -299,8 +313,11 @@ def infer_shapes(stage):
             ho = (s[1] + 2 * L["pad"] - L["kh"]) // L["stride"] + 1
             wo = (s[2] + 2 * L["pad"] - L["kw"]) // L["stride"] + 1
             o = (s[0], ho, wo)
-        elif k in (RELU, BATCHNORM2D, SOFTMAX_XENT):
+        elif k in (RELU, BATCHNORM2D, SOFTMAX_XENT, LAYERNORM, DROPOUT):
             o = s
+        elif k == GATED:
+            assert s[0] == L["cin"], (idx, s, L)
+            o = (L["cout"], s[1], s[2])
         elif k == ADD:
             s1 = inp if L["src1"] < 0 else shapes[L["src1"]]
             assert s == s1, (idx, s, s1)
@@ -320,7 +337,7 @@ def infer_shapes(stage):
 
 
 def conv_fc_macs_per_sample(stage):
-    """Forward multiply-accumulates per sample over CONV2D, LINEAR and LSTM layers."""
+    """Forward multiply-accumulates per sample over CONV2D, LINEAR, LSTM and GATED layers."""
     shapes = infer_shapes(stage)
     total = 0
     per_layer = []
@@ -332,6 +349,8 @@ def conv_fc_macs_per_sample(stage):
             m = L["cin"] * L["cout"]
         elif L["kind"] == LSTM:
             m = o[1] * 4 * L["cout"] * (L["cin"] + L["cout"])
+        elif L["kind"] == GATED:
+            m = o[1] * o[2] * 2 * L["cin"] * L["cout"]
         per_layer.append(m)
         total += m
     return total, per_layer

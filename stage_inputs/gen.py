@@ -62,7 +62,8 @@ def layer_params(stage, idx, perturb=False):
     conv: Kaiming-normal std sqrt(2/fan_in), fan_in = cin*kh*kw ('kaiming' stages) ;
     linear: Xavier-uniform bound sqrt(6/(fan_in+fan_out)) ('xavier' stages) ;
     lstm: w [4*hidden][cin+hidden] and (perturbed) bias uniform in +-1/sqrt(hidden) ;
-    batchnorm: w = gamma = 1, b = beta = 0 ; biases 0.
+    gated: w [2*cout][cin], as conv or linear ;
+    batchnorm, layernorm: w = gamma = 1, b = beta = 0 ; biases 0.
     perturb=True draws biases/beta ~ 0.1*N(0,1) and gamma ~ 1 + 0.1*N(0,1) instead, so that
     tests can see a dropped bias or scale term."""
     L = stage["layers"][idx]
@@ -84,7 +85,10 @@ def layer_params(stage, idx, perturb=False):
         if perturb:
             b = rb.uniform(-bound, bound, size=4 * hd).astype(np.float32)
         return w, b
-    elif k == C.BATCHNORM2D:
+    elif k == C.GATED:
+        shp = (2 * L["cout"], L["cin"])
+        fan_in, fan_out = L["cin"], 2 * L["cout"]
+    elif k in (C.BATCHNORM2D, C.LAYERNORM):
         g = np.ones(L["cout"], np.float32)
         b = np.zeros(L["cout"], np.float32)
         if perturb:
@@ -100,9 +104,9 @@ def layer_params(stage, idx, perturb=False):
         w = (r.standard_normal(shp, dtype=np.float32) * np.float32(np.sqrt(2.0 / fan_in)))
     b = None
     if L["has_bias"]:
-        b = np.zeros(L["cout"], np.float32)
+        b = np.zeros(shp[0], np.float32)
         if perturb:
-            b = (0.1 * rb.standard_normal(L["cout"])).astype(np.float32)
+            b = (0.1 * rb.standard_normal(shp[0])).astype(np.float32)
     return w.astype(np.float32), b
 
 
