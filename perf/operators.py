@@ -204,7 +204,7 @@ def _run_own(s):
             B.bapipe_stage_backward(s.handle, m, s.dy[m].data_ptr(), s.dx[m].data_ptr())
     out = {"y": s.y, "dx": s.dx}
     if s.params:
-        grads = s.accumulators.to(_torch_dtype(s.case))          # the update clears them
+        grads = s.accumulators.to(_torch_dtype(s.case), copy=True)          # the update clears them
     B.bapipe_stage_step(s.handle, LR)
     for n, v in s.params.items():
         at = s.at[n]
