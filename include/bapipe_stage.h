@@ -97,7 +97,8 @@ typedef enum {
  * act on every position (n, h, w) by itself; sequences are (channels, T, 1) tensors as for LSTM.
  * LAYERNORM: y = w (x - mean) / sqrt(var + eps) + b over the position's cin channels.
  * GATED: cout units; projections and activation are one kernel.  Both projections are kept per
- *   in-flight micro-batch, in the storage type; they need to be below 2 GiB.
+ *   in-flight micro-batch, as floats; in the storage type, as which their gradients are stored, they
+ *   need to be below 2 GiB.
  * DROPOUT: eps is the probability of an element to be dropped, 0 <= eps < 1.  The mask is computed
  *   where it is used and never stored.  Element e = ((n H + h) W + w) C + c of micro-batch m is
  *   dropped if word e mod 4 of Philox4x32-10 is below 2^32 eps (rounded to nearest); key: the seed,

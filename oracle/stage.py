@@ -13,8 +13,7 @@ input-gradient contribution in backward and their sum where a tensor feeds two l
 the working copy of conv/linear weight matrices.  Bias, gamma, beta, weight gradients,
 BN statistics, softmax and loss are never rounded.  Inside an LSTM layer the input projection
 of all steps and the pre-activation gradients are stored tensors too (rounded); the cell state
-and the recurrent sums are not.  A gated layer's projections are rounded for the backward pass (its
-output is made of the unrounded ones), and so are their gradients.  storage="exact" rounds nothing.
+and the recurrent sums are not.  A gated layer's projections are not rounded, their gradients are.  storage="exact" rounds nothing.
 """
 import numpy as np
 
@@ -119,7 +118,7 @@ class OracleStage:
                 y, extra = q(y), (xhat, inv)
             elif k == C.GATED:
                 y, both = ops.gated_fwd(a, q(self.w[i]), self.b[i], L["kh"])
-                y, extra = q(y), q(both)
+                y, extra = q(y), both
             elif k == C.DROPOUT:
                 extra = ops.dropout_factor(a.shape, L["eps"], self.dropout_seed, i + 65536 * (self.stage["stage_index"] - 1), mb,
                                            self.mini_batch)

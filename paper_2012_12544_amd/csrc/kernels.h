@@ -205,13 +205,17 @@ hipError_t layernorm_bwd(int dt, const void *x, const void *dy, const float *gam
                          GradEpi epi, int rows, int C, void *workspace, hipStream_t s);
 
 // ---- gated linear layer (kernels_gated.hip): h = act(x Wg^T + bg) (x Wu^T + bu), w [2F][C] with the gate rows first, bias [2F] or NULL
-// P [rows][2F] receives both projections in the storage type and, in gated_grad, the gradient of both, D
+// P [rows][2F] receives both projections (float), which gated_grad takes with dh to their gradients D [rows][2F] (storage type)
 enum { ACT_SIGMOID = 0, ACT_SILU = 1, ACT_GELU = 2, ACT_RELU = 3 };
-hipError_t gated_fwd(int dt, int act, const void *x, const void *w, const float *bias, void *P, void *h, int rows, int C, int F, hipStream_t s);
-hipError_t gated_grad(int dt, int act, const void *dh, void *P, int rows, int F, hipStream_t s);
-// dx = D W (wt: [C][2F]), dw += D^T x, db += column sums of D, of any sizes; even sizes of bf16 have conv_gather_mfma and conv_wgrad_mfma
+// whether the products take the bf16 MFMA kernels: conv_gather_mfma for dx = D W (wt: [C][2F]), conv_wgrad_mfma for dw += D^T x, with db
+bool gated_mfma(int dt, int rows, int C, int F);
+size_t gated_workspace(int dt, int rows, int C, int F);       // of the calls here
+// panels: w is kept in panels (GatherConv::wt_panels), for gated_mfma only
+hipError_t gated_fwd(int dt, int act, const void *x, const void *w, const float *bias, float *P, void *h, int rows, int C, int F, bool panels,
+                     void *workspace, hipStream_t s);
+hipError_t gated_grad(int dt, int act, const void *dh, const float *P, void *D, int rows, int F, hipStream_t s);
+// the other two products where gated_mfma says no
 hipError_t gated_dgrad_direct(int dt, const void *D, const void *wt, void *dx, GradEpi epi, int rows, int C, int F, hipStream_t s);
-size_t gated_wgrad_direct_workspace(int rows, int C, int F);
 hipError_t gated_wgrad_direct(int dt, const void *x, const void *D, float *dw, float *db, int rows, int C, int F, void *workspace, hipStream_t s);
 
 // ---- dropout (kernels_dropout.hip): y[e] = word(e) >= 2^32 p ? x[e] / (1-p) : 0, or with the gradient epilogue the same of dy

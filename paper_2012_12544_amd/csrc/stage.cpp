@@ -92,7 +92,9 @@ struct Layer {
     // copy of h that the recurrent products read, the buffer shared by the input projection
     // (forward) and the pre-activation gradients (backward) and the cell-gradient carry
     size_t off_gates = 0, off_cells = 0, off_hs = 0, off_pd = 0, off_dcn = 0;
-    // GATED: the slot keeps both projections, whose gradients take their place (off_pd)
+    // GATED: the slot keeps both projections (off_pd, float); their gradients have a place among the gradients (off_d)
+    size_t off_d = 0;
+    bool mfma = false;                   // its products run on the bf16 MFMA kernels
     bool groups = false;                 // its weight gradient may share a launch with others
     // LINEAR, a 1x1 convolution of 1x1 maps, and products that stream their filter (streams_filter), on the MFMA kernels: the copies that forward
     // and input gradient read are kept in panels (GatherConv::wt_panels).  LSTM: of its input block
@@ -287,11 +289,14 @@ GatherConv fwd_geom(const bapipe_stage *st, const Layer &L)
     }
     g.Hi = A.H; g.Wi = A.W; g.Ci = A.Cp;
     g.Ho = O.H; g.Wo = O.W; g.Co = O.C;
-    if (L.d.kind == BAPIPE_GATED) {              // both projections at every position
+    if (L.d.kind == BAPIPE_GATED) {              // both projections at every position, each a map of one pixel
+        g.N = st->mb * A.H * A.W;
+        g.Hi = g.Wi = g.Ho = g.Wo = 1;
         g.Co = 2 * L.d.cout;
         g.R = g.S = 1;
         g.s_out = g.s_in = 1;
         g.pad_h = g.pad_w = 0;
+        g.wt_panels = L.w_panels;
         return g;
     }
     g.R = L.d.kh; g.S = L.d.kw;
@@ -436,7 +441,7 @@ hipError_t refresh_transposed(bapipe_stage *st, Layer &L)
         if (e != hipSuccess) return e;
         return make_dgrad_filter(st->dt, L.w + (size_t)G * In, (char *)L.w_t + (size_t)G * In * es, G, 1, 1, H, st->stream);
     }
-    if (L.d.kind == BAPIPE_GATED) return make_dgrad_filter(st->dt, L.w, L.w_t, 2 * L.d.cout, 1, 1, L.cin_p, st->stream);
+    if (L.d.kind == BAPIPE_GATED) return make_dgrad_filter(st->dt, L.w, L.w_t, 2 * L.d.cout, 1, 1, L.cin_p, st->stream, L.wt_panels);
     int R = L.d.kind == BAPIPE_LINEAR ? 1 : L.d.kh, S = L.d.kind == BAPIPE_LINEAR ? 1 : L.d.kw;
     return make_dgrad_filter(st->dt, L.w, L.w_t, L.d.cout, R, S, L.cin_p, st->stream, L.wt_panels);
 }
@@ -458,7 +463,7 @@ void update_jobs(const bapipe_stage *st, const Layer &L, std::vector<SgdJob> &jo
         return;
     }
     if (L.d.kind == BAPIPE_GATED) {
-        jobs.push_back({L.w, L.dw, L.w_work, L.w_t, b, L.db, 2 * L.d.cout, 1, L.cin_p, false, false});
+        jobs.push_back({L.w, L.dw, L.w_work, L.w_t, b, L.db, 2 * L.d.cout, 1, L.cin_p, L.w_panels, L.wt_panels});
         return;
     }
     const int RS = L.d.kind == BAPIPE_LINEAR ? 1 : L.d.kh * L.d.kw;
@@ -727,9 +732,11 @@ int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
     case BAPIPE_GATED: {
         const Tensor &A = st->tensors[L.a];
         const GatherConv g = fwd_geom(st, L);
-        const bool tp = st->tap_begin(dt == DT_BF16 ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
-        HIPCHK(gated_fwd(dt, L.d.kh, a, L.w_work, L.bias, st->slot(c.mbid) + L.off_pd, o, rows_of(st, A), L.d.cin, L.d.cout, s));
-        st->tap_end(tp, conv_flop(g, L.d.cin), (double)A.bytes() + 3.0 * O.bytes() + (double)L.w_elems * dt_size(dt));
+        const bool tp = st->tap_begin(L.mfma ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
+        HIPCHK(gated_fwd(dt, L.d.kh, a, L.w_work, L.bias, (float *)(st->slot(c.mbid) + L.off_pd), o, rows_of(st, A), L.d.cin, L.d.cout, L.w_panels,
+                         st->work, s));
+        // x and the weights read, h and both projections (float) written
+        st->tap_end(tp, conv_flop(g, L.d.cin), (double)A.bytes() + O.bytes() + 8.0 * O.elems + (double)L.w_elems * dt_size(dt));
         break;
     }
     case BAPIPE_DROPOUT: {
@@ -819,6 +826,25 @@ int run_waiting_wgrads(bapipe_stage *st, hipStream_t s, char *work)
     return BAPIPE_OK;
 }
 
+// Runs a weight gradient, or leaves it to wait for others.  a_grad: the pass goes on with an input gradient; now: it does not wait
+int give_wgrad(bapipe_stage *st, const WgradLaunch &w, bool mf, bool a_grad, bool now)
+{
+    // a layer without an input gradient ends the pass's kernel chain: its weight gradient would only delay
+    // the end of the pass from the other stream
+    const double us = w.flop / kForkFlopPerUs + w.bytes / kForkBytesPerUs;
+    const bool small = w.layer->groups && (!mf || us < kGroupUs);
+    if (now || !(small || (mf && st->stream_w && a_grad))) return run_wgrad(st, w, mf, st->stream, st->work);
+    st->w_waiting.push_back(w);
+    st->w_waiting_us += us;
+    if (mf && st->stream_w && a_grad && st->w_waiting_us >= kForkUs) {    // what waits is complete on the backward stream at this point
+        HIPCHK(hipEventRecord(st->ev_g, st->stream));
+        HIPCHK(hipStreamWaitEvent(st->stream_w, st->ev_g, 0));
+        st->w_used = true;
+        return run_waiting_wgrads(st, st->stream_w, st->work_w);
+    }
+    return BAPIPE_OK;
+}
+
 int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
 {
     Layer &L = st->layers[li];
@@ -840,29 +866,11 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
             if (x != xk) HIPCHK(hipMemcpyAsync(xk, x, L.def_x_bytes, hipMemcpyDeviceToDevice, s));
             if (g != gk) HIPCHK(hipMemcpyAsync(gk, g, L.def_g_bytes, hipMemcpyDeviceToDevice, s));
         } else {
-            const bool mf = use_mfma_wgrad(st, cs);
             // the bias gradient rides along in either, and in the deferred GEMM; x, dy read, fp32 dw read and written
             const WgradLaunch w{x, g, &L, cs, flop, (double)A.bytes() + O.bytes() + 8.0 * L.w_elems};
-            // a layer without an input gradient ends the pass's kernel chain: its weight gradient would only delay
-            // the end of the pass from the other stream
-            const double us = w.flop / kForkFlopPerUs + w.bytes / kForkBytesPerUs;
-            const bool small = L.groups && (!mf || us < kGroupUs);
             // the caller's dy is read before dx may be stored over it
-            const bool now = c.dx_over_dy && g == c.dy_direct;
-            if (!c.profiling && !now && (small || (mf && st->stream_w && a_grad))) {
-                st->w_waiting.push_back(w);
-                st->w_waiting_us += us;
-                if (mf && st->stream_w && a_grad && st->w_waiting_us >= kForkUs) {    // what waits is complete on the backward stream at this point
-                    HIPCHK(hipEventRecord(st->ev_g, s));
-                    HIPCHK(hipStreamWaitEvent(st->stream_w, st->ev_g, 0));
-                    st->w_used = true;
-                    const int rc = run_waiting_wgrads(st, st->stream_w, st->work_w);
-                    if (rc != BAPIPE_OK) return rc;
-                }
-            } else {
-                const int rc = run_wgrad(st, w, mf, s, st->work);
-                if (rc != BAPIPE_OK) return rc;
-            }
+            const int rc = give_wgrad(st, w, use_mfma_wgrad(st, cs), a_grad, c.profiling || (c.dx_over_dy && g == c.dy_direct));
+            if (rc != BAPIPE_OK) return rc;
         }
         if (a_grad) {
             GatherConv dg = dgrad_geom(st, L);
@@ -990,22 +998,31 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
         break;
     }
     case BAPIPE_GATED: {
-        void *D = st->slot(c.mbid) + L.off_pd;
+        void *D = st->grads + L.off_d;
         const void *x = st->tptr(L.a, c.mbid);
         const int rows = rows_of(st, A);
-        const double flop = conv_flop(fwd_geom(st, L), L.d.cin), wbytes = (double)L.w_elems;
+        const double flop = conv_flop(fwd_geom(st, L), L.d.cin), dbytes = 2.0 * O.bytes();
         bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
-        HIPCHK(gated_grad(dt, L.d.kh, grad_ptr(st, L.o, c), D, rows, L.d.cout, s));
-        st->tap_end(tp, 0.0, 5.0 * O.bytes());
-        const int direct = dt == DT_BF16 ? BAPIPE_KC_CONV_WGRAD_MFMA : BAPIPE_KC_CONV_DIRECT;
-        tp = st->tap_begin(direct);
-        HIPCHK(gated_wgrad_direct(dt, x, D, L.dw, L.db, rows, L.d.cin, L.d.cout, st->work, s));
-        st->tap_end(tp, flop, (double)A.bytes() + 2.0 * O.bytes() + 8.0 * wbytes);
+        HIPCHK(gated_grad(dt, L.d.kh, grad_ptr(st, L.o, c), (const float *)(st->slot(c.mbid) + L.off_pd), D, rows, L.d.cout, s));
+        st->tap_end(tp, 0.0, (double)O.bytes() + 8.0 * O.elems + dbytes);
+        const WgradLaunch w{x, D, &L, conv_shape(st, L), flop, (double)A.bytes() + dbytes + 8.0 * L.w_elems};
+        if (L.mfma) {
+            const int rc = give_wgrad(st, w, true, a_grad, c.profiling);
+            if (rc != BAPIPE_OK) return rc;
+        } else {
+            tp = st->tap_begin(BAPIPE_KC_CONV_DIRECT);
+            HIPCHK(gated_wgrad_direct(dt, x, D, L.dw, L.db, rows, L.d.cin, L.d.cout, st->work, s));
+            st->tap_end(tp, w.flop, w.bytes);
+        }
         if (a_grad) {
             GradEpi e = epi_for(st, L.a, c);
-            tp = st->tap_begin(dt == DT_BF16 ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
-            HIPCHK(gated_dgrad_direct(dt, D, L.w_t, grad_ptr(st, L.a, c), e, rows, L.d.cin, L.d.cout, s));
-            st->tap_end(tp, flop, 2.0 * O.bytes() + wbytes * dt_size(dt) + (double)A.bytes() * (1.0 + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0)));
+            void *dx = grad_ptr(st, L.a, c);
+            tp = st->tap_begin(L.mfma ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
+            if (L.mfma)
+                HIPCHK(conv_gather_mfma(D, L.w_t, nullptr, dx, 0, e, dgrad_geom(st, L), st->work, st->tickets, s));
+            else
+                HIPCHK(gated_dgrad_direct(dt, D, L.w_t, dx, e, rows, L.d.cin, L.d.cout, s));
+            st->tap_end(tp, flop, dbytes + (double)L.w_elems * dt_size(dt) + (double)A.bytes() * (1.0 + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0)));
         }
         break;
     }
@@ -1437,9 +1454,21 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         }
         if (L.d.kind == BAPIPE_GATED) {
             const int rows = rows_of(st, A);
-            L.aux_off = L.off_pd = slot; L.aux_bytes = (size_t)rows * 2 * L.d.cout * es; slot += align_up(L.aux_bytes);
-            const size_t w = gated_wgrad_direct_workspace(rows, L.d.cin, L.d.cout);
+            L.aux_off = L.off_pd = slot; L.aux_bytes = (size_t)rows * 2 * L.d.cout * sizeof(float); slot += align_up(L.aux_bytes);
+            L.off_d = gr; gr += align_up((size_t)rows * 2 * L.d.cout * es);
+            L.mfma = gated_mfma(st->dt, rows, L.d.cin, L.d.cout);
+            size_t w = gated_workspace(st->dt, rows, L.d.cin, L.d.cout);
             work = w > work ? w : work;
+            if (L.mfma) {
+                const ConvShape cs = conv_shape(st, L);
+                const GatherConv dg = dgrad_geom(st, L);
+                L.w_panels = streams_filter(fwd_geom(st, L));
+                L.wt_panels = streams_filter(dg);
+                w = conv_gather_mfma_workspace(dg); work = w > work ? w : work;
+                w = conv_wgrad_mfma_workspace(cs); work = w > work ? w : work;
+                L.groups = conv_wgrad_mfma_groups(cs);
+                if (L.groups) grouped += align_up(w);
+            }
         }
         if (L.d.kind == BAPIPE_LSTM) {
             const int N = micro_batch, T = A.H, In = A.Cp, H = L.d.cout, G = 4 * H;

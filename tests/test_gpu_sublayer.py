@@ -181,7 +181,7 @@ def _check_gated(st, layout=B.NHWC):
     errs["dw"] = (_f64(got["dw0"]), orc.dw[0])
     if b is not None:
         errs["db"] = (_f64(got["db0"]), orc.db[0])
-    # Gradients in the 2-norm.  Float: chains of cin, 2 cout and rows additions.  bf16: the projections and their gradients are
+    # Gradients in the 2-norm.  Float: chains of cin, 2 cout and rows additions.  bf16: the gradients of the projections are
     # rounded, and where the sums of the two sides lie on both sides of a rounding border (noise of sqrt(cin) U against steps of 2^-7:
     # a share below 3e-3 at these sizes) they are a step apart: sqrt(3e-3) 2^-7 = 4e-4 of a tensor; each is rounded to dx once more,
     # where noise of that size flips a tenth of the elements by a step: sqrt(0.1) 2^-7 = 2.5e-3.
