@@ -198,11 +198,12 @@ hipError_t bn_bwd(int dt, const void *x, const void *dy, const float *gamma, con
 
 // ---- layer norm over the C channels of each of `rows` positions (kernels_layernorm.hip); stats: [2][rows] floats (mean, 1/std)
 size_t layernorm_workspace(int rows, int C);
+// copy: a second place for x; rest: for what rounding took from y, in the storage type (each NULL or as large as x)
 hipError_t layernorm_fwd(int dt, const void *x, const float *gamma, const float *beta, float eps, void *y, float *stats, int rows, int C,
-                         hipStream_t s);
-// dx may be NULL, or dy
-hipError_t layernorm_bwd(int dt, const void *x, const void *dy, const float *gamma, const float *stats, void *dx, float *dgamma, float *dbeta,
-                         GradEpi epi, int rows, int C, void *workspace, hipStream_t s);
+                         hipStream_t s, void *copy = nullptr, void *rest = nullptr);
+// dy_parts > 0: dy is that many float sums [dy_parts][rows][C] instead; dx may be NULL, or dy
+hipError_t layernorm_bwd(int dt, const void *x, const void *dy, int dy_parts, const float *gamma, const float *stats, void *dx, float *dgamma,
+                         float *dbeta, GradEpi epi, int rows, int C, void *workspace, hipStream_t s);
 
 // ---- gated linear layer (kernels_gated.hip): h = act(x Wg^T + bg) (x Wu^T + bu), w [2F][C] with the gate rows first, bias [2F] or NULL
 // P [rows][2F] receives both projections (float), which gated_grad takes with dh to their gradients D [rows][2F] (storage type)

@@ -2,6 +2,12 @@
 //   mean = sum x / C, var = sum (x - mean)^2 / C, inv = 1 / sqrt(var + eps), xhat = (x - mean) inv, y = gamma xhat + beta
 //   a = gamma dy;  dx = inv (a - sum a / C - xhat sum(a xhat) / C);  dgamma += sum over rows of dy xhat;  dbeta += sum over rows of dy
 // Everything between a load and a store is float; mean and inv of every row are kept for the backward pass.
+//
+// HBM bounds it: forward reads x and writes y, backward reads x and dy and writes dx, each once.  A row stays in the registers of
+// the threads that read it, so that its variance is taken around its own mean (E[x^2] - mean^2 of rows far from zero loses
+// all digits) without a second read.  A group of threads takes one row after another and keeps what belongs to its columns,
+// gamma and beta, or gamma and the sums of the columns' gradients: read for every row, the two floats of a bf16 element are twice
+// the bytes of the element's load and store.  The next row is requested before the present one's sums are formed.
 #include "dev_common.h"
 #include "kernels.h"
 
@@ -10,10 +16,261 @@ namespace {
 
 constexpr int TPB = 256;
 
-// sum over the block, for all its threads
+// ------------------------------------------------------------------ sums over the threads of a row
+// Of a wave: neighbours by data-parallel moves inside the vector unit, without LDS, the total broadcast from the last lane
+__device__ __forceinline__ float wave_total(float v)
+{
+    auto add = [&](auto moved) { v += __int_as_float(moved); };
+#define MOVED(ctrl, rows) __builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, rows, 0xF, true)
+    add(MOVED(0x111, 0xF));        // from the lane 1, 2, 4, 8 below, inside rows of 16 lanes
+    add(MOVED(0x112, 0xF));
+    add(MOVED(0x114, 0xF));
+    add(MOVED(0x118, 0xF));
+    add(MOVED(0x142, 0xA));        // the last lane of a row to the row behind it, 0 to 1 and 2 to 3
+    add(MOVED(0x143, 0xC));        // and of the lower half to the upper one
+#undef MOVED
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// Of the G threads of a group, for all of them.  Groups of 256 exchange their waves' totals in lds[2][WAVES]; two calls in turn use
+// different halves, so that one barrier a call is enough.
+template <int G>
+__device__ __forceinline__ float group_sum(float v, float *lds, int half)
+{
+    if constexpr (G < 64) {
+#pragma unroll
+        for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, G);
+        return v;
+    } else {
+        v = wave_total(v);
+        if constexpr (G == 64) return v;
+        constexpr int W = G / 64;
+        float *mine = lds + (half * (blockDim.x / 64)) + threadIdx.x / G * W;
+        if (threadIdx.x % 64 == 0) mine[threadIdx.x / 64 % W] = v;
+        __syncthreads();
+        float sum = mine[0];
+#pragma unroll
+        for (int w = 1; w < W; ++w) sum += mine[w];
+        return sum;
+    }
+}
+
+// ------------------------------------------------------------------ rows that fit their threads' registers
+// V = 16 / sizeof(T) values in one access at any address of T (global memory needs no more alignment than that); where a row
+// is no whole number of them (TAIL), the last ones of it are `left` < V single values, and zeros behind them
+template <class T, int V> struct vec_of {
+    T e[V];
+};
+template <bool TAIL, class T, int V> __device__ __forceinline__ void load_vec(vec_of<T, V> &to, const T *from, int left)
+{
+    if (!TAIL || left >= V) {
+        __builtin_memcpy(&to, from, sizeof(to));
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) to.e[j] = j < left ? from[j] : T{};
+}
+template <bool TAIL, class T, int V> __device__ __forceinline__ void store_vec(T *to, const vec_of<T, V> &from, int left)
+{
+    if (!TAIL || left >= V) {
+        __builtin_memcpy(to, &from, sizeof(from));
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (j < left) to[j] = from.e[j];
+}
+
+// Thread t of a group of G has columns (k G + t) V .. + V - 1, k < NV.
+template <class T, int V, int NV> struct row_regs {
+    vec_of<T, V> v[NV];
+    template <int G, bool TAIL> __device__ __forceinline__ void load(const T *row, int t, int C)
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * G + t) * V;
+            if (c < C) load_vec<TAIL>(v[k], row + c, C - c);
+        }
+    }
+};
+
+template <class T> struct FwdArgs {
+    const T *x;
+    const float *gamma, *beta;
+    T *y, *copy, *rest;       // copy: x once more, rest: what rounding took from y, each NULL or [rows][C]
+    float *stats, eps;
+    int rows, C;
+};
+
+template <class T, int NV, int G, bool TAIL>
+__global__ __launch_bounds__(TPB) void k_layernorm_fwd(FwdArgs<T> p)
+{
+    constexpr int V = 16 / sizeof(T);
+    __shared__ float lds[2 * TPB / 64];
+    const int t = threadIdx.x % G, C = p.C, step = gridDim.x * (TPB / G);
+    int row = blockIdx.x * (TPB / G) + threadIdx.x / G;
+    row_regs<float, V, NV> gamma, beta;
+    gamma.template load<G, TAIL>(p.gamma, t, C);
+    beta.template load<G, TAIL>(p.beta, t, C);
+    row_regs<T, V, NV> next;
+    if (row < p.rows) next.template load<G, TAIL>(p.x + (size_t)row * C, t, C);
+    const float per = 1.0f / C;
+    // columns behind the row's end
+    auto in = [&](int k, int j) { return (k * G + t) * V + (TAIL ? j : 0) < C; };
+    // all groups of a block take the same number of turns, for they meet at barriers
+    for (int first = blockIdx.x * (TPB / G); first < p.rows; first += step, row += step) {
+        const bool on = row < p.rows;
+        const row_regs<T, V, NV> x = next;
+        if (row + step < p.rows) next.template load<G, TAIL>(p.x + (size_t)(row + step) * C, t, C);
+        float f[NV][V], sum = 0.0f, sq = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                f[k][j] = in(k, j) ? to_f32(x.v[k].e[j]) : 0.0f;
+                sum += f[k][j];
+            }
+        const float mean = group_sum<G>(sum, lds, 0) * per;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                f[k][j] = in(k, j) ? f[k][j] - mean : 0.0f;
+                sq = fmaf(f[k][j], f[k][j], sq);
+            }
+        const float inv = 1.0f / sqrtf(group_sum<G>(sq, lds, 1) * per + p.eps);
+        if (!on) continue;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * G + t) * V;
+            if (c >= C) continue;
+            const size_t at = (size_t)row * C + c;
+            vec_of<T, V> y, rest;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float v = fmaf(f[k][j] * inv, gamma.v[k].e[j], beta.v[k].e[j]);
+                y.e[j] = from_f32<T>(v);
+                if (p.rest) rest.e[j] = from_f32<T>(v - to_f32(y.e[j]));
+            }
+            store_vec<TAIL>(p.y + at, y, C - c);
+            if (p.rest) store_vec<TAIL>(p.rest + at, rest, C - c);
+            if (p.copy) store_vec<TAIL>(p.copy + at, x.v[k], C - c);
+        }
+        if (t == 0) {
+            p.stats[row] = mean;
+            p.stats[p.rows + row] = inv;
+        }
+    }
+}
+
+template <class T> struct BwdArgs {
+    const T *x, *dy;
+    const float *dy_parts;    // instead of dy: its `parts` float sums [parts][rows][C]
+    int parts;
+    const float *gamma, *stats;
+    T *dx;                    // may be NULL, or dy
+    const T *old, *gate;
+    float *part;              // [gridDim.x][2][C]: sums over the block's rows of dy xhat and of dy
+    int rows, C;
+};
+
+// NT threads, NT / G groups whose columns' sums meet in LDS at the end, the upper half's added to the lower half's each time
+template <class T, int NV, int G, int NT, bool TAIL, bool PARTS>
+__global__ __launch_bounds__(NT) void k_layernorm_bwd(BwdArgs<T> p)
+{
+    extern __shared__ __align__(16) float lds[];
+    constexpr int V = 16 / sizeof(T), GROUPS = NT / G;
+    const int t = threadIdx.x % G, group = threadIdx.x / G, C = p.C, step = gridDim.x * GROUPS;
+    int row = blockIdx.x * GROUPS + group;
+    row_regs<float, V, NV> gamma;
+    gamma.template load<G, TAIL>(p.gamma, t, C);
+    float sg[NV][V] = {}, sb[NV][V] = {};
+    row_regs<T, V, NV> nx, nd;
+    auto request = [&](int r) {
+        nx.template load<G, TAIL>(p.x + (size_t)r * C, t, C);
+        if (!PARTS) nd.template load<G, TAIL>(p.dy + (size_t)r * C, t, C);
+    };
+    if (row < p.rows) request(row);
+    const float per = 1.0f / C;
+    for (int first = blockIdx.x * GROUPS; first < p.rows; first += step, row += step) {
+        const bool on = row < p.rows;
+        const row_regs<T, V, NV> xr = nx, dr = nd;
+        if (row + step < p.rows) request(row + step);
+        const float mean = on ? p.stats[row] : 0.0f, inv = on ? p.stats[p.rows + row] : 0.0f;
+        const size_t base = (size_t)row * C;
+        float xh[NV][V], d[NV][V], s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * G + t) * V;
+#pragma unroll
+            for (int j = 0; j < V; ++j) d[k][j] = 0.0f;
+            if constexpr (PARTS) {
+                if (on && c < C)
+                    for (int s = 0; s < p.parts; ++s) {
+                        vec_of<float, V> v;
+                        load_vec<TAIL>(v, p.dy_parts + (size_t)s * p.rows * C + base + c, C - c);
+#pragma unroll
+                        for (int j = 0; j < V; ++j) d[k][j] += v.e[j];
+                    }
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const bool in = on && c + (TAIL ? j : 0) < C;
+                if (!PARTS) d[k][j] = in ? to_f32(dr.v[k].e[j]) : 0.0f;
+                xh[k][j] = in ? (to_f32(xr.v[k].e[j]) - mean) * inv : 0.0f;
+                sg[k][j] = fmaf(d[k][j], xh[k][j], sg[k][j]);
+                sb[k][j] += d[k][j];
+                d[k][j] *= c < C ? gamma.v[k].e[j] : 0.0f;
+                s1 += d[k][j];
+                s2 = fmaf(d[k][j], xh[k][j], s2);
+            }
+        }
+        if (!p.dx) continue;
+        s1 = group_sum<G>(s1, lds, 0) * per;
+        s2 = group_sum<G>(s2, lds, 1) * per;
+        if (!on) continue;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * G + t) * V;
+            if (c >= C) continue;
+            vec_of<T, V> r, old, gate;
+            if (p.old) load_vec<TAIL>(old, p.old + base + c, C - c);
+            if (p.gate) load_vec<TAIL>(gate, p.gate + base + c, C - c);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float v = inv * (d[k][j] - s1 - xh[k][j] * s2);
+                r.e[j] = grad_out<T>(v, p.old != nullptr, p.old ? old.e[j] : from_f32<T>(0.0f), p.gate != nullptr, p.gate ? gate.e[j] : from_f32<T>(0.0f));
+            }
+            store_vec<TAIL>(p.dx + base + c, r, C - c);
+        }
+    }
+    __syncthreads();
+    // all columns of this thread, to and from [2][C]
+    auto columns = [&](auto f) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int c = (k * G + t) * V + j;
+                if (c < C) f(c, sg[k][j], sb[k][j]);
+            }
+    };
+#pragma unroll
+    for (int half = GROUPS / 2; half > 0; half /= 2) {
+        float *at = lds + (size_t)(group % half) * 2 * C;
+        if (group >= half && group < 2 * half) columns([&](int c, float g, float b) { at[c] = g; at[C + c] = b; });
+        __syncthreads();
+        if (group < half) columns([&](int c, float &g, float &b) { g += at[c]; b += at[C + c]; });
+        __syncthreads();
+    }
+    float *to = p.part + (size_t)blockIdx.x * 2 * C;
+    if (group == 0) columns([&](int c, float g, float b) { to[c] = g; to[C + c] = b; });
+}
+
+// ------------------------------------------------------------------ longer rows, read once for every sum
 __device__ __forceinline__ float block_sum(float v, float *lds)
 {
-    v = wave_sum(v);
+    v = wave_total(v);
     __syncthreads();
     if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
     __syncthreads();
@@ -23,122 +280,222 @@ __device__ __forceinline__ float block_sum(float v, float *lds)
     return sum;
 }
 
-// a block takes rows blockIdx.x, blockIdx.x + gridDim.x, ...
 template <class T>
-__global__ __launch_bounds__(TPB) void k_layernorm_fwd(const T *__restrict__ x, const float *__restrict__ gamma, const float *__restrict__ beta,
-                                                       float eps, T *__restrict__ y, float *__restrict__ stats, int rows, int C)
+__global__ __launch_bounds__(TPB) void k_layernorm_fwd_long(FwdArgs<T> p)
 {
     __shared__ float lds[TPB / 64];
-    for (int row = blockIdx.x; row < rows; row += gridDim.x) {
-    const T *xr = x + (size_t)row * C;
-    float sum = 0.0f;
-    for (int c = threadIdx.x; c < C; c += TPB) sum += to_f32(xr[c]);
-    const float mean = block_sum(sum, lds) / C;
-    float sq = 0.0f;
-    for (int c = threadIdx.x; c < C; c += TPB) {
-        const float d = to_f32(xr[c]) - mean;
-        sq += d * d;
-    }
-    const float inv = 1.0f / sqrtf(block_sum(sq, lds) / C + eps);
-    for (int c = threadIdx.x; c < C; c += TPB)
-        y[(size_t)row * C + c] = from_f32<T>((to_f32(xr[c]) - mean) * inv * gamma[c] + beta[c]);
-    if (threadIdx.x == 0) {
-        stats[row] = mean;
-        stats[rows + row] = inv;
-    }
+    for (int row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const size_t at = (size_t)row * p.C;
+        float sum = 0.0f, sq = 0.0f;
+        for (int c = threadIdx.x; c < p.C; c += TPB) sum += to_f32(p.x[at + c]);
+        const float mean = block_sum(sum, lds) / p.C;
+        for (int c = threadIdx.x; c < p.C; c += TPB) {
+            const float d = to_f32(p.x[at + c]) - mean;
+            sq += d * d;
+        }
+        const float inv = 1.0f / sqrtf(block_sum(sq, lds) / p.C + p.eps);
+        for (int c = threadIdx.x; c < p.C; c += TPB) {
+            const float v = fmaf((to_f32(p.x[at + c]) - mean) * inv, p.gamma[c], p.beta[c]);
+            const T y = from_f32<T>(v);
+            if (p.rest) p.rest[at + c] = from_f32<T>(v - to_f32(y));
+            if (p.copy) p.copy[at + c] = p.x[at + c];
+            p.y[at + c] = y;
+        }
+        if (threadIdx.x == 0) {
+            p.stats[row] = mean;
+            p.stats[p.rows + row] = inv;
+        }
     }
 }
 
+template <class T> __device__ __forceinline__ float dy_at(const BwdArgs<T> &p, size_t i)
+{
+    if (!p.dy_parts) return to_f32(p.dy[i]);
+    float v = 0.0f;
+    for (int s = 0; s < p.parts; ++s) v += p.dy_parts[(size_t)s * p.rows * p.C + i];
+    return v;
+}
+
 template <class T>
-__global__ __launch_bounds__(TPB) void k_layernorm_dx(const T *x, const T *dy, const float *__restrict__ gamma, const float *__restrict__ stats,
-                                                      T *dx, const T *old, const T *gate, int rows, int C)
+__global__ __launch_bounds__(TPB) void k_layernorm_dx_long(BwdArgs<T> p)
 {
     __shared__ float lds[TPB / 64];
-    for (int row = blockIdx.x; row < rows; row += gridDim.x) {
-    const size_t at = (size_t)row * C;
-    const float mean = stats[row], inv = stats[rows + row];
-    float s1 = 0.0f, s2 = 0.0f;
-    for (int c = threadIdx.x; c < C; c += TPB) {
-        const float a = to_f32(dy[at + c]) * gamma[c];
-        s1 += a;
-        s2 += a * ((to_f32(x[at + c]) - mean) * inv);
-    }
-    s1 = block_sum(s1, lds) / C;
-    s2 = block_sum(s2, lds) / C;
-    for (int c = threadIdx.x; c < C; c += TPB) {
-        const float a = to_f32(dy[at + c]) * gamma[c], xhat = (to_f32(x[at + c]) - mean) * inv;
-        dx[at + c] = grad_out<T>(inv * (a - s1 - xhat * s2), old != nullptr, old ? old[at + c] : from_f32<T>(0.0f), gate != nullptr,
-                                 gate ? gate[at + c] : from_f32<T>(0.0f));
-    }
+    for (int row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const size_t at = (size_t)row * p.C;
+        const float mean = p.stats[row], inv = p.stats[p.rows + row];
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int c = threadIdx.x; c < p.C; c += TPB) {
+            const float a = dy_at(p, at + c) * p.gamma[c];
+            s1 += a;
+            s2 += a * ((to_f32(p.x[at + c]) - mean) * inv);
+        }
+        s1 = block_sum(s1, lds) / p.C;
+        s2 = block_sum(s2, lds) / p.C;
+        for (int c = threadIdx.x; c < p.C; c += TPB) {
+            const float a = dy_at(p, at + c) * p.gamma[c], xhat = (to_f32(p.x[at + c]) - mean) * inv;
+            p.dx[at + c] = grad_out<T>(inv * (a - s1 - xhat * s2), p.old != nullptr, p.old ? p.old[at + c] : from_f32<T>(0.0f), p.gate != nullptr,
+                                       p.gate ? p.gate[at + c] : from_f32<T>(0.0f));
+        }
     }
 }
 
 // part[chunk][0 | 1][C]: sums of dy xhat and of dy over the chunk's rows, a column per thread
 template <class T>
-__global__ __launch_bounds__(TPB) void k_layernorm_columns(const T *__restrict__ x, const T *__restrict__ dy, const float *__restrict__ stats,
-                                                           float *__restrict__ part, int rows, int C, int rows_per_chunk)
+__global__ __launch_bounds__(TPB) void k_layernorm_columns(BwdArgs<T> p, int rows_per_chunk)
 {
     const int c = blockIdx.x * TPB + threadIdx.x;
-    if (c >= C) return;
-    const int r0 = blockIdx.y * rows_per_chunk, r1 = r0 + rows_per_chunk < rows ? r0 + rows_per_chunk : rows;
+    if (c >= p.C) return;
+    const int r0 = blockIdx.y * rows_per_chunk, r1 = r0 + rows_per_chunk < p.rows ? r0 + rows_per_chunk : p.rows;
     float g = 0.0f, b = 0.0f;
     for (int r = r0; r < r1; ++r) {
-        const float d = to_f32(dy[(size_t)r * C + c]);
-        g += d * ((to_f32(x[(size_t)r * C + c]) - stats[r]) * stats[rows + r]);
+        const float d = dy_at(p, (size_t)r * p.C + c);
+        g += d * ((to_f32(p.x[(size_t)r * p.C + c]) - p.stats[r]) * p.stats[p.rows + r]);
         b += d;
     }
-    part[(size_t)blockIdx.y * 2 * C + c] = g;
-    part[((size_t)blockIdx.y * 2 + 1) * C + c] = b;
+    p.part[(size_t)blockIdx.y * 2 * p.C + c] = g;
+    p.part[((size_t)blockIdx.y * 2 + 1) * p.C + c] = b;
 }
 
-// dgamma += , dbeta += the sums of all chunks, in chunk order
+// dgamma += , dbeta += the sums of all chunks: 16 columns a block, 16 threads each that take every 16th chunk and are added in
+// their order
 __global__ __launch_bounds__(TPB) void k_layernorm_params(const float *__restrict__ part, int chunks, int C, float *dgamma, float *dbeta)
 {
-    const int i = blockIdx.x * TPB + threadIdx.x;
-    if (i >= 2 * C) return;
-    double sum = 0.0;
-    for (int k = 0; k < chunks; ++k) sum += part[(size_t)k * 2 * C + i];
+    __shared__ float lds[16][17];
+    const int col = threadIdx.x % 16, lane = threadIdx.x / 16;
+    const long long i = (long long)blockIdx.x * 16 + col, n = 2ll * C;
+    float sum = 0.0f;
+    if (i < n) {
+        int k = lane;
+        for (; k + 48 < chunks; k += 64) {
+            float v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = part[(size_t)(k + 16 * u) * n + i];
+            sum += (v[0] + v[1]) + (v[2] + v[3]);
+        }
+        for (; k < chunks; k += 16) sum += part[(size_t)k * n + i];
+    }
+    lds[lane][col] = sum;
+    __syncthreads();
+    if (lane || i >= n) return;
+    float total = 0.0f;
+#pragma unroll
+    for (int u = 0; u < 16; ++u) total += lds[u][col];
     float *out = i < C ? dgamma + i : dbeta + (i - C);
-    *out += (float)sum;
+    *out += total;
 }
 
-unsigned grid_of(int rows) { return rows < 1 << 20 ? rows : 1 << 20; }
-int rows_per_chunk(int rows) { return rows < 64 * 256 ? 64 : (rows + 255) / 256; }
-int chunks_of(int rows) { return (rows + rows_per_chunk(rows) - 1) / rows_per_chunk(rows); }
+// ------------------------------------------------------------------ which kernel takes a row
+// G threads and NV accesses of each for a row, the smallest that fit it: a wave for a row of up to 4 a thread (forward) or 2 (backward,
+// which has two rows of registers and two sums for every column), four waves above.  G = 0: too long for registers.
+struct Shape {
+    int nv, g;
+};
+Shape shape_of(int dt, int C, bool fwd)
+{
+    const int v = dt == DT_F32 ? 4 : 8, n = (C + v - 1) / v;
+    for (int g = 8; g <= 64; g *= 2)
+        if (n <= g) return {1, g};
+    for (int nv = 2; nv <= (fwd ? 4 : 2); nv *= 2)
+        if (n <= 64 * nv) return {nv, 64};
+    for (int nv = 1; nv <= 8; nv *= 2)
+        if (n <= 256 * nv) return {nv, 256};
+    return {0, 0};
+}
+
+// Blocks of the backward pass: each leaves 8 C bytes of column sums for the kernel behind it, against 6 C bytes a row and more of its
+// own, so that a block takes 32 rows where that leaves enough of them, and four rounds of its groups at the least
+int bwd_blocks(int rows, int groups)
+{
+    const int most = (rows + 4 * groups - 1) / (4 * groups), long_ones = rows / 32, many = long_ones > 512 ? 512 : long_ones < 256 ? 256 : long_ones;
+    return most < many ? most : many;
+}
+constexpr int kLongChunks = 256;
 
 }  // namespace
 
-size_t layernorm_workspace(int rows, int C) { return (size_t)chunks_of(rows) * 2 * C * sizeof(float); }
+size_t layernorm_workspace(int rows, int C) { return (size_t)(rows < 512 ? rows : 512) * 2 * C * sizeof(float); }
 
-hipError_t layernorm_fwd(int dt, const void *x, const float *gamma, const float *beta, float eps, void *y, float *stats, int rows, int C, hipStream_t s)
+template <class T>
+static hipError_t fwd_t(int dt, FwdArgs<T> p, hipStream_t s)
 {
-    if (dt == DT_F32)
-        hipLaunchKernelGGL((k_layernorm_fwd<float>), dim3(grid_of(rows)), dim3(TPB), 0, s, (const float *)x, gamma, beta, eps, (float *)y, stats, rows, C);
-    else
-        hipLaunchKernelGGL((k_layernorm_fwd<bf16_t>), dim3(grid_of(rows)), dim3(TPB), 0, s, (const bf16_t *)x, gamma, beta, eps, (bf16_t *)y, stats, rows, C);
+    const Shape k = shape_of(dt, p.C, true);
+    const bool tail = p.C % (16 / sizeof(T)) != 0;
+    auto launch = [&](auto kernel, int groups) {
+        const int blocks = (p.rows + groups - 1) / groups, most = 256 * 8;
+        hipLaunchKernelGGL(kernel, dim3(blocks < most ? blocks : most), dim3(TPB), 0, s, p);
+        return hipGetLastError();
+    };
+#define FWD(NV, G)                                                                                  \
+    if (k.nv == NV && k.g == G)                                                                     \
+    return tail ? launch(k_layernorm_fwd<T, NV, G, true>, TPB / G) : launch(k_layernorm_fwd<T, NV, G, false>, TPB / G)
+    FWD(1, 8); FWD(1, 16); FWD(1, 32); FWD(1, 64); FWD(2, 64); FWD(4, 64); FWD(2, 256); FWD(4, 256); FWD(8, 256);
+#undef FWD
+    const dim3 grid(p.rows < (1 << 20) ? p.rows : 1 << 20);
+    hipLaunchKernelGGL(k_layernorm_fwd_long<T>, grid, dim3(TPB), 0, s, p);
     return hipGetLastError();
 }
 
 template <class T>
-static hipError_t layernorm_bwd_t(const T *x, const T *dy, const float *gamma, const float *stats, T *dx, float *dgamma, float *dbeta, GradEpi epi,
-                                  int rows, int C, float *part, hipStream_t s)
+static hipError_t bwd_t(int dt, BwdArgs<T> p, float *dgamma, float *dbeta, hipStream_t s)
 {
-    // before dx, which may take the place of dy
-    const int per = rows_per_chunk(rows), chunks = chunks_of(rows);
-    hipLaunchKernelGGL((k_layernorm_columns<T>), dim3((C + TPB - 1) / TPB, chunks), dim3(TPB), 0, s, x, dy, stats, part, rows, C, per);
-    hipLaunchKernelGGL(k_layernorm_params, dim3((2 * C + TPB - 1) / TPB), dim3(TPB), 0, s, part, chunks, C, dgamma, dbeta);
-    const T *old = epi.accum ? (const T *)(epi.accum_from ? epi.accum_from : dx) : nullptr;
-    if (dx)
-        hipLaunchKernelGGL((k_layernorm_dx<T>), dim3(grid_of(rows)), dim3(TPB), 0, s, x, dy, gamma, stats, dx, old, (const T *)epi.gate, rows, C);
+    const Shape k = shape_of(dt, p.C, false);
+    const bool tail = p.C % (16 / sizeof(T)) != 0;
+    int chunks = 0;
+    auto launch = [&](auto kernel, int threads, int groups) {
+        chunks = bwd_blocks(p.rows, groups);
+        const size_t meet = (size_t)(groups / 2) * 2 * p.C * sizeof(float), sums = 2 * threads / 64 * sizeof(float);
+        const size_t bytes = meet > sums ? meet : sums;
+        if (bytes > 64 * 1024) {
+            const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+            if (e != hipSuccess) return e;
+        }
+        hipLaunchKernelGGL(kernel, dim3(chunks), dim3(threads), bytes, s, p);
+        return hipGetLastError();
+    };
+    hipError_t e = hipErrorInvalidValue;
+    bool found = false;
+#define BWD(NV, G, NT)                                                                                             \
+    if (!found && k.nv == NV && k.g == G) {                                                                        \
+        found = true;                                                                                              \
+        if constexpr (sizeof(T) == 2) {                                                                            \
+            if (p.dy_parts) e = tail ? launch(k_layernorm_bwd<T, NV, G, NT, true, true>, NT, NT / G) : launch(k_layernorm_bwd<T, NV, G, NT, false, true>, NT, NT / G); \
+        }                                                                                                          \
+        if (!p.dy_parts) e = tail ? launch(k_layernorm_bwd<T, NV, G, NT, true, false>, NT, NT / G) : launch(k_layernorm_bwd<T, NV, G, NT, false, false>, NT, NT / G); \
+    }
+    BWD(1, 8, 512); BWD(1, 16, 512); BWD(1, 32, 512); BWD(1, 64, 512); BWD(2, 64, 512);
+    BWD(1, 256, 512); BWD(2, 256, 512); BWD(4, 256, 512); BWD(8, 256, 256);
+#undef BWD
+    if (!found) {
+        // the columns first, for dx may take the place of dy
+        const int per = p.rows < 64 * kLongChunks ? 64 : (p.rows + kLongChunks - 1) / kLongChunks;
+        chunks = (p.rows + per - 1) / per;
+        hipLaunchKernelGGL(k_layernorm_columns<T>, dim3((p.C + TPB - 1) / TPB, chunks), dim3(TPB), 0, s, p, per);
+        if (p.dx) hipLaunchKernelGGL(k_layernorm_dx_long<T>, dim3(p.rows < (1 << 20) ? p.rows : 1 << 20), dim3(TPB), 0, s, p);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_layernorm_params, dim3((unsigned)((2ll * p.C + 15) / 16)), dim3(TPB), 0, s, p.part, chunks, p.C, dgamma, dbeta);
     return hipGetLastError();
 }
 
-hipError_t layernorm_bwd(int dt, const void *x, const void *dy, const float *gamma, const float *stats, void *dx, float *dgamma, float *dbeta,
-                         GradEpi epi, int rows, int C, void *workspace, hipStream_t s)
+hipError_t layernorm_fwd(int dt, const void *x, const float *gamma, const float *beta, float eps, void *y, float *stats, int rows, int C, hipStream_t s,
+                         void *copy, void *rest)
 {
+    if (dt == DT_F32) return fwd_t<float>(dt, {(const float *)x, gamma, beta, (float *)y, (float *)copy, (float *)rest, stats, eps, rows, C}, s);
+    return fwd_t<bf16_t>(dt, {(const bf16_t *)x, gamma, beta, (bf16_t *)y, (bf16_t *)copy, (bf16_t *)rest, stats, eps, rows, C}, s);
+}
+
+hipError_t layernorm_bwd(int dt, const void *x, const void *dy, int dy_parts, const float *gamma, const float *stats, void *dx, float *dgamma,
+                         float *dbeta, GradEpi epi, int rows, int C, void *workspace, hipStream_t s)
+{
+    const void *old = epi.accum ? (epi.accum_from ? epi.accum_from : dx) : nullptr;
+    const float *parts = dy_parts ? (const float *)dy : nullptr;
+    if (parts) dy = nullptr;
     if (dt == DT_F32)
-        return layernorm_bwd_t((const float *)x, (const float *)dy, gamma, stats, (float *)dx, dgamma, dbeta, epi, rows, C, (float *)workspace, s);
-    return layernorm_bwd_t((const bf16_t *)x, (const bf16_t *)dy, gamma, stats, (bf16_t *)dx, dgamma, dbeta, epi, rows, C, (float *)workspace, s);
+        return bwd_t<float>(dt, {(const float *)x, (const float *)dy, parts, dy_parts, gamma, stats, (float *)dx, (const float *)old, (const float *)epi.gate,
+                                 (float *)workspace, rows, C}, dgamma, dbeta, s);
+    return bwd_t<bf16_t>(dt, {(const bf16_t *)x, (const bf16_t *)dy, parts, dy_parts, gamma, stats, (bf16_t *)dx, (const bf16_t *)old,
+                              (const bf16_t *)epi.gate, (float *)workspace, rows, C}, dgamma, dbeta, s);
 }
 
 }  // namespace bapipe

@@ -992,8 +992,8 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
             dx = grad_ptr(st, L.a, c);
         }
         const bool tp = st->tap_begin(BAPIPE_KC_BATCHNORM);
-        HIPCHK(layernorm_bwd(dt, st->tptr(L.a, c.mbid), grad_ptr(st, L.o, c), L.w, (const float *)(st->slot(c.mbid) + L.aux_off), dx, L.dw, L.db, e,
-                             rows_of(st, A), A.C, st->work, s));
+        HIPCHK(layernorm_bwd(dt, st->tptr(L.a, c.mbid), grad_ptr(st, L.o, c), 0, L.w, (const float *)(st->slot(c.mbid) + L.aux_off), dx, L.dw, L.db,
+                             e, rows_of(st, A), A.C, st->work, s));
         st->tap_end(tp, 0.0, (double)A.bytes() * (2.0 + (dx ? 1.0 : 0.0) + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0)));
         break;
     }
