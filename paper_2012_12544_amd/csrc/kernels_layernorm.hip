@@ -171,6 +171,7 @@ template <class T> struct BwdArgs {
     T *dx;                    // may be NULL, or dy
     const T *old, *gate;
     float *part;              // [gridDim.x][2][C]: sums over the block's rows of dy xhat and of dy
+    float *dgamma, *dbeta;    // where a lone block adds its own
     int rows, C;
 };
 
@@ -264,7 +265,9 @@ __global__ __launch_bounds__(NT) void k_layernorm_bwd(BwdArgs<T> p)
         __syncthreads();
     }
     float *to = p.part + (size_t)blockIdx.x * 2 * C;
-    if (group == 0) columns([&](int c, float g, float b) { to[c] = g; to[C + c] = b; });
+    if (group) return;
+    if (gridDim.x == 1) columns([&](int c, float g, float b) { p.dgamma[c] += g; p.dbeta[c] += b; });
+    else columns([&](int c, float g, float b) { to[c] = g; to[C + c] = b; });
 }
 
 // ------------------------------------------------------------------ longer rows, read once for every sum
@@ -436,7 +439,7 @@ static hipError_t fwd_t(int dt, FwdArgs<T> p, hipStream_t s)
 }
 
 template <class T>
-static hipError_t bwd_t(int dt, BwdArgs<T> p, float *dgamma, float *dbeta, hipStream_t s)
+static hipError_t bwd_t(int dt, BwdArgs<T> p, hipStream_t s)
 {
     const Shape k = shape_of(dt, p.C, false);
     const bool tail = p.C % (16 / sizeof(T)) != 0;
@@ -473,8 +476,8 @@ static hipError_t bwd_t(int dt, BwdArgs<T> p, float *dgamma, float *dbeta, hipSt
         if (p.dx) hipLaunchKernelGGL(k_layernorm_dx_long<T>, dim3(p.rows < (1 << 20) ? p.rows : 1 << 20), dim3(TPB), 0, s, p);
         e = hipGetLastError();
     }
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_layernorm_params, dim3((unsigned)((2ll * p.C + 15) / 16)), dim3(TPB), 0, s, p.part, chunks, p.C, dgamma, dbeta);
+    if (e != hipSuccess || (found && chunks == 1)) return e;
+    hipLaunchKernelGGL(k_layernorm_params, dim3((unsigned)((2ll * p.C + 15) / 16)), dim3(TPB), 0, s, p.part, chunks, p.C, p.dgamma, p.dbeta);
     return hipGetLastError();
 }
 
@@ -493,9 +496,9 @@ hipError_t layernorm_bwd(int dt, const void *x, const void *dy, int dy_parts, co
     if (parts) dy = nullptr;
     if (dt == DT_F32)
         return bwd_t<float>(dt, {(const float *)x, (const float *)dy, parts, dy_parts, gamma, stats, (float *)dx, (const float *)old, (const float *)epi.gate,
-                                 (float *)workspace, rows, C}, dgamma, dbeta, s);
+                                 (float *)workspace, dgamma, dbeta, rows, C}, s);
     return bwd_t<bf16_t>(dt, {(const bf16_t *)x, (const bf16_t *)dy, parts, dy_parts, gamma, stats, (bf16_t *)dx, (const bf16_t *)old,
-                              (const bf16_t *)epi.gate, (float *)workspace, rows, C}, dgamma, dbeta, s);
+                              (const bf16_t *)epi.gate, (float *)workspace, dgamma, dbeta, rows, C}, s);
 }
 
 }  // namespace bapipe

@@ -54,9 +54,9 @@ struct Tensor {
     // Input / output gradient of a linear layer whose weight gradient is deferred: the tensor (its gradient) lives
     // in that layer's per-mini-batch buffer, one copy per micro-batch, so that nothing has to be copied there.
     char *mb_store = nullptr, *gmb_store = nullptr;
-    // Gradient with two sources, a residual ADD (processed first in backward) and a conv: the ADD's share is not
-    // copied, the conv's input-gradient epilogue reads it where it lies (GradEpi::accum_from).  Layer index of
-    // that conv, or -1.
+    // Gradient with two sources, a residual ADD (processed first in backward) and a conv or layer norm: the ADD's share is not
+    // copied, the other's input-gradient epilogue reads it where it lies (GradEpi::accum_from).  Layer index of
+    // that conv or layer norm, or -1.
     int fanout_conv = -1;
     size_t bytes() const { return elems * esize; }
 };
@@ -611,6 +611,7 @@ struct FwdCtx {
     int mbid;
     const void *x_direct;
     bool profiling = false;      // layers are timed one at a time: nothing may rely on what the previous layer left behind
+    const void *x_copied = nullptr;      // the caller's x, which the first layer leaves in the stash as well
     // where the caller wants the last tensor as it is stored here; the kernel that writes that tensor last may store both
     void *y_direct = nullptr;
     void *y_nchw = nullptr;      // ... or wants it in NCHW
@@ -628,6 +629,15 @@ const void *in_ptr(bapipe_stage *st, int t, const FwdCtx &c)
 uint32_t dropout_layer(const bapipe_stage *st, int li) { return (uint32_t)li + 65536u * (uint32_t)(st->opts.stage_index - 1); }
 
 int rows_of(const bapipe_stage *st, const Tensor &T) { return st->mb * T.H * T.W; }
+
+// Where a layer that nobody reads behind this pass stores its output: the stage's last tensor goes to the caller, whose place `align`
+// bytes are enough for
+void *out_ptr(bapipe_stage *st, const Layer &L, FwdCtx &c, size_t align)
+{
+    if (L.o + 1 != (int)st->tensors.size() || st->tensors[L.o].stashed || !c.y_direct || (uintptr_t)c.y_direct % align) return st->tptr(L.o, c.mbid);
+    c.y_stored = true;
+    return c.y_direct;
+}
 
 int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
 {
@@ -725,16 +735,19 @@ int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
     case BAPIPE_LAYERNORM: {
         const Tensor &A = st->tensors[L.a];
         const bool tp = st->tap_begin(BAPIPE_KC_BATCHNORM);
-        HIPCHK(layernorm_fwd(dt, a, L.w, L.bias, L.d.eps, o, (float *)(st->slot(c.mbid) + L.aux_off), rows_of(st, A), A.C, s));
-        st->tap_end(tp, 0.0, 2.0 * A.bytes());                                   // read x, write y
+        const void *x = li == 0 && c.x_copied ? c.x_copied : a;
+        void *copy = x == a ? nullptr : const_cast<void *>(a);
+        HIPCHK(layernorm_fwd(dt, x, L.w, L.bias, L.d.eps, out_ptr(st, L, c, dt_size(dt)), (float *)(st->slot(c.mbid) + L.aux_off), rows_of(st, A), A.C,
+                             s, copy));
+        st->tap_end(tp, 0.0, (copy ? 3.0 : 2.0) * A.bytes());                    // read x, write y (and x)
         break;
     }
     case BAPIPE_GATED: {
         const Tensor &A = st->tensors[L.a];
         const GatherConv g = fwd_geom(st, L);
         const bool tp = st->tap_begin(L.mfma ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
-        HIPCHK(gated_fwd(dt, L.d.kh, a, L.w_work, L.bias, (float *)(st->slot(c.mbid) + L.off_pd), o, rows_of(st, A), L.d.cin, L.d.cout, L.w_panels,
-                         st->work, s));
+        HIPCHK(gated_fwd(dt, L.d.kh, a, L.w_work, L.bias, (float *)(st->slot(c.mbid) + L.off_pd), out_ptr(st, L, c, L.mfma ? 16 : dt_size(dt)),
+                         rows_of(st, A), L.d.cin, L.d.cout, L.w_panels, st->work, s));
         // x and the weights read, h and both projections (float) written
         st->tap_end(tp, conv_flop(g, L.d.cin), (double)A.bytes() + O.bytes() + 8.0 * O.elems + (double)L.w_elems * dt_size(dt));
         break;
@@ -742,7 +755,7 @@ int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
     case BAPIPE_DROPOUT: {
         GradEpi none{nullptr, 0};
         const bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
-        HIPCHK(dropout(dt, a, o, none, O.elems, L.d.eps, st->dropout_state, dropout_layer(st, li), c.mbid, s));
+        HIPCHK(dropout(dt, a, out_ptr(st, L, c, dt_size(dt)), none, O.elems, L.d.eps, st->dropout_state, dropout_layer(st, li), c.mbid, s));
         st->tap_end(tp, 0.0, 2.0 * O.bytes());
         break;
     }
@@ -990,6 +1003,10 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
         if (a_grad) {
             e = epi_for(st, L.a, c);
             dx = grad_ptr(st, L.a, c);
+            if (c.pending[A.root]) {                      // the residual ADD's share, added here instead of copied there
+                e.accum_from = c.pending[A.root];
+                c.pending[A.root] = nullptr;
+            }
         }
         const bool tp = st->tap_begin(BAPIPE_KC_BATCHNORM);
         HIPCHK(layernorm_bwd(dt, st->tptr(L.a, c.mbid), grad_ptr(st, L.o, c), 0, L.w, (const float *)(st->slot(c.mbid) + L.aux_off), dx, L.dw, L.db,
@@ -1579,14 +1596,16 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
             if (use_mfma_gather(st, dg)) { w = conv_gather_mfma_workspace(dg); work = w > work ? w : work; }
         }
     }
-    // residual fan-out: a tensor read by exactly one conv (MFMA gather input gradient, plain epilogue) and, later in
+    // residual fan-out: a tensor read by exactly one conv (MFMA gather input gradient, plain epilogue) or layer norm and, later in
     // the list, one ADD
     for (int t = 0; t < nt; ++t) {
         Tensor &T = st->tensors[t];
-        if (st->dt != DT_BF16 || T.root != t || !T.need_grad || T.galias >= 0 || T.consumers.size() != 2) continue;
+        if (T.root != t || !T.need_grad || T.galias >= 0 || T.consumers.size() != 2) continue;
         const int ic = T.consumers[0], ia = T.consumers[1];
         const Layer &Lc = st->layers[ic], &La = st->layers[ia];
-        if (ic >= ia || Lc.d.kind != BAPIPE_CONV2D || La.d.kind != BAPIPE_ADD || Lc.a != t || (La.a != t && La.b != t)) continue;
+        if (ic >= ia || La.d.kind != BAPIPE_ADD || Lc.a != t || (La.a != t && La.b != t)) continue;
+        if (Lc.d.kind == BAPIPE_LAYERNORM) T.fanout_conv = ic;
+        if (Lc.d.kind != BAPIPE_CONV2D || st->dt != DT_BF16) continue;
         const GatherConv dg = dgrad_geom(st, Lc);
         if (!use_mfma_gather(st, dg) || conv3x3_halo_supported(dg) || Lc.bnb_chunks) continue;
         T.fanout_conv = ic;
@@ -1687,6 +1706,8 @@ int bapipe_stage_forward(bapipe_stage_t *st, int mb_id, const void *x_dev, void 
         HIPCHK(nchw_to_nhwc(dt, x_dev, st->tptr(0, mb_id), none, st->mb, In.C, In.H, In.W, In.Cp, s));
     } else if (In.Cp != In.C) {
         HIPCHK(nhwc_repad(dt, x_dev, st->tptr(0, mb_id), (size_t)st->mb * In.H * In.W, In.C, In.Cp, s));
+    } else if (In.stashed && st->layers[0].d.kind == BAPIPE_LAYERNORM) {
+        c.x_copied = x_dev;
     } else if (In.stashed) {
         HIPCHK(hipMemcpyAsync(st->tptr(0, mb_id), x_dev, In.bytes(), hipMemcpyDeviceToDevice, s));
     } else {
@@ -1699,8 +1720,8 @@ int bapipe_stage_forward(bapipe_stage_t *st, int mb_id, const void *x_dev, void 
     const bool flat_of_spatial = O.root != last && R.H * R.W > 1;
     const bool relayout = O.esize == dt_size(dt) && ((st->opts.io_layout == BAPIPE_NCHW && R.H * R.W > 1) || flat_of_spatial);
     // a layer that reads the caller's x in place must not find y there already: where they overlap y is copied behind the last layer
-    const uintptr_t x0 = (uintptr_t)c.x_direct, y0 = (uintptr_t)y_dev;
-    const bool overlap = c.x_direct && y_dev && y0 < x0 + In.bytes() && x0 < y0 + O.bytes();
+    const uintptr_t x0 = (uintptr_t)(c.x_direct ? c.x_direct : c.x_copied), y0 = (uintptr_t)y_dev;
+    const bool overlap = x0 && y_dev && y0 < x0 + In.bytes() && x0 < y0 + O.bytes();
     if (!relayout && !overlap) c.y_direct = y_dev;
     if (relayout && !c.x_direct && R.Cp == R.C) c.y_nchw = y_dev;
     for (int i = 0; i < (int)st->layers.size(); ++i) {
