@@ -224,6 +224,9 @@ hipError_t gated_wgrad_direct(int dt, const void *x, const void *D, float *dw, f
 constexpr int kDropoutState = 3;
 hipError_t dropout(int dt, const void *x, void *y, GradEpi epi, size_t n, float p, const uint32_t *state, uint32_t layer, uint32_t mb,
                    hipStream_t s);
+// y = [relu](dropped x + other), the dropped x rounded to storage first
+hipError_t dropout_add(int dt, const void *x, const void *other, void *y, int relu, size_t n, float p, const uint32_t *state, uint32_t layer,
+                       uint32_t mb, hipStream_t s);
 hipError_t dropout_set(uint32_t *state, uint64_t seed, uint32_t mini_batch, hipStream_t s);
 hipError_t dropout_next(uint32_t *state, hipStream_t s);      // the next mini-batch
 

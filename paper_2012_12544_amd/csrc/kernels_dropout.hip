@@ -27,22 +27,67 @@ __device__ __forceinline__ words4 philox(uint32_t c0, uint32_t c1, uint32_t c2, 
     return {{c0, c1, c2, c3}};
 }
 
-// y[e] = word(e) >= threshold ? x[e] * scale : 0, for four elements of one counter a thread.
+// y[e] = word(e) >= threshold ? x[e] * scale : 0, sixteen bytes a thread: four elements of one counter, or eight of two.
 // state: seed (low, high word), number of the mini-batch - read from memory, so that a captured launch draws anew when it is replayed
-template <class T>
-__global__ __launch_bounds__(TPB) void k_dropout(const T *x, T *y, const T *old, const T *gate, size_t n, uint32_t threshold, float scale,
-                                                 const uint32_t *__restrict__ state, uint32_t layer, uint32_t mb)
+// HBM bounds it: twenty products of 32 x 32 bits for four words are what the vector unit has time for beside 4 bytes an element
+// (2^28 bf16 elements, us: copy alone 209, this 212; seven rounds 211).  other: a residual sum y = [relu](round(dropped x) + other).
+enum { PLAIN, GRADIENT, SUM };
+template <class T> struct DropArgs {
+    const T *x;
+    T *y;
+    const T *old, *gate;      // GRADIENT: see grad_out(); SUM: old is the other summand
+    size_t n;
+    uint32_t threshold;
+    float scale;
+    const uint32_t *state;
+    uint32_t layer, mb;
+    int relu;
+};
+
+template <class T, int MODE>
+__global__ __launch_bounds__(TPB) void k_dropout(DropArgs<T> p)
 {
-    const size_t i = (size_t)blockIdx.x * TPB + threadIdx.x, e0 = i * 4;
-    if (e0 >= n) return;
-    const words4 r = philox((uint32_t)i, layer, mb, state[2], state[0], state[1]);
+    constexpr int V = 16 / sizeof(T);
+    struct vec {
+        T e[V];
+    };
+    const size_t i = (size_t)blockIdx.x * TPB + threadIdx.x, e0 = i * V;
+    if (e0 >= p.n) return;
+    // at any address of T; the tensor's last elements one by one
+    const int left = p.n - e0 < V ? (int)(p.n - e0) : V;
+    auto load = [&](const T *from) {
+        vec v;
+        if (left == V) __builtin_memcpy(&v, from + e0, sizeof v);
+        else
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const size_t e = e0 + j;
-        if (e >= n) break;
-        const float v = r.w[j] >= threshold ? to_f32(x[e]) * scale : 0.0f;
-        y[e] = grad_out<T>(v, old != nullptr, old ? old[e] : from_f32<T>(0.0f), gate != nullptr, gate ? gate[e] : from_f32<T>(0.0f));
+            for (int j = 0; j < V; ++j) v.e[j] = j < left ? from[e0 + j] : T{};
+        return v;
+    };
+    const vec x = load(p.x);
+    vec old = {}, gate = {}, y;
+    if (MODE == SUM || (MODE == GRADIENT && p.old)) old = load(p.old);
+    if (MODE == GRADIENT && p.gate) gate = load(p.gate);
+    const uint32_t k0 = p.state[0], k1 = p.state[1], mini_batch = p.state[2];
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) {
+        const words4 r = philox((uint32_t)(i * (V / 4) + q), p.layer, p.mb, mini_batch, k0, k1);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int e = q * 4 + j;
+            const float v = r.w[j] >= p.threshold ? to_f32(x.e[e]) * p.scale : 0.0f;
+            if (MODE == PLAIN) y.e[e] = from_f32<T>(v);
+            else if (MODE == GRADIENT) y.e[e] = grad_out<T>(v, p.old != nullptr, old.e[e], p.gate != nullptr, gate.e[e]);
+            else {
+                const float sum = round_to<T>(v) + to_f32(old.e[e]);
+                y.e[e] = from_f32<T>(p.relu ? fmaxf(sum, 0.0f) : sum);
+            }
+        }
     }
+    if (left == V) __builtin_memcpy(p.y + e0, &y, sizeof y);
+    else
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (j < left) p.y[e0 + j] = y.e[j];
 }
 
 __global__ void k_dropout_set(uint32_t *state, uint32_t low, uint32_t high, uint32_t mini_batch)
@@ -55,23 +100,37 @@ __global__ void k_dropout_next(uint32_t *state) { state[2] += 1; }
 
 }  // namespace
 
-hipError_t dropout(int dt, const void *x, void *y, GradEpi epi, size_t n, float p, const uint32_t *state, uint32_t layer, uint32_t mb,
-                   hipStream_t s)
+template <class T, int MODE>
+static hipError_t launch(const void *x, void *y, const void *old, const void *gate, int relu, size_t n, float p, const uint32_t *state, uint32_t layer,
+                         uint32_t mb, hipStream_t s)
 {
     if (n == 0) return hipSuccess;
     // dropped where a word is below 2^32 p, which a probability just under one would round up to
     const double t = (double)p * 4294967296.0 + 0.5;
-    const uint32_t threshold = t < 4294967295.0 ? (uint32_t)t : 0xFFFFFFFFu;
-    const float scale = (float)(1.0 / (1.0 - (double)p));
-    const void *old = epi.accum ? (epi.accum_from ? epi.accum_from : y) : nullptr;
-    const dim3 grid((unsigned)((n + 4 * TPB - 1) / (4 * TPB)));
-    if (dt == DT_F32)
-        hipLaunchKernelGGL((k_dropout<float>), grid, dim3(TPB), 0, s, (const float *)x, (float *)y, (const float *)old, (const float *)epi.gate, n,
-                           threshold, scale, state, layer, mb);
-    else
-        hipLaunchKernelGGL((k_dropout<bf16_t>), grid, dim3(TPB), 0, s, (const bf16_t *)x, (bf16_t *)y, (const bf16_t *)old, (const bf16_t *)epi.gate,
-                           n, threshold, scale, state, layer, mb);
+    DropArgs<T> a{(const T *)x, (T *)y, (const T *)old, (const T *)gate, n, t < 4294967295.0 ? (uint32_t)t : 0xFFFFFFFFu,
+                  (float)(1.0 / (1.0 - (double)p)), state, layer, mb, relu};
+    constexpr size_t per_block = TPB * (16 / sizeof(T));
+    hipLaunchKernelGGL((k_dropout<T, MODE>), dim3((unsigned)((n + per_block - 1) / per_block)), dim3(TPB), 0, s, a);
     return hipGetLastError();
+}
+
+hipError_t dropout(int dt, const void *x, void *y, GradEpi epi, size_t n, float p, const uint32_t *state, uint32_t layer, uint32_t mb,
+                   hipStream_t s)
+{
+    const void *old = epi.accum ? (epi.accum_from ? epi.accum_from : y) : nullptr;
+    const bool plain = !old && !epi.gate;
+    if (dt == DT_F32)
+        return plain ? launch<float, PLAIN>(x, y, nullptr, nullptr, 0, n, p, state, layer, mb, s)
+                     : launch<float, GRADIENT>(x, y, old, epi.gate, 0, n, p, state, layer, mb, s);
+    return plain ? launch<bf16_t, PLAIN>(x, y, nullptr, nullptr, 0, n, p, state, layer, mb, s)
+                 : launch<bf16_t, GRADIENT>(x, y, old, epi.gate, 0, n, p, state, layer, mb, s);
+}
+
+hipError_t dropout_add(int dt, const void *x, const void *other, void *y, int relu, size_t n, float p, const uint32_t *state, uint32_t layer,
+                       uint32_t mb, hipStream_t s)
+{
+    if (dt == DT_F32) return launch<float, SUM>(x, y, other, nullptr, relu, n, p, state, layer, mb, s);
+    return launch<bf16_t, SUM>(x, y, other, nullptr, relu, n, p, state, layer, mb, s);
 }
 
 hipError_t dropout_set(uint32_t *state, uint64_t seed, uint32_t mini_batch, hipStream_t s)

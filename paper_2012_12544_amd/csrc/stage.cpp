@@ -87,6 +87,7 @@ struct Layer {
     // input-gradient kernel leaves the per-tile sums of dy and dy*xhat for that batch-norm's backward
     int bnb_chunks = 0;
     bool bwd_sums_given = false;
+    int drop = -1;         // ADD: the DROPOUT (layer index) that its pass does as well, which is then `fused`
     int fuse_add = -1;     // batch-norm: the residual ADD (layer index) whose sum this layer's normalisation pass stores
     // LSTM: per in-flight micro-batch the slot keeps the gates and cell states (float), the delayed
     // copy of h that the recurrent products read, the buffer shared by the input projection
@@ -721,7 +722,12 @@ int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
     case BAPIPE_ADD: {
         if (L.fused) break;                       // stored by the batch-norm that feeds it
         const bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
-        HIPCHK(add_fwd(dt, a, in_ptr(st, L.b, c), o, L.d.fuse_relu, O.elems, s));
+        if (L.drop >= 0) {
+            const Layer &D = st->layers[L.drop];
+            HIPCHK(dropout_add(dt, in_ptr(st, D.a, c), in_ptr(st, L.a == D.o ? L.b : L.a, c), out_ptr(st, L, c, dt_size(dt)), L.d.fuse_relu, O.elems,
+                               D.d.eps, st->dropout_state, dropout_layer(st, L.drop), c.mbid, s));
+        } else
+            HIPCHK(add_fwd(dt, a, in_ptr(st, L.b, c), o, L.d.fuse_relu, O.elems, s));
         st->tap_end(tp, 0.0, 3.0 * O.bytes());
         break;
     }
@@ -753,6 +759,7 @@ int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
         break;
     }
     case BAPIPE_DROPOUT: {
+        if (L.fused) break;                       // done by the ADD that reads it
         GradEpi none{nullptr, 0};
         const bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
         HIPCHK(dropout(dt, a, out_ptr(st, L, c, dt_size(dt)), none, O.elems, L.d.eps, st->dropout_state, dropout_layer(st, li), c.mbid, s));
@@ -1452,6 +1459,19 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         if (Bn.d.kind != BAPIPE_BATCHNORM2D || Bn.d.fuse_relu || T.consumers.size() != 1 || T.stashed || t == last_t) continue;
         Bn.fuse_add = i;
         S.fused = true;
+    }
+    // dropout -> residual ADD: the same where the ADD is a dropout's only reader.  What the dropout reads keeps its place until then
+    for (int i = 0; i < n_layers; ++i) {
+        Layer &S = st->layers[i];
+        if (S.d.kind != BAPIPE_ADD || S.fused) continue;
+        for (int t : {S.b, S.a}) {
+            if (t == 0 || root_of(t) != t || t == last_t || st->tensors[t].consumers.size() != 1 || st->tensors[t].stashed) continue;
+            Layer &D = st->layers[t - 1];
+            if (D.d.kind != BAPIPE_DROPOUT) continue;
+            S.drop = t - 1;
+            D.fused = true;
+            break;
+        }
     }
     size_t work = 256, flush = 0, grouped = 0;
     for (int i = 0; i < n_layers; ++i) {
