@@ -216,7 +216,7 @@ hipError_t gated_fwd(int dt, int act, const void *x, const void *w, const float 
                      void *workspace, hipStream_t s);
 hipError_t gated_grad(int dt, int act, const void *dh, const float *P, void *D, int rows, int F, hipStream_t s);
 // the other two products where gated_mfma says no
-hipError_t gated_dgrad_direct(int dt, const void *D, const void *wt, void *dx, GradEpi epi, int rows, int C, int F, hipStream_t s);
+hipError_t gated_dgrad_direct(int dt, const void *D, const void *wt, void *dx, GradEpi epi, int rows, int C, int F, void *workspace, hipStream_t s);
 hipError_t gated_wgrad_direct(int dt, const void *x, const void *D, float *dw, float *db, int rows, int C, int F, void *workspace, hipStream_t s);
 
 // ---- dropout (kernels_dropout.hip): y[e] = word(e) >= 2^32 p ? x[e] / (1-p) : 0, or with the gradient epilogue the same of dy

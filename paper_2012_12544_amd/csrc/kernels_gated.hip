@@ -4,49 +4,105 @@
 // g and u are kept in float for the backward pass, P [rows][2F].  Rounded to bf16 they were, with D's own rounding, what a
 // bf16 layer's gradients were off by most: 3.0e-3 of dW and dx against 64 bits (2-norm), 2.3e-3 so.
 // Products of bf16 whose widths are multiples of 8 run on the bf16 matrix cores, the others on the float ones.
-#include "dev_common.h"
 #include "kernels.h"
+#include "mfma_common.h"
+#include <type_traits>
 
 namespace bapipe {
 namespace {
 
 constexpr int TPB = 256;
-typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef f32x16_t f32x16;
 
-// act(g) and its derivative.  A ReLU's derivative at 0 is 0, as everywhere in the library.
-__device__ __forceinline__ float act_value(int act, float g)
+// act(g), and its derivative.  A ReLU's derivative at 0 is 0, as everywhere in the library.  A float layer takes the library's
+// exp and erfc; for a bf16 one, whose results are rounded to 8 bits, the hardware's exp2 and reciprocal (a few 2^-24 off, times |g|)
+// and, with t = 1 / (1 + 0.4 x), erfc(x) = exp(-x^2) t q(t), q a polynomial of degree 8 fitted here to erfcx(x) / t over
+// x >= 0 for the least largest relative error: 2.8e-7 in float arithmetic, in the tail as well, where 1 + erf is all
+// cancellation.  The library's erfc was a quarter of the forward kernel's time.
+template <class T> constexpr bool kFast = sizeof(T) == 2;
+template <bool FAST> __device__ __forceinline__ float exp_of(float x) { return FAST ? __builtin_amdgcn_exp2f(x * 1.44269504088896341f) : expf(x); }
+template <bool FAST> __device__ __forceinline__ float sigmoid_of(float g)
+{
+    const float e = 1.0f + exp_of<FAST>(-g);
+    return FAST ? __builtin_amdgcn_rcpf(e) : 1.0f / e;
+}
+// the normal distribution's cdf at g, given e = exp(-g^2 / 2)
+template <bool FAST> __device__ __forceinline__ float cdf_of(float g, float e)
+{
+    if (!FAST) return 0.5f * erfcf(-g * 0.70710678118654752f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.4f * 0.70710678118654752f, 1.0f));
+    float q = 0.05026213f;
+    q = fmaf(q, t, -0.18290149f);
+    q = fmaf(q, t, 0.16908546f);
+    q = fmaf(q, t, -0.00560756f);
+    q = fmaf(q, t, 0.14143144f);
+    q = fmaf(q, t, 0.16854198f);
+    q = fmaf(q, t, 0.2078427f);
+    q = fmaf(q, t, 0.2256696f);
+    q = fmaf(q, t, 0.22567586f);
+    const float half = 0.5f * t * q * e;                 // erfc(|x|) / 2
+    return g < 0.0f ? half : 1.0f - half;
+}
+template <bool FAST> __device__ __forceinline__ float act_value(int act, float g)
 {
     if (act == ACT_RELU) return fmaxf(g, 0.0f);
-    if (act == ACT_GELU) return g * (0.5f * erfcf(-g * 0.70710678118654752f));
-    const float s = 1.0f / (1.0f + expf(-g));
+    if (act == ACT_GELU) return g * cdf_of<FAST>(g, FAST ? exp_of<FAST>(-0.5f * g * g) : 0.0f);
+    const float s = sigmoid_of<FAST>(g);
     return act == ACT_SIGMOID ? s : g * s;
 }
-__device__ __forceinline__ void act_both(int act, float g, float &a, float &da)
+template <bool FAST> __device__ __forceinline__ void act_both(int act, float g, float &a, float &da)
 {
     if (act == ACT_RELU) {
         a = fmaxf(g, 0.0f);
         da = g > 0.0f ? 1.0f : 0.0f;
     } else if (act == ACT_GELU) {
-        const float cdf = 0.5f * erfcf(-g * 0.70710678118654752f);
+        const float e = exp_of<FAST>(-0.5f * g * g), cdf = cdf_of<FAST>(g, e);
         a = g * cdf;
-        da = cdf + g * expf(-0.5f * g * g) * 0.39894228040143268f;
+        da = fmaf(g * e, 0.39894228040143268f, cdf);
     } else {
-        const float s = 1.0f / (1.0f + expf(-g));
+        const float s = sigmoid_of<FAST>(g);
         a = act == ACT_SIGMOID ? s : g * s;
         da = act == ACT_SIGMOID ? s * (1.0f - s) : s * (1.0f + g * (1.0f - s));
     }
 }
 
-// Products on the float matrix cores (v_mfma_f32_32x32x2_f32, true float products), for any sizes: 128 x 128 of the output per block, a
-// wave 64 x 64 of it, 16 of the contracted dimension at a time, two such tiles in LDS, the next one's loads in flight in registers.
-constexpr int TILE = 128, DEPTH = 16;
-// [row][k] tiles: 20 floats a row, so that the 16-byte reads of eight neighbouring rows lie on different banks
-constexpr int PITCH = DEPTH + 4;
+// ------------------------------------------------------------------ any sizes
+// Products of float, on the float matrix cores (v_mfma_f32_32x32x2_f32, true float products), and of bf16 whose rows are no multiple
+// of 16 bytes.  Operands pass through registers, 16 bytes in one access at any address (global memory needs no more
+// alignment than an element's), a row's last ones one by one.  A block is 2 x 2 waves of 32 TM x 32 TN outputs; two tiles of the
+// contracted dimension in LDS, the next one's loads in flight while this one's products run.
+
+// 16 bytes of a row of which `left` elements are inside
+template <class T> __device__ __forceinline__ chunk16 load_chunk(const T *from, int left)
+{
+    constexpr int V = 16 / sizeof(T);
+    chunk16 c = {0u, 0u, 0u, 0u};
+    if (left >= V) __builtin_memcpy(&c, from, 16);
+    else if (left > 0) {
+        T e[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) e[j] = j < left ? from[j] : T{};
+        __builtin_memcpy(&c, e, 16);
+    }
+    return c;
+}
+
+// 32 x 32 products of two operands' rows over the 32 bytes of K that the two halves of a wave hold 16 bytes of each
+template <class T> __device__ __forceinline__ void multiply(f32x16 &acc, chunk16 a, chunk16 b)
+{
+    if constexpr (sizeof(T) == 2) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_frag(a), as_frag(b), acc, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[j]), __uint_as_float(b[j]), acc, 0, 0, 0);
+    }
+}
 
 enum { NT_FORWARD, NT_GRAD };
 struct NtArgs {
     const void *a, *b;        // [M][K], [N][K] (forward: [2N][K])
-    int M, N, K;
+    int M, N, K, k_per_split; // K split over blockIdx.y: part[split][M][N] (forward: [2N]) instead of the outputs
+    float *part;
     const float *bias;        // forward
     float *P;                 // forward: both projections [M][2N]
     void *out;                // h [M][N], or dx [M][N]
@@ -54,158 +110,187 @@ struct NtArgs {
     int act;
 };
 
-template <class T, int MODE>
+template <class T, int MODE, int TM, int TN>
 __global__ __launch_bounds__(TPB) void k_gated_nt(NtArgs p)
 {
-    __shared__ __align__(16) float lds[2][2][TILE][PITCH];
+    constexpr int V = 16 / sizeof(T), NQ = sizeof(T) == 2 ? 4 : 2, CPR = 2 * NQ, DEPTH = CPR * V;      // of K a tile
+    constexpr int PITCH = CPR * 16 + 16;           // bytes of a row: the reads of eight neighbouring rows lie on different banks
+    constexpr int RA = 64 * TM, RB = 64 * TN, LA = RA * CPR / TPB, LB = RB * CPR / TPB, ROWS = TPB / CPR;
+    constexpr bool FWD = MODE == NT_FORWARD;
+    static_assert(!FWD || TN == 2, "a wave has gates and linear parts of 32 units");
+    constexpr int WIDE = FWD ? RB / 2 : RB;        // outputs across
+    __shared__ __align__(16) unsigned char lds[2][(RA + RB) * PITCH];
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, wm = wave / 2, wn = wave % 2;
-    const T *a = (const T *)p.a, *b = (const T *)p.b;
-    constexpr int WIDE = MODE == NT_FORWARD ? TILE / 2 : TILE;
-    const int across = (p.N + WIDE - 1) / WIDE, m0 = blockIdx.x / across * TILE, n0 = blockIdx.x % across * WIDE;
-    // thread's elements: column tid % 16 of rows tid / 16 + 16 i
-    const int k = tid % DEPTH, r0 = tid / DEPTH;
-    constexpr int EACH = TILE * DEPTH / TPB;
-    float ra[EACH], rb[EACH];
-    auto weight_row = [&](int r) -> int {      // row of b behind row r of its tile, or -1
-        if (MODE == NT_GRAD) return n0 + r < p.N ? n0 + r : -1;
-        const int unit = n0 + r / 64 * 32 + r % 32;      // 32 units' gates, then the same units' linear parts
-        return unit < p.N ? (r % 64 < 32 ? unit : p.N + unit) : -1;
-    };
-    auto load = [&](int k0) {
+    const int across = (p.N + WIDE - 1) / WIDE, m0 = blockIdx.x / across * RA, n0 = blockIdx.x % across * WIDE;
+    const int first = blockIdx.y * p.k_per_split, last = first + p.k_per_split < p.K ? first + p.k_per_split : p.K;
+    // thread's chunks: column tid % CPR of rows tid / CPR + ROWS i
+    const int c = tid % CPR * V, r0 = tid / CPR;
+    const T *pa[LA], *pb[LB];
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int r = r0 + i * (TPB / DEPTH), wr = weight_row(r);
-            const bool in = k0 + k < p.K;
-            ra[i] = in && m0 + r < p.M ? to_f32(a[(size_t)(m0 + r) * p.K + k0 + k]) : 0.0f;
-            rb[i] = in && wr >= 0 ? to_f32(b[(size_t)wr * p.K + k0 + k]) : 0.0f;
-        }
-    };
-    auto store = [&](int buf) {
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            lds[buf][0][r0 + i * (TPB / DEPTH)][k] = ra[i];
-            lds[buf][1][r0 + i * (TPB / DEPTH)][k] = rb[i];
-        }
-    };
-    f32x16 acc[2][2] = {};
-    const int steps = (p.K + DEPTH - 1) / DEPTH;
-    load(0);
-    store(0);
-    for (int s = 0; s < steps; ++s) {
-        __syncthreads();
-        if (s + 1 < steps) load((s + 1) * DEPTH);
-        const int buf = s & 1;
-#pragma unroll
-        for (int q = 0; q < DEPTH / 8; ++q) {
-            // the two halves of a wave take k and k + 4 of each product's pair
-            const int kk = q * 8 + lane / 32 * 4;
-            float4 fa[2], fb[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                fa[i] = *reinterpret_cast<const float4 *>(&lds[buf][0][wm * 64 + i * 32 + lane % 32][kk]);
-                fb[i] = *reinterpret_cast<const float4 *>(&lds[buf][1][wn * 64 + i * 32 + lane % 32][kk]);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[i].x, fb[j].x, acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[i].y, fb[j].y, acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[i].z, fb[j].z, acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[i].w, fb[j].w, acc[i][j], 0, 0, 0);
-                }
-        }
-        if (s + 1 < steps) store(buf ^ 1);
+    for (int i = 0; i < LA; ++i) {
+        const int row = m0 + r0 + ROWS * i;
+        pa[i] = row < p.M ? (const T *)p.a + (size_t)row * p.K : nullptr;
     }
-    // register r of lane l: row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < LB; ++i) {
+        const int r = r0 + ROWS * i;               // forward: 32 units' gates, then the same units' linear parts, for each wave
+        const int n = FWD ? n0 + r / 64 * 32 + r % 32 : n0 + r;
+        pb[i] = n < p.N ? (const T *)p.b + (size_t)(FWD && r % 64 >= 32 ? p.N + n : n) * p.K : nullptr;
+    }
+    chunk16 ca[LA], cb[LB];
+    auto load = [&](int k0) {
+        const int left = last - k0 - c;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = m0 + wm * 64 + i * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
-            if (row >= p.M) continue;
-            if (MODE == NT_FORWARD) {
-                const int unit = n0 + wn * 32 + lane % 32;
-                if (unit >= p.N) continue;
-                const float g = acc[i][0][r] + (p.bias ? p.bias[unit] : 0.0f), u = acc[i][1][r] + (p.bias ? p.bias[p.N + unit] : 0.0f);
-                float *P = p.P + (size_t)row * 2 * p.N + unit;
-                P[0] = g;
-                P[p.N] = u;
-                ((T *)p.out)[(size_t)row * p.N + unit] = from_f32<T>(act_value(p.act, g) * u);
-            } else {
+        for (int i = 0; i < LA; ++i) ca[i] = load_chunk(pa[i] + k0 + c, pa[i] ? left : 0);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int col = n0 + wn * 64 + j * 32 + lane % 32;
-                    if (col >= p.N) continue;
-                    const size_t at = (size_t)row * p.N + col;
-                    const T *old = (const T *)p.old, *gate = (const T *)p.gate;
-                    ((T *)p.out)[at] = grad_out<T>(acc[i][j][r], old != nullptr, old ? old[at] : from_f32<T>(0.0f), gate != nullptr,
-                                                   gate ? gate[at] : from_f32<T>(0.0f));
-                }
-            }
-        }
-}
-
-// dw[M][N] += a^T b with a [rows][M], b [rows][N], over the rows of split blockIdx.y; with several splits part[split][M][N] = their sums
-template <class T>
-__global__ __launch_bounds__(TPB) void k_gated_tn(const T *__restrict__ a, const T *__restrict__ b, int rows, int M, int N, int rows_per_split,
-                                                  float *dw, float *part)
-{
-    __shared__ __align__(16) float lds[2][2][DEPTH][TILE];
-    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, wm = wave / 2, wn = wave % 2;
-    const int across = (N + TILE - 1) / TILE, m0 = blockIdx.x / across * TILE, n0 = blockIdx.x % across * TILE;
-    const int first = blockIdx.y * rows_per_split, last = first + rows_per_split < rows ? first + rows_per_split : rows;
-    const int c = tid % TILE, r0 = tid / TILE;
-    constexpr int EACH = TILE * DEPTH / TPB;
-    float ra[EACH], rb[EACH];
-    auto load = [&](int at) {
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int r = at + r0 + i * (TPB / TILE);
-            ra[i] = r < last && m0 + c < M ? to_f32(a[(size_t)r * M + m0 + c]) : 0.0f;
-            rb[i] = r < last && n0 + c < N ? to_f32(b[(size_t)r * N + n0 + c]) : 0.0f;
-        }
+        for (int i = 0; i < LB; ++i) cb[i] = load_chunk(pb[i] + k0 + c, pb[i] ? left : 0);
     };
     auto store = [&](int buf) {
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            lds[buf][0][r0 + i * (TPB / TILE)][c] = ra[i];
-            lds[buf][1][r0 + i * (TPB / TILE)][c] = rb[i];
-        }
+        for (int i = 0; i < LA; ++i) *reinterpret_cast<chunk16 *>(&lds[buf][(r0 + ROWS * i) * PITCH + tid % CPR * 16]) = ca[i];
+#pragma unroll
+        for (int i = 0; i < LB; ++i) *reinterpret_cast<chunk16 *>(&lds[buf][(RA + r0 + ROWS * i) * PITCH + tid % CPR * 16]) = cb[i];
     };
-    f32x16 acc[2][2] = {};
+    f32x16 acc[TM][TN] = {};
     const int steps = (last - first + DEPTH - 1) / DEPTH;
     load(first);
     store(0);
     for (int s = 0; s < steps; ++s) {
         __syncthreads();
         if (s + 1 < steps) load(first + (s + 1) * DEPTH);
-        const int buf = s & 1;
+        const unsigned char *buf = lds[s & 1];
 #pragma unroll
-        for (int q = 0; q < DEPTH / 2; ++q) {
-            const int kk = q * 2 + lane / 32;
-            float fa[2], fb[2];
+        for (int q = 0; q < NQ; ++q) {
+            const int at = (2 * q + lane / 32) * 16;
+            chunk16 fa[TM], fb[TN];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                fa[i] = lds[buf][0][kk][wm * 64 + i * 32 + lane % 32];
-                fb[i] = lds[buf][1][kk][wn * 64 + i * 32 + lane % 32];
-            }
+            for (int i = 0; i < TM; ++i) fa[i] = *reinterpret_cast<const chunk16 *>(buf + ((wm * TM + i) * 32 + lane % 32) * PITCH + at);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < TN; ++i) fb[i] = *reinterpret_cast<const chunk16 *>(buf + (RA + (wn * TN + i) * 32 + lane % 32) * PITCH + at);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[i], fb[j], acc[i][j], 0, 0, 0);
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) multiply<T>(acc[i][j], fa[i], fb[j]);
         }
-        if (s + 1 < steps) store(buf ^ 1);
+        if (s + 1 < steps) store((s + 1) & 1);
     }
+    // register r of lane l: row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const int row = m0 + wm * 64 + i * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
+            const int row = m0 + (wm * TM + i) * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
+            if (row >= p.M) continue;
+            if constexpr (FWD) {
+                const int unit = n0 + wn * 32 + lane % 32;
+                if (unit >= p.N) continue;
+                float *P = (p.part ? p.part + (size_t)blockIdx.y * p.M * 2 * p.N : p.P) + (size_t)row * 2 * p.N + unit;
+                const float g = acc[i][0][r] + (!p.part && p.bias ? p.bias[unit] : 0.0f), u = acc[i][1][r] + (!p.part && p.bias ? p.bias[p.N + unit] : 0.0f);
+                P[0] = g;
+                P[p.N] = u;
+                if (!p.part) ((T *)p.out)[(size_t)row * p.N + unit] = from_f32<T>(act_value<kFast<T>>(p.act, g) * u);
+            } else {
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    const int col = n0 + (wn * TN + j) * 32 + lane % 32;
+                    if (col >= p.N) continue;
+                    const size_t at = (size_t)row * p.N + col;
+                    const T *old = (const T *)p.old, *gate = (const T *)p.gate;
+                    if (p.part) p.part[(size_t)blockIdx.y * p.M * p.N + at] = acc[i][j][r];
+                    else
+                        ((T *)p.out)[at] = grad_out<T>(acc[i][j][r], old != nullptr, old ? old[at] : from_f32<T>(0.0f), gate != nullptr,
+                                                       gate ? gate[at] : from_f32<T>(0.0f));
+                }
+            }
+        }
+}
+
+// dw[M][N] += a^T b with a [rows][M], b [rows][N], over the rows of split blockIdx.y; with several splits part[split][M][N] = their sums.
+// A step is 32 rows of bf16, read across the rows by transposing reads (tr_frag), or 16 of float.
+template <class T, int TM, int TN>
+__global__ __launch_bounds__(TPB) void k_gated_tn(const T *__restrict__ a, const T *__restrict__ b, int rows, int M, int N, int rows_per_split,
+                                                  float *dw, float *part)
+{
+    constexpr int V = 16 / sizeof(T), DEPTH = sizeof(T) == 2 ? 32 : 16, CA = 64 * TM, CB = 64 * TN;
+    constexpr int LA = DEPTH * CA / V / TPB, LB = DEPTH * CB / V / TPB;
+    static_assert(LA >= 1 && LB >= 1, "a chunk for every thread");
+    __shared__ __align__(16) T lds[2][DEPTH * (CA + CB)];
+    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, wm = wave / 2, wn = wave % 2;
+    const int across = (N + CB - 1) / CB, m0 = blockIdx.x / across * CA, n0 = blockIdx.x % across * CB;
+    const int first = blockIdx.y * rows_per_split, last = first + rows_per_split < rows ? first + rows_per_split : rows;
+    chunk16 ca[LA], cb[LB];
+    auto fetch = [&](auto &to, const T *from, int width, int c0, int at, auto columns) {
+        constexpr int CPR = decltype(columns)::value / V;
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(to) / sizeof(to[0])); ++i) {
+            const int id = tid + TPB * i, r = at + id / CPR, c = c0 + id % CPR * V;
+            to[i] = load_chunk(from + (size_t)r * width + c, r < last ? width - c : 0);
+        }
+    };
+    auto load = [&](int at) {
+        fetch(ca, a, M, m0, at, std::integral_constant<int, CA>{});
+        fetch(cb, b, N, n0, at, std::integral_constant<int, CB>{});
+    };
+    auto put = [&](T *tile, auto &from, auto columns) {
+        constexpr int C = decltype(columns)::value, CPR = C / V;
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(from) / sizeof(from[0])); ++i) {
+            const int id = tid + TPB * i, r = id / CPR, c = id % CPR;
+            const int slot = sizeof(T) == 2 ? ((((c >> 1) ^ wg_swz<C>(r)) << 1) | (c & 1)) : c;
+            *reinterpret_cast<chunk16 *>(tile + r * C + slot * V) = from[i];
+        }
+    };
+    auto store = [&](int buf) {
+        put(lds[buf], ca, std::integral_constant<int, CA>{});
+        put(lds[buf] + DEPTH * CA, cb, std::integral_constant<int, CB>{});
+    };
+    f32x16 acc[TM][TN] = {};
+    const int steps = (last - first + DEPTH - 1) / DEPTH;
+    load(first);
+    store(0);
+    for (int s = 0; s < steps; ++s) {
+        __syncthreads();
+        if (s + 1 < steps) load(first + (s + 1) * DEPTH);
+        const T *ta = lds[s & 1], *tb = ta + DEPTH * CA;
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int q = 0; q < DEPTH / 16; ++q) {
+                bf16x8_t fa[TM], fb[TN];
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fa[i] = tr_frag<CA>((const uint16_t *)ta, (wm * TM + i) * 32, q * 16, lane);
+#pragma unroll
+                for (int i = 0; i < TN; ++i) fb[i] = tr_frag<CB>((const uint16_t *)tb, (wn * TN + i) * 32, q * 16, lane);
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < DEPTH / 2; ++q) {
+                const int k = q * 2 + lane / 32;
+                float fa[TM], fb[TN];
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fa[i] = ta[k * CA + (wm * TM + i) * 32 + lane % 32];
+#pragma unroll
+                for (int i = 0; i < TN; ++i) fb[i] = tb[k * CB + (wn * TN + i) * 32 + lane % 32];
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[i], fb[j], acc[i][j], 0, 0, 0);
+            }
+        }
+        if (s + 1 < steps) store((s + 1) & 1);
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = m0 + (wm * TM + i) * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
             if (row >= M) continue;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int col = n0 + wn * 64 + j * 32 + lane % 32;
+            for (int j = 0; j < TN; ++j) {
+                const int col = n0 + (wn * TN + j) * 32 + lane % 32;
                 if (col >= N) continue;
                 if (part) part[((size_t)blockIdx.y * M + row) * N + col] = acc[i][j][r];
                 else dw[(size_t)row * N + col] += acc[i][j][r];
@@ -213,28 +298,52 @@ __global__ __launch_bounds__(TPB) void k_gated_tn(const T *__restrict__ a, const
         }
 }
 
-// dw[i] += the sums of all splits, in their order
+// dw[i] += the sums of all splits, in their order; n a multiple of V
+template <int V>
 __global__ __launch_bounds__(TPB) void k_gated_tn_join(const float *__restrict__ part, int splits, size_t n, float *dw)
+{
+    const size_t i = ((size_t)blockIdx.x * TPB + threadIdx.x) * V;
+    if (i >= n) return;
+    typedef vec_t<float, V> vec;
+    vec sum = {};
+    for (int k = 0; k < splits; ++k) {
+        const vec v = *reinterpret_cast<const vec *>(part + (size_t)k * n + i);
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum.e[j] += v.e[j];
+    }
+    vec d = *reinterpret_cast<vec *>(dw + i);
+#pragma unroll
+    for (int j = 0; j < V; ++j) d.e[j] += sum.e[j];
+    *reinterpret_cast<vec *>(dw + i) = d;
+}
+
+// dx from the sums of all splits, part[split][n]
+template <class T>
+__global__ __launch_bounds__(TPB) void k_gated_grad_join(const float *__restrict__ part, int splits, size_t n, T *out, const T *old, const T *gate)
 {
     const size_t i = (size_t)blockIdx.x * TPB + threadIdx.x;
     if (i >= n) return;
     float sum = 0.0f;
     for (int k = 0; k < splits; ++k) sum += part[(size_t)k * n + i];
-    dw[i] += sum;
+    out[i] = grad_out<T>(sum, old != nullptr, old ? old[i] : from_f32<T>(0.0f), gate != nullptr, gate ? gate[i] : from_f32<T>(0.0f));
 }
 
-// Projections of four units from the sums of a product whose K was in `splits` parts, part[split][rows][2F]; F a multiple of 4
+// Projections of V units from the sums of a product whose K was in `splits` parts, part[split][rows][2F]; F a multiple of V, h aligned
+// to V elements
+template <class T, int V>
 __global__ __launch_bounds__(TPB) void k_gated_join(const float *__restrict__ part, int splits, const float *__restrict__ bias, float *__restrict__ P,
-                                                    bf16_t *__restrict__ h, int rows, int F, int act)
+                                                    T *__restrict__ h, int rows, int F, int act)
 {
-    const size_t i = ((size_t)blockIdx.x * TPB + threadIdx.x) * 4, n = (size_t)rows * F;
+    typedef vec_t<float, V> vecf;
+    const size_t i = ((size_t)blockIdx.x * TPB + threadIdx.x) * V, n = (size_t)rows * F;
     if (i >= n) return;
     const size_t row = i / F, at = row * 2 * F + (i - row * F);
     const int unit = (int)(i - row * F);
-    float4 g = make_float4(0.f, 0.f, 0.f, 0.f), u = g;
-    auto add = [](float4 &t, const float *from) {
-        const float4 v = *reinterpret_cast<const float4 *>(from);
-        t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+    vecf g = {}, u = {};
+    auto add = [](vecf &t, const float *from) {
+        const vecf v = *reinterpret_cast<const vecf *>(from);
+#pragma unroll
+        for (int j = 0; j < V; ++j) t.e[j] += v.e[j];
     };
     for (int k = 0; k < splits; ++k) {
         add(g, part + (size_t)k * 2 * n + at);
@@ -244,12 +353,12 @@ __global__ __launch_bounds__(TPB) void k_gated_join(const float *__restrict__ pa
         add(g, bias + unit);
         add(u, bias + F + unit);
     }
-    *reinterpret_cast<float4 *>(P + at) = g;
-    *reinterpret_cast<float4 *>(P + at + F) = u;
-    uint2 v;
-    v.x = pack_bf16(act_value(act, g.x) * u.x, act_value(act, g.y) * u.y);
-    v.y = pack_bf16(act_value(act, g.z) * u.z, act_value(act, g.w) * u.w);
-    *reinterpret_cast<uint2 *>(h + i) = v;
+    *reinterpret_cast<vecf *>(P + at) = g;
+    *reinterpret_cast<vecf *>(P + at + F) = u;
+    vec_t<T, V> v;
+#pragma unroll
+    for (int j = 0; j < V; ++j) v.e[j] = from_f32<T>(act_value<kFast<T>>(act, g.e[j]) * u.e[j]);
+    *reinterpret_cast<vec_t<T, V> *>(h + i) = v;
 }
 
 // D from dh and the projections, V units a thread (F a multiple of V, dh aligned to V elements)
@@ -267,7 +376,7 @@ __global__ __launch_bounds__(TPB) void k_gated_grad(const T *__restrict__ dh, co
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         float a, da;
-        act_both(act, g.e[j], a, da);
+        act_both<kFast<T>>(act, g.e[j], a, da);
         const float v = to_f32(d.e[j]);
         dg.e[j] = from_f32<T>(v * u.e[j] * da);
         du.e[j] = from_f32<T>(v * a);
@@ -276,21 +385,170 @@ __global__ __launch_bounds__(TPB) void k_gated_grad(const T *__restrict__ dh, co
     *reinterpret_cast<vec *>(D + at + F) = du;
 }
 
-struct TnPlan {
-    int splits, rows_per_split;
+// ------------------------------------------------------------------ bf16, many rows: both projections, activation and product in one kernel
+// A block takes BP rows and BU units, a tile of 2 BU weight rows: their gates' and their linear parts'.  A wave has WT_P rows
+// of WT_U units, gates and linear parts of the same units in the same lanes, so that the activation meets both in registers.
+// Tiles of 64 of K come HBM / L2 -> LDS without passing registers into a ring of two (see mfma_common.h; the swizzle of a tile's
+// 16-byte chunks is applied by choosing which one a lane fetches).  Fragments are read one step of 16 ahead of the products that
+// need them; the barrier that publishes the next tile lies before a tile's last products, when every wave has all of the tile in registers, and
+// the slot is filled again at once.
+// `rest`: x is the sum of two tensors; K is walked twice with the same weights.
+struct MmArgs {
+    const bf16_t *x, *rest, *w;      // [rows][K], [2F][K]
+    int rows, K, F;
+    const float *bias;
+    float *P;                        // [rows][2F]
+    bf16_t *out;                     // h [rows][F]
+    unsigned x_bytes, w_bytes;
+    int tiles_p, tiles_u, act;
 };
-// two blocks for every unit, splits of 256 rows at the least
-TnPlan tn_plan(int rows, int M, int N)
+
+// Rows of tiles that go together: the 32 blocks that an XCD's units run at a time are then about 8 x 4 tiles and ask the L2 for 12 operand
+// tiles, in one row of tiles for 33
+constexpr int MM_ROWS = 8;
+
+template <int BP, int BU, int WP, int WU>
+__global__ __launch_bounds__(WP *WU * 64, 2) void k_gated_mfma(MmArgs p)
 {
-    const long long tiles = (long long)((M + TILE - 1) / TILE) * ((N + TILE - 1) / TILE);
-    long long splits = 512 / tiles;
-    const long long most = (rows + 255) / 256;
+    constexpr int NW = WP * WU, BK = 64, BC = 2 * BU, STAGE = (BP + BC) * BK;
+    constexpr int XL = BP / (8 * NW), WL = BC / (8 * NW);       // wave-wide loads a tile, 8 rows each
+    constexpr int TP = BP / WP / 32, TU = BU / WU / 32, KSUB = BK / 16;
+    static_assert(XL >= 1 && WL >= 1 && TP >= 1 && TU >= 1, "tile and waves");
+    extern __shared__ __align__(16) unsigned char smem[];
+    const lds_addr_of lds_of(smem);
+    uint16_t *ring = reinterpret_cast<uint16_t *>(smem);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wp = wave % WP, wu = wave / WP;
+    auto swz = [](int row) { return (row >> 1) & 7; };
+    const int lrow = lane / 8, lc = (lane % 8) ^ swz(wave * 8 + lrow);      // the same for every load: they lie 8 NW rows apart
+
+    const int bid = xcd_remap(blockIdx.x, gridDim.x);
+    const int per = MM_ROWS * p.tiles_u, first = bid / per * MM_ROWS, here = p.tiles_p - first < MM_ROWS ? p.tiles_p - first : MM_ROWS;
+    const int row0 = (first + bid % per % here) * BP, unit0 = bid % per / here * BU;
+
+    constexpr unsigned OOB = 0x80000000u;
+    __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(p.x), 0, (int)p.x_bytes, 0x00020000);
+    __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(p.w), 0, (int)p.w_bytes, 0x00020000);
+    // rows past the end lie behind the buffer and read zeros; gates past the last unit read linear parts, whose products nobody stores
+    unsigned xoff[XL], woff[WL];
+#pragma unroll
+    for (int i = 0; i < XL; ++i) xoff[i] = ((unsigned)(row0 + (i * NW + wave) * 8 + lrow) * (unsigned)p.K + 8u * lc) * 2u;
+#pragma unroll
+    for (int i = 0; i < WL; ++i) {
+        const int r = (i * NW + wave) * 8 + lrow, row = r < BU ? unit0 + r : p.F + unit0 + r - BU;
+        woff[i] = ((unsigned)row * (unsigned)p.K + 8u * lc) * 2u;
+    }
+    const int KT = (p.K + BK - 1) / BK, n_it = p.rest ? 2 * KT : KT;
+    int at = 0;                              // next tile to ask for
+    auto issue = [&](int slot) {
+        uint16_t *sw = ring + slot * STAGE, *sx = sw + BC * BK;
+        if (at == KT && p.rest) xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(p.rest), 0, (int)p.x_bytes, 0x00020000);
+        const int k0 = (at < KT ? at : at - KT) * BK;
+        const bool in = at < n_it && k0 + 8 * lc < p.K;
+        const unsigned ko = (unsigned)k0 * 2u;
+#pragma unroll
+        for (int i = 0; i < XL; ++i) dma16(xr, lds_of(sx + (i * NW + wave) * 8 * BK), in ? xoff[i] + ko : OOB);
+#pragma unroll
+        for (int i = 0; i < WL; ++i) dma16(wr, lds_of(sw + (i * NW + wave) * 8 * BK), in ? woff[i] + ko : OOB);
+        ++at;
+    };
+    f32x16 acc[TP][2 * TU];
+#pragma unroll
+    for (int a = 0; a < TP; ++a)
+#pragma unroll
+        for (int b = 0; b < 2 * TU; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.0f;
+    const int frow = lane & 31, fhalf = lane >> 5;
+    auto load_frags = [&](int slot, int k16, bf16x8_t(&fx)[TP], bf16x8_t(&fw)[2 * TU]) {
+        const uint16_t *cw = ring + slot * STAGE, *cx = cw + BC * BK;
+        const int ch = 2 * k16 + fhalf;
+#pragma unroll
+        for (int b = 0; b < 2 * TU; ++b) {
+            const int row = b / TU * BU + (wu * TU + b % TU) * 32 + frow;
+            fw[b] = as_frag(*reinterpret_cast<const chunk16 *>(cw + row * BK + ((ch ^ swz(row)) << 3)));
+        }
+#pragma unroll
+        for (int a = 0; a < TP; ++a) {
+            const int row = (wp * TP + a) * 32 + frow;
+            fx[a] = as_frag(*reinterpret_cast<const chunk16 *>(cx + row * BK + ((ch ^ swz(row)) << 3)));
+        }
+    };
+    auto products = [&](const bf16x8_t(&fx)[TP], const bf16x8_t(&fw)[2 * TU]) {
+#pragma unroll
+        for (int a = 0; a < TP; ++a)
+#pragma unroll
+            for (int b = 0; b < 2 * TU; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[a], fw[b], acc[a][b], 0, 0, 0);
+    };
+    issue(0);
+    issue(1);
+    WAIT_VMCNT(XL + WL);
+    WAIT_LGKMCNT(0);
+    __builtin_amdgcn_s_barrier();
+    bf16x8_t fx[2][TP], fw[2][2 * TU];
+    load_frags(0, 0, fx[0], fw[0]);
+    for (int it = 0; it < n_it; ++it) {
+        const int slot = it & 1;
+#pragma unroll
+        for (int j = 0; j + 1 < KSUB; ++j) {
+            load_frags(slot, j + 1, fx[(j + 1) & 1], fw[(j + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(0);               // keep the reads ahead of the products that hide them
+            products(fx[j & 1], fw[j & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        WAIT_LGKMCNT(0);                                     // this wave has read all of the tile
+        WAIT_VMCNT(0);                                       // its share of the next one has landed
+        __builtin_amdgcn_s_barrier();
+        load_frags(slot ^ 1, 0, fx[0], fw[0]);
+        __builtin_amdgcn_sched_barrier(0);
+        issue(slot);
+        products(fx[1], fw[1]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    WAIT_VMCNT(0);
+    // register r of lane l: row 8 (r / 4) + 4 (l / 32) + r % 4, unit l % 32
+#pragma unroll
+    for (int b = 0; b < TU; ++b) {
+        const int unit = unit0 + (wu * TU + b) * 32 + frow;
+        if (unit >= p.F) continue;
+        const float bg = p.bias ? p.bias[unit] : 0.0f, bu = p.bias ? p.bias[p.F + unit] : 0.0f;
+#pragma unroll
+        for (int a = 0; a < TP; ++a)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int row = row0 + (wp * TP + a) * 32 + 8 * (r / 4) + 4 * fhalf + r % 4;
+                if (row >= p.rows) continue;
+                const float g = acc[a][b][r] + bg, u = acc[a][TU + b][r] + bu;
+                float *P = p.P + (size_t)row * 2 * p.F + unit;
+                P[0] = g;
+                P[p.F] = u;
+                p.out[(size_t)row * p.F + unit] = from_f32<bf16_t>(act_value<true>(p.act, g) * u);
+            }
+    }
+}
+
+// How a product of any sizes is cut: tiles of 128 x 128, or 64 rows of them where there are few, and the contracted dimension in splits
+// where those do not make two blocks for every unit either; a split is 256 long at the least
+struct AnyPlan {
+    bool small;
+    int splits, per_split;
+};
+AnyPlan any_plan(long long rows, long long across, int tile_across, int small_across, int K)
+{
+    auto tiles = [&](int r, int c) { return ((rows + r - 1) / r) * ((across + c - 1) / c); };
+    AnyPlan p;
+    p.small = tiles(128, tile_across) < 512;
+    const long long t = p.small ? tiles(64, small_across) : tiles(128, tile_across);
+    long long splits = 512 / t;
+    const long long most = (K + 255) / 256;
     splits = splits < 1 ? 1 : splits > most ? most : splits;
-    TnPlan p;
-    p.rows_per_split = (int)((rows + splits - 1) / splits);
-    p.splits = (rows + p.rows_per_split - 1) / p.rows_per_split;
+    p.per_split = (int)(((K + splits - 1) / splits + 63) / 64 * 64);
+    p.splits = (K + p.per_split - 1) / p.per_split;
     return p;
 }
+AnyPlan forward_plan(int rows, int C, int F) { return any_plan(rows, F, 64, 64, C); }
+AnyPlan dgrad_plan(int rows, int C, int F) { return any_plan(rows, C, 128, 64, 2 * F); }
+AnyPlan wgrad_plan(int rows, int C, int F) { return any_plan(2ll * F, C, 128, 64, rows); }
 
 }  // namespace
 
@@ -313,12 +571,19 @@ bool gated_mfma(int dt, int rows, int C, int F)
            conv_gather_mfma_supported(rows_product(rows, 2 * F, C, false)) && conv_wgrad_mfma_supported({rows, 1, 1, C, 1, 1, 2 * F, 1, 1, 1, 0});
 }
 
+// Up to 64 rows the weights' bytes are what takes the time, and the gather kernel splits K over as many blocks as it takes to stream them.
+// (K above 2^20: the offsets of rows past a tensor's end may not pass 2^32.)
+static bool streams_weights(int rows, int C) { return rows <= 64 || C > 1 << 20; }
+
 size_t gated_workspace(int dt, int rows, int C, int F)
 {
-    if (gated_mfma(dt, rows, C, F)) return conv_gather_mfma_raw_workspace(rows_product(rows, C, 2 * F, false));
-    const TnPlan p = tn_plan(rows, 2 * F, C);
-    const size_t part = p.splits > 1 ? (size_t)p.splits * 2 * F * C * sizeof(float) : 0, sums = colsum_workspace(rows, 2 * F);
-    return part > sums ? part : sums;
+    if (gated_mfma(dt, rows, C, F)) return streams_weights(rows, C) ? conv_gather_mfma_raw_workspace(rows_product(rows, C, 2 * F, false)) : 0;
+    auto sums = [](const AnyPlan &p, size_t n) { return p.splits > 1 ? (size_t)p.splits * n * sizeof(float) : 0; };
+    size_t most = colsum_workspace(rows, 2 * F);
+    for (const size_t v : {sums(forward_plan(rows, C, F), (size_t)rows * 2 * F), sums(dgrad_plan(rows, C, F), (size_t)rows * C),
+                           sums(wgrad_plan(rows, C, F), (size_t)2 * F * C)})
+        most = v > most ? v : most;
+    return most;
 }
 
 #define GATED_T(dt, ...)                                              \
@@ -327,23 +592,55 @@ size_t gated_workspace(int dt, int rows, int C, int F)
         else { using T = bf16_t; __VA_ARGS__; }                       \
     } while (0)
 
+template <int BP, int BU, int WP, int WU>
+static hipError_t launch_mfma(MmArgs a, hipStream_t s)
+{
+    constexpr int bytes = 2 * (BP + 2 * BU) * 64 * 2;
+    auto kernel = k_gated_mfma<BP, BU, WP, WU>;
+    if (bytes > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+    }
+    a.tiles_p = (a.rows + BP - 1) / BP;
+    a.tiles_u = (a.F + BU - 1) / BU;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)a.tiles_p * a.tiles_u), dim3(WP * WU * 64), bytes, s, a);
+    return hipGetLastError();
+}
+
+static hipError_t join(int dt, int act, const float *part, int splits, const float *bias, float *P, void *h, int rows, int F, hipStream_t s)
+{
+    const size_t n = (size_t)rows * F;
+    const bool four = F % 4 == 0 && (uintptr_t)h % (4 * dt_size(dt)) == 0;       // the caller's h may lie anywhere
+    const dim3 grid((unsigned)((n / (four ? 4 : 1) + TPB - 1) / TPB));
+    if (four) GATED_T(dt, hipLaunchKernelGGL((k_gated_join<T, 4>), grid, dim3(TPB), 0, s, part, splits, bias, P, (T *)h, rows, F, act));
+    else GATED_T(dt, hipLaunchKernelGGL((k_gated_join<T, 1>), grid, dim3(TPB), 0, s, part, splits, bias, P, (T *)h, rows, F, act));
+    return hipGetLastError();
+}
+
 hipError_t gated_fwd(int dt, int act, const void *x, const void *w, const float *bias, float *P, void *h, int rows, int C, int F, bool panels,
                      void *workspace, hipStream_t s)
 {
+    if (gated_mfma(dt, rows, C, F) && !streams_weights(rows, C)) {
+        if (panels) return hipErrorInvalidValue;
+        MmArgs a{(const bf16_t *)x, nullptr, (const bf16_t *)w, rows, C, F, bias, P, (bf16_t *)h, (unsigned)((size_t)rows * C * 2),
+                 (unsigned)((size_t)2 * F * C * 2), 0, 0, act};
+        if ((long long)((rows + 255) / 256) * ((F + 127) / 128) >= 192) return launch_mfma<256, 128, 2, 4>(a, s);
+        return launch_mfma<128, 64, 2, 2>(a, s);
+    }
     if (gated_mfma(dt, rows, C, F)) {
         int splits = 0;
         const hipError_t e = conv_gather_mfma_raw(x, w, rows_product(rows, C, 2 * F, panels), (float *)workspace, &splits, s);
         if (e != hipSuccess) return e;
-        const size_t n = (size_t)rows * F / 4;
-        hipLaunchKernelGGL(k_gated_join, dim3((unsigned)((n + TPB - 1) / TPB)), dim3(TPB), 0, s, (const float *)workspace, splits, bias, P, (bf16_t *)h,
-                           rows, F, act);
-        return hipGetLastError();
+        return join(dt, act, (const float *)workspace, splits, bias, P, h, rows, F, s);
     }
     if (panels) return hipErrorInvalidValue;
-    NtArgs a{x, w, rows, F, C, bias, P, h, nullptr, nullptr, act};
-    const dim3 grid((unsigned)((F + TILE / 2 - 1) / (TILE / 2)) * ((rows + TILE - 1) / TILE));
-    GATED_T(dt, hipLaunchKernelGGL((k_gated_nt<T, NT_FORWARD>), grid, dim3(TPB), 0, s, a));
-    return hipGetLastError();
+    const AnyPlan p = forward_plan(rows, C, F);
+    NtArgs a{x, w, rows, F, C, p.per_split, p.splits > 1 ? (float *)workspace : nullptr, bias, P, h, nullptr, nullptr, act};
+    const dim3 grid((unsigned)((F + 63) / 64) * ((rows + (p.small ? 63 : 127)) / (p.small ? 64 : 128)), p.splits);
+    if (p.small) GATED_T(dt, hipLaunchKernelGGL((k_gated_nt<T, NT_FORWARD, 1, 2>), grid, dim3(TPB), 0, s, a));
+    else GATED_T(dt, hipLaunchKernelGGL((k_gated_nt<T, NT_FORWARD, 2, 2>), grid, dim3(TPB), 0, s, a));
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || p.splits == 1 ? e : join(dt, act, (const float *)workspace, p.splits, bias, P, h, rows, F, s);
 }
 
 hipError_t gated_grad(int dt, int act, const void *dh, const float *P, void *D, int rows, int F, hipStream_t s)
@@ -356,25 +653,36 @@ hipError_t gated_grad(int dt, int act, const void *dh, const float *P, void *D, 
     return hipGetLastError();
 }
 
-hipError_t gated_dgrad_direct(int dt, const void *D, const void *wt, void *dx, GradEpi epi, int rows, int C, int F, hipStream_t s)
+hipError_t gated_dgrad_direct(int dt, const void *D, const void *wt, void *dx, GradEpi epi, int rows, int C, int F, void *workspace, hipStream_t s)
 {
     const void *old = epi.accum ? (epi.accum_from ? epi.accum_from : dx) : nullptr;
-    NtArgs a{D, wt, rows, C, 2 * F, nullptr, nullptr, dx, old, epi.gate, 0};
-    const dim3 grid((unsigned)((C + TILE - 1) / TILE) * ((rows + TILE - 1) / TILE));
-    GATED_T(dt, hipLaunchKernelGGL((k_gated_nt<T, NT_GRAD>), grid, dim3(TPB), 0, s, a));
+    const AnyPlan p = dgrad_plan(rows, C, F);
+    NtArgs a{D, wt, rows, C, 2 * F, p.per_split, p.splits > 1 ? (float *)workspace : nullptr, nullptr, nullptr, dx, old, epi.gate, 0};
+    const int tile = p.small ? 64 : 128;
+    const dim3 grid((unsigned)((C + tile - 1) / tile) * ((rows + tile - 1) / tile), p.splits);
+    if (p.small) GATED_T(dt, hipLaunchKernelGGL((k_gated_nt<T, NT_GRAD, 1, 1>), grid, dim3(TPB), 0, s, a));
+    else GATED_T(dt, hipLaunchKernelGGL((k_gated_nt<T, NT_GRAD, 2, 2>), grid, dim3(TPB), 0, s, a));
+    if (p.splits > 1) {
+        const size_t n = (size_t)rows * C;
+        GATED_T(dt, hipLaunchKernelGGL((k_gated_grad_join<T>), dim3((unsigned)((n + TPB - 1) / TPB)), dim3(TPB), 0, s, (const float *)workspace, p.splits, n,
+                                       (T *)dx, (const T *)old, (const T *)epi.gate));
+    }
     return hipGetLastError();
 }
 
 hipError_t gated_wgrad_direct(int dt, const void *x, const void *D, float *dw, float *db, int rows, int C, int F, void *workspace, hipStream_t s)
 {
     const int M = 2 * F;
-    const TnPlan p = tn_plan(rows, M, C);
+    const AnyPlan p = wgrad_plan(rows, C, F);
     float *part = p.splits > 1 ? (float *)workspace : nullptr;
-    const dim3 grid((unsigned)((C + TILE - 1) / TILE) * ((M + TILE - 1) / TILE), p.splits);
-    GATED_T(dt, hipLaunchKernelGGL((k_gated_tn<T>), grid, dim3(TPB), 0, s, (const T *)D, (const T *)x, rows, M, C, p.rows_per_split, dw, part));
+    const int tile = p.small ? 64 : 128;
+    const dim3 grid((unsigned)((C + tile - 1) / tile) * ((M + tile - 1) / tile), p.splits);
+    if (p.small) GATED_T(dt, hipLaunchKernelGGL((k_gated_tn<T, 1, 1>), grid, dim3(TPB), 0, s, (const T *)D, (const T *)x, rows, M, C, p.per_split, dw, part));
+    else GATED_T(dt, hipLaunchKernelGGL((k_gated_tn<T, 2, 2>), grid, dim3(TPB), 0, s, (const T *)D, (const T *)x, rows, M, C, p.per_split, dw, part));
     if (part) {
         const size_t n = (size_t)M * C;
-        hipLaunchKernelGGL(k_gated_tn_join, dim3((unsigned)((n + TPB - 1) / TPB)), dim3(TPB), 0, s, part, p.splits, n, dw);
+        if (n % 4 == 0) hipLaunchKernelGGL(k_gated_tn_join<4>, dim3((unsigned)((n / 4 + TPB - 1) / TPB)), dim3(TPB), 0, s, part, p.splits, n, dw);
+        else hipLaunchKernelGGL(k_gated_tn_join<1>, dim3((unsigned)((n + TPB - 1) / TPB)), dim3(TPB), 0, s, part, p.splits, n, dw);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !db) return e;

@@ -1045,7 +1045,7 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
             if (L.mfma)
                 HIPCHK(conv_gather_mfma(D, L.w_t, nullptr, dx, 0, e, dgrad_geom(st, L), st->work, st->tickets, s));
             else
-                HIPCHK(gated_dgrad_direct(dt, D, L.w_t, dx, e, rows, L.d.cin, L.d.cout, s));
+                HIPCHK(gated_dgrad_direct(dt, D, L.w_t, dx, e, rows, L.d.cin, L.d.cout, st->work, s));
             st->tap_end(tp, flop, dbytes + (double)L.w_elems * dt_size(dt) + (double)A.bytes() * (1.0 + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0)));
         }
         break;
