@@ -72,12 +72,12 @@ template <bool FAST> __device__ __forceinline__ void act_both(int act, float g, 
 // alignment than an element's), a row's last ones one by one.  A block is 2 x 2 waves of 32 TM x 32 TN outputs; two tiles of the
 // contracted dimension in LDS, the next one's loads in flight while this one's products run.
 
-// 16 bytes of a row of which `left` elements are inside
-template <class T> __device__ __forceinline__ chunk16 load_chunk(const T *from, int left)
+// 16 bytes of a row, or where it may end before them (a tile's last ones, at one place of the program) those of `left` elements
+template <bool ENDS, class T> __device__ __forceinline__ chunk16 load_chunk(const T *from, int left)
 {
     constexpr int V = 16 / sizeof(T);
     chunk16 c = {0u, 0u, 0u, 0u};
-    if (left >= V) __builtin_memcpy(&c, from, 16);
+    if (!ENDS || left >= V) __builtin_memcpy(&c, from, 16);
     else if (left > 0) {
         T e[V];
 #pragma unroll
@@ -87,15 +87,18 @@ template <class T> __device__ __forceinline__ chunk16 load_chunk(const T *from, 
     return c;
 }
 
-// 32 x 32 products of two operands' rows over the 32 bytes of K that the two halves of a wave hold 16 bytes of each
-template <class T> __device__ __forceinline__ void multiply(f32x16 &acc, chunk16 a, chunk16 b)
+// All products of a wave's TM x TN tiles over the 32 bytes of K that its two halves hold 16 bytes of each
+template <class T, int TM, int TN> __device__ __forceinline__ void multiply(f32x16 (&acc)[TM][TN], const chunk16 (&a)[TM], const chunk16 (&b)[TN])
 {
-    if constexpr (sizeof(T) == 2) {
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_frag(a), as_frag(b), acc, 0, 0, 0);
-    } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[j]), __uint_as_float(b[j]), acc, 0, 0, 0);
-    }
+    for (int k = 0; k < (sizeof(T) == 2 ? 1 : 4); ++k)
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                if constexpr (sizeof(T) == 2) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_frag(a[i]), as_frag(b[j]), acc[i][j], 0, 0, 0);
+                else acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[i][k]), __uint_as_float(b[j][k]), acc[i][j], 0, 0, 0);
+            }
 }
 
 enum { NT_FORWARD, NT_GRAD };
@@ -113,7 +116,7 @@ struct NtArgs {
 template <class T, int MODE, int TM, int TN>
 __global__ __launch_bounds__(TPB) void k_gated_nt(NtArgs p)
 {
-    constexpr int V = 16 / sizeof(T), NQ = sizeof(T) == 2 ? 4 : 2, CPR = 2 * NQ, DEPTH = CPR * V;      // of K a tile
+    constexpr int V = 16 / sizeof(T), NQ = 4, CPR = 2 * NQ, DEPTH = CPR * V;      // of K a tile
     constexpr int PITCH = CPR * 16 + 16;           // bytes of a row: the reads of eight neighbouring rows lie on different banks
     constexpr int RA = 64 * TM, RB = 64 * TN, LA = RA * CPR / TPB, LB = RB * CPR / TPB, ROWS = TPB / CPR;
     constexpr bool FWD = MODE == NT_FORWARD;
@@ -129,21 +132,27 @@ __global__ __launch_bounds__(TPB) void k_gated_nt(NtArgs p)
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
         const int row = m0 + r0 + ROWS * i;
-        pa[i] = row < p.M ? (const T *)p.a + (size_t)row * p.K : nullptr;
+        pa[i] = (const T *)p.a + (size_t)(row < p.M ? row : p.M - 1) * p.K + c;      // nobody stores the rows behind the last
     }
 #pragma unroll
     for (int i = 0; i < LB; ++i) {
         const int r = r0 + ROWS * i;               // forward: 32 units' gates, then the same units' linear parts, for each wave
         const int n = FWD ? n0 + r / 64 * 32 + r % 32 : n0 + r;
-        pb[i] = n < p.N ? (const T *)p.b + (size_t)(FWD && r % 64 >= 32 ? p.N + n : n) * p.K : nullptr;
+        const int unit = n < p.N ? n : p.N - 1;
+        pb[i] = (const T *)p.b + (size_t)(FWD && r % 64 >= 32 ? p.N + unit : unit) * p.K + c;
     }
     chunk16 ca[LA], cb[LB];
-    auto load = [&](int k0) {
+    auto load_all = [&](int k0, auto ends) {
+        constexpr bool ENDS = decltype(ends)::value;
         const int left = last - k0 - c;
 #pragma unroll
-        for (int i = 0; i < LA; ++i) ca[i] = load_chunk(pa[i] + k0 + c, pa[i] ? left : 0);
+        for (int i = 0; i < LA; ++i) ca[i] = load_chunk<ENDS>(pa[i] + k0, left);
 #pragma unroll
-        for (int i = 0; i < LB; ++i) cb[i] = load_chunk(pb[i] + k0 + c, pb[i] ? left : 0);
+        for (int i = 0; i < LB; ++i) cb[i] = load_chunk<ENDS>(pb[i] + k0, left);
+    };
+    auto load = [&](int k0) {
+        if (k0 + DEPTH <= last) load_all(k0, std::false_type{});
+        else load_all(k0, std::true_type{});
     };
     auto store = [&](int buf) {
 #pragma unroll
@@ -159,18 +168,21 @@ __global__ __launch_bounds__(TPB) void k_gated_nt(NtArgs p)
         __syncthreads();
         if (s + 1 < steps) load(first + (s + 1) * DEPTH);
         const unsigned char *buf = lds[s & 1];
+        chunk16 fa[2][TM], fb[2][TN];
+        auto read = [&](int q) {
+            const int at = (2 * q + lane / 32) * 16;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) fa[q & 1][i] = *reinterpret_cast<const chunk16 *>(buf + ((wm * TM + i) * 32 + lane % 32) * PITCH + at);
+#pragma unroll
+            for (int i = 0; i < TN; ++i) fb[q & 1][i] = *reinterpret_cast<const chunk16 *>(buf + (RA + (wn * TN + i) * 32 + lane % 32) * PITCH + at);
+        };
+        read(0);
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-            const int at = (2 * q + lane / 32) * 16;
-            chunk16 fa[TM], fb[TN];
-#pragma unroll
-            for (int i = 0; i < TM; ++i) fa[i] = *reinterpret_cast<const chunk16 *>(buf + ((wm * TM + i) * 32 + lane % 32) * PITCH + at);
-#pragma unroll
-            for (int i = 0; i < TN; ++i) fb[i] = *reinterpret_cast<const chunk16 *>(buf + (RA + (wn * TN + i) * 32 + lane % 32) * PITCH + at);
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) multiply<T>(acc[i][j], fa[i], fb[j]);
+            if (q + 1 < NQ) read(q + 1);
+            __builtin_amdgcn_sched_barrier(0);       // the next reads ahead of the products that hide them
+            multiply<T>(acc, fa[q & 1], fb[q & 1]);
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (s + 1 < steps) store((s + 1) & 1);
     }
@@ -206,12 +218,12 @@ __global__ __launch_bounds__(TPB) void k_gated_nt(NtArgs p)
 }
 
 // dw[M][N] += a^T b with a [rows][M], b [rows][N], over the rows of split blockIdx.y; with several splits part[split][M][N] = their sums.
-// A step is 32 rows of bf16, read across the rows by transposing reads (tr_frag), or 16 of float.
+// A step is 32 rows, of bf16 read across the rows by transposing reads (tr_frag).
 template <class T, int TM, int TN>
 __global__ __launch_bounds__(TPB) void k_gated_tn(const T *__restrict__ a, const T *__restrict__ b, int rows, int M, int N, int rows_per_split,
                                                   float *dw, float *part)
 {
-    constexpr int V = 16 / sizeof(T), DEPTH = sizeof(T) == 2 ? 32 : 16, CA = 64 * TM, CB = 64 * TN;
+    constexpr int V = 16 / sizeof(T), DEPTH = 32, CA = 64 * TM, CB = 64 * TN;
     constexpr int LA = DEPTH * CA / V / TPB, LB = DEPTH * CB / V / TPB;
     static_assert(LA >= 1 && LB >= 1, "a chunk for every thread");
     __shared__ __align__(16) T lds[2][DEPTH * (CA + CB)];
@@ -219,12 +231,15 @@ __global__ __launch_bounds__(TPB) void k_gated_tn(const T *__restrict__ a, const
     const int across = (N + CB - 1) / CB, m0 = blockIdx.x / across * CA, n0 = blockIdx.x % across * CB;
     const int first = blockIdx.y * rows_per_split, last = first + rows_per_split < rows ? first + rows_per_split : rows;
     chunk16 ca[LA], cb[LB];
+    // Columns behind the last are never stored, so that a row's last 16 bytes may go on into the rows behind it, where there are some
     auto fetch = [&](auto &to, const T *from, int width, int c0, int at, auto columns) {
         constexpr int CPR = decltype(columns)::value / V;
+        const bool inside = at + DEPTH <= last && (size_t)(at + DEPTH) * width + V <= (size_t)rows * width;
 #pragma unroll
         for (int i = 0; i < (int)(sizeof(to) / sizeof(to[0])); ++i) {
             const int id = tid + TPB * i, r = at + id / CPR, c = c0 + id % CPR * V;
-            to[i] = load_chunk(from + (size_t)r * width + c, r < last ? width - c : 0);
+            if (inside) to[i] = load_chunk<false>(from + (size_t)r * width + (c < width ? c : 0), V);
+            else to[i] = load_chunk<true>(from + (size_t)r * width + c, r < last ? width - c : 0);
         }
     };
     auto load = [&](int at) {
@@ -266,18 +281,31 @@ __global__ __launch_bounds__(TPB) void k_gated_tn(const T *__restrict__ a, const
                     for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
             }
         } else {
+            constexpr int AHEAD = 4;                     // rows' pairs read before the products that need them
+            float fa[2][AHEAD][TM], fb[2][AHEAD][TN];
+            auto read = [&](int h) {
 #pragma unroll
-            for (int q = 0; q < DEPTH / 2; ++q) {
-                const int k = q * 2 + lane / 32;
-                float fa[TM], fb[TN];
+                for (int q = 0; q < AHEAD; ++q) {
+                    const int k = (h * AHEAD + q) * 2 + lane / 32;
 #pragma unroll
-                for (int i = 0; i < TM; ++i) fa[i] = ta[k * CA + (wm * TM + i) * 32 + lane % 32];
+                    for (int i = 0; i < TM; ++i) fa[h & 1][q][i] = ta[k * CA + (wm * TM + i) * 32 + lane % 32];
 #pragma unroll
-                for (int i = 0; i < TN; ++i) fb[i] = tb[k * CB + (wn * TN + i) * 32 + lane % 32];
+                    for (int i = 0; i < TN; ++i) fb[h & 1][q][i] = tb[k * CB + (wn * TN + i) * 32 + lane % 32];
+                }
+            };
+            read(0);
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
+            for (int h = 0; h < DEPTH / 2 / AHEAD; ++h) {
+                if (h + 1 < DEPTH / 2 / AHEAD) read(h + 1);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[i], fb[j], acc[i][j], 0, 0, 0);
+                for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[h & 1][q][i], fb[h & 1][q][j], acc[i][j], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (s + 1 < steps) store((s + 1) & 1);
@@ -527,28 +555,37 @@ __global__ __launch_bounds__(WP *WU * 64, 2) void k_gated_mfma(MmArgs p)
     }
 }
 
-// How a product of any sizes is cut: tiles of 128 x 128, or 64 rows of them where there are few, and the contracted dimension in splits
-// where those do not make two blocks for every unit either; a split is 256 long at the least
+// How a product of any sizes is cut: into tiles of 128 x 128, or of 64 rows, and the contracted dimension into splits of 256 at the
+// least.  The units take their blocks in step, so what counts is the fullest unit's share of the products: `each` outputs a block, for a
+// lone block, whose barriers nobody fills, half as many again, and for splits their sums written and read (a float's 8 bytes
+// against products at about 30 a byte).
 struct AnyPlan {
     bool small;
     int splits, per_split;
 };
-AnyPlan any_plan(long long rows, long long across, int tile_across, int small_across, int K)
+AnyPlan any_plan(long long rows, long long across, int tile_across, int small_across, int K, int sums)
 {
-    auto tiles = [&](int r, int c) { return ((rows + r - 1) / r) * ((across + c - 1) / c); };
-    AnyPlan p;
-    p.small = tiles(128, tile_across) < 512;
-    const long long t = p.small ? tiles(64, small_across) : tiles(128, tile_across);
-    long long splits = 512 / t;
-    const long long most = (K + 255) / 256;
-    splits = splits < 1 ? 1 : splits > most ? most : splits;
-    p.per_split = (int)(((K + splits - 1) / splits + 63) / 64 * 64);
-    p.splits = (K + p.per_split - 1) / p.per_split;
-    return p;
+    AnyPlan best{};
+    double least = 1e300;
+    for (const bool small : {false, true}) {
+        const int r = small ? 64 : 128, c = small ? small_across : tile_across;
+        const long long tiles = ((rows + r - 1) / r) * ((across + c - 1) / c);
+        for (long long splits = 1; splits <= (K + 255) / 256 && (splits == 1 || tiles * splits <= 1024); ++splits) {
+            const int per = (int)(((K + splits - 1) / splits + 63) / 64 * 64);
+            const long long full = (tiles * ((K + per - 1) / per) + 255) / 256;
+            const double cost = (double)(full == 1 ? 1.5 : full) * r * c * sums * (small ? 1.15 : 1.0) * per +
+                                (splits > 1 ? (double)rows * across * sums * splits * 8 * 30 / 256 : 0.0);
+            if (cost < least) {
+                least = cost;
+                best = {small, (K + per - 1) / per, per};
+            }
+        }
+    }
+    return best;
 }
-AnyPlan forward_plan(int rows, int C, int F) { return any_plan(rows, F, 64, 64, C); }
-AnyPlan dgrad_plan(int rows, int C, int F) { return any_plan(rows, C, 128, 64, 2 * F); }
-AnyPlan wgrad_plan(int rows, int C, int F) { return any_plan(2ll * F, C, 128, 64, rows); }
+AnyPlan forward_plan(int rows, int C, int F) { return any_plan(rows, F, 64, 64, C, 2); }
+AnyPlan dgrad_plan(int rows, int C, int F) { return any_plan(rows, C, 128, 64, 2 * F, 1); }
+AnyPlan wgrad_plan(int rows, int C, int F) { return any_plan(2ll * F, C, 128, 64, rows, 1); }
 
 }  // namespace
 
