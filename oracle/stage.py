@@ -13,7 +13,8 @@ input-gradient contribution in backward and their sum where a tensor feeds two l
 the working copy of conv/linear weight matrices.  Bias, gamma, beta, weight gradients,
 BN statistics, softmax and loss are never rounded.  Inside an LSTM layer the input projection
 of all steps and the pre-activation gradients are stored tensors too (rounded); the cell state
-and the recurrent sums are not.  A gated layer's projections are not rounded, their gradients are.  storage="exact" rounds nothing.
+and the recurrent sums are not.  A gated layer's projections are not rounded, their gradients
+are; the gradients that layer norm, gated layer and 1x1 convolution hand to each other are not.  storage="exact" rounds nothing.
 """
 import numpy as np
 
@@ -47,12 +48,28 @@ class OracleStage:
             self.b.append(None if b is None else np.array(b, dtype=np.float64))
             self.dw.append(None if w is None else np.zeros(w.shape))
             self.db.append(None if b is None else np.zeros(b.shape))
+        self.readers = {}
+        for i, L in enumerate(self.layers):
+            for t in [L["src0"]] + ([L["src1"]] if L["kind"] == C.ADD else []):
+                self.readers.setdefault(t, []).append(i)
+        self.float_grads = {t for t in range(len(self.layers)) if self._float_grad(t)}
         self.stash = {}
         self.loss = {}
         self.trace = None          # set to {} to record, per (mb, layer), the masked output gradient and dx
         self.n_fwd = self.n_bwd = 0
         self.peak_in_flight = 0
         self.dropout_seed = self.mini_batch = 0        # key and last counter word of the DROPOUT layers' masks
+
+    def _float_grad(self, t):
+        """Whether the gradient of layer t's output is not rounded: of a layer norm that only a gated layer reads, of a gated layer
+        that only a 1x1 convolution of widths that are multiples of 8 does."""
+        if len(self.readers.get(t, [])) != 1:
+            return False
+        P, N = self.layers[t], self.layers[self.readers[t][0]]
+        if P["kind"] == C.LAYERNORM:
+            return N["kind"] == C.GATED
+        return (P["kind"] == C.GATED and N["kind"] == C.CONV2D and (N["kh"], N["stride"], N["pad"]) == (1, 1, 0) and
+                N["cin"] % 8 == 0 and N["cout"] % 8 == 0)
 
     # ---- schedule bookkeeping -------------------------------------------------------
     def _claim(self, mb):
@@ -73,7 +90,7 @@ class OracleStage:
         self._claim(mb)
         q = self.q
         x = np.asarray(x, dtype=np.float64)
-        outs, aux = [], []
+        outs, aux, fine_norm = [], [], {}
 
         def src(t):
             return x if t < 0 else outs[t]
@@ -115,9 +132,12 @@ class OracleStage:
                 y, extra = ops.lstm_fwd(a, q(self.w[i]), self.b[i], round16=self.storage == "bf16")
             elif k == C.LAYERNORM:
                 y, xhat, inv = ops.layernorm_fwd(a, self.w[i], self.b[i], L["eps"])
+                fine_norm[i] = y
                 y, extra = q(y), (xhat, inv)
             elif k == C.GATED:
-                y, both = ops.gated_fwd(a, q(self.w[i]), self.b[i], L["kh"])
+                # the decisions of a ReLU gate are taken on what a layer norm that only it reads has computed, not on what it stores
+                fine = fine_norm.get(L["src0"], a) if L["kh"] == C.GATE_RELU and self.readers.get(L["src0"]) == [i] else a
+                y, both = ops.gated_fwd(fine, q(self.w[i]), self.b[i], L["kh"])
                 y, extra = q(y), both
             elif k == C.DROPOUT:
                 extra = ops.dropout_factor(a.shape, L["eps"], self.dropout_seed, i + 65536 * (self.stage["stage_index"] - 1), mb,
@@ -148,7 +168,8 @@ class OracleStage:
         def give(t, c):
             if t < 0 and not need_in:
                 return
-            c = q(c)
+            if t not in self.float_grads:
+                c = q(c)
             if self.trace is not None:
                 self.trace[(mb, cur[0])]["dx"] = c
             G[t] = c if t not in G else q(G[t] + c)

@@ -210,13 +210,16 @@ hipError_t layernorm_bwd(int dt, const void *x, const void *dy, int dy_parts, co
 enum { ACT_SIGMOID = 0, ACT_SILU = 1, ACT_GELU = 2, ACT_RELU = 3 };
 // whether the products take the bf16 MFMA kernels: conv_gather_mfma for dx = D W (wt: [C][2F]), conv_wgrad_mfma for dw += D^T x, with db
 bool gated_mfma(int dt, int rows, int C, int F);
-size_t gated_workspace(int dt, int rows, int C, int F);       // of the calls here
-// panels: w is kept in panels (GatherConv::wt_panels), for gated_mfma only
-hipError_t gated_fwd(int dt, int act, const void *x, const void *w, const float *bias, float *P, void *h, int rows, int C, int F, bool panels,
+size_t gated_workspace(int dt, int rows, int C, int F, bool rest);       // of the calls here
+// rest: NULL, or a second tensor whose sum with x is the layer's input; panels: w is kept in panels (GatherConv::wt_panels), for gated_mfma only
+hipError_t gated_fwd(int dt, int act, const void *x, const void *rest, const void *w, const float *bias, float *P, void *h, int rows, int C, int F, bool panels,
                      void *workspace, hipStream_t s);
-hipError_t gated_grad(int dt, int act, const void *dh, const float *P, void *D, int rows, int F, hipStream_t s);
+// dh_parts > 0: dh is that many float sums [dh_parts][rows][F] instead
+hipError_t gated_grad(int dt, int act, const void *dh, int dh_parts, const float *P, void *D, int rows, int F, hipStream_t s);
 // the other two products where gated_mfma says no
-hipError_t gated_dgrad_direct(int dt, const void *D, const void *wt, void *dx, GradEpi epi, int rows, int C, int F, void *workspace, hipStream_t s);
+// parts: dx receives the gated_dgrad_parts float sums [parts][rows][C] of the product
+int gated_dgrad_parts(int rows, int C, int F);
+hipError_t gated_dgrad_direct(int dt, const void *D, const void *wt, void *dx, bool parts, GradEpi epi, int rows, int C, int F, void *workspace, hipStream_t s);
 hipError_t gated_wgrad_direct(int dt, const void *x, const void *D, float *dw, float *db, int rows, int C, int F, void *workspace, hipStream_t s);
 
 // ---- dropout (kernels_dropout.hip): y[e] = word(e) >= 2^32 p ? x[e] / (1-p) : 0, or with the gradient epilogue the same of dy

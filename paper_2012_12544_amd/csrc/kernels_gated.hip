@@ -389,25 +389,37 @@ __global__ __launch_bounds__(TPB) void k_gated_join(const float *__restrict__ pa
     *reinterpret_cast<vec_t<T, V> *>(h + i) = v;
 }
 
-// D from dh and the projections, V units a thread (F a multiple of V, dh aligned to V elements)
+// D from dh and the projections, V units a thread (F a multiple of V, dh aligned to V elements).  dh_parts: instead of dh its `parts`
+// float sums [parts][n]
 template <class T, int V>
-__global__ __launch_bounds__(TPB) void k_gated_grad(const T *__restrict__ dh, const float *__restrict__ P, T *__restrict__ D, size_t n, int F, int act)
+__global__ __launch_bounds__(TPB) void k_gated_grad(const T *__restrict__ dh, const float *__restrict__ dh_parts, int parts, const float *__restrict__ P,
+                                                    T *__restrict__ D, size_t n, int F, int act)
 {
     const size_t i = ((size_t)blockIdx.x * TPB + threadIdx.x) * V;
     if (i >= n) return;
     const size_t row = i / F, at = row * 2 * F + (i - row * F);
     typedef vec_t<T, V> vec;
     typedef vec_t<float, V> vecf;
-    const vec d = *reinterpret_cast<const vec *>(dh + i);
+    float d[V] = {};
+    if (dh_parts) {
+        for (int k = 0; k < parts; ++k) {
+            const vecf v = *reinterpret_cast<const vecf *>(dh_parts + (size_t)k * n + i);
+#pragma unroll
+            for (int j = 0; j < V; ++j) d[j] += v.e[j];
+        }
+    } else {
+        const vec v = *reinterpret_cast<const vec *>(dh + i);
+#pragma unroll
+        for (int j = 0; j < V; ++j) d[j] = to_f32(v.e[j]);
+    }
     const vecf g = *reinterpret_cast<const vecf *>(P + at), u = *reinterpret_cast<const vecf *>(P + at + F);
     vec dg, du;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         float a, da;
         act_both<kFast<T>>(act, g.e[j], a, da);
-        const float v = to_f32(d.e[j]);
-        dg.e[j] = from_f32<T>(v * u.e[j] * da);
-        du.e[j] = from_f32<T>(v * a);
+        dg.e[j] = from_f32<T>(d[j] * u.e[j] * da);
+        du.e[j] = from_f32<T>(d[j] * a);
     }
     *reinterpret_cast<vec *>(D + at) = dg;
     *reinterpret_cast<vec *>(D + at + F) = du;
@@ -612,12 +624,14 @@ bool gated_mfma(int dt, int rows, int C, int F)
 // (K above 2^20: the offsets of rows past a tensor's end may not pass 2^32.)
 static bool streams_weights(int rows, int C) { return rows <= 64 || C > 1 << 20; }
 
-size_t gated_workspace(int dt, int rows, int C, int F)
+size_t gated_workspace(int dt, int rows, int C, int F, bool rest)
 {
-    if (gated_mfma(dt, rows, C, F)) return streams_weights(rows, C) ? conv_gather_mfma_raw_workspace(rows_product(rows, C, 2 * F, false)) : 0;
+    const size_t walks = rest ? 2 : 1;
+    if (gated_mfma(dt, rows, C, F)) return streams_weights(rows, C) ? walks * conv_gather_mfma_raw_workspace(rows_product(rows, C, 2 * F, false)) : 0;
     auto sums = [](const AnyPlan &p, size_t n) { return p.splits > 1 ? (size_t)p.splits * n * sizeof(float) : 0; };
     size_t most = colsum_workspace(rows, 2 * F);
-    for (const size_t v : {sums(forward_plan(rows, C, F), (size_t)rows * 2 * F), sums(dgrad_plan(rows, C, F), (size_t)rows * C),
+    const AnyPlan f = forward_plan(rows, C, F);
+    for (const size_t v : {f.splits * walks > 1 ? f.splits * walks * rows * 2 * F * sizeof(float) : 0, sums(dgrad_plan(rows, C, F), (size_t)rows * C),
                            sums(wgrad_plan(rows, C, F), (size_t)2 * F * C)})
         most = v > most ? v : most;
     return most;
@@ -654,52 +668,63 @@ static hipError_t join(int dt, int act, const float *part, int splits, const flo
     return hipGetLastError();
 }
 
-hipError_t gated_fwd(int dt, int act, const void *x, const void *w, const float *bias, float *P, void *h, int rows, int C, int F, bool panels,
+hipError_t gated_fwd(int dt, int act, const void *x, const void *rest, const void *w, const float *bias, float *P, void *h, int rows, int C, int F, bool panels,
                      void *workspace, hipStream_t s)
 {
     if (gated_mfma(dt, rows, C, F) && !streams_weights(rows, C)) {
         if (panels) return hipErrorInvalidValue;
-        MmArgs a{(const bf16_t *)x, nullptr, (const bf16_t *)w, rows, C, F, bias, P, (bf16_t *)h, (unsigned)((size_t)rows * C * 2),
+        MmArgs a{(const bf16_t *)x, (const bf16_t *)rest, (const bf16_t *)w, rows, C, F, bias, P, (bf16_t *)h, (unsigned)((size_t)rows * C * 2),
                  (unsigned)((size_t)2 * F * C * 2), 0, 0, act};
         if ((long long)((rows + 255) / 256) * ((F + 127) / 128) >= 192) return launch_mfma<256, 128, 2, 4>(a, s);
         return launch_mfma<128, 64, 2, 2>(a, s);
     }
     if (gated_mfma(dt, rows, C, F)) {
-        int splits = 0;
-        const hipError_t e = conv_gather_mfma_raw(x, w, rows_product(rows, C, 2 * F, panels), (float *)workspace, &splits, s);
+        int splits = 0, more = 0;
+        const GatherConv g = rows_product(rows, C, 2 * F, panels);
+        hipError_t e = conv_gather_mfma_raw(x, w, g, (float *)workspace, &splits, s);
+        if (e == hipSuccess && rest) e = conv_gather_mfma_raw(rest, w, g, (float *)workspace + (size_t)splits * rows * 2 * F, &more, s);
         if (e != hipSuccess) return e;
+        splits += more;
         return join(dt, act, (const float *)workspace, splits, bias, P, h, rows, F, s);
     }
     if (panels) return hipErrorInvalidValue;
     const AnyPlan p = forward_plan(rows, C, F);
-    NtArgs a{x, w, rows, F, C, p.per_split, p.splits > 1 ? (float *)workspace : nullptr, bias, P, h, nullptr, nullptr, act};
+    const int splits = p.splits * (rest ? 2 : 1);
     const dim3 grid((unsigned)((F + 63) / 64) * ((rows + (p.small ? 63 : 127)) / (p.small ? 64 : 128)), p.splits);
-    if (p.small) GATED_T(dt, hipLaunchKernelGGL((k_gated_nt<T, NT_FORWARD, 1, 2>), grid, dim3(TPB), 0, s, a));
-    else GATED_T(dt, hipLaunchKernelGGL((k_gated_nt<T, NT_FORWARD, 2, 2>), grid, dim3(TPB), 0, s, a));
+    for (int walk = 0; walk * p.splits < splits; ++walk) {
+        float *part = splits > 1 ? (float *)workspace + (size_t)walk * p.splits * rows * 2 * F : nullptr;
+        NtArgs a{walk ? rest : x, w, rows, F, C, p.per_split, part, bias, P, h, nullptr, nullptr, act};
+        if (p.small) GATED_T(dt, hipLaunchKernelGGL((k_gated_nt<T, NT_FORWARD, 1, 2>), grid, dim3(TPB), 0, s, a));
+        else GATED_T(dt, hipLaunchKernelGGL((k_gated_nt<T, NT_FORWARD, 2, 2>), grid, dim3(TPB), 0, s, a));
+    }
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess || p.splits == 1 ? e : join(dt, act, (const float *)workspace, p.splits, bias, P, h, rows, F, s);
+    return e != hipSuccess || splits == 1 ? e : join(dt, act, (const float *)workspace, splits, bias, P, h, rows, F, s);
 }
 
-hipError_t gated_grad(int dt, int act, const void *dh, const float *P, void *D, int rows, int F, hipStream_t s)
+hipError_t gated_grad(int dt, int act, const void *dh, int dh_parts, const float *P, void *D, int rows, int F, hipStream_t s)
 {
+    const float *parts = dh_parts ? (const float *)dh : nullptr;
     const size_t n = (size_t)rows * F;
-    const bool four = F % 4 == 0 && (uintptr_t)dh % (4 * dt_size(dt)) == 0;      // the caller's dh may lie anywhere
+    const bool four = F % 4 == 0 && (parts || (uintptr_t)dh % (4 * dt_size(dt)) == 0);      // the caller's dh may lie anywhere
     const dim3 grid((unsigned)((n / (four ? 4 : 1) + TPB - 1) / TPB));
-    if (four) GATED_T(dt, hipLaunchKernelGGL((k_gated_grad<T, 4>), grid, dim3(TPB), 0, s, (const T *)dh, P, (T *)D, n, F, act));
-    else GATED_T(dt, hipLaunchKernelGGL((k_gated_grad<T, 1>), grid, dim3(TPB), 0, s, (const T *)dh, P, (T *)D, n, F, act));
+    if (four) GATED_T(dt, hipLaunchKernelGGL((k_gated_grad<T, 4>), grid, dim3(TPB), 0, s, (const T *)dh, parts, dh_parts, P, (T *)D, n, F, act));
+    else GATED_T(dt, hipLaunchKernelGGL((k_gated_grad<T, 1>), grid, dim3(TPB), 0, s, (const T *)dh, parts, dh_parts, P, (T *)D, n, F, act));
     return hipGetLastError();
 }
 
-hipError_t gated_dgrad_direct(int dt, const void *D, const void *wt, void *dx, GradEpi epi, int rows, int C, int F, void *workspace, hipStream_t s)
+int gated_dgrad_parts(int rows, int C, int F) { return dgrad_plan(rows, C, F).splits; }
+
+hipError_t gated_dgrad_direct(int dt, const void *D, const void *wt, void *dx, bool parts, GradEpi epi, int rows, int C, int F, void *workspace,
+                              hipStream_t s)
 {
     const void *old = epi.accum ? (epi.accum_from ? epi.accum_from : dx) : nullptr;
     const AnyPlan p = dgrad_plan(rows, C, F);
-    NtArgs a{D, wt, rows, C, 2 * F, p.per_split, p.splits > 1 ? (float *)workspace : nullptr, nullptr, nullptr, dx, old, epi.gate, 0};
+    NtArgs a{D, wt, rows, C, 2 * F, p.per_split, parts ? (float *)dx : p.splits > 1 ? (float *)workspace : nullptr, nullptr, nullptr, dx, old, epi.gate, 0};
     const int tile = p.small ? 64 : 128;
     const dim3 grid((unsigned)((C + tile - 1) / tile) * ((rows + tile - 1) / tile), p.splits);
     if (p.small) GATED_T(dt, hipLaunchKernelGGL((k_gated_nt<T, NT_GRAD, 1, 1>), grid, dim3(TPB), 0, s, a));
     else GATED_T(dt, hipLaunchKernelGGL((k_gated_nt<T, NT_GRAD, 2, 2>), grid, dim3(TPB), 0, s, a));
-    if (p.splits > 1) {
+    if (p.splits > 1 && !parts) {
         const size_t n = (size_t)rows * C;
         GATED_T(dt, hipLaunchKernelGGL((k_gated_grad_join<T>), dim3((unsigned)((n + TPB - 1) / TPB)), dim3(TPB), 0, s, (const float *)workspace, p.splits, n,
                                        (T *)dx, (const T *)old, (const T *)epi.gate));

@@ -58,6 +58,15 @@ struct Tensor {
     // copied, the other's input-gradient epilogue reads it where it lies (GradEpi::accum_from).  Layer index of
     // that conv or layer norm, or -1.
     int fanout_conv = -1;
+    // Gradient of a layer norm's output that only a GATED reads, or of a GATED's that only a 1x1 convolution does: the float sums of the
+    // product that makes it, so many of them, instead of their rounded total.  It is read by one kernel, which forms a product's operand or
+    // a row's sums, and every rounding on the way through the sublayer is one more of its gradients' errors: 2-norm of dW and
+    // dgamma against 64 bits 4.2e-3 and 3.9e-3 with them, 3.8e-3 and 3.5e-3 so.
+    int gparts = 0;
+    // What rounding took from a layer norm's output that only a GATED of ReLU reads, in the transient arena: the product takes both.  The
+    // derivative of the activation jumps, and with an input of 8 bits 7 of 10^4 gates are on the wrong side, 2.6e-2 of dW.
+    bool rest = false;
+    size_t rest_off = 0;
     size_t bytes() const { return elems * esize; }
 };
 
@@ -744,18 +753,18 @@ int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
         const void *x = li == 0 && c.x_copied ? c.x_copied : a;
         void *copy = x == a ? nullptr : const_cast<void *>(a);
         HIPCHK(layernorm_fwd(dt, x, L.w, L.bias, L.d.eps, out_ptr(st, L, c, dt_size(dt)), (float *)(st->slot(c.mbid) + L.aux_off), rows_of(st, A), A.C,
-                             s, copy));
-        st->tap_end(tp, 0.0, (copy ? 3.0 : 2.0) * A.bytes());                    // read x, write y (and x)
+                             s, copy, O.rest ? st->transient + O.rest_off : nullptr));
+        st->tap_end(tp, 0.0, (2.0 + (copy ? 1.0 : 0.0) + (O.rest ? 1.0 : 0.0)) * A.bytes());      // read x, write y (and x, and the rest of y)
         break;
     }
     case BAPIPE_GATED: {
         const Tensor &A = st->tensors[L.a];
         const GatherConv g = fwd_geom(st, L);
         const bool tp = st->tap_begin(L.mfma ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
-        HIPCHK(gated_fwd(dt, L.d.kh, a, L.w_work, L.bias, (float *)(st->slot(c.mbid) + L.off_pd), out_ptr(st, L, c, L.mfma ? 16 : dt_size(dt)),
+        HIPCHK(gated_fwd(dt, L.d.kh, a, A.rest ? st->transient + A.rest_off : nullptr, L.w_work, L.bias, (float *)(st->slot(c.mbid) + L.off_pd), out_ptr(st, L, c, L.mfma ? 16 : dt_size(dt)),
                          rows_of(st, A), L.d.cin, L.d.cout, L.w_panels, st->work, s));
         // x and the weights read, h and both projections (float) written
-        st->tap_end(tp, conv_flop(g, L.d.cin), (double)A.bytes() + O.bytes() + 8.0 * O.elems + (double)L.w_elems * dt_size(dt));
+        st->tap_end(tp, conv_flop(g, L.d.cin) * (A.rest ? 2.0 : 1.0), A.bytes() * (A.rest ? 2.0 : 1.0) + O.bytes() + 8.0 * O.elems + (double)L.w_elems * dt_size(dt));
         break;
     }
     case BAPIPE_DROPOUT: {
@@ -903,7 +912,10 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
             void *dx = grad_ptr(st, L.a, c);
             const bool mf = use_mfma_gather(st, dg);
             const bool tp = st->tap_begin(mf ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
-            if (mf && L.bnb_chunks && !c.profiling && (e.gate || e.accum)) {
+            if (A.gparts) {
+                int parts = 0;
+                HIPCHK(conv_gather_mfma_raw(g, L.w_t, dg, (float *)dx, &parts, s));
+            } else if (mf && L.bnb_chunks && !c.profiling && (e.gate || e.accum)) {
                 const Layer &B = st->layers[li - 1];
                 HIPCHK(conv_gather_mfma(g, L.w_t, nullptr, dx, 0, e, dg, st->work, st->tickets, s, (float *)st->work,
                                         st->tptr(B.a, c.mbid), (const float *)(st->slot(c.mbid) + B.aux_off)));
@@ -914,7 +926,7 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
                 HIPCHK(conv_gather_direct(dt, g, L.w_t, nullptr, dx, 0, e, dg, s));
             // dy and filter read, dx written, plus the gate and the previous dx where the epilogue uses them
             st->tap_end(tp, flop, (double)O.bytes() + (double)L.w_elems * dt_size(dt) +
-                                      (double)A.bytes() * (1.0 + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0)));
+                                      (A.gparts ? 4.0 * A.gparts * A.elems : A.bytes() * (1.0 + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0))));
         }
         break;
     }
@@ -1016,7 +1028,7 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
             }
         }
         const bool tp = st->tap_begin(BAPIPE_KC_BATCHNORM);
-        HIPCHK(layernorm_bwd(dt, st->tptr(L.a, c.mbid), grad_ptr(st, L.o, c), 0, L.w, (const float *)(st->slot(c.mbid) + L.aux_off), dx, L.dw, L.db,
+        HIPCHK(layernorm_bwd(dt, st->tptr(L.a, c.mbid), grad_ptr(st, L.o, c), O.gparts, L.w, (const float *)(st->slot(c.mbid) + L.aux_off), dx, L.dw, L.db,
                              e, rows_of(st, A), A.C, st->work, s));
         st->tap_end(tp, 0.0, (double)A.bytes() * (2.0 + (dx ? 1.0 : 0.0) + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0)));
         break;
@@ -1027,8 +1039,8 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
         const int rows = rows_of(st, A);
         const double flop = conv_flop(fwd_geom(st, L), L.d.cin), dbytes = 2.0 * O.bytes();
         bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
-        HIPCHK(gated_grad(dt, L.d.kh, grad_ptr(st, L.o, c), (const float *)(st->slot(c.mbid) + L.off_pd), D, rows, L.d.cout, s));
-        st->tap_end(tp, 0.0, (double)O.bytes() + 8.0 * O.elems + dbytes);
+        HIPCHK(gated_grad(dt, L.d.kh, grad_ptr(st, L.o, c), O.gparts, (const float *)(st->slot(c.mbid) + L.off_pd), D, rows, L.d.cout, s));
+        st->tap_end(tp, 0.0, (O.gparts ? 4.0 * O.gparts * O.elems : (double)O.bytes()) + 8.0 * O.elems + dbytes);
         const WgradLaunch w{x, D, &L, conv_shape(st, L), flop, (double)A.bytes() + dbytes + 8.0 * L.w_elems};
         if (L.mfma) {
             const int rc = give_wgrad(st, w, true, a_grad, c.profiling);
@@ -1042,11 +1054,15 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
             GradEpi e = epi_for(st, L.a, c);
             void *dx = grad_ptr(st, L.a, c);
             tp = st->tap_begin(L.mfma ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
-            if (L.mfma)
+            int parts = 0;
+            if (L.mfma && A.gparts)
+                HIPCHK(conv_gather_mfma_raw(D, L.w_t, dgrad_geom(st, L), (float *)dx, &parts, s));
+            else if (L.mfma)
                 HIPCHK(conv_gather_mfma(D, L.w_t, nullptr, dx, 0, e, dgrad_geom(st, L), st->work, st->tickets, s));
             else
-                HIPCHK(gated_dgrad_direct(dt, D, L.w_t, dx, e, rows, L.d.cin, L.d.cout, st->work, s));
-            st->tap_end(tp, flop, dbytes + (double)L.w_elems * dt_size(dt) + (double)A.bytes() * (1.0 + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0)));
+                HIPCHK(gated_dgrad_direct(dt, D, L.w_t, dx, A.gparts > 0, e, rows, L.d.cin, L.d.cout, st->work, s));
+            st->tap_end(tp, flop, dbytes + (double)L.w_elems * dt_size(dt) +
+                                      (A.gparts ? 4.0 * A.gparts * A.elems : A.bytes() * (1.0 + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0))));
         }
         break;
     }
@@ -1421,6 +1437,20 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
             return create_fail(BAPIPE_E_UNSUPPORTED, "softmax input must be an un-gated tensor used only by the loss");
     }
 
+    // what stays in float between the layers of a bf16 sublayer
+    for (int t = 1; t < last_t && st->dt == DT_BF16; ++t) {
+        Tensor &T = st->tensors[t];
+        if (T.root != t || T.consumers.size() != 1) continue;
+        const Layer &P = st->layers[t - 1], &N = st->layers[T.consumers[0]];
+        const bool by_gated = P.d.kind == BAPIPE_LAYERNORM && N.d.kind == BAPIPE_GATED;
+        const bool by_conv = P.d.kind == BAPIPE_GATED && N.d.kind == BAPIPE_CONV2D && N.d.kh == 1 && N.d.kw == 1 && N.d.stride == 1 && N.d.pad == 0;
+        if (!by_gated && !by_conv) continue;
+        const int rows = rows_of(st, T);
+        if (by_gated && !gated_mfma(st->dt, rows, N.d.cin, N.d.cout)) T.gparts = gated_dgrad_parts(rows, N.d.cin, N.d.cout);
+        else if (const GatherConv dg = dgrad_geom(st, N); use_mfma_gather(st, dg)) T.gparts = (int)(conv_gather_mfma_raw_workspace(dg) / (T.elems * sizeof(float)));
+        T.rest = by_gated && N.d.kh == BAPIPE_GATE_RELU;
+    }
+
     // ---- memory plan
     size_t slot = 0, trans = 0, gr = 0;
     for (int t = 0; t < nt; ++t) {
@@ -1428,7 +1458,8 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         if (T.root != t) continue;
         if (T.stashed) { T.off = slot; slot += align_up(T.bytes()); }
         else { T.off = trans; trans += align_up(T.bytes()); }
-        if (T.need_grad && t != last_t) { T.goff = gr; gr += align_up(T.bytes()); }
+        if (T.rest) { T.rest_off = trans; trans += align_up(T.bytes()); }
+        if (T.need_grad && t != last_t) { T.goff = gr; gr += align_up(T.gparts ? T.elems * T.gparts * sizeof(float) : T.bytes()); }
     }
     {   // gradient of the stage output (ingest target when the caller's dy cannot be used in place)
         Tensor &T = st->tensors[root_of(last_t)];
@@ -1494,7 +1525,7 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
             L.aux_off = L.off_pd = slot; L.aux_bytes = (size_t)rows * 2 * L.d.cout * sizeof(float); slot += align_up(L.aux_bytes);
             L.off_d = gr; gr += align_up((size_t)rows * 2 * L.d.cout * es);
             L.mfma = gated_mfma(st->dt, rows, L.d.cin, L.d.cout);
-            size_t w = gated_workspace(st->dt, rows, L.d.cin, L.d.cout);
+            size_t w = gated_workspace(st->dt, rows, L.d.cin, L.d.cout, A.rest);
             work = w > work ? w : work;
             if (L.mfma) {
                 const ConvShape cs = conv_shape(st, L);
