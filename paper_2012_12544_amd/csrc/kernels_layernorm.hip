@@ -8,8 +8,8 @@
 // all digits) without a second read.  A group of threads takes one row after another and keeps what belongs to its columns,
 // gamma and beta, or gamma and the sums of the columns' gradients: read for every row, the two floats of a bf16 element are twice
 // the bytes of the element's load and store.  The next row is requested before the present one's sums are formed.
-#include "dev_common.h"
 #include "kernels.h"
+#include "mfma_common.h"
 
 namespace bapipe {
 namespace {
@@ -55,6 +55,13 @@ __device__ __forceinline__ float group_sum(float v, float *lds, int half)
     }
 }
 
+// The thread's group in its block, known to be the same for a wave where it is: a row's address is then none of its registers'
+template <int G> __device__ __forceinline__ int group_of()
+{
+    const int group = threadIdx.x / G;
+    return G >= 64 ? __builtin_amdgcn_readfirstlane(group) : group;
+}
+
 // ------------------------------------------------------------------ rows that fit their threads' registers
 // V = 16 / sizeof(T) values in one access at any address of T (global memory needs no more alignment than that); where a row
 // is no whole number of them (TAIL), the last ones of it are `left` < V single values, and zeros behind them
@@ -81,14 +88,54 @@ template <bool TAIL, class T, int V> __device__ __forceinline__ void store_vec(T
         if (j < left) to[j] = from.e[j];
 }
 
+// Values of T stay packed as they were read: taken apart, two bf16 would be two registers
+template <bool TAIL, class T> __device__ __forceinline__ chunk16 load_packed(const T *from, int left)
+{
+    vec_of<T, 16 / sizeof(T)> v;
+    load_vec<TAIL>(v, from, left);
+    return __builtin_bit_cast(chunk16, v);
+}
+template <class T> __device__ __forceinline__ float value(chunk16 c, int j)
+{
+    if constexpr (sizeof(T) == 4) return __uint_as_float(c[j]);
+    else return __uint_as_float(j % 2 ? c[j / 2] & 0xFFFF0000u : c[j / 2] << 16);
+}
+
 // Thread t of a group of G has columns (k G + t) V .. + V - 1, k < NV.
-template <class T, int V, int NV> struct row_regs {
-    vec_of<T, V> v[NV];
+template <class T, int NV> struct row_regs {
+    static constexpr int V = 16 / sizeof(T);
+    chunk16 v[NV];
     template <int G, bool TAIL> __device__ __forceinline__ void load(const T *row, int t, int C)
     {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * G + t) * V;
+            v[k] = chunk16{0u, 0u, 0u, 0u};
+            if (c < C) v[k] = load_packed<TAIL>(row + c, C - c);
+        }
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) v[k] = chunk16{0u, 0u, 0u, 0u};
+    }
+    __device__ __forceinline__ float at(int k, int j) const { return value<T>(v[k], j); }
+    // what was computed from the values so far is not to be kept for later
+    __device__ __forceinline__ void forget()
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(v[k]));
+    }
+};
+template <int V, int NV> struct column_regs {
+    vec_of<float, V> v[NV];
+    template <int G, bool TAIL> __device__ __forceinline__ void load(const float *row, int t, int C)
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * G + t) * V;
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[k].e[j] = 0.0f;
             if (c < C) load_vec<TAIL>(v[k], row + c, C - c);
         }
     }
@@ -108,11 +155,11 @@ __global__ __launch_bounds__(TPB) void k_layernorm_fwd(FwdArgs<T> p)
     constexpr int V = 16 / sizeof(T);
     __shared__ float lds[2 * TPB / 64];
     const int t = threadIdx.x % G, C = p.C, step = gridDim.x * (TPB / G);
-    int row = blockIdx.x * (TPB / G) + threadIdx.x / G;
-    row_regs<float, V, NV> gamma, beta;
+    int row = blockIdx.x * (TPB / G) + group_of<G>();
+    column_regs<V, NV> gamma, beta;
     gamma.template load<G, TAIL>(p.gamma, t, C);
     beta.template load<G, TAIL>(p.beta, t, C);
-    row_regs<T, V, NV> next;
+    row_regs<T, NV> next;
     if (row < p.rows) next.template load<G, TAIL>(p.x + (size_t)row * C, t, C);
     const float per = 1.0f / C;
     // columns behind the row's end
@@ -120,14 +167,14 @@ __global__ __launch_bounds__(TPB) void k_layernorm_fwd(FwdArgs<T> p)
     // all groups of a block take the same number of turns, for they meet at barriers
     for (int first = blockIdx.x * (TPB / G); first < p.rows; first += step, row += step) {
         const bool on = row < p.rows;
-        const row_regs<T, V, NV> x = next;
+        const row_regs<T, NV> x = next;
         if (row + step < p.rows) next.template load<G, TAIL>(p.x + (size_t)(row + step) * C, t, C);
         float f[NV][V], sum = 0.0f, sq = 0.0f;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                f[k][j] = in(k, j) ? to_f32(x.v[k].e[j]) : 0.0f;
+                f[k][j] = in(k, j) ? x.at(k, j) : 0.0f;
                 sum += f[k][j];
             }
         const float mean = group_sum<G>(sum, lds, 0) * per;
@@ -154,7 +201,7 @@ __global__ __launch_bounds__(TPB) void k_layernorm_fwd(FwdArgs<T> p)
             }
             store_vec<TAIL>(p.y + at, y, C - c);
             if (p.rest) store_vec<TAIL>(p.rest + at, rest, C - c);
-            if (p.copy) store_vec<TAIL>(p.copy + at, x.v[k], C - c);
+            if (p.copy) store_vec<TAIL>(p.copy + at, __builtin_bit_cast(vec_of<T, V>, x.v[k]), C - c);
         }
         if (t == 0) {
             p.stats[row] = mean;
@@ -175,74 +222,104 @@ template <class T> struct BwdArgs {
     int rows, C;
 };
 
-// NT threads, NT / G groups whose columns' sums meet in LDS at the end, the upper half's added to the lower half's each time
-template <class T, int NV, int G, int NT, bool TAIL, bool PARTS>
-__global__ __launch_bounds__(NT) void k_layernorm_bwd(BwdArgs<T> p)
+// NT threads, NT / G groups whose columns' sums meet in LDS at the end, the upper half's added to the lower half's each time.
+// A row is taken from its packed values twice, for the sums and for dx: kept as floats in between, two rows of them, it cost twice
+// the registers, and rows of 8192 spilled (142 MB x 2 forward, 2 x 403 MB backward: 341 us of 165 at the copy's rate).
+template <class T, int NV, int G, int NT, bool TAIL, bool PARTS, bool EPI>
+__global__ __launch_bounds__(NT, NV == 1 || (NV == 2 && !EPI) ? 4 : 2) void k_layernorm_bwd(BwdArgs<T> p)
 {
     extern __shared__ __align__(16) float lds[];
     constexpr int V = 16 / sizeof(T), GROUPS = NT / G;
-    const int t = threadIdx.x % G, group = threadIdx.x / G, C = p.C, step = gridDim.x * GROUPS;
+    const int t = threadIdx.x % G, group = group_of<G>(), C = p.C, step = gridDim.x * GROUPS;
     int row = blockIdx.x * GROUPS + group;
-    row_regs<float, V, NV> gamma;
+    column_regs<V, NV> gamma;
     gamma.template load<G, TAIL>(p.gamma, t, C);
     float sg[NV][V] = {}, sb[NV][V] = {};
-    row_regs<T, V, NV> nx, nd;
+    row_regs<T, NV> nx, nd;
+    float nmean = 0.0f, ninv = 0.0f;
     auto request = [&](int r) {
+        nmean = p.stats[r];
+        ninv = p.stats[p.rows + r];
         nx.template load<G, TAIL>(p.x + (size_t)r * C, t, C);
         if (!PARTS) nd.template load<G, TAIL>(p.dy + (size_t)r * C, t, C);
     };
+    nx.clear();
+    nd.clear();
     if (row < p.rows) request(row);
     const float per = 1.0f / C;
     for (int first = blockIdx.x * GROUPS; first < p.rows; first += step, row += step) {
         const bool on = row < p.rows;
-        const row_regs<T, V, NV> xr = nx, dr = nd;
+        row_regs<T, NV> x = nx, dy = nd;
+        const float mean = nmean, inv = ninv;
         if (row + step < p.rows) request(row + step);
-        const float mean = on ? p.stats[row] : 0.0f, inv = on ? p.stats[p.rows + row] : 0.0f;
+        else {                                           // behind its last row a group adds nothing to anything
+            nmean = ninv = 0.0f;
+            nx.clear();
+            nd.clear();
+        }
         const size_t base = (size_t)row * C;
-        float xh[NV][V], d[NV][V], s1 = 0.0f, s2 = 0.0f;
+        float sums[PARTS ? NV : 1][V];
+        if constexpr (PARTS) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int c = (k * G + t) * V;
+            for (int k = 0; k < NV; ++k) {
+                const int c = (k * G + t) * V;
 #pragma unroll
-            for (int j = 0; j < V; ++j) d[k][j] = 0.0f;
-            if constexpr (PARTS) {
+                for (int j = 0; j < V; ++j) sums[k][j] = 0.0f;
                 if (on && c < C)
                     for (int s = 0; s < p.parts; ++s) {
                         vec_of<float, V> v;
                         load_vec<TAIL>(v, p.dy_parts + (size_t)s * p.rows * C + base + c, C - c);
 #pragma unroll
-                        for (int j = 0; j < V; ++j) d[k][j] += v.e[j];
+                        for (int j = 0; j < V; ++j) sums[k][j] += v.e[j];
                     }
             }
+        }
+        // dy and xhat of a column; behind the row's end dy is 0
+        auto column = [&](int k, int j, float &d, float &xh) {
+            d = PARTS ? sums[PARTS ? k : 0][j] : dy.at(k, j);
+            xh = (x.at(k, j) - mean) * inv;
+        };
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const bool in = on && c + (TAIL ? j : 0) < C;
-                if (!PARTS) d[k][j] = in ? to_f32(dr.v[k].e[j]) : 0.0f;
-                xh[k][j] = in ? (to_f32(xr.v[k].e[j]) - mean) * inv : 0.0f;
-                sg[k][j] = fmaf(d[k][j], xh[k][j], sg[k][j]);
-                sb[k][j] += d[k][j];
-                d[k][j] *= c < C ? gamma.v[k].e[j] : 0.0f;
-                s1 += d[k][j];
-                s2 = fmaf(d[k][j], xh[k][j], s2);
+                float d, xh;
+                column(k, j, d, xh);
+                const float dx = d * xh, g = gamma.v[k].e[j];
+                sg[k][j] += dx;
+                sb[k][j] += d;
+                s1 = fmaf(d, g, s1);
+                s2 = fmaf(dx, g, s2);
             }
+            __builtin_amdgcn_sched_barrier(0);           // one access's columns at a time, or all of them are in registers at once
         }
         if (!p.dx) continue;
         s1 = group_sum<G>(s1, lds, 0) * per;
         s2 = group_sum<G>(s2, lds, 1) * per;
         if (!on) continue;
+        x.forget();
+        dy.forget();
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * G + t) * V;
             if (c >= C) continue;
-            vec_of<T, V> r, old, gate;
-            if (p.old) load_vec<TAIL>(old, p.old + base + c, C - c);
-            if (p.gate) load_vec<TAIL>(gate, p.gate + base + c, C - c);
+            vec_of<T, V> r;
+            chunk16 old, gate;
+            if (EPI && p.old) old = load_packed<TAIL>(p.old + base + c, C - c);
+            if (EPI && p.gate) gate = load_packed<TAIL>(p.gate + base + c, C - c);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float v = inv * (d[k][j] - s1 - xh[k][j] * s2);
-                r.e[j] = grad_out<T>(v, p.old != nullptr, p.old ? old.e[j] : from_f32<T>(0.0f), p.gate != nullptr, p.gate ? gate.e[j] : from_f32<T>(0.0f));
+                float d, xh;
+                column(k, j, d, xh);
+                const float v = inv * (d * gamma.v[k].e[j] - s1 - xh * s2);
+                if constexpr (!EPI) r.e[j] = from_f32<T>(v);
+                else
+                    r.e[j] = grad_out<T>(v, p.old != nullptr, from_f32<T>(p.old ? value<T>(old, j) : 0.0f), p.gate != nullptr,
+                                         from_f32<T>(p.gate ? value<T>(gate, j) : 0.0f));
             }
             store_vec<TAIL>(p.dx + base + c, r, C - c);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     __syncthreads();
@@ -389,28 +466,27 @@ __global__ __launch_bounds__(TPB) void k_layernorm_params(const float *__restric
 
 // ------------------------------------------------------------------ which kernel takes a row
 // G threads and NV accesses of each for a row, the smallest that fit it: a wave for a row of up to 4 a thread (forward) or 2 (backward,
-// which has two rows of registers and two sums for every column), four waves above.  G = 0: too long for registers.
+// which has two rows of registers and two sums for every column: of 4 it spills), then four and eight waves.  G = 0: too long for registers.
 struct Shape {
     int nv, g;
 };
 Shape shape_of(int dt, int C, bool fwd)
 {
     const int v = dt == DT_F32 ? 4 : 8, n = (C + v - 1) / v;
-    for (int g = 8; g <= 64; g *= 2)
-        if (n <= g) return {1, g};
-    for (int nv = 2; nv <= (fwd ? 4 : 2); nv *= 2)
-        if (n <= 64 * nv) return {nv, 64};
-    for (int nv = 1; nv <= 8; nv *= 2)
-        if (n <= 256 * nv) return {nv, 256};
+    static const Shape forward[] = {{1, 8}, {1, 16}, {1, 32}, {1, 64}, {2, 64}, {4, 64}, {2, 256}, {4, 256}, {8, 256}};
+    static const Shape backward[] = {{1, 8}, {1, 16}, {1, 32}, {1, 64}, {2, 64}, {1, 256}, {2, 256}, {2, 512}, {4, 512}};
+    for (const Shape &k : fwd ? forward : backward)
+        if (n <= k.nv * k.g) return k;
     return {0, 0};
 }
 
 // Blocks of the backward pass: each leaves 8 C bytes of column sums for the kernel behind it, against 6 C bytes a row and more of its
-// own, so that a block takes 32 rows where that leaves enough of them, and four rounds of its groups at the least
+// own, so that a block takes 32 rows where that leaves two for every unit; up to four rounds of one block's groups do without that kernel
 int bwd_blocks(int rows, int groups)
 {
-    const int most = (rows + 4 * groups - 1) / (4 * groups), long_ones = rows / 32, many = long_ones > 512 ? 512 : long_ones < 256 ? 256 : long_ones;
-    return most < many ? most : many;
+    if (rows <= 4 * groups) return 1;
+    const int all = (rows + groups - 1) / groups, long_ones = rows / 32, many = long_ones > 512 ? 512 : long_ones < 256 ? 256 : long_ones;
+    return all < many ? all : many;
 }
 constexpr int kLongChunks = 256;
 
@@ -457,17 +533,21 @@ static hipError_t bwd_t(int dt, BwdArgs<T> p, hipStream_t s)
     };
     hipError_t e = hipErrorInvalidValue;
     bool found = false;
+    const bool epi = p.old || p.gate;
+#define BWD_(NV, G, NT, TAIL, PARTS) \
+    (epi ? launch(k_layernorm_bwd<T, NV, G, NT, TAIL, PARTS, true>, NT, NT / G) : launch(k_layernorm_bwd<T, NV, G, NT, TAIL, PARTS, false>, NT, NT / G))
 #define BWD(NV, G, NT)                                                                                             \
     if (!found && k.nv == NV && k.g == G) {                                                                        \
         found = true;                                                                                              \
         if constexpr (sizeof(T) == 2) {                                                                            \
-            if (p.dy_parts) e = tail ? launch(k_layernorm_bwd<T, NV, G, NT, true, true>, NT, NT / G) : launch(k_layernorm_bwd<T, NV, G, NT, false, true>, NT, NT / G); \
+            if (p.dy_parts) e = tail ? BWD_(NV, G, NT, true, true) : BWD_(NV, G, NT, false, true);                 \
         }                                                                                                          \
-        if (!p.dy_parts) e = tail ? launch(k_layernorm_bwd<T, NV, G, NT, true, false>, NT, NT / G) : launch(k_layernorm_bwd<T, NV, G, NT, false, false>, NT, NT / G); \
+        if (!p.dy_parts) e = tail ? BWD_(NV, G, NT, true, false) : BWD_(NV, G, NT, false, false);                  \
     }
     BWD(1, 8, 512); BWD(1, 16, 512); BWD(1, 32, 512); BWD(1, 64, 512); BWD(2, 64, 512);
-    BWD(1, 256, 512); BWD(2, 256, 512); BWD(4, 256, 512); BWD(8, 256, 256);
+    BWD(1, 256, 512); BWD(2, 256, 512); BWD(2, 512, 512); BWD(4, 512, 512);
 #undef BWD
+#undef BWD_
     if (!found) {
         // the columns first, for dx may take the place of dy
         const int per = p.rows < 64 * kLongChunks ? 64 : (p.rows + kLongChunks - 1) / kLongChunks;
