@@ -425,20 +425,29 @@ __global__ __launch_bounds__(TPB) void k_gated_grad(const T *__restrict__ dh, co
     *reinterpret_cast<vec *>(D + at + F) = du;
 }
 
-// ------------------------------------------------------------------ bf16, many rows: both projections, activation and product in one kernel
-// A block takes BP rows and BU units, a tile of 2 BU weight rows: their gates' and their linear parts'.  A wave has WT_P rows
-// of WT_U units, gates and linear parts of the same units in the same lanes, so that the activation meets both in registers.
-// Tiles of 64 of K come HBM / L2 -> LDS without passing registers into a ring of two (see mfma_common.h; the swizzle of a tile's
-// 16-byte chunks is applied by choosing which one a lane fetches).  Fragments are read one step of 16 ahead of the products that
+// ------------------------------------------------------------------ many rows of whole 16 bytes
+// One kernel for three products of rows with rows, x [rows][K] and w [.][K]:
+//   MM_FORWARD  both projections, activation and product.  A block's weights are the gates and the linear parts of BU units, a wave's
+//               those of the same units in the same lanes, so that the activation meets both in registers
+//   MM_PROJECT  dh of a 1x1 convolution's input gradient, w its transposed filter [F][K], turned into D from the projections at once:
+//               dh is neither stored nor rounded
+//   MM_DX       dx = D W of a float layer (of a bf16 one it is the gather kernel's)
+// A block takes BP rows and 2 BU weight rows, a wave BP / WP of BU / WU units (MM_FORWARD) or twice as many columns.
+// Tiles of 128 bytes of K come HBM / L2 -> LDS without passing registers into a ring of two (see mfma_common.h; the swizzle of a tile's
+// 16-byte chunks is applied by choosing which one a lane fetches).  Fragments are read one step of 32 bytes ahead of the products that
 // need them; the barrier that publishes the next tile lies before a tile's last products, when every wave has all of the tile in registers, and
 // the slot is filled again at once.
+// 8192 rows, 4096->11008 of bf16, us (two products of 739 GFLOP each): MM_FORWARD 1420, 721 MB of projections and 180 of h among them, the gather
+// kernel alone on as large a product 1316.
 // `rest`: x is the sum of two tensors; K is walked twice with the same weights.
+enum { MM_FORWARD, MM_PROJECT, MM_DX };
 struct MmArgs {
-    const bf16_t *x, *rest, *w;      // [rows][K], [2F][K]
-    int rows, K, F;
+    const void *x, *rest, *w;        // [rows][K], [2F or N][K]
+    int rows, K, N;                  // N: units or columns
     const float *bias;
-    float *P;                        // [rows][2F]
-    bf16_t *out;                     // h [rows][F]
+    float *P;                        // [rows][2N], written or (MM_PROJECT) read
+    void *out;                       // h [rows][N], D [rows][2N], dx [rows][N]
+    const void *old, *gate;          // MM_DX: see grad_out()
     unsigned x_bytes, w_bytes;
     int tiles_p, tiles_u, act;
 };
@@ -447,85 +456,82 @@ struct MmArgs {
 // tiles, in one row of tiles for 33
 constexpr int MM_ROWS = 8;
 
-template <int BP, int BU, int WP, int WU>
+template <class T, int MODE, int BP, int BU, int WP, int WU>
 __global__ __launch_bounds__(WP *WU * 64, 2) void k_gated_mfma(MmArgs p)
 {
-    constexpr int NW = WP * WU, BK = 64, BC = 2 * BU, STAGE = (BP + BC) * BK;
+    constexpr bool FWD = MODE == MM_FORWARD;
+    constexpr int ES = sizeof(T), NW = WP * WU, BKB = 128, BC = 2 * BU, STAGE = (BP + BC) * BKB;      // bytes
     constexpr int XL = BP / (8 * NW), WL = BC / (8 * NW);       // wave-wide loads a tile, 8 rows each
-    constexpr int TP = BP / WP / 32, TU = BU / WU / 32, KSUB = BK / 16;
+    constexpr int TP = BP / WP / 32, TC = 2 * BU / WU / 32, TU = TC / 2, KSUB = BKB / 32;
     static_assert(XL >= 1 && WL >= 1 && TP >= 1 && TU >= 1, "tile and waves");
     extern __shared__ __align__(16) unsigned char smem[];
     const lds_addr_of lds_of(smem);
-    uint16_t *ring = reinterpret_cast<uint16_t *>(smem);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wp = wave % WP, wu = wave / WP;
     auto swz = [](int row) { return (row >> 1) & 7; };
     const int lrow = lane / 8, lc = (lane % 8) ^ swz(wave * 8 + lrow);      // the same for every load: they lie 8 NW rows apart
 
+    constexpr int WIDE = FWD ? BU : BC;
     const int bid = xcd_remap(blockIdx.x, gridDim.x);
     const int per = MM_ROWS * p.tiles_u, first = bid / per * MM_ROWS, here = p.tiles_p - first < MM_ROWS ? p.tiles_p - first : MM_ROWS;
-    const int row0 = (first + bid % per % here) * BP, unit0 = bid % per / here * BU;
+    const int row0 = (first + bid % per % here) * BP, col0 = bid % per / here * WIDE;
 
     constexpr unsigned OOB = 0x80000000u;
-    __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(p.x), 0, (int)p.x_bytes, 0x00020000);
-    __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(p.w), 0, (int)p.w_bytes, 0x00020000);
+    __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p.x), 0, (int)p.x_bytes, 0x00020000);
+    __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p.w), 0, (int)p.w_bytes, 0x00020000);
     // rows past the end lie behind the buffer and read zeros; gates past the last unit read linear parts, whose products nobody stores
+    const unsigned pitch = (unsigned)p.K * ES;
     unsigned xoff[XL], woff[WL];
 #pragma unroll
-    for (int i = 0; i < XL; ++i) xoff[i] = ((unsigned)(row0 + (i * NW + wave) * 8 + lrow) * (unsigned)p.K + 8u * lc) * 2u;
+    for (int i = 0; i < XL; ++i) xoff[i] = (unsigned)(row0 + (i * NW + wave) * 8 + lrow) * pitch + 16u * lc;
 #pragma unroll
     for (int i = 0; i < WL; ++i) {
-        const int r = (i * NW + wave) * 8 + lrow, row = r < BU ? unit0 + r : p.F + unit0 + r - BU;
-        woff[i] = ((unsigned)row * (unsigned)p.K + 8u * lc) * 2u;
+        const int r = (i * NW + wave) * 8 + lrow, row = !FWD || r < BU ? col0 + r : p.N + col0 + r - BU;
+        woff[i] = (unsigned)row * pitch + 16u * lc;
     }
-    const int KT = (p.K + BK - 1) / BK, n_it = p.rest ? 2 * KT : KT;
+    const int KT = (int)((pitch + BKB - 1) / BKB), n_it = p.rest ? 2 * KT : KT;
     int at = 0;                              // next tile to ask for
     auto issue = [&](int slot) {
-        uint16_t *sw = ring + slot * STAGE, *sx = sw + BC * BK;
-        if (at == KT && p.rest) xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t *>(p.rest), 0, (int)p.x_bytes, 0x00020000);
-        const int k0 = (at < KT ? at : at - KT) * BK;
-        const bool in = at < n_it && k0 + 8 * lc < p.K;
-        const unsigned ko = (unsigned)k0 * 2u;
+        unsigned char *sw = smem + slot * STAGE, *sx = sw + BC * BKB;
+        if (at == KT && p.rest) xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p.rest), 0, (int)p.x_bytes, 0x00020000);
+        const unsigned ko = (unsigned)(at < KT ? at : at - KT) * BKB;
+        const bool in = at < n_it && ko + 16u * lc < pitch;
 #pragma unroll
-        for (int i = 0; i < XL; ++i) dma16(xr, lds_of(sx + (i * NW + wave) * 8 * BK), in ? xoff[i] + ko : OOB);
+        for (int i = 0; i < XL; ++i) dma16(xr, lds_of(sx + (i * NW + wave) * 8 * BKB), in ? xoff[i] + ko : OOB);
 #pragma unroll
-        for (int i = 0; i < WL; ++i) dma16(wr, lds_of(sw + (i * NW + wave) * 8 * BK), in ? woff[i] + ko : OOB);
+        for (int i = 0; i < WL; ++i) dma16(wr, lds_of(sw + (i * NW + wave) * 8 * BKB), in ? woff[i] + ko : OOB);
         ++at;
     };
-    f32x16 acc[TP][2 * TU];
+    f32x16 acc[TP][TC];
 #pragma unroll
     for (int a = 0; a < TP; ++a)
 #pragma unroll
-        for (int b = 0; b < 2 * TU; ++b)
+        for (int b = 0; b < TC; ++b)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.0f;
     const int frow = lane & 31, fhalf = lane >> 5;
-    auto load_frags = [&](int slot, int k16, bf16x8_t(&fx)[TP], bf16x8_t(&fw)[2 * TU]) {
-        const uint16_t *cw = ring + slot * STAGE, *cx = cw + BC * BK;
-        const int ch = 2 * k16 + fhalf;
+    // column of a wave's tile b inside the block's weight rows
+    auto tile_row = [&](int b) { return FWD ? b / TU * BU + (wu * TU + b % TU) * 32 : (wu * TC + b) * 32; };
+    auto load_frags = [&](int slot, int k, chunk16(&fx)[TP], chunk16(&fw)[TC]) {
+        const unsigned char *cw = smem + slot * STAGE, *cx = cw + BC * BKB;
+        const int ch = 2 * k + fhalf;
 #pragma unroll
-        for (int b = 0; b < 2 * TU; ++b) {
-            const int row = b / TU * BU + (wu * TU + b % TU) * 32 + frow;
-            fw[b] = as_frag(*reinterpret_cast<const chunk16 *>(cw + row * BK + ((ch ^ swz(row)) << 3)));
+        for (int b = 0; b < TC; ++b) {
+            const int row = tile_row(b) + frow;
+            fw[b] = *reinterpret_cast<const chunk16 *>(cw + row * BKB + ((ch ^ swz(row)) << 4));
         }
 #pragma unroll
         for (int a = 0; a < TP; ++a) {
             const int row = (wp * TP + a) * 32 + frow;
-            fx[a] = as_frag(*reinterpret_cast<const chunk16 *>(cx + row * BK + ((ch ^ swz(row)) << 3)));
+            fx[a] = *reinterpret_cast<const chunk16 *>(cx + row * BKB + ((ch ^ swz(row)) << 4));
         }
-    };
-    auto products = [&](const bf16x8_t(&fx)[TP], const bf16x8_t(&fw)[2 * TU]) {
-#pragma unroll
-        for (int a = 0; a < TP; ++a)
-#pragma unroll
-            for (int b = 0; b < 2 * TU; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[a], fw[b], acc[a][b], 0, 0, 0);
     };
     issue(0);
     issue(1);
     WAIT_VMCNT(XL + WL);
     WAIT_LGKMCNT(0);
     __builtin_amdgcn_s_barrier();
-    bf16x8_t fx[2][TP], fw[2][2 * TU];
+    chunk16 fx[2][TP], fw[2][TC];
     load_frags(0, 0, fx[0], fw[0]);
     for (int it = 0; it < n_it; ++it) {
         const int slot = it & 1;
@@ -533,7 +539,7 @@ __global__ __launch_bounds__(WP *WU * 64, 2) void k_gated_mfma(MmArgs p)
         for (int j = 0; j + 1 < KSUB; ++j) {
             load_frags(slot, j + 1, fx[(j + 1) & 1], fw[(j + 1) & 1]);
             __builtin_amdgcn_sched_barrier(0);               // keep the reads ahead of the products that hide them
-            products(fx[j & 1], fw[j & 1]);
+            multiply<T>(acc, fx[j & 1], fw[j & 1]);
             __builtin_amdgcn_sched_barrier(0);
         }
         WAIT_LGKMCNT(0);                                     // this wave has read all of the tile
@@ -542,28 +548,70 @@ __global__ __launch_bounds__(WP *WU * 64, 2) void k_gated_mfma(MmArgs p)
         load_frags(slot ^ 1, 0, fx[0], fw[0]);
         __builtin_amdgcn_sched_barrier(0);
         issue(slot);
-        products(fx[1], fw[1]);
+        multiply<T>(acc, fx[1], fw[1]);
         __builtin_amdgcn_sched_barrier(0);
     }
     WAIT_VMCNT(0);
-    // register r of lane l: row 8 (r / 4) + 4 (l / 32) + r % 4, unit l % 32
+    // register r of lane l: row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32
+    auto row_of = [&](int a, int r) { return row0 + (wp * TP + a) * 32 + 8 * (r / 4) + 4 * fhalf + r % 4; };
+    if constexpr (FWD) {
 #pragma unroll
-    for (int b = 0; b < TU; ++b) {
-        const int unit = unit0 + (wu * TU + b) * 32 + frow;
-        if (unit >= p.F) continue;
-        const float bg = p.bias ? p.bias[unit] : 0.0f, bu = p.bias ? p.bias[p.F + unit] : 0.0f;
+        for (int b = 0; b < TU; ++b) {
+            const int unit = col0 + tile_row(b) + frow;
+            if (unit >= p.N) continue;
+            const float bg = p.bias ? p.bias[unit] : 0.0f, bu = p.bias ? p.bias[p.N + unit] : 0.0f;
 #pragma unroll
-        for (int a = 0; a < TP; ++a)
+            for (int a = 0; a < TP; ++a)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = row0 + (wp * TP + a) * 32 + 8 * (r / 4) + 4 * fhalf + r % 4;
-                if (row >= p.rows) continue;
-                const float g = acc[a][b][r] + bg, u = acc[a][TU + b][r] + bu;
-                float *P = p.P + (size_t)row * 2 * p.F + unit;
-                P[0] = g;
-                P[p.F] = u;
-                p.out[(size_t)row * p.F + unit] = from_f32<bf16_t>(act_value<true>(p.act, g) * u);
+                for (int r = 0; r < 16; ++r) {
+                    const int row = row_of(a, r);
+                    if (row >= p.rows) continue;
+                    const float g = acc[a][b][r] + bg, u = acc[a][TU + b][r] + bu;
+                    float *P = p.P + (size_t)row * 2 * p.N + unit;
+                    P[0] = g;
+                    P[p.N] = u;
+                    ((T *)p.out)[(size_t)row * p.N + unit] = from_f32<T>(act_value<kFast<T>>(p.act, g) * u);
+                }
+        }
+    } else {
+#pragma unroll
+        for (int b = 0; b < TC; ++b) {
+            const int col = col0 + tile_row(b) + frow;
+            if (col >= p.N) continue;
+#pragma unroll
+            for (int a = 0; a < TP; ++a) {
+                if constexpr (MODE == MM_PROJECT) {
+                    float g[16], u[16];                      // asked for together
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int row = row_of(a, r);
+                        const float *P = p.P + (size_t)(row < p.rows ? row : p.rows - 1) * 2 * p.N + col;
+                        g[r] = P[0];
+                        u[r] = P[p.N];
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int row = row_of(a, r);
+                        float v, dv;
+                        act_both<kFast<T>>(p.act, g[r], v, dv);
+                        if (row >= p.rows) continue;
+                        T *D = (T *)p.out + (size_t)row * 2 * p.N + col;
+                        D[0] = from_f32<T>(acc[a][b][r] * u[r] * dv);
+                        D[p.N] = from_f32<T>(acc[a][b][r] * v);
+                    }
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int row = row_of(a, r);
+                        if (row >= p.rows) continue;
+                        const size_t i = (size_t)row * p.N + col;
+                        const T *old = (const T *)p.old, *gate = (const T *)p.gate;
+                        ((T *)p.out)[i] = grad_out<T>(acc[a][b][r], old != nullptr, old ? old[i] : from_f32<T>(0.0f), gate != nullptr,
+                                                      gate ? gate[i] : from_f32<T>(0.0f));
+                    }
+                }
             }
+        }
     }
 }
 
@@ -620,14 +668,50 @@ bool gated_mfma(int dt, int rows, int C, int F)
            conv_gather_mfma_supported(rows_product(rows, 2 * F, C, false)) && conv_wgrad_mfma_supported({rows, 1, 1, C, 1, 1, 2 * F, 1, 1, 1, 0});
 }
 
-// Up to 64 rows the weights' bytes are what takes the time, and the gather kernel splits K over as many blocks as it takes to stream them.
-// (K above 2^20: the offsets of rows past a tensor's end may not pass 2^32.)
-static bool streams_weights(int rows, int C) { return rows <= 64 || C > 1 << 20; }
+template <class T, int MODE, int BP, int BU, int WP, int WU>
+static hipError_t launch_mm_tile(MmArgs a, hipStream_t s)
+{
+    constexpr int bytes = 2 * (BP + 2 * BU) * 128, wide = MODE == MM_FORWARD ? BU : 2 * BU;
+    auto kernel = k_gated_mfma<T, MODE, BP, BU, WP, WU>;
+    if (bytes > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+    }
+    a.tiles_p = (a.rows + BP - 1) / BP;
+    a.tiles_u = (a.N + wide - 1) / wide;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)a.tiles_p * a.tiles_u), dim3(WP * WU * 64), bytes, s, a);
+    return hipGetLastError();
+}
+
+// tiles of a product, counted in weight rows
+static long long mm_tiles(int rows, long long weight_rows, int tile_p, int tile_w) { return (rows + tile_p - 1) / tile_p * ((weight_rows + tile_w - 1) / tile_w); }
+
+// The tile whose rounds of the chip are the least work: a block of 256 x 256 or 256 x 128 to a unit, or two of 128 x 128, whose products
+// take 1.05 and 1.15 times as long each (4096 rows, 2048->5632, us: 704 of the first, three rounds, 204; 2816 of the last, six, 234)
+template <class T, int MODE> static hipError_t launch_mm(MmArgs a, hipStream_t s)
+{
+    const long long w = MODE == MM_FORWARD ? 2ll * a.N : a.N;
+    auto rounds = [&](int tile_p, int tile_w, int slots) { return (double)((mm_tiles(a.rows, w, tile_p, tile_w) + slots - 1) / slots); };
+    const double whole = rounds(256, 256, 256) * 4.0, half = rounds(256, 128, 256) * 2.0 * 1.05, small = rounds(128, 128, 512) * 2.0 * 1.15;
+    if (whole <= half && whole <= small) return launch_mm_tile<T, MODE, 256, 128, 2, 4>(a, s);
+    if (half <= small) return launch_mm_tile<T, MODE, 256, 64, 4, 2>(a, s);
+    return launch_mm_tile<T, MODE, 128, 64, 2, 2>(a, s);
+}
+
+// Whether k_gated_mfma takes a product: rows of whole 16 bytes, offsets that 32 bits hold, those of a tile's rows behind the last ones among
+// them, and tiles enough for it.  Of few the other kernels split K (forward, us, this / those: bf16, 1024 rows, 1024->1024, 128 tiles, 18.9 / 16.8,
+// 2048 rows, 512->1024, 256 tiles, 16.4 / 23.6; float, 2048 rows, 512->1024, 256 tiles, 45.6 / 43.7).
+static bool mm_takes(int dt, int rows, int K, long long weight_rows)
+{
+    const size_t es = dt_size(dt);
+    return K * es % 16 == 0 && K * es <= 2u << 20 && (size_t)rows * K * es < (1u << 31) && (size_t)weight_rows * K * es < (1u << 31) && rows > 64 &&
+           mm_tiles(rows, weight_rows, 128, 128) >= (dt == DT_F32 ? 512 : 192);
+}
 
 size_t gated_workspace(int dt, int rows, int C, int F, bool rest)
 {
     const size_t walks = rest ? 2 : 1;
-    if (gated_mfma(dt, rows, C, F)) return streams_weights(rows, C) ? walks * conv_gather_mfma_raw_workspace(rows_product(rows, C, 2 * F, false)) : 0;
+    if (gated_mfma(dt, rows, C, F)) return mm_takes(dt, rows, C, 2ll * F) ? 0 : walks * conv_gather_mfma_raw_workspace(rows_product(rows, C, 2 * F, false));
     auto sums = [](const AnyPlan &p, size_t n) { return p.splits > 1 ? (size_t)p.splits * n * sizeof(float) : 0; };
     size_t most = colsum_workspace(rows, 2 * F);
     const AnyPlan f = forward_plan(rows, C, F);
@@ -643,21 +727,6 @@ size_t gated_workspace(int dt, int rows, int C, int F, bool rest)
         else { using T = bf16_t; __VA_ARGS__; }                       \
     } while (0)
 
-template <int BP, int BU, int WP, int WU>
-static hipError_t launch_mfma(MmArgs a, hipStream_t s)
-{
-    constexpr int bytes = 2 * (BP + 2 * BU) * 64 * 2;
-    auto kernel = k_gated_mfma<BP, BU, WP, WU>;
-    if (bytes > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (e != hipSuccess) return e;
-    }
-    a.tiles_p = (a.rows + BP - 1) / BP;
-    a.tiles_u = (a.F + BU - 1) / BU;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)a.tiles_p * a.tiles_u), dim3(WP * WU * 64), bytes, s, a);
-    return hipGetLastError();
-}
-
 static hipError_t join(int dt, int act, const float *part, int splits, const float *bias, float *P, void *h, int rows, int F, hipStream_t s)
 {
     const size_t n = (size_t)rows * F;
@@ -671,12 +740,11 @@ static hipError_t join(int dt, int act, const float *part, int splits, const flo
 hipError_t gated_fwd(int dt, int act, const void *x, const void *rest, const void *w, const float *bias, float *P, void *h, int rows, int C, int F, bool panels,
                      void *workspace, hipStream_t s)
 {
-    if (gated_mfma(dt, rows, C, F) && !streams_weights(rows, C)) {
+    if (mm_takes(dt, rows, C, 2ll * F)) {
         if (panels) return hipErrorInvalidValue;
-        MmArgs a{(const bf16_t *)x, (const bf16_t *)rest, (const bf16_t *)w, rows, C, F, bias, P, (bf16_t *)h, (unsigned)((size_t)rows * C * 2),
-                 (unsigned)((size_t)2 * F * C * 2), 0, 0, act};
-        if ((long long)((rows + 255) / 256) * ((F + 127) / 128) >= 192) return launch_mfma<256, 128, 2, 4>(a, s);
-        return launch_mfma<128, 64, 2, 2>(a, s);
+        const size_t es = dt_size(dt);
+        MmArgs a{x, rest, w, rows, C, F, bias, P, h, nullptr, nullptr, (unsigned)((size_t)rows * C * es), (unsigned)((size_t)2 * F * C * es), 0, 0, act};
+        return dt == DT_F32 ? launch_mm<float, MM_FORWARD>(a, s) : launch_mm<bf16_t, MM_FORWARD>(a, s);
     }
     if (gated_mfma(dt, rows, C, F)) {
         int splits = 0, more = 0;
@@ -712,12 +780,26 @@ hipError_t gated_grad(int dt, int act, const void *dh, int dh_parts, const float
     return hipGetLastError();
 }
 
+bool gated_projects(int rows, int K, int F) { return F % 8 == 0 && mm_takes(DT_BF16, rows, K, F); }
+
+hipError_t gated_project(int act, const void *dz, const void *wt, const float *P, void *D, int rows, int K, int F, hipStream_t s)
+{
+    if (!gated_projects(rows, K, F)) return hipErrorInvalidValue;
+    MmArgs a{dz, nullptr, wt, rows, K, F, nullptr, const_cast<float *>(P), D, nullptr, nullptr, (unsigned)((size_t)rows * K * 2),
+             (unsigned)((size_t)F * K * 2), 0, 0, act};
+    return launch_mm<bf16_t, MM_PROJECT>(a, s);
+}
+
 int gated_dgrad_parts(int rows, int C, int F) { return dgrad_plan(rows, C, F).splits; }
 
 hipError_t gated_dgrad_direct(int dt, const void *D, const void *wt, void *dx, bool parts, GradEpi epi, int rows, int C, int F, void *workspace,
                               hipStream_t s)
 {
     const void *old = epi.accum ? (epi.accum_from ? epi.accum_from : dx) : nullptr;
+    if (!parts && dt == DT_F32 && mm_takes(dt, rows, 2 * F, C)) {
+        MmArgs a{D, nullptr, wt, rows, 2 * F, C, nullptr, nullptr, dx, old, epi.gate, (unsigned)((size_t)rows * 2 * F * 4), (unsigned)((size_t)2 * F * C * 4), 0, 0, 0};
+        return launch_mm<float, MM_DX>(a, s);
+    }
     const AnyPlan p = dgrad_plan(rows, C, F);
     NtArgs a{D, wt, rows, C, 2 * F, p.per_split, parts ? (float *)dx : p.splits > 1 ? (float *)workspace : nullptr, nullptr, nullptr, dx, old, epi.gate, 0};
     const int tile = p.small ? 64 : 128;

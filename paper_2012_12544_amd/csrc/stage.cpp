@@ -63,6 +63,8 @@ struct Tensor {
     // a row's sums, and every rounding on the way through the sublayer is one more of its gradients' errors: 2-norm of dW and
     // dgamma against 64 bits 4.2e-3 and 3.9e-3 with them, 3.8e-3 and 3.5e-3 so.
     int gparts = 0;
+    // ... and where the convolution's kernel makes the gradients of the GATED's projections of it at once it is not stored at all
+    bool projected = false;
     // What rounding took from a layer norm's output that only a GATED of ReLU reads, in the transient arena: the product takes both.  The
     // derivative of the activation jumps, and with an input of 8 bits 7 of 10^4 gates are on the wrong side, 2.6e-2 of dW.
     bool rest = false;
@@ -912,7 +914,10 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
             void *dx = grad_ptr(st, L.a, c);
             const bool mf = use_mfma_gather(st, dg);
             const bool tp = st->tap_begin(mf ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
-            if (A.gparts) {
+            if (A.projected) {
+                const Layer &G = st->layers[L.a - 1];
+                HIPCHK(gated_project(G.d.kh, g, L.w_t, (const float *)(st->slot(c.mbid) + G.off_pd), st->grads + G.off_d, rows_of(st, A), L.d.cout, L.d.cin, s));
+            } else if (A.gparts) {
                 int parts = 0;
                 HIPCHK(conv_gather_mfma_raw(g, L.w_t, dg, (float *)dx, &parts, s));
             } else if (mf && L.bnb_chunks && !c.profiling && (e.gate || e.accum)) {
@@ -926,7 +931,9 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
                 HIPCHK(conv_gather_direct(dt, g, L.w_t, nullptr, dx, 0, e, dg, s));
             // dy and filter read, dx written, plus the gate and the previous dx where the epilogue uses them
             st->tap_end(tp, flop, (double)O.bytes() + (double)L.w_elems * dt_size(dt) +
-                                      (A.gparts ? 4.0 * A.gparts * A.elems : A.bytes() * (1.0 + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0))));
+                                      (A.projected ? 8.0 * A.elems + 2.0 * A.bytes()
+                                       : A.gparts  ? 4.0 * A.gparts * A.elems
+                                                   : A.bytes() * (1.0 + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0))));
         }
         break;
     }
@@ -1038,8 +1045,9 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
         const void *x = st->tptr(L.a, c.mbid);
         const int rows = rows_of(st, A);
         const double flop = conv_flop(fwd_geom(st, L), L.d.cin), dbytes = 2.0 * O.bytes();
-        bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
-        HIPCHK(gated_grad(dt, L.d.kh, grad_ptr(st, L.o, c), O.gparts, (const float *)(st->slot(c.mbid) + L.off_pd), D, rows, L.d.cout, s));
+        bool tp = !O.projected && st->tap_begin(BAPIPE_KC_ELEMENTWISE);
+        if (!O.projected)            // else the convolution that reads the output has made D
+            HIPCHK(gated_grad(dt, L.d.kh, grad_ptr(st, L.o, c), O.gparts, (const float *)(st->slot(c.mbid) + L.off_pd), D, rows, L.d.cout, s));
         st->tap_end(tp, 0.0, (O.gparts ? 4.0 * O.gparts * O.elems : (double)O.bytes()) + 8.0 * O.elems + dbytes);
         const WgradLaunch w{x, D, &L, conv_shape(st, L), flop, (double)A.bytes() + dbytes + 8.0 * L.w_elems};
         if (L.mfma) {
@@ -1446,6 +1454,8 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         const bool by_conv = P.d.kind == BAPIPE_GATED && N.d.kind == BAPIPE_CONV2D && N.d.kh == 1 && N.d.kw == 1 && N.d.stride == 1 && N.d.pad == 0;
         if (!by_gated && !by_conv) continue;
         const int rows = rows_of(st, T);
+        T.projected = by_conv && gated_mfma(st->dt, rows, P.d.cin, P.d.cout) && gated_projects(rows, N.d.cout, N.d.cin) && use_mfma_gather(st, dgrad_geom(st, N));
+        if (T.projected) continue;
         if (by_gated && !gated_mfma(st->dt, rows, N.d.cin, N.d.cout)) T.gparts = gated_dgrad_parts(rows, N.d.cin, N.d.cout);
         else if (const GatherConv dg = dgrad_geom(st, N); use_mfma_gather(st, dg)) T.gparts = (int)(conv_gather_mfma_raw_workspace(dg) / (T.elems * sizeof(float)));
         T.rest = by_gated && N.d.kh == BAPIPE_GATE_RELU;
@@ -1459,7 +1469,7 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         if (T.stashed) { T.off = slot; slot += align_up(T.bytes()); }
         else { T.off = trans; trans += align_up(T.bytes()); }
         if (T.rest) { T.rest_off = trans; trans += align_up(T.bytes()); }
-        if (T.need_grad && t != last_t) { T.goff = gr; gr += align_up(T.gparts ? T.elems * T.gparts * sizeof(float) : T.bytes()); }
+        if (T.need_grad && t != last_t && !T.projected) { T.goff = gr; gr += align_up(T.gparts ? T.elems * T.gparts * sizeof(float) : T.bytes()); }
     }
     {   // gradient of the stage output (ingest target when the caller's dy cannot be used in place)
         Tensor &T = st->tensors[root_of(last_t)];
