@@ -120,6 +120,9 @@ struct WgradJob {
 // the same for small float layers with a bias, for which the first function says yes
 bool conv_wgrad_direct_groups(const ConvShape &c);
 hipError_t conv_wgrad_direct_jobs(const WgradJob *jobs, int n, void *workspace, size_t workspace_bytes, hipStream_t s);
+// The same product of two matrices, dw [K][C] += dy^T x, planned for a dw whose bytes count
+size_t rows_wgrad_mfma_workspace(int rows, int C, int K);
+hipError_t rows_wgrad_mfma(const void *x, const void *dy, float *dw, float *db, void *workspace, int rows, int C, int K, hipStream_t s);
 bool conv_wgrad_mfma_groups(const ConvShape &c);      // whether it fills so little of the chip that it should wait for others
 hipError_t conv_wgrad_mfma_jobs(const WgradJob *jobs, int n, void *workspace, size_t workspace_bytes, hipStream_t s, bool beside);
 

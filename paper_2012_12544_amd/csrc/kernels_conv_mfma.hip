@@ -1651,6 +1651,44 @@ size_t conv_wgrad_mfma_workspace(const ConvShape &c)
 
 // products of one tile shape that wait for their launch, and the partial sums that wait for theirs
 namespace {
+namespace {
+// The plan of a product of two matrices of `rows` rows, dw [K][C], that has to fill the chip by itself.  A large dw is written and read again for
+// every split, which is what its few rounds of the chip are weighed against: us, of a round of 512 blocks of 256 x 128 (or 256 of 256 x 256, 512
+// of 128 x 128, half of it) for every row, and of the sums' bytes.  (22016x4096 from 8192 rows, 256 x 128 in two splits 1442 + 266 us, 256 x 256
+// whole 1371; 11264x2048 from 4096 rows 178 + 70, 128 x 128 whole 242.)
+WgradPlan rows_plan(const ConvShape &c)
+{
+    WgradPlan p = wgrad_plan(c, false);
+    if (p.kg != 1) return p;
+    double least = 1e300;
+    const WgradPlan was = p;
+    struct Tile {
+        int ko, ci, slots;
+        double us;
+    };
+    static const Tile tiles[] = {{256, 256, 256, 0.0304}, {256, 128, 512, 0.032}, {128, 128, 512, 0.0184}};
+    for (const Tile &t : tiles) {
+        if (t.ko == 256 && was.bko != 256) continue;                                      // narrow or few rows
+        if (t.ci == 256 && (c.K % 256 || c.C % 256)) continue;
+        const int tk = (c.K + t.ko - 1) / t.ko, tn = (c.C + t.ci - 1) / t.ci;
+        for (int splits = 1; splits <= 16 && (splits == 1 || c.N / splits >= 512); ++splits) {
+            const int per = ((c.N + splits - 1) / splits + 31) / 32 * 32, n = (c.N + per - 1) / per;
+            const long long blocks = (long long)tk * tn * n;
+            const double cost = (double)((blocks + t.slots - 1) / t.slots) * per * t.us + (n > 1 ? (double)c.K * c.C * 4 * (n + 2) / 5.4e6 : 0.0);
+            if (cost >= least) continue;
+            least = cost;
+            p.bko = t.ko;
+            p.bci = t.ci;
+            p.tiles_ko = tk;
+            p.tiles_n = tn;
+            p.splits = n;
+            p.pix_per_split = per;
+        }
+    }
+    return p;
+}
+}  // namespace
+
 struct WgradBatch {
     WgradGroup g;
     SplitkGroup r;
@@ -1766,6 +1804,33 @@ hipError_t conv_wgrad_mfma_jobs(const WgradJob *jobs, int n, void *workspace, si
         if (e != hipSuccess) return e;
     }
     return launch_all();
+}
+
+size_t rows_wgrad_mfma_workspace(int rows, int C, int K)
+{
+    const ConvShape c{rows, 1, 1, C, 1, 1, K, 1, 1, 1, 0};
+    const WgradPlan p = rows_plan(c);
+    return p.splits == 1 ? 0 : (size_t)p.splits * ((size_t)K * C + K) * sizeof(float);
+}
+
+hipError_t rows_wgrad_mfma(const void *x, const void *dy, float *dw, float *db, void *workspace, int rows, int C, int K, hipStream_t s)
+{
+    const ConvShape c{rows, 1, 1, C, 1, 1, K, 1, 1, 1, 0};
+    if (!conv_wgrad_mfma_supported(c)) return hipErrorInvalidValue;
+    const WgradPlan p = rows_plan(c);
+    const int direct = p.splits == 1, tiles = p.tiles_ko * p.tiles_n;
+    const size_t total_w = (size_t)K * C, total = total_w + (db ? K : 0);
+    float *part = direct ? dw : (float *)workspace;
+    WgradBatch b;
+    b.bko = p.bko;
+    b.bci = p.bci;
+    b.kg = p.kg;
+    b.g.n = 1;
+    b.g.a[0] = {(const bf16_t *)x, nullptr, (const bf16_t *)dy, part, nullptr, !db ? nullptr : (direct ? db : part + total_w), total, c, tiles, p.tiles_n,
+                p.splits, tiles * p.splits, p.pix_per_split, p.part_tiles, direct, (unsigned)((size_t)rows * C * 2), (unsigned)((size_t)rows * K * 2)};
+    b.r.n = direct ? 0 : 1;
+    b.r.a[0] = {part, dw, db, total_w, total, p.splits, (int)((total / 4 + 63) / 64)};
+    return launch_batch(b, s);
 }
 
 hipError_t conv_wgrad_mfma(const void *x, const void *dy, float *dw, float *db, void *workspace,

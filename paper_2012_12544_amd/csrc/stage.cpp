@@ -827,7 +827,9 @@ GradEpi epi_for(bapipe_stage *st, int t, BwdCtx &c, int pool_gate_t = -1)
 int run_wgrad(bapipe_stage *st, const WgradLaunch &w, bool mfma, hipStream_t s, char *work)
 {
     const bool tp = st->tap_begin(mfma ? BAPIPE_KC_CONV_WGRAD_MFMA : BAPIPE_KC_CONV_DIRECT, s);
-    if (mfma)
+    if (w.layer->d.kind == BAPIPE_GATED)
+        HIPCHK(rows_wgrad_mfma(w.x, w.dy, w.layer->dw, w.layer->db, work, w.shape.N, w.shape.C, w.shape.K, s));
+    else if (mfma)
         HIPCHK(conv_wgrad_mfma(w.x, w.dy, w.layer->dw, w.layer->db, work, w.shape, s, st->stream_b || st->stream_w));
     else
         HIPCHK(conv_wgrad_direct(st->dt, w.x, w.dy, w.layer->dw, w.layer->db, work, w.shape, s));
@@ -841,12 +843,18 @@ int run_waiting_wgrads(bapipe_stage *st, hipStream_t s, char *work)
     std::vector<WgradJob> jobs;
     double flop = 0.0, bytes = 0.0;
     for (const WgradLaunch &w : st->w_waiting) {
+        if (w.layer->d.kind == BAPIPE_GATED && !w.layer->groups) {       // has a plan of its own: the same sums on every stream
+            const int rc = run_wgrad(st, w, true, s, work);
+            if (rc != BAPIPE_OK) return rc;
+            continue;
+        }
         jobs.push_back({w.x, w.dy, w.layer->dw, w.layer->db, w.shape});
         flop += w.flop;
         bytes += w.bytes;
     }
     st->w_waiting.clear();
     st->w_waiting_us = 0.0;
+    if (jobs.empty()) return BAPIPE_OK;
     const bool direct = st->dt == DT_F32;
     const bool tp = st->tap_begin(direct ? BAPIPE_KC_CONV_DIRECT : BAPIPE_KC_CONV_WGRAD_MFMA, s);
     if (direct)
@@ -1543,7 +1551,8 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
                 L.w_panels = streams_filter(fwd_geom(st, L));
                 L.wt_panels = streams_filter(dg);
                 w = conv_gather_mfma_workspace(dg); work = w > work ? w : work;
-                w = conv_wgrad_mfma_workspace(cs); work = w > work ? w : work;
+                w = rows_wgrad_mfma_workspace(rows, L.d.cin, 2 * L.d.cout); work = w > work ? w : work;
+                w = conv_wgrad_mfma_workspace(cs); work = w > work ? w : work;      // where it shares a launch
                 L.groups = conv_wgrad_mfma_groups(cs);
                 if (L.groups) grouped += align_up(w);
             }

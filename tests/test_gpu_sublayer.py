@@ -443,6 +443,17 @@ def test_further_streams_and_the_static_workspace_change_nothing(dtype):
             assert np.array_equal(got[k], ref[k]), (kw, k)
 
 
+def test_large_products_are_the_same_on_every_stream():
+    """Enough rows and weights for the kernels that fill the chip by themselves, and a weight gradient that is not split like a convolution's."""
+    st = sublayer(c=1024, units=4096, seq=512, micro_batch=2, n_micro=2, stage_index=1, n_stages=2)
+    ref = gpu_minibatch(st)
+    assert all(np.all(np.isfinite(v)) for v in ref.values())
+    for kw in (dict(backward_stream=True, eager_sync=False), dict(wgrad_stream=True, eager_sync=False)):
+        got = gpu_minibatch(st, **kw)
+        for k in ref:
+            assert np.array_equal(got[k], ref[k]), (kw, k)
+
+
 def _device_io(st):
     xs, gs = stage_io(st)
     to = lambda a: torch.from_numpy(a).permute(0, 2, 3, 1).contiguous().to(DEV, tdtype(st))  # noqa: E731
