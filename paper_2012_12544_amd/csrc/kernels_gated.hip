@@ -437,7 +437,7 @@ __global__ __launch_bounds__(TPB) void k_gated_grad(const T *__restrict__ dh, co
 // 16-byte chunks is applied by choosing which one a lane fetches).  Fragments are read one step of 32 bytes ahead of the products that
 // need them; the barrier that publishes the next tile lies before a tile's last products, when every wave has all of the tile in registers, and
 // the slot is filled again at once.
-// 8192 rows, 4096->11008 of bf16, us (two products of 739 GFLOP each): MM_FORWARD 1420, 721 MB of projections and 180 of h among them, the gather
+// 8192 rows, 4096->11008 of bf16, us (two products of 739 GFLOP each): MM_FORWARD 1310, 721 MB of projections and 180 of h among them, the gather
 // kernel alone on as large a product 1316.
 // `rest`: x is the sum of two tensors; K is walked twice with the same weights.
 enum { MM_FORWARD, MM_PROJECT, MM_DX };
@@ -452,9 +452,10 @@ struct MmArgs {
     int tiles_p, tiles_u, act;
 };
 
-// Rows of tiles that go together: the 32 blocks that an XCD's units run at a time are then about 8 x 4 tiles and ask the L2 for 12 operand
-// tiles, in one row of tiles for 33
-constexpr int MM_ROWS = 8;
+// Rows of tiles that go together: the 32 blocks that an XCD's units run at a time are then 4 x 8 tiles and ask the L2 for 12 operand tiles, in
+// one row of tiles for 33.  MM_FORWARD at the size above, us, with 2, 4, 8 and 16 rows together: 1358, 1327, 1343, 1460; with 4 and the
+// projections stored past the L2 1310.
+constexpr int MM_ROWS = 4;
 
 template <class T, int MODE, int BP, int BU, int WP, int WU>
 __global__ __launch_bounds__(WP *WU * 64, 2) void k_gated_mfma(MmArgs p)
@@ -567,9 +568,9 @@ __global__ __launch_bounds__(WP *WU * 64, 2) void k_gated_mfma(MmArgs p)
                     const int row = row_of(a, r);
                     if (row >= p.rows) continue;
                     const float g = acc[a][b][r] + bg, u = acc[a][TU + b][r] + bu;
-                    float *P = p.P + (size_t)row * 2 * p.N + unit;
-                    P[0] = g;
-                    P[p.N] = u;
+                    float *P = p.P + (size_t)row * 2 * p.N + unit;          // read again by the backward pass: not through the L2
+                    __builtin_nontemporal_store(g, P);
+                    __builtin_nontemporal_store(u, P + p.N);
                     ((T *)p.out)[(size_t)row * p.N + unit] = from_f32<T>(act_value<kFast<T>>(p.act, g) * u);
                 }
         }

@@ -201,6 +201,16 @@ def test_gated(dtype, c, units, seq, micro_batch, bias):
     _check_gated(_stage(_one("gated", c, units, act=(c + units) % 4, bias=bias), dtype, (c, seq, 1), micro_batch, 1))
 
 
+@pytest.mark.parametrize("dtype,c,units,seq,bias", [
+    (C.BF16, 72, 1600, 515, 1), (C.BF16, 72, 1601, 515, 0), (C.BF16, 200, 1603, 513, 1), (C.BF16, 40, 10240, 150, 0), (C.BF16, 16, 19201, 64, 1),
+    (C.BF16, 32, 4096, 1024, 1), (C.BF16, 8, 4097, 1000, 0), (C.FP32, 20, 2050, 1023, 1), (C.FP32, 4, 19203, 150, 0), (C.FP32, 36, 4096, 1023, 0),
+    (C.FP32, 512, 8, 8192, 1), (C.FP32, 516, 38, 8200, 0),
+])
+def test_gated_of_many_tiles(dtype, c, units, seq, bias):
+    """Products that fill the chip unsplit: tiles of every size, a K that ends inside one, rows and units that do."""
+    _check_gated(_stage(_one("gated", c, units, act=(c + units) % 4, bias=bias), dtype, (c, seq, 1), 2, 1))
+
+
 @pytest.mark.parametrize("dtype", [C.FP32, C.BF16])
 @pytest.mark.parametrize("act", range(4))
 @pytest.mark.parametrize("c,units,seq", [(48, 80, 70), (30, 41, 33), (64, 64, 300)])
@@ -421,9 +431,44 @@ def test_among_other_layers(name, dtype, c):
 @pytest.mark.parametrize("kw", [
     dict(c=24, units=40, seq=5), dict(c=33, units=50, seq=7), dict(c=64, units=176, seq=40, micro_batch=3, act=C.GATE_GELU, bias=0),
     dict(c=128, units=352, seq=1, micro_batch=1), dict(c=256, units=704, seq=65, n_micro=2), dict(c=520, units=1000, seq=9, act=C.GATE_RELU),
+    dict(c=33, units=50, seq=70, act=C.GATE_RELU), dict(c=64, units=96, seq=130, n_micro=2, act=C.GATE_RELU), dict(c=8, units=24, seq=1, micro_batch=1),
 ])
 def test_sublayer(dtype, kw):
     compare_minibatch(sublayer(dtype=dtype, **kw))
+
+
+@pytest.mark.parametrize("dtype,kw", [
+    (C.BF16, dict(c=64, units=1600, seq=1030)), (C.BF16, dict(c=40, units=1608, seq=1025, bias=0)), (C.BF16, dict(c=24, units=19200, seq=150)),
+    (C.BF16, dict(c=16, units=4096, seq=2048, act=C.GATE_GELU)), (C.BF16, dict(c=72, units=1608, seq=520, act=C.GATE_RELU)),
+    (C.FP32, dict(c=16, units=2056, seq=2050)),
+])
+def test_sublayer_of_many_tiles(dtype, kw):
+    """The products that fill the chip unsplit, the convolution's input gradient that makes the projections' gradients among them."""
+    compare_minibatch(sublayer(dtype=dtype, n_micro=1, stage_index=1, n_stages=1, **kw))
+
+
+def test_a_large_weight_gradient_over_micro_batches():
+    """dw of 8192 x 1024 from two micro-batches of 1024 rows, against a product in 64 bits of what the device itself holds: x and D,
+    each D worked out from the device's own forward product in 64 bits and rounded as the layer rounds it."""
+    c, f, rows = 1024, 4096, 1024
+    st = _stage(_one("gated", c, f, act=C.GATE_SIGMOID), C.BF16, (c, rows, 1), 1, 2)
+    (w, _), = params = gen.all_params(st, perturb=True)
+    xs, gs = stage_io(st)
+    got = _run(st, xs, gs, params)["dw0"]
+    on = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(DEV).to(tdtype(st)).double()  # noqa: E731
+    W, ref, size = on(w), 0, 0
+    for x, dy in zip(xs, gs):
+        x, dy = on(_rows(x)), on(_rows(dy))
+        P = x @ W.t()
+        a = torch.sigmoid(P[:, :f])
+        D = torch.cat([dy * P[:, f:] * a * (1 - a), dy * a], 1)
+        ref = ref + D.t() @ x
+        size = size + D.abs().t() @ x.abs()
+    off = (torch.from_numpy(_f64(got)).to(DEV) - ref).abs()
+    # D rounded once, and values 1e-4 of themselves off in it; 2048 additions in floats
+    assert torch.all(off <= (HALF[C.BF16] + 1e-4 + 2048 * U) * size)
+    # roundings are independent: the norm of their sum over n terms is HALF / sqrt(3) of the terms' norm, not of the terms' sum
+    assert float(off.norm() / ref.norm()) <= HALF[C.BF16]
 
 
 def test_sublayer_without_an_input_gradient():
