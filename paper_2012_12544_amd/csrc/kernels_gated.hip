@@ -217,34 +217,43 @@ __global__ __launch_bounds__(TPB) void k_gated_nt(NtArgs p)
         }
 }
 
-// dw[M][N] += a^T b with a [rows][M], b [rows][N], over the rows of split blockIdx.y; with several splits part[split][M][N] = their sums.
-// A step is 32 rows, of bf16 read across the rows by transposing reads (tr_frag).
+// dw[M][N] += a^T b with a [rows][M], b [rows][N], and (where db is not NULL) db[M] += the columns' sums of a, over the rows of split
+// blockIdx.y; with several splits part[split][M][N] and, behind all of it, [split][M] = their sums.
+// A step is 64 rows of bf16 (of 32, whose loads the products do not cover, dw of 4006 x 1001 from 8192 rows took 121 us instead of 106), read
+// across the rows by transposing reads (tr_frag), or 32 of float.  The first blocks of a row of tiles sum a's columns as they pass
+// (a pass of its own over a of 1024 x 4096 floats: 9 us).
 template <class T, int TM, int TN>
 __global__ __launch_bounds__(TPB) void k_gated_tn(const T *__restrict__ a, const T *__restrict__ b, int rows, int M, int N, int rows_per_split,
-                                                  float *dw, float *part)
+                                                  float *dw, float *db, float *part)
 {
-    constexpr int V = 16 / sizeof(T), DEPTH = 32, CA = 64 * TM, CB = 64 * TN;
+    constexpr int V = 16 / sizeof(T), DEPTH = 128 / sizeof(T), CA = 64 * TM, CB = 64 * TN;
     constexpr int LA = DEPTH * CA / V / TPB, LB = DEPTH * CB / V / TPB;
     static_assert(LA >= 1 && LB >= 1, "a chunk for every thread");
+    static_assert(TPB % (CA / V) == 0, "a thread's chunks of a have the same columns");
     __shared__ __align__(16) T lds[2][DEPTH * (CA + CB)];
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, wm = wave / 2, wn = wave % 2;
     const int across = (N + CB - 1) / CB, m0 = blockIdx.x / across * CA, n0 = blockIdx.x % across * CB;
     const int first = blockIdx.y * rows_per_split, last = first + rows_per_split < rows ? first + rows_per_split : rows;
     chunk16 ca[LA], cb[LB];
-    // Columns behind the last are never stored, so that a row's last 16 bytes may go on into the rows behind it, where there are some
-    auto fetch = [&](auto &to, const T *from, int width, int c0, int at, auto columns) {
+    // Columns behind the last are never stored, so that a row's last 16 bytes may go on into the rows behind it, where there are some.
+    // One test for all of a step's loads: with one for each they waited for one another (dw of 4006 x 1001 from 8192 rows 210 us)
+    auto fetch = [&](auto &to, const T *from, int width, int c0, int at, auto columns, auto ends) {
         constexpr int CPR = decltype(columns)::value / V;
-        const bool inside = at + DEPTH <= last && (size_t)(at + DEPTH) * width + V <= (size_t)rows * width;
 #pragma unroll
         for (int i = 0; i < (int)(sizeof(to) / sizeof(to[0])); ++i) {
             const int id = tid + TPB * i, r = at + id / CPR, c = c0 + id % CPR * V;
-            if (inside) to[i] = load_chunk<false>(from + (size_t)r * width + (c < width ? c : 0), V);
+            if constexpr (!decltype(ends)::value) to[i] = load_chunk<false>(from + (size_t)r * width + (c < width ? c : 0), V);
             else to[i] = load_chunk<true>(from + (size_t)r * width + c, r < last ? width - c : 0);
         }
     };
+    auto load_all = [&](int at, auto ends) {
+        fetch(ca, a, M, m0, at, std::integral_constant<int, CA>{}, ends);
+        fetch(cb, b, N, n0, at, std::integral_constant<int, CB>{}, ends);
+    };
+    const int narrow = M < N ? M : N;
     auto load = [&](int at) {
-        fetch(ca, a, M, m0, at, std::integral_constant<int, CA>{});
-        fetch(cb, b, N, n0, at, std::integral_constant<int, CB>{});
+        if (at + DEPTH <= last && (size_t)(rows - at - DEPTH) * narrow >= V) load_all(at, std::false_type{});
+        else load_all(at, std::true_type{});
     };
     auto put = [&](T *tile, auto &from, auto columns) {
         constexpr int C = decltype(columns)::value, CPR = C / V;
@@ -255,7 +264,14 @@ __global__ __launch_bounds__(TPB) void k_gated_tn(const T *__restrict__ a, const
             *reinterpret_cast<chunk16 *>(tile + r * C + slot * V) = from[i];
         }
     };
+    float column[V] = {};
+    const bool sums = db && n0 == 0;
     auto store = [&](int buf) {
+        if (sums)
+#pragma unroll
+            for (int i = 0; i < LA; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) column[j] += chunk_value<T>(ca[i], j);
         put(lds[buf], ca, std::integral_constant<int, CA>{});
         put(lds[buf] + DEPTH * CA, cb, std::integral_constant<int, CB>{});
     };
@@ -324,14 +340,33 @@ __global__ __launch_bounds__(TPB) void k_gated_tn(const T *__restrict__ a, const
                 else dw[(size_t)row * N + col] += acc[i][j][r];
             }
         }
+    if (!sums) return;
+    __syncthreads();
+    float *meet = reinterpret_cast<float *>(lds[0]);       // [TPB / (CA / V)][CA]
+#pragma unroll
+    for (int j = 0; j < V; ++j) meet[tid * V + j] = column[j];
+    __syncthreads();
+    if (tid >= CA || m0 + tid >= M) return;
+    float sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < TPB / (CA / V); ++r) sum += meet[r * CA + tid];
+    if (part) part[(size_t)gridDim.y * M * N + (size_t)blockIdx.y * M + m0 + tid] = sum;
+    else db[m0 + tid] += sum;
 }
 
-// dw[i] += the sums of all splits, in their order; n a multiple of V
+// dw[n] += the sums of all splits part[split][n], in their order, and where db is not NULL db[m] += those of the [split][m] behind them; n and
+// m multiples of V
 template <int V>
-__global__ __launch_bounds__(TPB) void k_gated_tn_join(const float *__restrict__ part, int splits, size_t n, float *dw)
+__global__ __launch_bounds__(TPB) void k_gated_tn_join(const float *__restrict__ part, int splits, size_t n, float *dw, size_t m, float *db)
 {
-    const size_t i = ((size_t)blockIdx.x * TPB + threadIdx.x) * V;
-    if (i >= n) return;
+    size_t i = ((size_t)blockIdx.x * TPB + threadIdx.x) * V;
+    if (i >= n) {
+        i -= n;
+        if (!db || i >= m) return;
+        part += splits * n;
+        n = m;
+        dw = db;
+    }
     typedef vec_t<float, V> vec;
     vec sum = {};
     for (int k = 0; k < splits; ++k) {
@@ -714,10 +749,10 @@ size_t gated_workspace(int dt, int rows, int C, int F, bool rest)
     const size_t walks = rest ? 2 : 1;
     if (gated_mfma(dt, rows, C, F)) return mm_takes(dt, rows, C, 2ll * F) ? 0 : walks * conv_gather_mfma_raw_workspace(rows_product(rows, C, 2 * F, false));
     auto sums = [](const AnyPlan &p, size_t n) { return p.splits > 1 ? (size_t)p.splits * n * sizeof(float) : 0; };
-    size_t most = colsum_workspace(rows, 2 * F);
+    size_t most = 0;
     const AnyPlan f = forward_plan(rows, C, F);
     for (const size_t v : {f.splits * walks > 1 ? f.splits * walks * rows * 2 * F * sizeof(float) : 0, sums(dgrad_plan(rows, C, F), (size_t)rows * C),
-                           sums(wgrad_plan(rows, C, F), (size_t)2 * F * C)})
+                           sums(wgrad_plan(rows, C, F), (size_t)2 * F * (C + 1))})
         most = v > most ? v : most;
     return most;
 }
@@ -822,16 +857,14 @@ hipError_t gated_wgrad_direct(int dt, const void *x, const void *D, float *dw, f
     float *part = p.splits > 1 ? (float *)workspace : nullptr;
     const int tile = p.small ? 64 : 128;
     const dim3 grid((unsigned)((C + tile - 1) / tile) * ((M + tile - 1) / tile), p.splits);
-    if (p.small) GATED_T(dt, hipLaunchKernelGGL((k_gated_tn<T, 1, 1>), grid, dim3(TPB), 0, s, (const T *)D, (const T *)x, rows, M, C, p.per_split, dw, part));
-    else GATED_T(dt, hipLaunchKernelGGL((k_gated_tn<T, 2, 2>), grid, dim3(TPB), 0, s, (const T *)D, (const T *)x, rows, M, C, p.per_split, dw, part));
+    if (p.small) GATED_T(dt, hipLaunchKernelGGL((k_gated_tn<T, 1, 1>), grid, dim3(TPB), 0, s, (const T *)D, (const T *)x, rows, M, C, p.per_split, dw, db, part));
+    else GATED_T(dt, hipLaunchKernelGGL((k_gated_tn<T, 2, 2>), grid, dim3(TPB), 0, s, (const T *)D, (const T *)x, rows, M, C, p.per_split, dw, db, part));
     if (part) {
-        const size_t n = (size_t)M * C;
-        if (n % 4 == 0) hipLaunchKernelGGL(k_gated_tn_join<4>, dim3((unsigned)((n / 4 + TPB - 1) / TPB)), dim3(TPB), 0, s, part, p.splits, n, dw);
-        else hipLaunchKernelGGL(k_gated_tn_join<1>, dim3((unsigned)((n + TPB - 1) / TPB)), dim3(TPB), 0, s, part, p.splits, n, dw);
+        const size_t n = (size_t)M * C, all = n + (db ? M : 0);
+        if (n % 4 == 0 && M % 4 == 0) hipLaunchKernelGGL(k_gated_tn_join<4>, dim3((unsigned)((all / 4 + TPB - 1) / TPB)), dim3(TPB), 0, s, part, p.splits, n, dw, (size_t)M, db);
+        else hipLaunchKernelGGL(k_gated_tn_join<1>, dim3((unsigned)((all + TPB - 1) / TPB)), dim3(TPB), 0, s, part, p.splits, n, dw, (size_t)M, db);
     }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !db) return e;
-    return colsum_accumulate(dt, D, rows, M, db, workspace, s);
+    return hipGetLastError();
 }
 
 }  // namespace bapipe

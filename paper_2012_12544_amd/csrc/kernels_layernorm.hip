@@ -95,11 +95,6 @@ template <bool TAIL, class T> __device__ __forceinline__ chunk16 load_packed(con
     load_vec<TAIL>(v, from, left);
     return __builtin_bit_cast(chunk16, v);
 }
-template <class T> __device__ __forceinline__ float value(chunk16 c, int j)
-{
-    if constexpr (sizeof(T) == 4) return __uint_as_float(c[j]);
-    else return __uint_as_float(j % 2 ? c[j / 2] & 0xFFFF0000u : c[j / 2] << 16);
-}
 
 // Thread t of a group of G has columns (k G + t) V .. + V - 1, k < NV.
 template <class T, int NV> struct row_regs {
@@ -119,7 +114,7 @@ template <class T, int NV> struct row_regs {
 #pragma unroll
         for (int k = 0; k < NV; ++k) v[k] = chunk16{0u, 0u, 0u, 0u};
     }
-    __device__ __forceinline__ float at(int k, int j) const { return value<T>(v[k], j); }
+    __device__ __forceinline__ float at(int k, int j) const { return chunk_value<T>(v[k], j); }
     // what was computed from the values so far is not to be kept for later
     __device__ __forceinline__ void forget()
     {
@@ -315,8 +310,8 @@ __global__ __launch_bounds__(NT, NV == 1 || (NV == 2 && !EPI) ? 4 : 2) void k_la
                 const float v = inv * (d * gamma.v[k].e[j] - s1 - xh * s2);
                 if constexpr (!EPI) r.e[j] = from_f32<T>(v);
                 else
-                    r.e[j] = grad_out<T>(v, p.old != nullptr, from_f32<T>(p.old ? value<T>(old, j) : 0.0f), p.gate != nullptr,
-                                         from_f32<T>(p.gate ? value<T>(gate, j) : 0.0f));
+                    r.e[j] = grad_out<T>(v, p.old != nullptr, from_f32<T>(p.old ? chunk_value<T>(old, j) : 0.0f), p.gate != nullptr,
+                                         from_f32<T>(p.gate ? chunk_value<T>(gate, j) : 0.0f));
             }
             store_vec<TAIL>(p.dx + base + c, r, C - c);
             __builtin_amdgcn_sched_barrier(0);
@@ -523,11 +518,7 @@ static hipError_t bwd_t(int dt, BwdArgs<T> p, hipStream_t s)
     auto launch = [&](auto kernel, int threads, int groups) {
         chunks = bwd_blocks(p.rows, groups);
         const size_t meet = (size_t)(groups / 2) * 2 * p.C * sizeof(float), sums = 2 * threads / 64 * sizeof(float);
-        const size_t bytes = meet > sums ? meet : sums;
-        if (bytes > 64 * 1024) {
-            const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-            if (e != hipSuccess) return e;
-        }
+        const size_t bytes = meet > sums ? meet : sums;        // at most 32 KB
         hipLaunchKernelGGL(kernel, dim3(chunks), dim3(threads), bytes, s, p);
         return hipGetLastError();
     };

@@ -44,6 +44,12 @@ struct lds_addr_of {
 };
 
 __device__ __forceinline__ bf16x8_t as_frag(chunk16 c) { return __builtin_bit_cast(bf16x8_t, c); }
+// value j of the four floats or eight bf16 in it
+template <class T> __device__ __forceinline__ float chunk_value(chunk16 c, int j)
+{
+    if constexpr (sizeof(T) == 4) return __uint_as_float(c[j]);
+    else return __uint_as_float(j % 2 ? c[j / 2] & 0xFFFF0000u : c[j / 2] << 16);
+}
 
 // acc + the 8 bf16 values of an MFMA operand fragment (v_dot2c_f32_bf16 against a pair of ones)
 __device__ __forceinline__ float frag_sum(bf16x8_t f, float acc)
