@@ -219,6 +219,12 @@ template <class T> struct BwdArgs {
 
 // Floats from one group's columns' sums in LDS to the next one's: groups that share a wave write to different banks
 constexpr int meet_pitch(int nv, int v, int g) { return nv * v * 2 * g + (g < 64 ? g : 0); }
+// Whether gamma stays in LDS, behind the words that the waves' totals take: where sums, values and gamma of 16 columns are a few registers more
+// than the 128 with which two blocks fit a unit.  Spilled, those were 24 KB of a row of 8192 beside its own 49 KB (bf16, 16384 rows: 208
+// us, so 175; 8192 rows of 5000: 109 and 73).  Floats, 8 columns, fit (8192 rows of 4096: 84, so 86); with what an epilogue adds it is
+// one block either way.
+constexpr bool shared_gamma(int nv, int v, int g, bool epi) { return nv * v == 16 && g >= 256 && !epi; }
+constexpr int kGammaAt = 64;
 
 // NT threads, NT / G groups whose columns' sums meet in LDS at the end.  (In three rounds of halves, with the sums of a thread's columns
 // side by side, 3200 rows of 1024 bf16 took 15.8 us instead of 11.7.)
@@ -231,8 +237,25 @@ __global__ __launch_bounds__(NT, NV == 1 || (NV == 2 && !EPI) ? 4 : 2) void k_la
     constexpr int V = 16 / sizeof(T), GROUPS = NT / G;
     const int t = threadIdx.x % G, group = group_of<G>(), C = p.C, step = gridDim.x * GROUPS;
     int row = blockIdx.x * GROUPS + group;
+    constexpr bool SHARED = shared_gamma(NV, V, G, EPI);
+    float *const gamma_lds = lds + kGammaAt;
     column_regs<V, NV> gamma;
     gamma.template load<G, TAIL>(p.gamma, t, C);
+    if constexpr (SHARED) {
+        if (group == 0)
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int q = 0; q < V / 4; ++q) __builtin_memcpy(gamma_lds + ((k * (V / 4) + q) * G + t) * 4, &gamma.v[k].e[q * 4], 16);
+        __syncthreads();
+    }
+    auto gammas = [&](int k) {
+        if constexpr (!SHARED) return gamma.v[k];
+        vec_of<float, V> g;
+#pragma unroll
+        for (int q = 0; q < V / 4; ++q) __builtin_memcpy(&g.e[q * 4], gamma_lds + ((k * (V / 4) + q) * G + t) * 4, 16);
+        return g;
+    };
     float sg[NV][V] = {}, sb[NV][V] = {};
     row_regs<T, NV> nx, nd;
     float nmean = 0.0f, ninv = 0.0f;
@@ -281,11 +304,12 @@ __global__ __launch_bounds__(NT, NV == 1 || (NV == 2 && !EPI) ? 4 : 2) void k_la
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
+            const vec_of<float, V> ga = gammas(k);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 float d, xh;
                 column(k, j, d, xh);
-                const float dx = d * xh, g = gamma.v[k].e[j];
+                const float dx = d * xh, g = ga.e[j];
                 sg[k][j] += dx;
                 sb[k][j] += d;
                 s1 = fmaf(d, g, s1);
@@ -303,6 +327,7 @@ __global__ __launch_bounds__(NT, NV == 1 || (NV == 2 && !EPI) ? 4 : 2) void k_la
         for (int k = 0; k < NV; ++k) {
             const int c = (k * G + t) * V;
             if (c >= C) continue;
+            const vec_of<float, V> ga = gammas(k);
             vec_of<T, V> r;
             chunk16 old, gate;
             if (EPI && p.old) old = load_packed<TAIL>(p.old + base + c, C - c);
@@ -311,7 +336,7 @@ __global__ __launch_bounds__(NT, NV == 1 || (NV == 2 && !EPI) ? 4 : 2) void k_la
             for (int j = 0; j < V; ++j) {
                 float d, xh;
                 column(k, j, d, xh);
-                const float v = inv * (d * gamma.v[k].e[j] - s1 - xh * s2);
+                const float v = inv * (d * ga.e[j] - s1 - xh * s2);
                 if constexpr (!EPI) r.e[j] = from_f32<T>(v);
                 else
                     r.e[j] = grad_out<T>(v, p.old != nullptr, from_f32<T>(p.old ? chunk_value<T>(old, j) : 0.0f), p.gate != nullptr,
@@ -532,16 +557,18 @@ static hipError_t bwd_t(int dt, BwdArgs<T> p, hipStream_t s)
     const Shape k = shape_of(dt, p.C, false);
     const bool tail = p.C % (16 / sizeof(T)) != 0;
     int chunks = 0;
+    const bool epi = p.old || p.gate;
     auto launch = [&](auto kernel, int threads, int groups) {
         chunks = bwd_blocks(p.rows, groups);
-        const size_t meet = groups > 1 ? (size_t)groups * meet_pitch(k.nv, 16 / (int)sizeof(T), k.g) * sizeof(float) : 0, sums = 2 * threads / 64 * sizeof(float);
-        const size_t bytes = meet > sums ? meet : sums;        // at most 64 KB
+        const int v = 16 / (int)sizeof(T);
+        const size_t meet = groups > 1 ? (size_t)groups * meet_pitch(k.nv, v, k.g) : 0;
+        const size_t loop = shared_gamma(k.nv, v, k.g, epi) ? kGammaAt + (size_t)k.nv * v * k.g : 2 * threads / 64;
+        const size_t bytes = (meet > loop ? meet : loop) * sizeof(float);        // at most 64 KB
         hipLaunchKernelGGL(kernel, dim3(chunks), dim3(threads), bytes, s, p);
         return hipGetLastError();
     };
     hipError_t e = hipErrorInvalidValue;
     bool found = false;
-    const bool epi = p.old || p.gate;
 #define BWD_(NV, G, NT, TAIL, PARTS) \
     (epi ? launch(k_layernorm_bwd<T, NV, G, NT, TAIL, PARTS, true>, NT, NT / G) : launch(k_layernorm_bwd<T, NV, G, NT, TAIL, PARTS, false>, NT, NT / G))
 #define BWD(NV, G, NT)                                                                                             \
