@@ -349,34 +349,43 @@ __global__ __launch_bounds__(NT, NV == 1 || (NV == 2 && !EPI) ? 4 : 2) void k_la
     float *to = p.part + (size_t)blockIdx.x * 2 * C;
     const bool lone = gridDim.x == 1;
     if constexpr (GROUPS == 1) {
-        auto columns = [&](auto f) {
+        // whole accesses: one float after another, 32 bytes apart across the threads, took 175 us instead of 162 at 16384 rows of 8192
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * G + t) * V;
+            if (c >= C) continue;
+            vec_of<float, V> g, b;
+            if (lone) {
+                load_vec<TAIL>(g, p.dgamma + c, C - c);
+                load_vec<TAIL>(b, p.dbeta + c, C - c);
+            }
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const int c = (k * G + t) * V + j;
-                    if (c < C) f(c, sg[k][j], sb[k][j]);
-                }
-        };
-        if (lone) columns([&](int c, float g, float b) { p.dgamma[c] += g; p.dbeta[c] += b; });
-        else columns([&](int c, float g, float b) { to[c] = g; to[C + c] = b; });
+            for (int j = 0; j < V; ++j) {
+                g.e[j] = (lone ? g.e[j] : 0.0f) + sg[k][j];
+                b.e[j] = (lone ? b.e[j] : 0.0f) + sb[k][j];
+            }
+            store_vec<TAIL>(lone ? p.dgamma + c : to + c, g, C - c);
+            store_vec<TAIL>(lone ? p.dbeta + c : to + C + c, b, C - c);
+        }
     } else {
-        // a group's sums in the order access, value, gamma or beta, thread, so that neighbours write and read neighbours
+        // a group's sums in the order access, value, gamma or beta, thread, a value's threads turned by 64 / V places from one value to the next:
+        // neighbours write the sums of one value and read those of neighbouring columns, either from different banks
         constexpr int N = NV * V * 2 * G, PITCH = meet_pitch(NV, V, G);
+        auto place = [](int k, int j, int beta, int t) { return ((k * V + j) * 2 + beta) * G + (t ^ (j * (64 / V) & (G - 1))); };
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                lds[group * PITCH + (k * V + j) * 2 * G + t] = sg[k][j];
-                lds[group * PITCH + ((k * V + j) * 2 + 1) * G + t] = sb[k][j];
+                lds[group * PITCH + place(k, j, 0, t)] = sg[k][j];
+                lds[group * PITCH + place(k, j, 1, t)] = sb[k][j];
             }
         __syncthreads();
         for (int v = threadIdx.x; v < N; v += NT) {
+            const int j = v % V, u = v / V % G, beta = v / V / G % 2, k = v / V / G / 2, c = (k * G + u) * V + j;
             float sum = 0.0f;
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) sum += lds[g * PITCH + v];
-            const int c = (v / G / 2 / V * G + v % G) * V + v / G / 2 % V, beta = v / G % 2;
+            for (int g = 0; g < GROUPS; ++g) sum += lds[g * PITCH + place(k, j, beta, u)];
             if (c >= C) continue;
             if (lone) (beta ? p.dbeta : p.dgamma)[c] += sum;
             else to[beta * C + c] = sum;
