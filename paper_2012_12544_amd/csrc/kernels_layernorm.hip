@@ -145,12 +145,12 @@ template <class T> struct FwdArgs {
 };
 
 template <class T, int NV, int G, bool TAIL>
-__global__ __launch_bounds__(TPB) void k_layernorm_fwd(FwdArgs<T> p)
+__global__ __launch_bounds__(G > TPB ? G : TPB) void k_layernorm_fwd(FwdArgs<T> p)
 {
-    constexpr int V = 16 / sizeof(T);
-    __shared__ float lds[2 * TPB / 64];
-    const int t = threadIdx.x % G, C = p.C, step = gridDim.x * (TPB / G);
-    int row = blockIdx.x * (TPB / G) + group_of<G>();
+    constexpr int V = 16 / sizeof(T), GROUPS = G > TPB ? 1 : TPB / G;
+    __shared__ float lds[2 * GROUPS * G / 64];
+    const int t = threadIdx.x % G, C = p.C, step = gridDim.x * GROUPS;
+    int row = blockIdx.x * GROUPS + group_of<G>();
     column_regs<V, NV> gamma, beta;
     gamma.template load<G, TAIL>(p.gamma, t, C);
     beta.template load<G, TAIL>(p.beta, t, C);
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(TPB) void k_layernorm_fwd(FwdArgs<T> p)
     // columns behind the row's end
     auto in = [&](int k, int j) { return (k * G + t) * V + (TAIL ? j : 0) < C; };
     // all groups of a block take the same number of turns, for they meet at barriers
-    for (int first = blockIdx.x * (TPB / G); first < p.rows; first += step, row += step) {
+    for (int first = blockIdx.x * GROUPS; first < p.rows; first += step, row += step) {
         const bool on = row < p.rows;
         const row_regs<T, NV> x = next;
         if (row + step < p.rows) next.template load<G, TAIL>(p.x + (size_t)(row + step) * C, t, C);
@@ -519,7 +519,7 @@ struct Shape {
 Shape shape_of(int dt, int C, bool fwd)
 {
     const int v = dt == DT_F32 ? 4 : 8, n = (C + v - 1) / v;
-    static const Shape forward[] = {{1, 8}, {1, 16}, {1, 32}, {1, 64}, {2, 64}, {4, 64}, {2, 256}, {4, 256}, {8, 256}};
+    static const Shape forward[] = {{1, 8}, {1, 16}, {1, 32}, {1, 64}, {2, 64}, {4, 64}, {2, 256}, {4, 256}, {4, 512}};
     static const Shape backward[] = {{1, 8}, {1, 16}, {1, 32}, {1, 64}, {2, 64}, {1, 256}, {2, 256}, {2, 512}, {4, 512}};
     for (const Shape &k : fwd ? forward : backward)
         if (n <= k.nv * k.g) return k;
@@ -545,15 +545,15 @@ static hipError_t fwd_t(int dt, FwdArgs<T> p, hipStream_t s)
 {
     const Shape k = shape_of(dt, p.C, true);
     const bool tail = p.C % (16 / sizeof(T)) != 0;
-    auto launch = [&](auto kernel, int groups) {
-        const int blocks = (p.rows + groups - 1) / groups, most = 256 * 8;
-        hipLaunchKernelGGL(kernel, dim3(blocks < most ? blocks : most), dim3(TPB), 0, s, p);
+    auto launch = [&](auto kernel, int g) {
+        const int groups = g > TPB ? 1 : TPB / g, blocks = (p.rows + groups - 1) / groups, most = 256 * 8;
+        hipLaunchKernelGGL(kernel, dim3(blocks < most ? blocks : most), dim3(groups * g), 0, s, p);
         return hipGetLastError();
     };
 #define FWD(NV, G)                                                                                  \
     if (k.nv == NV && k.g == G)                                                                     \
-    return tail ? launch(k_layernorm_fwd<T, NV, G, true>, TPB / G) : launch(k_layernorm_fwd<T, NV, G, false>, TPB / G)
-    FWD(1, 8); FWD(1, 16); FWD(1, 32); FWD(1, 64); FWD(2, 64); FWD(4, 64); FWD(2, 256); FWD(4, 256); FWD(8, 256);
+    return tail ? launch(k_layernorm_fwd<T, NV, G, true>, G) : launch(k_layernorm_fwd<T, NV, G, false>, G)
+    FWD(1, 8); FWD(1, 16); FWD(1, 32); FWD(1, 64); FWD(2, 64); FWD(4, 64); FWD(2, 256); FWD(4, 256); FWD(4, 512);
 #undef FWD
     const dim3 grid(p.rows < (1 << 20) ? p.rows : 1 << 20);
     hipLaunchKernelGGL(k_layernorm_fwd_long<T>, grid, dim3(TPB), 0, s, p);
