@@ -91,7 +91,8 @@ typedef enum {
  * stage input; producers must precede consumers.  fuse_relu applies max(.,0) to the output
  * of CONV2D / BATCHNORM2D / ADD / LINEAR.  cin/cout: channels (features for LINEAR;
  * BATCHNORM2D and LAYERNORM need cin == cout == channels of their input; GATED: channels of its
- * input and of its output).  fuse_relu of LAYERNORM, GATED and DROPOUT must be 0.
+ * input and of its output).  fuse_relu of LAYERNORM, GATED and DROPOUT must be 0, and what they read
+ * is no FLATTENed map of more than one pixel (E_UNSUPPORTED; put DROPOUT in front of the FLATTEN).
  *
  * The layers of a transformer's feed-forward sublayer, x + DROPOUT(CONV2D 1x1(GATED(LAYERNORM(x)))),
  * act on every position (n, h, w) by itself; sequences are (channels, T, 1) tensors as for LSTM.
@@ -103,7 +104,7 @@ typedef enum {
  *   where it is used and never stored.  Element e = ((n H + h) W + w) C + c of micro-batch m is
  *   dropped if word e mod 4 of Philox4x32-10 is below 2^32 eps (rounded to nearest); key: the seed,
  *   low word first; counter: e / 4, layer index + 65536 (stage_index - 1), m, number of the
- *   mini-batch.  See bapipe_stage_set_dropout. */
+ *   mini-batch.  See bapipe_stage_set_dropout.  A stage that only evaluates is created with eps 0. */
 typedef struct {
     int32_t kind;
     int32_t cin, cout;
@@ -242,7 +243,9 @@ int bapipe_stage_set_dropout(bapipe_stage_t *st, uint64_t seed, uint32_t mini_ba
  * records; *n receives the number of layers; E_INVALID if cap < n_layers.
  * Where the stage runs two layers as one kernel, the time is reported on the layer that launches
  * it and the other reports 0: a max-pool done in the epilogue of the conv before it (forward),
- * a residual ADD whose sum is stored by the batch-norm before it (forward).  Linear layers, whose
+ * a residual ADD whose sum is stored by the batch-norm before it (forward), a dropout done by the
+ * ADD that alone reads it (forward).  The gradients of a GATED layer's projections are reported on
+ * the 1x1 convolution behind it where that convolution's kernel makes them.  Linear layers, whose
  * weight gradient the stage defers to `step`, are timed with that GEMM run per micro-batch: an
  * upper bound for what the schedule pays. */
 int bapipe_profile_layers(bapipe_stage_t *st, int warmup, int iters,

@@ -8,9 +8,11 @@
 //             w [K][R][S][C] for forward, flipped channel-transposed [C][R][S][K] for dgrad
 //   stash     depth x slot ; a slot holds, for one in-flight micro-batch, exactly the tensors
 //             backward reads again: layer inputs of conv/linear/BN, ReLU gates, pool indices,
-//             BN statistics, softmax output.  depth = min(M, N-i+1) (x2 for 1F1B-SO).
+//             BN and layer norm statistics, both projections of a gated layer (float), softmax
+//             output.  depth = min(M, N-i+1) (x2 for 1F1B-SO).
 //   transient forward tensors nobody reads in backward (reused by every micro-batch)
-//   grads     one buffer per tensor that receives an activation gradient (reused)
+//   grads     one buffer per tensor that receives an activation gradient (reused), and the
+//             gradients of a gated layer's projections
 //   workspace split-K / column-reduction partials
 #include <hip/hip_runtime.h>
 
@@ -1257,6 +1259,10 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         Tensor &O = st->tensors[L.o];
         O.esize = es; O.root = L.o; O.producer = i;
         if (A.esize != es) return create_fail(BAPIPE_E_SHAPE, "layer %d: consumes the softmax output", i);
+        // a flattened map keeps the map's order in memory, which of its readers only LINEAR knows of
+        const Tensor &RA = st->tensors[A.root];
+        if (A.root != L.a && RA.H * RA.W > 1 && (d.kind == BAPIPE_LAYERNORM || d.kind == BAPIPE_GATED || d.kind == BAPIPE_DROPOUT))
+            return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: a flattened map as input; DROPOUT may stand in front of the FLATTEN", i);
         switch (d.kind) {
         case BAPIPE_CONV2D: {
             if (d.kh <= 0 || d.kw <= 0 || d.stride <= 0 || d.pad < 0 || d.cin <= 0 || d.cout <= 0)

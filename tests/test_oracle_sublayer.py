@@ -159,6 +159,20 @@ def test_what_create_takes_and_refuses():
     assert _status(_one("dropout", 0.5), n_stages=65536, stage_index=65536) == B.E_OOM
 
 
+@pytest.mark.parametrize("method,args", [("layernorm", (32,)), ("gated", (32, 8)), ("dropout", (0.5,))])
+def test_a_flattened_map_is_refused(method, args):
+    """Its elements lie in the map's order, not in that of the features; one of single pixels is a tensor like any other."""
+    def layers(flattened):
+        b = C._Builder()
+        b.layernorm(8 if flattened else 32, src=-1)
+        b.flatten()
+        getattr(b, method)(*args)
+        return b.layers
+
+    assert _status(layers(True), shape=(8, 4, 1)) == B.E_UNSUPPORTED
+    assert _status(layers(False), shape=(32, 1, 1)) == B.E_OOM
+
+
 def test_set_dropout_without_a_stage():
     assert B.load().bapipe_stage_set_dropout(None, ct.c_uint64(1), ct.c_uint32(0)) == B.E_INVALID
 
