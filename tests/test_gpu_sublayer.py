@@ -550,6 +550,33 @@ def test_a_captured_mini_batch_draws_anew_at_every_replay(dtype, c, units):
     captured.close()
 
 
+def test_captured_where_the_convolution_makes_the_projections_gradients():
+    """The large products captured before anything ran them, profiled and replayed."""
+    st = sublayer(c=64, units=1600, seq=1030, n_micro=2, stage_index=1, n_stages=1)
+    params = gen.all_params(st, perturb=True)
+    captured, eager = GpuStage(st, params), GpuStage(st, params)
+    io_c, io_e = _device_io(st), _device_io(st)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=captured.stream):
+        _enqueue(captured, st, io_c)
+    for replay in range(3):
+        graph.replay()
+        rec = B.bapipe_profile_layers(eager.h, 0, 1, len(st["layers"]))
+        assert all(r["fwd_ms"] > 0 for r in rec[:3]) and all(r["bwd_ms"] > 0 for r in rec[:4])
+        _enqueue(eager, st, io_e)
+        torch.cuda.synchronize()
+        for a, b in zip(io_c[2] + io_c[3], io_e[2] + io_e[3]):
+            assert torch.equal(a, b), replay
+        for i, (w, b) in enumerate(params):
+            if w is not None:
+                for a, r in zip(captured.get_params(i), eager.get_params(i)):
+                    assert a is None or np.array_equal(a, r), (replay, i)
+    del graph
+    captured.close()
+    eager.close()
+
+
 def test_two_stages_at_once():
     """Handles are independent: two stages on two streams, and one of them alone."""
     sts = [sublayer(c=128, units=320, seq=65, n_micro=4), sublayer(c=256, units=192, seq=33, n_micro=4, act=C.GATE_GELU)]
