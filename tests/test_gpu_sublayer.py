@@ -274,6 +274,23 @@ def test_dropout(dtype, shape, micro_batch, p):
 
 
 @pytest.mark.parametrize("dtype", [C.FP32, C.BF16])
+@pytest.mark.parametrize("seq", [40, 1101])
+def test_dropout_in_a_residual_sum_of_any_size(dtype, seq):
+    """x + dropout(x) and its gradient, below and above the size from which loads pass by the caches."""
+    b = C._Builder()
+    b.dropout(0.3, src=-1)
+    b.addl(0, -1, relu=0)
+    st = _stage(b.layers, dtype, (2047, seq, 1), 2, 2)
+    xs, gs = stage_io(st)
+    got = _run(st, xs, gs, [(None, None)] * 2)
+    for m in range(2):
+        for name, v in (("y", xs[m]), ("dx", gs[m])):
+            dropped = torch.from_numpy(np.float32(_dropped(st, v, 0.3, m)))
+            want = (dropped + torch.from_numpy(np.float32(v))).to(tdtype(st)).double().numpy()
+            assert np.array_equal(got["%s%d" % (name, m)], want), (name, m)
+
+
+@pytest.mark.parametrize("dtype", [C.FP32, C.BF16])
 def test_dropout_from_nchw_numbers_the_same_elements(dtype):
     st = _stage(_one("dropout", 0.3), dtype, (24, 5, 7), 3, 2)
     xs, gs = stage_io(st)
