@@ -254,15 +254,16 @@ def gated_fwd(x, w, b, act):
     return gate(act, both[:, :F])[0] * both[:, F:], both
 
 
-def gated_bwd(x, w, both, act, dy, dw, db, q=lambda a: a):
-    """Returns dx; accumulates into dw, db.  q rounds the gradients of the projections, which are stored."""
+def gated_bwd(x, w, both, act, dy, dw, db, q=lambda a: a, fine=False):
+    """Returns dx; accumulates into dw, db.  q rounds the gradients of the projections, which are stored; fine: not those that dx is made of."""
     F = w.shape[0] // 2
     a, da = gate(act, both[:, :F])
-    D = q(np.concatenate([dy * both[:, F:] * da, dy * a], axis=1))
+    exact = np.concatenate([dy * both[:, F:] * da, dy * a], axis=1)
+    D = q(exact)
     dw += np.tensordot(D, x, axes=([0, 2, 3], [0, 2, 3]))
     if db is not None:
         db += D.sum(axis=(0, 2, 3))
-    return np.tensordot(D, w, axes=([1], [0])).transpose(0, 3, 1, 2)
+    return np.tensordot(exact if fine else D, w, axes=([1], [0])).transpose(0, 3, 1, 2)
 
 
 def philox4x32(counter, key):

@@ -228,7 +228,8 @@ class OracleStage:
                 if wants:
                     give(L["src0"], dx)
             elif k == C.GATED:
-                dx = ops.gated_bwd(a, q(self.w[i]), aux[i], L["kh"], g, self.dw[i], self.db[i], q)
+                # of a layer norm of up to 64 channels, not even those that make its output's gradient are rounded
+                dx = ops.gated_bwd(a, q(self.w[i]), aux[i], L["kh"], g, self.dw[i], self.db[i], q, L["src0"] in self.float_grads and L["cin"] <= 64)
                 if wants:
                     give(L["src0"], dx)
             elif k == C.DROPOUT:

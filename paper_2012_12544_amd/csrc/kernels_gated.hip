@@ -447,10 +447,10 @@ __global__ __launch_bounds__(TPB) void k_gated_join(const float *__restrict__ pa
 }
 
 // D from dh and the projections, V units a thread (F a multiple of V, dh aligned to V elements).  dh_parts: instead of dh its `parts`
-// float sums [parts][n]
+// float sums [parts][n].  rest: NULL, or what rounding takes from D
 template <class T, int V>
 __global__ __launch_bounds__(TPB) void k_gated_grad(const T *__restrict__ dh, const float *__restrict__ dh_parts, int parts, const float *__restrict__ P,
-                                                    T *__restrict__ D, size_t n, int F, int act)
+                                                    T *__restrict__ D, T *__restrict__ rest, size_t n, int F, int act)
 {
     const size_t i = ((size_t)blockIdx.x * TPB + threadIdx.x) * V;
     if (i >= n) return;
@@ -470,16 +470,22 @@ __global__ __launch_bounds__(TPB) void k_gated_grad(const T *__restrict__ dh, co
         for (int j = 0; j < V; ++j) d[j] = to_f32(v.e[j]);
     }
     const vecf g = *reinterpret_cast<const vecf *>(P + at), u = *reinterpret_cast<const vecf *>(P + at + F);
-    vec dg, du;
+    vec dg, du, rg, ru;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         float a, da;
         act_both<kFast<T>>(act, g.e[j], a, da);
-        dg.e[j] = from_f32<T>(d[j] * u.e[j] * da);
-        du.e[j] = from_f32<T>(d[j] * a);
+        const float vg = d[j] * u.e[j] * da, vu = d[j] * a;
+        dg.e[j] = from_f32<T>(vg);
+        du.e[j] = from_f32<T>(vu);
+        rg.e[j] = from_f32<T>(vg - to_f32(dg.e[j]));
+        ru.e[j] = from_f32<T>(vu - to_f32(du.e[j]));
     }
     *reinterpret_cast<vec *>(D + at) = dg;
     *reinterpret_cast<vec *>(D + at + F) = du;
+    if (!rest) return;
+    *reinterpret_cast<vec *>(rest + at) = rg;
+    *reinterpret_cast<vec *>(rest + at + F) = ru;
 }
 
 // ------------------------------------------------------------------ many rows of whole 16 bytes
@@ -507,6 +513,7 @@ struct MmArgs {
     const void *old, *gate;          // MM_DX: see grad_out()
     unsigned x_bytes, w_bytes;
     int tiles_p, tiles_u, act;
+    void *out_rest = nullptr;        // MM_PROJECT: what rounding takes from D, or NULL
 };
 
 // Rows of tiles that go together: the 32 blocks that an XCD's units run at a time are then 4 x 8 tiles and ask the L2 for 12 operand tiles, in
@@ -654,8 +661,13 @@ __global__ __launch_bounds__(WP *WU * 64, 2) void k_gated_mfma(MmArgs p)
                         act_both<kFast<T>>(p.act, g[r], v, dv);
                         if (row >= p.rows) continue;
                         T *D = (T *)p.out + (size_t)row * 2 * p.N + col;
-                        D[0] = from_f32<T>(acc[a][b][r] * u[r] * dv);
-                        D[p.N] = from_f32<T>(acc[a][b][r] * v);
+                        const float dg = acc[a][b][r] * u[r] * dv, du = acc[a][b][r] * v;
+                        D[0] = from_f32<T>(dg);
+                        D[p.N] = from_f32<T>(du);
+                        if (!p.out_rest) continue;
+                        T *rest = (T *)p.out_rest + (size_t)row * 2 * p.N + col;
+                        rest[0] = from_f32<T>(dg - round_to<T>(dg));
+                        rest[p.N] = from_f32<T>(du - round_to<T>(du));
                     }
                 } else {
 #pragma unroll
@@ -827,24 +839,24 @@ hipError_t gated_fwd(int dt, int act, const void *x, const void *rest, const voi
     return e != hipSuccess || splits == 1 ? e : join(dt, act, (const float *)workspace, splits, bias, P, h, rows, F, s);
 }
 
-hipError_t gated_grad(int dt, int act, const void *dh, int dh_parts, const float *P, void *D, int rows, int F, hipStream_t s)
+hipError_t gated_grad(int dt, int act, const void *dh, int dh_parts, const float *P, void *D, void *rest, int rows, int F, hipStream_t s)
 {
     const float *parts = dh_parts ? (const float *)dh : nullptr;
     const size_t n = (size_t)rows * F;
     const bool four = F % 4 == 0 && (parts || (uintptr_t)dh % (4 * dt_size(dt)) == 0);      // the caller's dh may lie anywhere
     const dim3 grid((unsigned)((n / (four ? 4 : 1) + TPB - 1) / TPB));
-    if (four) GATED_T(dt, hipLaunchKernelGGL((k_gated_grad<T, 4>), grid, dim3(TPB), 0, s, (const T *)dh, parts, dh_parts, P, (T *)D, n, F, act));
-    else GATED_T(dt, hipLaunchKernelGGL((k_gated_grad<T, 1>), grid, dim3(TPB), 0, s, (const T *)dh, parts, dh_parts, P, (T *)D, n, F, act));
+    if (four) GATED_T(dt, hipLaunchKernelGGL((k_gated_grad<T, 4>), grid, dim3(TPB), 0, s, (const T *)dh, parts, dh_parts, P, (T *)D, (T *)rest, n, F, act));
+    else GATED_T(dt, hipLaunchKernelGGL((k_gated_grad<T, 1>), grid, dim3(TPB), 0, s, (const T *)dh, parts, dh_parts, P, (T *)D, (T *)rest, n, F, act));
     return hipGetLastError();
 }
 
 bool gated_projects(int rows, int K, int F) { return F % 8 == 0 && mm_takes(DT_BF16, rows, K, F); }
 
-hipError_t gated_project(int act, const void *dz, const void *wt, const float *P, void *D, int rows, int K, int F, hipStream_t s)
+hipError_t gated_project(int act, const void *dz, const void *wt, const float *P, void *D, void *rest, int rows, int K, int F, hipStream_t s)
 {
     if (!gated_projects(rows, K, F)) return hipErrorInvalidValue;
     MmArgs a{dz, nullptr, wt, rows, K, F, nullptr, const_cast<float *>(P), D, nullptr, nullptr, (unsigned)((size_t)rows * K * 2),
-             (unsigned)((size_t)F * K * 2), 0, 0, act};
+             (unsigned)((size_t)F * K * 2), 0, 0, act, rest};
     return launch_mm<bf16_t, MM_PROJECT>(a, s);
 }
 

@@ -38,6 +38,8 @@ constexpr size_t kTapMaxEvents = 2 * (1u << 18);   // event pairs the measuremen
 
 size_t align_up(size_t v, size_t a = 256) { return (v + a - 1) / a * a; }
 
+constexpr int kFineChannels = 64;        // see Tensor::fine
+
 struct Tensor {
     int C = 0, H = 0, W = 0;
     int Cp = 0;            // channels as laid out in HBM (>= C: a narrow stage input is zero-padded)
@@ -71,6 +73,10 @@ struct Tensor {
     // derivative of the activation jumps, and with an input of 8 bits 7 of 10^4 gates are on the wrong side, 2.6e-2 of dW.
     bool rest = false;
     size_t rest_off = 0;
+    // `gparts` are of two products, with the rounded gradients of the GATED's projections and with what rounding took from them: of a layer
+    // norm of few channels, whose dgamma and dbeta have too few elements for their roundings to average out (16 channels: 2-norm of dgamma
+    // against 64 bits 3.4e-3 in the mean, 4.8e-3 in the worst of eight).  The product into few columns costs little.
+    bool fine = false;
     size_t bytes() const { return elems * esize; }
 };
 
@@ -107,7 +113,7 @@ struct Layer {
     // (forward) and the pre-activation gradients (backward) and the cell-gradient carry
     size_t off_gates = 0, off_cells = 0, off_hs = 0, off_pd = 0, off_dcn = 0;
     // GATED: the slot keeps both projections (off_pd, float); their gradients have a place among the gradients (off_d)
-    size_t off_d = 0;
+    size_t off_d = 0, off_d_rest = 0;    // off_d_rest: see Tensor::fine
     bool mfma = false;                   // its products run on the bf16 MFMA kernels
     bool groups = false;                 // its weight gradient may share a launch with others
     // LINEAR, a 1x1 convolution of 1x1 maps, and products that stream their filter (streams_filter), on the MFMA kernels: the copies that forward
@@ -642,6 +648,9 @@ const void *in_ptr(bapipe_stage *st, int t, const FwdCtx &c)
 // DROPOUT layers of different stages of a pipeline draw differently under one seed
 uint32_t dropout_layer(const bapipe_stage *st, int li) { return (uint32_t)li + 65536u * (uint32_t)(st->opts.stage_index - 1); }
 
+// Where what rounding takes from the gradients of a GATED's projections goes, or NULL
+void *d_rest(const bapipe_stage *st, const Layer &L) { return st->tensors[L.a].fine ? st->grads + L.off_d_rest : nullptr; }
+
 int rows_of(const bapipe_stage *st, const Tensor &T) { return st->mb * T.H * T.W; }
 
 // Where a layer that nobody reads behind this pass stores its output: the stage's last tensor goes to the caller, whose place `align`
@@ -926,7 +935,7 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
             const bool tp = st->tap_begin(mf ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
             if (A.projected) {
                 const Layer &G = st->layers[L.a - 1];
-                HIPCHK(gated_project(G.d.kh, g, L.w_t, (const float *)(st->slot(c.mbid) + G.off_pd), st->grads + G.off_d, rows_of(st, A), L.d.cout, L.d.cin, s));
+                HIPCHK(gated_project(G.d.kh, g, L.w_t, (const float *)(st->slot(c.mbid) + G.off_pd), st->grads + G.off_d, d_rest(st, G), rows_of(st, A), L.d.cout, L.d.cin, s));
             } else if (A.gparts) {
                 int parts = 0;
                 HIPCHK(conv_gather_mfma_raw(g, L.w_t, dg, (float *)dx, &parts, s));
@@ -1051,13 +1060,13 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
         break;
     }
     case BAPIPE_GATED: {
-        void *D = st->grads + L.off_d;
+        void *D = st->grads + L.off_d, *Dr = d_rest(st, L);
         const void *x = st->tptr(L.a, c.mbid);
         const int rows = rows_of(st, A);
         const double flop = conv_flop(fwd_geom(st, L), L.d.cin), dbytes = 2.0 * O.bytes();
         bool tp = !O.projected && st->tap_begin(BAPIPE_KC_ELEMENTWISE);
         if (!O.projected)            // else the convolution that reads the output has made D
-            HIPCHK(gated_grad(dt, L.d.kh, grad_ptr(st, L.o, c), O.gparts, (const float *)(st->slot(c.mbid) + L.off_pd), D, rows, L.d.cout, s));
+            HIPCHK(gated_grad(dt, L.d.kh, grad_ptr(st, L.o, c), O.gparts, (const float *)(st->slot(c.mbid) + L.off_pd), D, Dr, rows, L.d.cout, s));
         st->tap_end(tp, 0.0, (O.gparts ? 4.0 * O.gparts * O.elems : (double)O.bytes()) + 8.0 * O.elems + dbytes);
         const WgradLaunch w{x, D, &L, conv_shape(st, L), flop, (double)A.bytes() + dbytes + 8.0 * L.w_elems};
         if (L.mfma) {
@@ -1073,13 +1082,17 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
             void *dx = grad_ptr(st, L.a, c);
             tp = st->tap_begin(L.mfma ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
             int parts = 0;
-            if (L.mfma && A.gparts)
+            float *second = (float *)dx + A.gparts / 2 * A.elems;
+            if (L.mfma && A.gparts) {
                 HIPCHK(conv_gather_mfma_raw(D, L.w_t, dgrad_geom(st, L), (float *)dx, &parts, s));
-            else if (L.mfma)
+                if (Dr) HIPCHK(conv_gather_mfma_raw(Dr, L.w_t, dgrad_geom(st, L), second, &parts, s));
+            } else if (L.mfma)
                 HIPCHK(conv_gather_mfma(D, L.w_t, nullptr, dx, 0, e, dgrad_geom(st, L), st->work, st->tickets, s));
-            else
+            else {
                 HIPCHK(gated_dgrad_direct(dt, D, L.w_t, dx, A.gparts > 0, e, rows, L.d.cin, L.d.cout, st->work, s));
-            st->tap_end(tp, flop, dbytes + (double)L.w_elems * dt_size(dt) +
+                if (Dr) HIPCHK(gated_dgrad_direct(dt, Dr, L.w_t, second, true, e, rows, L.d.cin, L.d.cout, st->work, s));
+            }
+            st->tap_end(tp, flop * (Dr ? 2.0 : 1.0), dbytes * (Dr ? 2.0 : 1.0) + (double)L.w_elems * dt_size(dt) +
                                       (A.gparts ? 4.0 * A.gparts * A.elems : A.bytes() * (1.0 + (e.gate ? 1.0 : 0.0) + (e.accum ? 1.0 : 0.0))));
         }
         break;
@@ -1473,6 +1486,8 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         if (by_gated && !gated_mfma(st->dt, rows, N.d.cin, N.d.cout)) T.gparts = gated_dgrad_parts(rows, N.d.cin, N.d.cout);
         else if (const GatherConv dg = dgrad_geom(st, N); use_mfma_gather(st, dg)) T.gparts = (int)(conv_gather_mfma_raw_workspace(dg) / (T.elems * sizeof(float)));
         T.rest = by_gated && N.d.kh == BAPIPE_GATE_RELU;
+        T.fine = by_gated && T.gparts && T.C <= kFineChannels;
+        if (T.fine) T.gparts *= 2;
     }
 
     // ---- memory plan
@@ -1548,6 +1563,7 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
             const int rows = rows_of(st, A);
             L.aux_off = L.off_pd = slot; L.aux_bytes = (size_t)rows * 2 * L.d.cout * sizeof(float); slot += align_up(L.aux_bytes);
             L.off_d = gr; gr += align_up((size_t)rows * 2 * L.d.cout * es);
+            if (A.fine) { L.off_d_rest = gr; gr += align_up((size_t)rows * 2 * L.d.cout * es); }
             L.mfma = gated_mfma(st->dt, rows, L.d.cin, L.d.cout);
             size_t w = gated_workspace(st->dt, rows, L.d.cin, L.d.cout, A.rest);
             work = w > work ? w : work;
