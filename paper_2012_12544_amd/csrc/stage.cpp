@@ -74,8 +74,8 @@ struct Tensor {
     bool rest = false;
     size_t rest_off = 0;
     // `gparts` are of two products, with the rounded gradients of the GATED's projections and with what rounding took from them: of a layer
-    // norm of few channels, whose dgamma and dbeta have too few elements for their roundings to average out (16 channels: 2-norm of dgamma
-    // against 64 bits 3.4e-3 in the mean, 4.8e-3 in the worst of eight).  The product into few columns costs little.
+    // norm of few channels, whose dgamma and dbeta have too few elements for their roundings to average out (16 channels, 672 units, 1154 rows:
+    // 2-norm of dgamma against 64 bits 5.1e-3, so 3.7e-3; a mini-batch of two takes 137 us instead of 130).
     bool fine = false;
     size_t bytes() const { return elems * esize; }
 };
