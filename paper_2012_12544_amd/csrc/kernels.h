@@ -219,10 +219,11 @@ hipError_t gated_fwd(int dt, int act, const void *x, const void *rest, const voi
                      void *workspace, hipStream_t s);
 // dh_parts > 0: dh is that many float sums [dh_parts][rows][F] instead
 hipError_t gated_grad(int dt, int act, const void *dh, int dh_parts, const float *P, void *D, void *rest, int rows, int F, hipStream_t s);
-// the other two products where gated_mfma says no
-// The input gradient of a 1x1 convolution behind the layer, dh = dz W2 (wt: [F][K], rows as they are), and D from it in one kernel, bf16
+// The input gradient of a 1x1 convolution behind the layer, dh = dz W2 (wt: [F][K], rows as they are; panels, GatherConv::wt_panels, are refused), and
+// D from it in one kernel, bf16
 bool gated_projects(int rows, int K, int F);
-hipError_t gated_project(int act, const void *dz, const void *wt, const float *P, void *D, void *rest, int rows, int K, int F, hipStream_t s);
+hipError_t gated_project(int act, const void *dz, const void *wt, bool panels, const float *P, void *D, void *rest, int rows, int K, int F, hipStream_t s);
+// The other two products where gated_mfma says no.
 // parts: dx receives the gated_dgrad_parts float sums [parts][rows][C] of the product
 int gated_dgrad_parts(int rows, int C, int F);
 hipError_t gated_dgrad_direct(int dt, const void *D, const void *wt, void *dx, bool parts, GradEpi epi, int rows, int C, int F, void *workspace, hipStream_t s);

@@ -852,9 +852,9 @@ hipError_t gated_grad(int dt, int act, const void *dh, int dh_parts, const float
 
 bool gated_projects(int rows, int K, int F) { return F % 8 == 0 && mm_takes(DT_BF16, rows, K, F); }
 
-hipError_t gated_project(int act, const void *dz, const void *wt, const float *P, void *D, void *rest, int rows, int K, int F, hipStream_t s)
+hipError_t gated_project(int act, const void *dz, const void *wt, bool panels, const float *P, void *D, void *rest, int rows, int K, int F, hipStream_t s)
 {
-    if (!gated_projects(rows, K, F)) return hipErrorInvalidValue;
+    if (panels || !gated_projects(rows, K, F)) return hipErrorInvalidValue;
     MmArgs a{dz, nullptr, wt, rows, K, F, nullptr, const_cast<float *>(P), D, nullptr, nullptr, (unsigned)((size_t)rows * K * 2),
              (unsigned)((size_t)F * K * 2), 0, 0, act, rest};
     return launch_mm<bf16_t, MM_PROJECT>(a, s);

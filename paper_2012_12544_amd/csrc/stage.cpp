@@ -936,7 +936,8 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
             const bool tp = st->tap_begin(mf ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
             if (A.projected) {
                 const Layer &G = st->layers[L.a - 1];
-                HIPCHK(gated_project(G.d.kh, g, L.w_t, (const float *)(st->slot(c.mbid) + G.off_pd), st->grads + G.off_d, d_rest(st, G), rows_of(st, A), L.d.cout, L.d.cin, s));
+                HIPCHK(gated_project(G.d.kh, g, L.w_t, L.wt_panels, (const float *)(st->slot(c.mbid) + G.off_pd), st->grads + G.off_d, d_rest(st, G),
+                                     rows_of(st, A), L.d.cout, L.d.cin, s));
             } else if (A.gparts) {
                 int parts = 0;
                 HIPCHK(conv_gather_mfma_raw(g, L.w_t, dg, (float *)dx, &parts, s));
@@ -1651,7 +1652,8 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
             const bool flat = L.d.kind == BAPIPE_LINEAR || flat_conv;
             const GatherConv fg = fwd_geom(st, L), dg = dgrad_geom(st, L);
             L.w_panels = (flat ? L.cin_p % 32 == 0 : streams_filter(fg)) && use_mfma_gather(st, fg);
-            L.wt_panels = (flat ? L.d.cout % 32 == 0 : streams_filter(dg)) && use_mfma_gather(st, dg);
+            // what makes the projections' gradients of a GATED reads rows
+            L.wt_panels = (flat ? L.d.cout % 32 == 0 : streams_filter(dg)) && use_mfma_gather(st, dg) && !A.projected;
         }
         if (L.d.kind == BAPIPE_CONV2D || L.d.kind == BAPIPE_LINEAR) {
             ConvShape cs = conv_shape(st, L);
