@@ -39,6 +39,13 @@ template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float f)
 // value as it will read back from storage of type T
 template <class T> __device__ __forceinline__ float round_to(float f) { return to_f32(from_f32<T>(f)); }
 
+// what rounding took from f; of what is not finite, or no longer is when rounded, nothing: inf - inf would make a NaN of the sum of both
+__device__ __forceinline__ float rounding_took(float f, float rounded)
+{
+    const float r = f - rounded;
+    return fabsf(r) < __builtin_inff() ? r : 0.0f;
+}
+
 // Aligned vector of V storage elements: one 16-byte access for V*sizeof(T) == 16.
 template <class T, int V> struct alignas(sizeof(T) * V) vec_t {
     T e[V];

@@ -478,8 +478,8 @@ __global__ __launch_bounds__(TPB) void k_gated_grad(const T *__restrict__ dh, co
         const float vg = d[j] * u.e[j] * da, vu = d[j] * a;
         dg.e[j] = from_f32<T>(vg);
         du.e[j] = from_f32<T>(vu);
-        rg.e[j] = from_f32<T>(vg - to_f32(dg.e[j]));
-        ru.e[j] = from_f32<T>(vu - to_f32(du.e[j]));
+        rg.e[j] = from_f32<T>(rounding_took(vg, to_f32(dg.e[j])));
+        ru.e[j] = from_f32<T>(rounding_took(vu, to_f32(du.e[j])));
     }
     *reinterpret_cast<vec *>(D + at) = dg;
     *reinterpret_cast<vec *>(D + at + F) = du;
@@ -666,8 +666,8 @@ __global__ __launch_bounds__(WP *WU * 64, 2) void k_gated_mfma(MmArgs p)
                         D[p.N] = from_f32<T>(du);
                         if (!p.out_rest) continue;
                         T *rest = (T *)p.out_rest + (size_t)row * 2 * p.N + col;
-                        rest[0] = from_f32<T>(dg - round_to<T>(dg));
-                        rest[p.N] = from_f32<T>(du - round_to<T>(du));
+                        rest[0] = from_f32<T>(rounding_took(dg, round_to<T>(dg)));
+                        rest[p.N] = from_f32<T>(rounding_took(du, round_to<T>(du)));
                     }
                 } else {
 #pragma unroll

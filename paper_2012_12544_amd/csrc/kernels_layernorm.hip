@@ -192,7 +192,7 @@ __global__ __launch_bounds__(G > TPB ? G : TPB) void k_layernorm_fwd(FwdArgs<T> 
             for (int j = 0; j < V; ++j) {
                 const float v = fmaf(f[k][j] * inv, gamma.v[k].e[j], beta.v[k].e[j]);
                 y.e[j] = from_f32<T>(v);
-                if (p.rest) rest.e[j] = from_f32<T>(v - to_f32(y.e[j]));
+                if (p.rest) rest.e[j] = from_f32<T>(rounding_took(v, to_f32(y.e[j])));
             }
             store_vec<TAIL>(p.y + at, y, C - c);
             if (p.rest) store_vec<TAIL>(p.rest + at, rest, C - c);
@@ -423,7 +423,7 @@ __global__ __launch_bounds__(TPB) void k_layernorm_fwd_long(FwdArgs<T> p)
         for (int c = threadIdx.x; c < p.C; c += TPB) {
             const float v = fmaf((to_f32(p.x[at + c]) - mean) * inv, p.gamma[c], p.beta[c]);
             const T y = from_f32<T>(v);
-            if (p.rest) p.rest[at + c] = from_f32<T>(v - to_f32(y));
+            if (p.rest) p.rest[at + c] = from_f32<T>(rounding_took(v, to_f32(y)));
             if (p.copy) p.copy[at + c] = p.x[at + c];
             p.y[at + c] = y;
         }

@@ -1,12 +1,14 @@
 """Calls of layer norm, gated layer and dropout beyond those of test_gpu_sublayer.py."""
 import numpy as np
 import pytest
+import torch
 
 from gpu_harness import GpuStage, compare_minibatch, stage_io
+from oracle import ops
 from paper_2012_12544_amd import binding as B
 from stage_inputs import configs as C
 from stage_inputs import gen
-from test_gpu_sublayer import _rows
+from test_gpu_sublayer import _f64, _rows, _stage
 from test_oracle_sublayer import sublayer
 
 pytestmark = pytest.mark.gpu
@@ -46,3 +48,51 @@ def test_positions_in_the_batch_or_in_a_sequence_are_the_same(kw):
         out.append(got)
     for a, b in zip(*out):
         assert np.array_equal(a, b) and np.any(a)
+
+
+# ------------------------------------------------------------------------------ what is not finite
+@pytest.mark.parametrize("c,units,seq", [(16, 40, 6), (16, 4096, 2048), (15, 40, 6)])
+def test_an_infinite_gradient_of_a_narrow_layer_norm(c, units, seq):
+    """dy that overflowed in one element: the gradients that it reaches are infinite, as the sums say, not NaN, and rows that it does
+    not reach are what they were.  Narrow layer norms take what rounding took from the projections' gradients as well."""
+    b = C._Builder()
+    b.layernorm(c, src=-1)
+    b.gated(c, units, act=C.GATE_SIGMOID, bias=1)
+    b.conv(units, 8, 1)
+    st = _stage(b.layers, C.BF16, (c, seq, 1), 1, 1)
+    params = gen.all_params(st, perturb=True)
+    # positive weights and linear parts, moderate gates: every product that dy enters is positive
+    w = np.abs(params[1][0]) * np.float32(0.5) + np.float32(0.01)
+    bias = np.concatenate([np.zeros(units), np.full(units, 16 * w.sum(1).max())]).astype(np.float32)
+    params[1] = (w, bias)
+    params[2] = (np.abs(params[2][0]) + np.float32(0.01), params[2][1])
+    xs, gs = stage_io(st)
+    dy = gs[0].copy()
+    dy[0, 0, 3] = np.inf
+    g = GpuStage(st, params)
+    g.forward(0, xs[0])
+    dx = _rows(g.backward(0, dy))
+    dgamma, dbeta = g.grads(0)
+    g.close()
+    xhat = ops.layernorm_fwd(_f64(torch.from_numpy(xs[0]).bfloat16().float().numpy()), np.ones(c), np.zeros(c), 1e-5)[1]
+    assert np.all(np.isfinite(dx[[0, 1, 2, 4, 5]]))
+    assert np.all(dbeta == np.inf), dbeta
+    assert np.array_equal(dgamma, np.sign(_rows(xhat)[3]) * np.inf), dgamma
+
+
+def test_an_infinite_output_of_a_layer_norm_in_front_of_a_relu():
+    """What rounding took from it is nothing."""
+    c, units = 24, 40
+    b = C._Builder()
+    b.layernorm(c, src=-1)
+    b.gated(c, units, act=C.GATE_RELU, bias=1)
+    st = _stage(b.layers, C.BF16, (c, 5, 1), 2, 1)
+    params = gen.all_params(st, perturb=True)
+    gamma, beta = params[0]
+    beta = beta.copy()
+    beta[7] = np.inf
+    params[0], params[1] = (gamma, beta), (np.abs(params[1][0]) + np.float32(0.01), params[1][1])
+    g = GpuStage(st, params)
+    y = g.forward(0, stage_io(st)[0][0])
+    g.close()
+    assert np.all(y == np.inf)
