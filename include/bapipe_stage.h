@@ -84,7 +84,7 @@ typedef enum {
     BAPIPE_GATE_SIGMOID = 0, /* 1 / (1 + exp(-g))                                           */
     BAPIPE_GATE_SILU = 1,    /* g / (1 + exp(-g))                                           */
     BAPIPE_GATE_GELU = 2,    /* g (1 + erf(g / sqrt 2)) / 2                                 */
-    BAPIPE_GATE_RELU = 3     /* max(g, 0)                                                   */
+    BAPIPE_GATE_RELU = 3     /* max(g, 0), NaN of NaN                                       */
 } bapipe_gate_t;
 
 /* One layer of the stage.  src0/src1: index of the producing layer in the list, -1 = the

@@ -14,7 +14,7 @@ namespace {
 constexpr int TPB = 256;
 typedef f32x16_t f32x16;
 
-// act(g), and its derivative.  A ReLU's derivative at 0 is 0, as everywhere in the library.  A float layer takes the library's
+// act(g), and its derivative.  A ReLU's derivative at 0 is 0, as everywhere in the library; of NaN its value is NaN.  A float layer takes the library's
 // exp and erfc; for a bf16 one, whose results are rounded to 8 bits, the hardware's exp2 and reciprocal (a few 2^-24 off, times |g|)
 // and, with t = 1 / (1 + 0.4 x), erfc(x) = exp(-x^2) t q(t), q a polynomial of degree 8 fitted here to erfcx(x) / t over
 // x >= 0 for the least largest relative error: 2.8e-7 in float arithmetic, in the tail as well, where 1 + erf is all
@@ -45,7 +45,7 @@ template <bool FAST> __device__ __forceinline__ float cdf_of(float g, float e)
 }
 template <bool FAST> __device__ __forceinline__ float act_value(int act, float g)
 {
-    if (act == ACT_RELU) return fmaxf(g, 0.0f);
+    if (act == ACT_RELU) return g <= 0.0f ? 0.0f : g;
     if (act == ACT_GELU) return g * cdf_of<FAST>(g, FAST ? exp_of<FAST>(-0.5f * g * g) : 0.0f);
     const float s = sigmoid_of<FAST>(g);
     return act == ACT_SIGMOID ? s : g * s;
@@ -53,7 +53,7 @@ template <bool FAST> __device__ __forceinline__ float act_value(int act, float g
 template <bool FAST> __device__ __forceinline__ void act_both(int act, float g, float &a, float &da)
 {
     if (act == ACT_RELU) {
-        a = fmaxf(g, 0.0f);
+        a = g <= 0.0f ? 0.0f : g;
         da = g > 0.0f ? 1.0f : 0.0f;
     } else if (act == ACT_GELU) {
         const float e = exp_of<FAST>(-0.5f * g * g), cdf = cdf_of<FAST>(g, e);

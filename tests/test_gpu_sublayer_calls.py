@@ -8,7 +8,7 @@ from oracle import ops
 from paper_2012_12544_amd import binding as B
 from stage_inputs import configs as C
 from stage_inputs import gen
-from test_gpu_sublayer import _f64, _rows, _stage
+from test_gpu_sublayer import _f64, _one, _rows, _run, _stage
 from test_oracle_sublayer import sublayer
 
 pytestmark = pytest.mark.gpu
@@ -96,3 +96,24 @@ def test_an_infinite_output_of_a_layer_norm_in_front_of_a_relu():
     y = g.forward(0, stage_io(st)[0][0])
     g.close()
     assert np.all(y == np.inf)
+
+
+@pytest.mark.parametrize("dtype,c,units,rows", [(C.FP32, 24, 40, 9), (C.FP32, 16, 2056, 2050), (C.BF16, 24, 40, 9), (C.BF16, 25, 41, 9), (C.BF16, 64, 1600, 2060)])
+def test_a_relu_gate_that_is_no_number(dtype, c, units, rows):
+    """max(g, 0) of NaN is NaN: a parameter that went wrong shows in the output and in the gradients that the unit's value enters."""
+    st = _stage(_one("gated", c, units, act=C.GATE_RELU, bias=1), dtype, (c, rows, 1), 1, 1)
+    (w, bias), = params = gen.all_params(st, perturb=True)
+    xs, gs = stage_io(st)
+    ref = _run(st, xs, gs, params)
+    bias = bias.copy()
+    bias[3] = np.nan
+    g = GpuStage(st, [(w, bias)])
+    y = _rows(g.forward(0, xs[0]))
+    g.backward(0, gs[0])
+    dw, db = g.grads(0)
+    g.close()
+    others = np.arange(units) != 3
+    assert np.all(np.isnan(y[:, 3])) and np.array_equal(y[:, others], _rows(ref["y0"])[:, others])
+    assert np.isnan(db[units + 3]) and np.all(np.isnan(dw[units + 3]))
+    keep = np.concatenate([others, others])
+    assert np.array_equal(dw[keep], ref["dw0"][keep]) and np.array_equal(db[keep], ref["db0"][keep])
