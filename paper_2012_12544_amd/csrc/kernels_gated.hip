@@ -60,9 +60,10 @@ template <bool FAST> __device__ __forceinline__ void act_both(int act, float g, 
         a = g * cdf;
         da = fmaf(g * e, 0.39894228040143268f, cdf);
     } else {
-        const float s = sigmoid_of<FAST>(g);
+        // 1 - s of s within rounding of 1 has no digits left; exp(-g) s has all of them
+        const float e = exp_of<FAST>(-g), s = FAST ? __builtin_amdgcn_rcpf(1.0f + e) : 1.0f / (1.0f + e), rest = g > 0.0f ? e * s : 1.0f - s;
         a = act == ACT_SIGMOID ? s : g * s;
-        da = act == ACT_SIGMOID ? s * (1.0f - s) : s * (1.0f + g * (1.0f - s));
+        da = act == ACT_SIGMOID ? s * rest : s * (1.0f + g * rest);
     }
 }
 

@@ -1,14 +1,17 @@
-"""Calls of layer norm, gated layer and dropout beyond those of test_gpu_sublayer.py."""
+"""Calls of layer norm, gated layer and dropout beyond those of test_gpu_sublayer.py.
+
+Rounding to storage is off by at most HALF relative to the value; U is that of a float."""
 import numpy as np
 import pytest
 import torch
 
-from gpu_harness import GpuStage, compare_minibatch, stage_io
+from gpu_harness import GpuStage, compare_minibatch, stage_io, tdtype
 from oracle import ops
+from oracle.stage import OracleStage
 from paper_2012_12544_amd import binding as B
 from stage_inputs import configs as C
 from stage_inputs import gen
-from test_gpu_sublayer import _f64, _one, _rows, _run, _stage
+from test_gpu_sublayer import HALF, U, _f64, _one, _rows, _run, _stage
 from test_oracle_sublayer import sublayer
 
 pytestmark = pytest.mark.gpu
@@ -117,3 +120,29 @@ def test_a_relu_gate_that_is_no_number(dtype, c, units, rows):
     assert np.isnan(db[units + 3]) and np.all(np.isnan(dw[units + 3]))
     keep = np.concatenate([others, others])
     assert np.array_equal(dw[keep], ref["dw0"][keep]) and np.array_equal(db[keep], ref["db0"][keep])
+
+
+# ------------------------------------------------------------------------------ saturated gates
+@pytest.mark.parametrize("dtype", [C.FP32, C.BF16])
+@pytest.mark.parametrize("at", [-15.0, -9.0, 9.0, 12.0, 15.0])
+def test_the_derivative_of_a_saturated_sigmoid(dtype, at):
+    """s (1 - s) of s within rounding of 1: the gates' weight gradients have all their digits."""
+    c, units, seq = 8, 16, 40
+    st = _stage(_one("gated", c, units, act=C.GATE_SIGMOID, bias=1), dtype, (c, seq, 1), 1, 1)
+    (w, bias), = params = gen.all_params(st, perturb=True)
+    bias = np.concatenate([np.full(units, at, np.float32), bias[units:]])
+    xs, gs = stage_io(st)
+    got = _f64(_run(st, xs, gs, [(w, bias)])["dw0"])[:units]
+    orc = OracleStage(dict(st), [(w, bias)])
+    W, x, dy = orc.q(_f64(w)), _rows(torch.from_numpy(xs[0]).to(tdtype(st)).double().numpy()), _rows(torch.from_numpy(gs[0]).to(tdtype(st)).double().numpy())
+    both = x @ W.T + bias
+    e = np.exp(-np.abs(both[:, :units]))
+    dg = dy * both[:, units:] * e / (1 + e) ** 2
+    # an error of the gate's argument is one of dg, relative; of exp's argument, scaled by log2 e, the hardware's exp2 has |g| 2U more.  32 U
+    # for the products; the other projection's own error enters in absolute terms; a chain of seq additions; bf16: D is rounded once
+    size = np.abs(x) @ np.abs(W).T + np.abs(bias)
+    eg, eu = (c + 2) * U * size[:, :units], (c + 2) * U * size[:, units:]
+    off = np.abs(dg) * (eg + (4 * abs(at) + 32) * U + (HALF[dtype] if dtype == C.BF16 else 0)) + np.abs(dy) * eu * e / (1 + e) ** 2
+    bound = off.T @ np.abs(x) + seq * U * (np.abs(dg).T @ np.abs(x))
+    worst = float(np.max(np.abs(got - dg.T @ x) / bound))
+    assert worst <= 1
