@@ -200,7 +200,7 @@ hipError_t bn_bwd(int dt, const void *x, const void *dy, const float *gamma, con
                   void *workspace, hipStream_t s, int pre_chunks = 0);
 
 // ---- layer norm over the C channels of each of `rows` positions (kernels_layernorm.hip); stats: [2][rows] floats (mean, 1/std)
-size_t layernorm_workspace(int rows, int C);
+size_t layernorm_workspace(int dt, int rows, int C);
 // copy: a second place for x; rest: for what rounding took from y, in the storage type (each NULL or as large as x)
 hipError_t layernorm_fwd(int dt, const void *x, const float *gamma, const float *beta, float eps, void *y, float *stats, int rows, int C,
                          hipStream_t s, void *copy = nullptr, void *rest = nullptr);
@@ -213,7 +213,7 @@ hipError_t layernorm_bwd(int dt, const void *x, const void *dy, int dy_parts, co
 enum { ACT_SIGMOID = 0, ACT_SILU = 1, ACT_GELU = 2, ACT_RELU = 3 };
 // whether the products take the bf16 MFMA kernels: conv_gather_mfma for dx = D W (wt: [C][2F]), conv_wgrad_mfma for dw += D^T x, with db
 bool gated_mfma(int dt, int rows, int C, int F);
-size_t gated_workspace(int dt, int rows, int C, int F, bool rest);       // of the calls here
+size_t gated_workspace(int dt, int rows, int C, int F, bool rest, bool parts);       // of the calls here; rest, parts: as they are called
 // rest: NULL, or a second tensor whose sum with x is the layer's input; panels: w is kept in panels (GatherConv::wt_panels), for gated_mfma only
 hipError_t gated_fwd(int dt, int act, const void *x, const void *rest, const void *w, const float *bias, float *P, void *h, int rows, int C, int F, bool panels,
                      void *workspace, hipStream_t s);

@@ -779,16 +779,15 @@ static bool mm_takes(int dt, int rows, int K, long long weight_rows)
            mm_tiles(rows, weight_rows, 128, 128) >= (dt == DT_F32 ? 512 : 192);
 }
 
-size_t gated_workspace(int dt, int rows, int C, int F, bool rest)
+size_t gated_workspace(int dt, int rows, int C, int F, bool rest, bool parts)
 {
     const size_t walks = rest ? 2 : 1;
     if (gated_mfma(dt, rows, C, F)) return mm_takes(dt, rows, C, 2ll * F) ? 0 : walks * conv_gather_mfma_raw_workspace(rows_product(rows, C, 2 * F, false));
-    auto sums = [](const AnyPlan &p, size_t n) { return p.splits > 1 ? (size_t)p.splits * n * sizeof(float) : 0; };
-    size_t most = 0;
-    const AnyPlan f = forward_plan(rows, C, F);
-    for (const size_t v : {f.splits * walks > 1 ? f.splits * walks * rows * 2 * F * sizeof(float) : 0, sums(dgrad_plan(rows, C, F), (size_t)rows * C),
-                           sums(wgrad_plan(rows, C, F), (size_t)2 * F * (C + 1))})
-        most = v > most ? v : most;
+    auto sums = [](size_t splits, size_t n) { return splits > 1 ? splits * n * sizeof(float) : 0; };
+    size_t most = sums(wgrad_plan(rows, C, F).splits, (size_t)2 * F * (C + 1));
+    const size_t forward = mm_takes(dt, rows, C, 2ll * F) ? 0 : sums(forward_plan(rows, C, F).splits * walks, (size_t)rows * 2 * F);
+    const size_t dgrad = parts || (dt == DT_F32 && mm_takes(dt, rows, 2 * F, C)) ? 0 : sums(dgrad_plan(rows, C, F).splits, (size_t)rows * C);
+    for (const size_t v : {forward, dgrad}) most = v > most ? v : most;
     return most;
 }
 

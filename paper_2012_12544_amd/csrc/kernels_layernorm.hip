@@ -534,11 +534,22 @@ int bwd_blocks(int rows, int groups)
     const int all = (rows + groups - 1) / groups, long_ones = rows / 32, many = long_ones > 512 ? 512 : long_ones < 256 ? 256 : long_ones;
     return all < many ? all : many;
 }
-constexpr int kLongChunks = 256;
+// Rows whose columns' sums a thread of the long rows' kernel adds up: at most 256 such chunks
+int long_chunk(int rows)
+{
+    constexpr int most = 256;
+    return rows < 64 * most ? 64 : (rows + most - 1) / most;
+}
+constexpr int kBwdThreads = 512;
 
 }  // namespace
 
-size_t layernorm_workspace(int rows, int C) { return (size_t)(rows < 512 ? rows : 512) * 2 * C * sizeof(float); }
+size_t layernorm_workspace(int dt, int rows, int C)
+{
+    const Shape k = shape_of(dt, C, false);
+    const int blocks = k.g ? bwd_blocks(rows, kBwdThreads / k.g) : (rows + long_chunk(rows) - 1) / long_chunk(rows);
+    return k.g && blocks == 1 ? 0 : (size_t)blocks * 2 * C * sizeof(float);      // a lone block adds its own
+}
 
 template <class T>
 static hipError_t fwd_t(int dt, FwdArgs<T> p, hipStream_t s)
@@ -580,21 +591,21 @@ static hipError_t bwd_t(int dt, BwdArgs<T> p, hipStream_t s)
     bool found = false;
 #define BWD_(NV, G, NT, TAIL, PARTS) \
     (epi ? launch(k_layernorm_bwd<T, NV, G, NT, TAIL, PARTS, true>, NT, NT / G) : launch(k_layernorm_bwd<T, NV, G, NT, TAIL, PARTS, false>, NT, NT / G))
-#define BWD(NV, G, NT)                                                                                             \
-    if (!found && k.nv == NV && k.g == G) {                                                                        \
-        found = true;                                                                                              \
-        if constexpr (sizeof(T) == 2) {                                                                            \
-            if (p.dy_parts) e = tail ? BWD_(NV, G, NT, true, true) : BWD_(NV, G, NT, false, true);                 \
-        }                                                                                                          \
-        if (!p.dy_parts) e = tail ? BWD_(NV, G, NT, true, false) : BWD_(NV, G, NT, false, false);                  \
+#define BWD(NV, G)                                                                                                             \
+    if (!found && k.nv == NV && k.g == G) {                                                                                    \
+        found = true;                                                                                                          \
+        if constexpr (sizeof(T) == 2) {                                                                                        \
+            if (p.dy_parts) e = tail ? BWD_(NV, G, kBwdThreads, true, true) : BWD_(NV, G, kBwdThreads, false, true);           \
+        }                                                                                                                      \
+        if (!p.dy_parts) e = tail ? BWD_(NV, G, kBwdThreads, true, false) : BWD_(NV, G, kBwdThreads, false, false);            \
     }
-    BWD(1, 8, 512); BWD(1, 16, 512); BWD(1, 32, 512); BWD(1, 64, 512); BWD(2, 64, 512);
-    BWD(1, 256, 512); BWD(2, 256, 512); BWD(2, 512, 512); BWD(4, 512, 512);
+    BWD(1, 8); BWD(1, 16); BWD(1, 32); BWD(1, 64); BWD(2, 64);
+    BWD(1, 256); BWD(2, 256); BWD(2, 512); BWD(4, 512);
 #undef BWD
 #undef BWD_
     if (!found) {
         // the columns first, for dx may take the place of dy
-        const int per = p.rows < 64 * kLongChunks ? 64 : (p.rows + kLongChunks - 1) / kLongChunks;
+        const int per = long_chunk(p.rows);
         chunks = (p.rows + per - 1) / per;
         hipLaunchKernelGGL(k_layernorm_columns<T>, dim3((p.C + TPB - 1) / TPB, chunks), dim3(TPB), 0, s, p, per);
         if (p.dx) hipLaunchKernelGGL(k_layernorm_dx_long<T>, dim3(p.rows < (1 << 20) ? p.rows : 1 << 20), dim3(TPB), 0, s, p);

@@ -1558,7 +1558,7 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         if (L.d.kind == BAPIPE_LAYERNORM) {
             const int rows = rows_of(st, A);
             L.aux_off = slot; L.aux_bytes = 2 * sizeof(float) * (size_t)rows; slot += align_up(L.aux_bytes);
-            const size_t w = layernorm_workspace(rows, A.C);
+            const size_t w = layernorm_workspace(st->dt, rows, A.C);
             work = w > work ? w : work;
         }
         if (L.d.kind == BAPIPE_GATED) {
@@ -1567,18 +1567,20 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
             L.off_d = gr; gr += align_up((size_t)rows * 2 * L.d.cout * es);
             if (A.fine) { L.off_d_rest = gr; gr += align_up((size_t)rows * 2 * L.d.cout * es); }
             L.mfma = gated_mfma(st->dt, rows, L.d.cin, L.d.cout);
-            size_t w = gated_workspace(st->dt, rows, L.d.cin, L.d.cout, A.rest);
+            size_t w = gated_workspace(st->dt, rows, L.d.cin, L.d.cout, A.rest, A.gparts > 0);
             work = w > work ? w : work;
             if (L.mfma) {
                 const ConvShape cs = conv_shape(st, L);
                 const GatherConv dg = dgrad_geom(st, L);
                 L.w_panels = streams_filter(fwd_geom(st, L));
                 L.wt_panels = streams_filter(dg);
-                w = conv_gather_mfma_workspace(dg); work = w > work ? w : work;
+                if (!A.gparts) { w = conv_gather_mfma_workspace(dg); work = w > work ? w : work; }      // else its sums are the gradient
                 w = rows_wgrad_mfma_workspace(rows, L.d.cin, 2 * L.d.cout); work = w > work ? w : work;
-                w = conv_wgrad_mfma_workspace(cs); work = w > work ? w : work;      // where it shares a launch
                 L.groups = conv_wgrad_mfma_groups(cs);
-                if (L.groups) grouped += align_up(w);
+                if (L.groups) {                              // it may share a launch
+                    w = conv_wgrad_mfma_workspace(cs); work = w > work ? w : work;
+                    grouped += align_up(w);
+                }
             }
         }
         if (L.d.kind == BAPIPE_LSTM) {
@@ -1684,11 +1686,12 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
             work = w > work ? w : work;
             GatherConv fg = fwd_geom(st, L), dg = dgrad_geom(st, L);
             if (use_mfma_gather(st, fg)) { w = conv_gather_mfma_workspace(fg); work = w > work ? w : work; }
-            if (use_mfma_gather(st, dg)) { w = conv_gather_mfma_workspace(dg); work = w > work ? w : work; }
+            const bool dx_parts = A.gparts || A.projected;      // the gradient does not pass through the workspace
+            if (use_mfma_gather(st, dg) && !dx_parts) { w = conv_gather_mfma_workspace(dg); work = w > work ? w : work; }
             // the plans these launches take beside kernels of further streams (bapipe_stage_set_streams)
             fg.beside = dg.beside = 1;
             if (use_mfma_gather(st, fg)) { w = conv_gather_mfma_workspace(fg); work = w > work ? w : work; }
-            if (use_mfma_gather(st, dg)) { w = conv_gather_mfma_workspace(dg); work = w > work ? w : work; }
+            if (use_mfma_gather(st, dg) && !dx_parts) { w = conv_gather_mfma_workspace(dg); work = w > work ? w : work; }
         }
     }
     // residual fan-out: a tensor read by exactly one conv (MFMA gather input gradient, plain epilogue) or layer norm and, later in
