@@ -85,10 +85,11 @@ bool conv3x3_halo_pool_supported(const GatherConv &g);
 hipError_t conv3x3_halo_pool_mfma(const void *in, const void *wt, const float *bias, int relu, void *pool_out,
                                   uint8_t *pool_idx, const GatherConv &g, hipStream_t s);
 // The same implicit GEMM leaving raw fp32 sums: part[split][pixel][co], *splits partial results the
-// caller adds up (no bias, no epilogue, no rounding).  Used for the recurrent products of the LSTM.
+// caller adds up (no bias, no epilogue, no rounding).  Used for the recurrent products of the LSTM, and for gradients that stay float
+// sums between layers.  expected: 0, or how many part has room for and its reader adds up; another count is refused
 size_t conv_gather_mfma_raw_workspace(const GatherConv &g);
 hipError_t conv_gather_mfma_raw(const void *in, const void *wt, const GatherConv &g, float *part, int *splits,
-                                hipStream_t s);
+                                hipStream_t s, int expected = 0);
 bool wgrad3x3_units(const ConvShape &c);          // whether the map comes apart into units of 8x16 pixels, as both of these need it
 bool wgrad3x3_halo_supported(const ConvShape &c);
 size_t wgrad3x3_halo_workspace(const ConvShape &c);

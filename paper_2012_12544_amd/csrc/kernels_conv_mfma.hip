@@ -1624,10 +1624,11 @@ size_t conv_gather_mfma_raw_workspace(const GatherConv &g)
 }
 
 hipError_t conv_gather_mfma_raw(const void *in, const void *wt, const GatherConv &g, float *part, int *splits,
-                                hipStream_t s)
+                                hipStream_t s, int expected)
 {
     if (!conv_gather_mfma_supported(g) || !part || !splits || g.Co % 4 != 0) return hipErrorInvalidValue;
     const GatherPlan p = gather_plan(g);
+    if (expected && p.splits != expected) return hipErrorInvalidValue;
     *splits = p.splits;
     if ((long long)g.N * g.Ho * g.Wo == 0) return hipSuccess;
     const GradEpi none{nullptr, 0};

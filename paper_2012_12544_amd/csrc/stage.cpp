@@ -940,7 +940,7 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
                                      rows_of(st, A), L.d.cout, L.d.cin, s));
             } else if (A.gparts) {
                 int parts = 0;
-                HIPCHK(conv_gather_mfma_raw(g, L.w_t, dg, (float *)dx, &parts, s));
+                HIPCHK(conv_gather_mfma_raw(g, L.w_t, dg, (float *)dx, &parts, s, A.gparts));
             } else if (mf && L.bnb_chunks && !c.profiling && (e.gate || e.accum)) {
                 const Layer &B = st->layers[li - 1];
                 HIPCHK(conv_gather_mfma(g, L.w_t, nullptr, dx, 0, e, dg, st->work, st->tickets, s, (float *)st->work,
@@ -1084,10 +1084,11 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
             void *dx = grad_ptr(st, L.a, c);
             tp = st->tap_begin(L.mfma ? BAPIPE_KC_CONV_GATHER_MFMA : BAPIPE_KC_CONV_DIRECT);
             int parts = 0;
-            float *second = (float *)dx + A.gparts / 2 * A.elems;
+            const int each = Dr ? A.gparts / 2 : A.gparts;           // float sums of either product
+            float *second = (float *)dx + each * A.elems;
             if (L.mfma && A.gparts) {
-                HIPCHK(conv_gather_mfma_raw(D, L.w_t, dgrad_geom(st, L), (float *)dx, &parts, s));
-                if (Dr) HIPCHK(conv_gather_mfma_raw(Dr, L.w_t, dgrad_geom(st, L), second, &parts, s));
+                HIPCHK(conv_gather_mfma_raw(D, L.w_t, dgrad_geom(st, L), (float *)dx, &parts, s, each));
+                if (Dr) HIPCHK(conv_gather_mfma_raw(Dr, L.w_t, dgrad_geom(st, L), second, &parts, s, each));
             } else if (L.mfma)
                 HIPCHK(conv_gather_mfma(D, L.w_t, nullptr, dx, 0, e, dgrad_geom(st, L), st->work, st->tickets, s));
             else {
