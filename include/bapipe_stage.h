@@ -170,7 +170,8 @@ int bapipe_stage_forward(bapipe_stage_t *st, int mb_id, const void *x_dev, void 
  * dy_dev_or_labels: device; gradient w.r.t. the stage output (layout/type as y), or, when
  * the last layer is SOFTMAX_XENT, micro_batch int32 class labels.
  * dx_dev: device, receives the gradient w.r.t. the stage input (layout/type as x); may be
- * NULL; ignored when need_input_grad == 0.
+ * NULL; ignored when need_input_grad == 0.  It may lie over dy_dev, at its address or shifted:
+ * where a kernel that stores dx would meet one that still reads dy, dx is copied there at the end.
  * Legal order: ids ascending, each after its own forward; otherwise E_ORDER. */
 int bapipe_stage_backward(bapipe_stage_t *st, int mb_id, const void *dy_dev_or_labels,
                           void *dx_dev);

@@ -183,6 +183,7 @@ struct bapipe_stage {
     float *losses = nullptr;                 // and, behind them, the tickets of conv_gather_mfma: of the handle's stream, of the backward stream
     uint32_t *dropout_state = nullptr;       // behind those: seed and mini-batch number of the DROPOUT layers
     bool has_dropout = false;
+    bool dx_at_dy = false, dx_across_dy = false;      // see dx_may_lie_over_dy: at the same address, at any other
     unsigned *tickets = nullptr, *tickets_f = nullptr, *tickets_b = nullptr;      // as work: of the pass being enqueued, of either
     size_t params_bytes = 0, slot_bytes = 0, transient_bytes = 0, grads_bytes = 0, work_bytes = 0;
     size_t flush_bytes = 0;                  // workspace of flush_deferred, whatever part of a mini-batch it finds
@@ -811,7 +812,7 @@ struct BwdCtx {
     std::vector<const void *> pending;   // per tensor: an ADD's share of its gradient that the tensor's conv will add (fanout_conv)
     bool profiling = false;        // profiler: run every kernel of the layer now (no deferral)
     int bn_sums_ready = -1;        // batch-norm layer whose backward sums the last conv left in the workspace
-    bool dx_over_dy = false;       // dx_direct overlaps dy_direct
+    bool dx_over_dy = false;       // the caller's dx overlaps dy_direct
 };
 
 void *grad_ptr(bapipe_stage *st, int t, BwdCtx &c)
@@ -1173,6 +1174,46 @@ hipError_t static_scratch(char **out)
     }
     *out = g_scratch_ptr[dev];
     return hipSuccess;
+}
+
+// Whether the kernels of a backward pass may store dx over the caller's dy, at its very address (same) or shifted against it: nothing that still
+// reads dy runs behind what stores dx, and what does both does it element by element or row by row.
+bool dx_may_lie_over_dy(const bapipe_stage *st, bool same)
+{
+    auto root = [&](int t) { return st->tensors[t].root; };
+    auto place = [&](int t) {                                  // whose gradient's place the gradient of t is
+        for (t = root(t); st->tensors[t].galias >= 0;) t = root(st->tensors[t].galias);
+        return t;
+    };
+    const int dy = root((int)st->tensors.size() - 1);
+    bool stored = false, changed = false;                      // something in dx's place; other than dy
+    std::vector<char> reads_late(st->layers.size(), 0);        // an ADD's share that a layer's own epilogue adds
+    for (int i = (int)st->layers.size() - 1; i >= 0; --i) {
+        const Layer &L = st->layers[i];
+        const int kind = L.d.kind;
+        if (kind == BAPIPE_FLATTEN) continue;
+        const bool own = place(L.o) == dy, late = reads_late[i], reads = own || late;
+        if (reads && changed) return false;
+        for (int t : {L.a, L.b}) {
+            if (t < 0 || !st->tensors[root(t)].need_grad) continue;
+            const int taker = st->tensors[root(t)].fanout_conv;
+            if (kind == BAPIPE_ADD && taker >= 0) {
+                if (reads) reads_late[taker] = 1;
+                continue;
+            }
+            if (root(t) != 0) continue;
+            if (own && kind == BAPIPE_ADD && same && !stored) {                 // dy copied onto itself
+                stored = true;
+                continue;
+            }
+            const bool by_element = kind == BAPIPE_ADD || kind == BAPIPE_RELU || kind == BAPIPE_DROPOUT || kind == BAPIPE_LAYERNORM;
+            // GATED has read all of its output's gradient before its input's is stored
+            if (own && !(same && by_element) && kind != BAPIPE_GATED) return false;
+            if (late && !same) return false;
+            stored = changed = true;
+        }
+    }
+    return true;
 }
 
 }  // namespace
@@ -1709,6 +1750,8 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         if (!use_mfma_gather(st, dg) || conv3x3_halo_supported(dg) || Lc.bnb_chunks) continue;
         T.fanout_conv = ic;
     }
+    st->dx_at_dy = dx_may_lie_over_dy(st, true);
+    st->dx_across_dy = dx_may_lie_over_dy(st, false);
     st->slot_bytes = align_up(slot);
     st->transient_bytes = trans;
     st->grads_bytes = gr;
@@ -1890,8 +1933,9 @@ int bapipe_stage_backward(bapipe_stage_t *st, int mb_id, const void *dy_dev_or_l
             c.dy_direct = dy_dev_or_labels;
         }
         c.written[r] = 1;
-        const uintptr_t dx0 = (uintptr_t)c.dx_direct, dy0 = (uintptr_t)c.dy_direct;
+        const uintptr_t dx0 = want_dx ? (uintptr_t)dx_dev : 0, dy0 = (uintptr_t)c.dy_direct;
         c.dx_over_dy = dx0 && dy0 && dx0 < dy0 + O.bytes() && dy0 < dx0 + In.bytes();
+        if (c.dx_over_dy && !(dx0 == dy0 ? st->dx_at_dy : st->dx_across_dy)) c.dx_direct = nullptr;      // it goes there behind the last layer
     }
     st->w_waiting.clear();                   // of a pass that failed
     st->w_waiting_us = 0.0;
@@ -1906,7 +1950,9 @@ int bapipe_stage_backward(bapipe_stage_t *st, int mb_id, const void *dy_dev_or_l
     for (const void *p : c.pending)
         if (p) return st->fail(BAPIPE_E_DEVICE, "backward: a residual gradient was left for a conv that never took it");
     if (want_dx && !c.dx_direct) {
-        if (nhwc)
+        if ((nhwc || In.H * In.W == 1) && In.Cp == In.C)
+            HIPCHK(hipMemcpyAsync(dx_dev, st->gptr(0), In.bytes(), hipMemcpyDeviceToDevice, s));
+        else if (nhwc)
             HIPCHK(nhwc_repad(dt, st->gptr(0), dx_dev, (size_t)st->mb * In.H * In.W, In.Cp, In.C, s));
         else
             HIPCHK(nhwc_to_nchw(dt, st->gptr(0), dx_dev, st->mb, In.C, In.H, In.W, In.Cp, s));

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from gpu_harness import GpuStage, compare_minibatch, stage_io, tdtype
+from gpu_harness import DEV, GpuStage, compare_minibatch, stage_io, tdtype
 from oracle import ops
 from oracle.stage import OracleStage
 from paper_2012_12544_amd import binding as B
@@ -146,3 +146,66 @@ def test_the_derivative_of_a_saturated_sigmoid(dtype, at):
     bound = off.T @ np.abs(x) + seq * U * (np.abs(dg).T @ np.abs(x))
     worst = float(np.max(np.abs(got - dg.T @ x) / bound))
     assert worst <= 1
+
+
+# ------------------------------------------------------------------------------ dx over dy
+def _over(b, kind, c):
+    if kind == "sublayer":
+        b.layernorm(c, src=-1)
+        b.gated(c, 2 * c, act=C.GATE_SILU, bias=1)
+        b.conv(2 * c, c, 1)
+        b.dropout(0.2)
+        b.addl(3, -1, relu=0)
+    elif kind == "side by side":       # two readers of the input, whose gradients share dy's place
+        b.layernorm(c, src=-1)
+        b.gated(c, c, act=C.GATE_GELU, bias=1, src=-1)
+        b.addl(0, 1, relu=0)
+    elif kind == "dropped twice":
+        b.dropout(0.2, src=-1)
+        b.dropout(0.3, src=-1)
+        b.addl(0, 1, relu=0)
+    elif kind == "dropout and sum":
+        b.dropout(0.2, src=-1)
+        b.addl(0, -1, relu=0)
+    elif kind == "norm and sum":
+        b.layernorm(c, src=-1)
+        b.addl(-1, 0, relu=0)
+    elif kind == "gated and sum":
+        b.gated(c, c, act=C.GATE_SIGMOID, src=-1)
+        b.addl(0, -1, relu=0)
+    elif kind == "convolutions":
+        b.conv(c, c, 1, src=-1)
+        b.conv(c, c, 3, src=-1)
+        b.addl(0, 1, relu=0)
+    else:
+        getattr(b, kind)(*dict(layernorm=(c,), gated=(c, c), dropout=(0.2,), conv=(c, c, 3), bn=(c,), relu=())[kind], src=-1)
+
+
+@pytest.mark.parametrize("dtype", [C.FP32, C.BF16])
+@pytest.mark.parametrize("streams", [1, 3])
+@pytest.mark.parametrize("kind", ["sublayer", "side by side", "dropped twice", "dropout and sum", "norm and sum", "gated and sum", "convolutions", "layernorm",
+                                  "gated", "dropout", "conv", "bn", "relu"])
+def test_dx_over_dy(kind, streams, dtype):
+    """At dy's address, rows behind it and rows in front of it: the gradients that dx apart from dy gives, bit for bit."""
+    c, rows = 64, 700
+    b = C._Builder()
+    _over(b, kind, c)
+    st = C._stage("over", b.layers, dtype, (c, 1, rows), 2, 1, 1, 1, 1, C.BASE_SEED + 82, "xavier")
+    xs, gs = stage_io(st)
+    dy = torch.from_numpy(gs[0]).permute(0, 2, 3, 1).reshape(-1).to(DEV, tdtype(st))
+    n, room = dy.numel(), 3 * c
+    ref = None
+    for shift in (None, 0, 3 * c, -3 * c, c // 2):
+        g = GpuStage(st, gen.all_params(st, perturb=True), backward_stream=streams == 3)
+        g.forward(0, xs[0])
+        buf = torch.zeros(n + 2 * room, device=DEV, dtype=dy.dtype)
+        buf[room:room + n] = dy
+        dx = torch.zeros_like(dy) if shift is None else buf[room + shift:room + shift + n]
+        torch.cuda.synchronize()
+        B.bapipe_stage_backward(g.h, 0, buf[room:].data_ptr(), dx.data_ptr())
+        torch.cuda.synchronize()
+        got = [dx.clone().cpu().float().numpy()] + [a for i, (w, _) in enumerate(g.params) if w is not None for a in g.grads(i) if a is not None]
+        g.close()
+        ref = ref or got
+        for a, r in zip(got, ref):
+            assert np.array_equal(a, r) and np.any(a), (kind, shift)
