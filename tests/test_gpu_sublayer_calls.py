@@ -209,3 +209,55 @@ def test_dx_over_dy(kind, streams, dtype):
         ref = ref or got
         for a, r in zip(got, ref):
             assert np.array_equal(a, r) and np.any(a), (kind, shift)
+
+
+# ------------------------------------------------------------------------------ filters that are streamed
+@pytest.mark.parametrize("c,units,rows", [
+    (2048, 4128, 1), (2048, 4128, 64), (2048, 4128, 65),         # both copies in panels, the last ones of rows that take them
+    (2080, 4104, 5), (2056, 4112, 5),                            # only the one that forward reads, only the other
+])
+def test_gated_of_filters_that_are_streamed(c, units, rows):
+    st = _stage(_one("gated", c, units, act=C.GATE_SILU, bias=1), C.BF16, (c, rows, 1), 1, 1)
+    compare_minibatch(st)
+
+
+def test_sublayer_of_filters_that_are_streamed():
+    compare_minibatch(sublayer(c=2080, units=4112, seq=1, micro_batch=3, n_micro=1, stage_index=1, n_stages=1))
+
+
+# ------------------------------------------------------------------------------ a slope and the library's own difference quotient
+@pytest.mark.parametrize("act", [C.GATE_SIGMOID, C.GATE_SILU, C.GATE_GELU])
+def test_the_slope_along_many_directions(act):
+    """Float, along directions of one coordinate each and random ones: (f(x + h v) - f(x - h v)) / 2h of the library's own forward pass
+    against its dx.  What the third derivative leaves of it is the oracle's alone: its quotient at h against its own dx."""
+    st = sublayer(c=16, units=24, seq=2, micro_batch=64, n_micro=1, act=act, dtype=C.FP32, stage_index=1, n_stages=1, p=0.2)
+    params = gen.all_params(st, perturb=True)
+    xs, gs = stage_io(st)
+    h, x0 = 2.0 ** -4, _f64(xs[0])
+    # 64 samples of 2 x 16 elements: 32 directions along one coordinate of one position, 32 random ones
+    v = np.random.default_rng(5).standard_normal((64, 16, 2, 1))
+    for i in range(32):
+        v[i] = 0
+        v[i, i % 16, i // 16] = 1
+    plus, minus = (np.float32(x0 + s * h * v) for s in (1, -1))
+    v = (_f64(plus) - _f64(minus)) / (2 * h)                      # what the floats are apart
+    per_sample = lambda a, b: np.sum(_f64(a) * _f64(b), axis=(1, 2, 3))  # noqa: E731
+
+    def values(x):
+        g, o = GpuStage(st, params), OracleStage(st, params)
+        y = per_sample(g.forward(0, x), gs[0])
+        g.close()
+        return y, per_sample(o.forward(0, _f64(x)), gs[0])
+
+    g, orc = GpuStage(st, params), OracleStage(st, params)
+    y = g.forward(0, xs[0])
+    orc.forward(0, x0)
+    slope, exact = per_sample(g.backward(0, gs[0]), v), per_sample(orc.backward(0, gs[0]), v)
+    g.close()
+    (yp, op), (ym, om) = values(plus), values(minus)
+    got, curve = (yp - ym) / (2 * h), np.abs((op - om) / (2 * h) - exact)
+    # 64 U of every output, either side of the quotient: sums of 24 and 16 terms, the layer norm's, the activation's
+    noise = 64 * U * np.sum(np.abs(gs[0]) * (1 + np.abs(y)), axis=(1, 2, 3)) / h
+    size = np.abs(exact) + 1e-3 * np.linalg.norm(gs[0].reshape(64, -1), axis=1)
+    assert np.all(np.abs(got - slope) <= curve + noise + 1e-4 * size), float(np.max((np.abs(got - slope) - curve - noise) / size))
+    assert np.median((curve + noise) / size) <= 0.01             # a wrong dx would not hide in what is allowed
