@@ -46,6 +46,7 @@ struct Tensor {
     size_t elems = 0;      // per micro-batch, physical (Cp channels)
     size_t esize = 0;      // bytes per element
     int root = -1;         // storage owner (FLATTEN outputs alias their input)
+    bool map_order = false;        // a flattened map of several pixels, or made of one element by element: its features lie in the map's order
     int producer = -1;     // layer index, -1 for the stage input
     bool stashed = false;  // kept per in-flight micro-batch
     bool need_grad = false;
@@ -1316,9 +1317,8 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         Tensor &O = st->tensors[L.o];
         O.esize = es; O.root = L.o; O.producer = i;
         if (A.esize != es) return create_fail(BAPIPE_E_SHAPE, "layer %d: consumes the softmax output", i);
-        // a flattened map keeps the map's order in memory, which of its readers only LINEAR knows of
-        const Tensor &RA = st->tensors[A.root];
-        if (A.root != L.a && RA.H * RA.W > 1 && (d.kind == BAPIPE_LAYERNORM || d.kind == BAPIPE_GATED || d.kind == BAPIPE_DROPOUT))
+        // which of its readers only LINEAR knows of
+        if (A.map_order && (d.kind == BAPIPE_LAYERNORM || d.kind == BAPIPE_GATED || d.kind == BAPIPE_DROPOUT))
             return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: a flattened map as input; DROPOUT may stand in front of the FLATTEN", i);
         switch (d.kind) {
         case BAPIPE_CONV2D: {
@@ -1439,6 +1439,8 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         default:
             return create_fail(BAPIPE_E_INVALID, "layer %d: unknown kind %d", i, d.kind);
         }
+        if (d.kind == BAPIPE_FLATTEN) O.map_order = A.map_order || A.H * A.W > 1;
+        else if (d.kind != BAPIPE_LINEAR && d.kind != BAPIPE_CONV2D && d.kind != BAPIPE_LSTM) O.map_order = A.map_order || (L.b >= 0 && st->tensors[L.b].map_order);
         O.Cp = O.C;
         O.elems = (size_t)micro_batch * O.C * O.H * O.W;
         st->tensors[L.a].consumers.push_back(i);

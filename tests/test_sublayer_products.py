@@ -1,7 +1,11 @@
-"""What the products of layer norm and gated layer refuse, asked without a GPU: nothing is launched."""
+"""What layer norm, gated layer and dropout refuse, and their products, asked without a GPU: nothing is launched."""
 import ctypes as ct
 
+import pytest
+
 from paper_2012_12544_amd import binding as B
+from stage_inputs import configs as C
+from test_oracle_sublayer import _status
 
 SOMEWHERE = ct.c_void_p(1 << 40)          # an address; nothing is read or written there
 INVALID = 1                               # hipErrorInvalidValue
@@ -48,3 +52,28 @@ def test_another_number_of_float_sums_than_there_is_room_for_is_refused():
     assert n > 1
     for expected in (1, n - 1, n + 1):
         assert f(SOMEWHERE, SOMEWHERE, ct.byref(g), SOMEWHERE, ct.byref(splits), None, ct.c_int(expected)) == (0 if expected == n else INVALID)
+
+
+@pytest.mark.parametrize("method,args", [("layernorm", (32,)), ("gated", (32, 8)), ("dropout", (0.5,))])
+@pytest.mark.parametrize("between", ["relu", "sum", "norm", "relu, sum"])
+def test_what_is_made_of_a_flattened_map_element_by_element_is_refused(method, args, between):
+    """Its elements still lie in the map's order; behind a LINEAR layer they are in order again."""
+    def layers(flattened, linear=False):
+        b = C._Builder()
+        c = 8 if flattened else 32
+        t = b.dropout(0.1, src=-1) if flattened else b.layernorm(c, src=-1)
+        t = b.flatten(src=t)
+        if "relu" in between:
+            t = b.relu(src=t)
+        if "sum" in between:
+            t = b.addl(b.linear(32, 32, src=t), t, relu=0)
+        if between == "norm":
+            t = b.bn(32, src=t)
+        if linear:
+            b.linear(32, 32, src=t)
+        getattr(b, method)(*args)
+        return b.layers
+
+    assert _status(layers(True), shape=(8, 4, 1)) == B.E_UNSUPPORTED
+    assert _status(layers(True, linear=True), shape=(8, 4, 1)) == B.E_OOM
+    assert _status(layers(False), shape=(32, 1, 1)) == B.E_OOM
