@@ -92,12 +92,14 @@ typedef enum {
  * of CONV2D / BATCHNORM2D / ADD / LINEAR.  cin/cout: channels (features for LINEAR;
  * BATCHNORM2D and LAYERNORM need cin == cout == channels of their input; GATED: channels of its
  * input and of its output).  fuse_relu of LAYERNORM, GATED and DROPOUT must be 0, and what they read
- * is no FLATTENed map of more than one pixel (E_UNSUPPORTED; put DROPOUT in front of the FLATTEN).
+ * is no FLATTENed map of more than one pixel, nor made of one by RELU, ADD or BATCHNORM2D
+ * (E_UNSUPPORTED; put DROPOUT in front of the FLATTEN).
  *
  * The layers of a transformer's feed-forward sublayer, x + DROPOUT(CONV2D 1x1(GATED(LAYERNORM(x)))),
  * act on every position (n, h, w) by itself; sequences are (channels, T, 1) tensors as for LSTM.
  * LAYERNORM: y = w (x - mean) / sqrt(var + eps) + b over the position's cin channels.
- * GATED: cout units; projections and activation are one kernel.  Both projections are kept per
+ * GATED: cout units; projections and activation are one kernel where the product fills the GPU
+ *   without splitting cin, else a second one applies the activation.  Both projections are kept per
  *   in-flight micro-batch, as floats; in the storage type, as which their gradients are stored, they
  *   need to be below 2 GiB.
  * DROPOUT: eps is the probability of an element to be dropped, 0 <= eps < 1.  The mask is computed

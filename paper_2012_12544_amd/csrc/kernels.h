@@ -212,7 +212,8 @@ hipError_t layernorm_bwd(int dt, const void *x, const void *dy, int dy_parts, co
 // ---- gated linear layer (kernels_gated.hip): h = act(x Wg^T + bg) (x Wu^T + bu), w [2F][C] with the gate rows first, bias [2F] or NULL
 // P [rows][2F] receives both projections (float), which gated_grad takes with dh to their gradients D [rows][2F] (storage type)
 enum { ACT_SIGMOID = 0, ACT_SILU = 1, ACT_GELU = 2, ACT_RELU = 3 };
-// whether the products take the bf16 MFMA kernels: conv_gather_mfma for dx = D W (wt: [C][2F]), conv_wgrad_mfma for dw += D^T x, with db
+// whether the products take the bf16 MFMA kernels: conv_gather_mfma or its raw form for dx = D W (wt: [C][2F]), rows_wgrad_mfma for dw += D^T x, with
+// db, or conv_wgrad_mfma_jobs where it shares a launch
 bool gated_mfma(int dt, int rows, int C, int F);
 size_t gated_workspace(int dt, int rows, int C, int F, bool rest, bool parts);       // of the calls here; rest, parts: as they are called
 // rest: NULL, or a second tensor whose sum with x is the layer's input; panels: w is kept in panels (GatherConv::wt_panels), for gated_mfma only

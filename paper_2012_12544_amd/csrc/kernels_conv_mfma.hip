@@ -1650,8 +1650,6 @@ size_t conv_wgrad_mfma_workspace(const ConvShape &c)
     return p.splits == 1 ? 0 : (size_t)p.splits * ((size_t)c.K * c.R * c.S * c.C + c.K) * sizeof(float);
 }
 
-// products of one tile shape that wait for their launch, and the partial sums that wait for theirs
-namespace {
 namespace {
 // The plan of a product of two matrices of `rows` rows, dw [K][C], that has to fill the chip by itself.  A large dw is written and read again for
 // every split, which is what its few rounds of the chip are weighed against: us, of a round of 512 blocks of 256 x 128 (or 256 of 256 x 256, 512
@@ -1688,8 +1686,8 @@ WgradPlan rows_plan(const ConvShape &c)
     }
     return p;
 }
-}  // namespace
 
+// products of one tile shape that wait for their launch, and the partial sums that wait for theirs
 struct WgradBatch {
     WgradGroup g;
     SplitkGroup r;

@@ -501,8 +501,8 @@ __global__ __launch_bounds__(TPB) void k_gated_grad(const T *__restrict__ dh, co
 // 16-byte chunks is applied by choosing which one a lane fetches).  Fragments are read one step of 32 bytes ahead of the products that
 // need them; the barrier that publishes the next tile lies before a tile's last products, when every wave has all of the tile in registers, and
 // the slot is filled again at once.
-// 8192 rows, 4096->11008 of bf16, us (two products of 739 GFLOP each): MM_FORWARD 1310, 721 MB of projections and 180 of h among them, the gather
-// kernel alone on as large a product 1316.
+// 8192 rows, 4096->11008 of bf16, us (1478 GFLOP), launched by itself time after time: MM_FORWARD 1310, 721 MB of projections and 180 of h among them, the
+// gather kernel alone on as large a product 1316.  Between the other kernels of a mini-batch it takes 1440 to 1452.
 // `rest`: x is the sum of two tensors; K is walked twice with the same weights.
 enum { MM_FORWARD, MM_PROJECT, MM_DX };
 struct MmArgs {
@@ -758,7 +758,8 @@ static hipError_t launch_mm_tile(MmArgs a, hipStream_t s)
 static long long mm_tiles(int rows, long long weight_rows, int tile_p, int tile_w) { return (rows + tile_p - 1) / tile_p * ((weight_rows + tile_w - 1) / tile_w); }
 
 // The tile whose rounds of the chip are the least work: a block of 256 x 256 or 256 x 128 to a unit, or two of 128 x 128, whose products
-// take 1.05 and 1.15 times as long each (4096 rows, 2048->5632, us: 704 of the first, three rounds, 204; 2816 of the last, six, 234)
+// take 1.05 and 1.15 times as long each (4096 rows, 2048->5632, us, by itself: 704 of the first, three rounds, 204; 2816 of the last, six, 234; the first
+// between the other kernels of a mini-batch 226 to 229)
 template <class T, int MODE> static hipError_t launch_mm(MmArgs a, hipStream_t s)
 {
     const long long w = MODE == MM_FORWARD ? 2ll * a.N : a.N;

@@ -229,7 +229,7 @@ constexpr int kGammaAt = 64;
 // NT threads, NT / G groups whose columns' sums meet in LDS at the end.  (In three rounds of halves, with the sums of a thread's columns
 // side by side, 3200 rows of 1024 bf16 took 15.8 us instead of 11.7.)
 // A row is taken from its packed values twice, for the sums and for dx: kept as floats in between, two rows of them, it cost twice
-// the registers, and rows of 8192 spilled (142 MB x 2 forward, 2 x 403 MB backward: 341 us of 165 at the copy's rate).
+// the registers, and rows of 8192 spilled (16384 of them, bf16: 341 us where the 805 MB of x, dy and dx take 155 at the copy's rate).
 template <class T, int NV, int G, int NT, bool TAIL, bool PARTS, bool EPI>
 __global__ __launch_bounds__(NT, NV == 1 || (NV == 2 && !EPI) ? 4 : 2) void k_layernorm_bwd(BwdArgs<T> p)
 {

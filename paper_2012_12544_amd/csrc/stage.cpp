@@ -62,7 +62,7 @@ struct Tensor {
     // Gradient with two sources, a residual ADD (processed first in backward) and a conv or layer norm: the ADD's share is not
     // copied, the other's input-gradient epilogue reads it where it lies (GradEpi::accum_from).  Layer index of
     // that conv or layer norm, or -1.
-    int fanout_conv = -1;
+    int fanout_to = -1;
     // Gradient of a layer norm's output that only a GATED reads, or of a GATED's that only a 1x1 convolution does: the float sums of the
     // product that makes it, so many of them, instead of their rounded total.  It is read by one kernel, which forms a product's operand or
     // a row's sums, and every rounding on the way through the sublayer is one more of its gradients' errors: 2-norm of dW and
@@ -810,7 +810,7 @@ struct BwdCtx {
     const int32_t *labels;
     const void *dy_nchw = nullptr;       // caller's NCHW gradient, read where it lies by the max-pool that is the last layer
     std::vector<char> written;
-    std::vector<const void *> pending;   // per tensor: an ADD's share of its gradient that the tensor's conv will add (fanout_conv)
+    std::vector<const void *> pending;   // per tensor: an ADD's share of its gradient that another of its readers will add (fanout_to)
     bool profiling = false;        // profiler: run every kernel of the layer now (no deferral)
     int bn_sums_ready = -1;        // batch-norm layer whose backward sums the last conv left in the workspace
     bool dx_over_dy = false;       // the caller's dx overlaps dy_direct
@@ -1011,7 +1011,7 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
         double bytes = 0.0;
         if (a_grad && st->tensors[A.root].galias == L.o) {
             c.written[A.root] = 1;
-        } else if (a_grad && st->tensors[A.root].fanout_conv >= 0 && !c.profiling && !c.written[A.root]) {
+        } else if (a_grad && st->tensors[A.root].fanout_to >= 0 && !c.profiling && !c.written[A.root]) {
             c.pending[A.root] = g;                        // taken by that conv's input-gradient epilogue
             c.written[A.root] = 1;
         } else if (a_grad) {
@@ -1022,7 +1022,7 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
         const int rb = st->tensors[L.b].root;
         if (st->tensors[rb].need_grad && st->tensors[rb].galias == L.o) {
             c.written[rb] = 1;
-        } else if (st->tensors[rb].need_grad && st->tensors[rb].fanout_conv >= 0 && !c.profiling && !c.written[rb]) {
+        } else if (st->tensors[rb].need_grad && st->tensors[rb].fanout_to >= 0 && !c.profiling && !c.written[rb]) {
             c.pending[rb] = g;
             c.written[rb] = 1;
         } else if (st->tensors[rb].need_grad) {
@@ -1197,7 +1197,7 @@ bool dx_may_lie_over_dy(const bapipe_stage *st, bool same)
         if (reads && changed) return false;
         for (int t : {L.a, L.b}) {
             if (t < 0 || !st->tensors[root(t)].need_grad) continue;
-            const int taker = st->tensors[root(t)].fanout_conv;
+            const int taker = st->tensors[root(t)].fanout_to;
             if (kind == BAPIPE_ADD && taker >= 0) {
                 if (reads) reads_late[taker] = 1;
                 continue;
@@ -1373,7 +1373,6 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
             if (d.kh < BAPIPE_GATE_SIGMOID || d.kh > BAPIPE_GATE_RELU) return create_fail(BAPIPE_E_INVALID, "layer %d: unknown activation %d", i, d.kh);
             if (A.C != d.cin) return create_fail(BAPIPE_E_SHAPE, "layer %d: cin=%d but input has %d channels", i, d.cin, A.C);
             if (d.fuse_relu) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: a gated layer has no fused ReLU", i);
-            if (A.Cp != A.C) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: gated input with padded channels", i);
             if ((size_t)micro_batch * A.H * A.W * 2 * d.cout * es >= ((size_t)1 << 31))
                 return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: projections of 2 GiB or more per micro-batch", i);
             O.C = d.cout; O.H = A.H; O.W = A.W;
@@ -1746,11 +1745,11 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         const int ic = T.consumers[0], ia = T.consumers[1];
         const Layer &Lc = st->layers[ic], &La = st->layers[ia];
         if (ic >= ia || La.d.kind != BAPIPE_ADD || Lc.a != t || (La.a != t && La.b != t)) continue;
-        if (Lc.d.kind == BAPIPE_LAYERNORM) T.fanout_conv = ic;
+        if (Lc.d.kind == BAPIPE_LAYERNORM) T.fanout_to = ic;
         if (Lc.d.kind != BAPIPE_CONV2D || st->dt != DT_BF16) continue;
         const GatherConv dg = dgrad_geom(st, Lc);
         if (!use_mfma_gather(st, dg) || conv3x3_halo_supported(dg) || Lc.bnb_chunks) continue;
-        T.fanout_conv = ic;
+        T.fanout_to = ic;
     }
     st->dx_at_dy = dx_may_lie_over_dy(st, true);
     st->dx_across_dy = dx_may_lie_over_dy(st, false);
@@ -1950,7 +1949,7 @@ int bapipe_stage_backward(bapipe_stage_t *st, int mb_id, const void *dy_dev_or_l
         if (rc != BAPIPE_OK) return rc;
     }
     for (const void *p : c.pending)
-        if (p) return st->fail(BAPIPE_E_DEVICE, "backward: a residual gradient was left for a conv that never took it");
+        if (p) return st->fail(BAPIPE_E_DEVICE, "backward: a residual gradient was left for a layer that never took it");
     if (want_dx && !c.dx_direct) {
         if ((nhwc || In.H * In.W == 1) && In.Cp == In.C)
             HIPCHK(hipMemcpyAsync(dx_dev, st->gptr(0), In.bytes(), hipMemcpyDeviceToDevice, s));
