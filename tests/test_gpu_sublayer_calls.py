@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from gpu_harness import DEV, GpuStage, compare_minibatch, stage_io, tdtype
+from gpu_harness import DEV, GpuStage, compare_minibatch, gpu_minibatch, stage_io, tdtype
 from oracle import ops
 from oracle.stage import OracleStage
 from paper_2012_12544_amd import binding as B
@@ -51,6 +51,21 @@ def test_positions_in_the_batch_or_in_a_sequence_are_the_same(kw):
         out.append(got)
     for a, b in zip(*out):
         assert np.array_equal(a, b) and np.any(a)
+
+
+@pytest.mark.parametrize("kw", [dict(c=64, units=320, micro_batch=70), dict(c=96, units=352, micro_batch=500), dict(c=160, units=640, micro_batch=1500),
+                                dict(c=1024, units=2048, micro_batch=130), dict(c=72, units=328, micro_batch=333, act=C.GATE_RELU)])
+def test_sublayer_of_some_maps_of_one_pixel(kw):
+    """Too few tiles for that kernel: gradients between the layers are float sums of products whose filters are in panels."""
+    compare_minibatch(sublayer(seq=1, n_micro=2, stage_index=1, n_stages=1, **kw))
+
+
+def test_a_large_sublayer_on_the_static_workspace():
+    """The same bits as on the stage's own."""
+    st = sublayer(c=1024, units=4096, seq=512, micro_batch=4, n_micro=2, stage_index=1, n_stages=2)
+    ref, got = gpu_minibatch(st), gpu_minibatch(st, static=True)
+    for k in ref:
+        assert np.array_equal(got[k], ref[k]) and np.any(ref[k]), k
 
 
 # ------------------------------------------------------------------------------ what is not finite
