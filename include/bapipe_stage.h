@@ -37,7 +37,7 @@
  *    sequence-to-sequence workload, Sec. IV-A; hidden size cout, zero initial state, gates in
  *    the order input, forget, candidate, output): w is [4*cout][cin+cout], row q*cout + j =
  *    gate q of unit j, first the cin input weights, then the cout recurrent ones; b is
- *    [4*cout] (the sum of PyTorch's two bias vectors).  Layer norm: w = gamma, b = beta.  Gated:
+ *    [4*cout] (the sum of PyTorch's two bias vectors).  Layer norm: w = gamma, b = beta.  Rotary: w = gains.  Gated:
  *    w is [2*cout][cin], the cout rows of the gate, to which the activation applies, before the
  *    cout rows of the other projection; b is [2*cout].
  */
@@ -76,7 +76,9 @@ typedef enum {
     BAPIPE_LSTM = 9,         /* LSTM over the H axis of a (cin, T, 1) tensor -> (cout, T, 1) */
     BAPIPE_LAYERNORM = 10,   /* over the channels of each position, biased variance         */
     BAPIPE_GATED = 11,       /* act(x Wg^T + bg) * (x Wu^T + bu) at each position           */
-    BAPIPE_DROPOUT = 12      /* y = x / (1 - eps), or 0 with probability eps                */
+    BAPIPE_DROPOUT = 12,     /* y = x / (1 - eps), or 0 with probability eps                */
+    BAPIPE_ROTARY = 13,      /* query and key heads turned by their position, norms before  */
+    BAPIPE_ATTENTION = 14    /* softmax(q k^T / sqrt(d)) v of every query head              */
 } bapipe_layer_kind_t;
 
 /* Activation of BAPIPE_GATED, in its descriptor's kh. */
@@ -87,12 +89,19 @@ typedef enum {
     BAPIPE_GATE_RELU = 3     /* max(g, 0), NaN of NaN                                       */
 } bapipe_gate_t;
 
+/* Which channels of a head turn together, in a ROTARY's stride: j and j + pad / 2, or 2 j and 2 j + 1. */
+typedef enum { BAPIPE_ROTARY_HALVES = 0, BAPIPE_ROTARY_PAIRS = 1 } bapipe_rotary_layout_t;
+
+/* Keys that a position sees, in an ATTENTION's stride: all of its sequence, those up to itself, or a span of its
+ * own (bapipe_stage_set_spans: documents, a prefix, a window, padding). */
+typedef enum { BAPIPE_MASK_NONE = 0, BAPIPE_MASK_CAUSAL = 1, BAPIPE_MASK_SPANS = 2 } bapipe_mask_t;
+
 /* One layer of the stage.  src0/src1: index of the producing layer in the list, -1 = the
  * stage input; producers must precede consumers.  fuse_relu applies max(.,0) to the output
  * of CONV2D / BATCHNORM2D / ADD / LINEAR.  cin/cout: channels (features for LINEAR;
  * BATCHNORM2D and LAYERNORM need cin == cout == channels of their input; GATED: channels of its
- * input and of its output).  fuse_relu of LAYERNORM, GATED and DROPOUT must be 0, and what they read
- * is no FLATTENed map of more than one pixel, nor made of one by RELU, ADD or BATCHNORM2D
+ * input and of its output).  fuse_relu of LAYERNORM, GATED, DROPOUT, ROTARY and ATTENTION must be 0, and what they
+ * read is no FLATTENed map of more than one pixel, nor made of one by RELU, ADD or BATCHNORM2D
  * (E_UNSUPPORTED; put DROPOUT in front of the FLATTEN).
  *
  * The layers of a transformer's feed-forward sublayer, x + DROPOUT(CONV2D 1x1(GATED(LAYERNORM(x)))),
@@ -106,7 +115,23 @@ typedef enum {
  *   where it is used and never stored.  Element e = ((n H + h) W + w) C + c of micro-batch m is
  *   dropped if word e mod 4 of Philox4x32-10 is below 2^32 eps (rounded to nearest); key: the seed,
  *   low word first; counter: e / 4, layer index + 65536 (stage_index - 1), m, number of the
- *   mini-batch.  See bapipe_stage_set_dropout.  A stage that only evaluates is created with eps 0. */
+ *   mini-batch.  See bapipe_stage_set_dropout.  A stage that only evaluates is created with eps 0.
+ *
+ * Those of its attention sublayer, x + CONV2D 1x1(ATTENTION(ROTARY(CONV2D 1x1(LAYERNORM(x))))), work on
+ * (channels, T, 1) tensors whose channels hold kh query heads, then kw key heads, then kw value heads of
+ * d = cin / (kh + 2 kw) <= 256 channels each (wider ones: E_UNSUPPORTED); query heads h kh / kw to
+ * (h + 1) kh / kw - 1 share key and value head h.
+ * ROTARY: cout = cin; the first pad channels (even, 0 to d) of query and key heads turn in pairs as stride says,
+ *   channels (a, b) of pair j at position t of its sequence to (a cos - b sin, a sin + b cos) of the angle
+ *   t base^(-2 j / pad); see bapipe_stage_set_rotary.  has_bias = 1: each query and key head is first divided by its root mean
+ *   square, sqrt(mean(x^2) + eps), and multiplied by gains, w [2][d]: of query heads, of key heads, one at create.
+ *   has_bias = 0: eps must be 0, no parameters.  Value heads pass unchanged.
+ * ATTENTION: cout = kh d.  Score of query i and key j: q_i k_j / sqrt(d); with eps > 0 capped to eps tanh(score / eps);
+ *   with pad > 0 less 2^(-pad (h + 1) / kh) |i - j| in query head h (pad up to 64).  Softmax over the keys that stride
+ *   lets the position see; one that sees none gets zeros and gives no gradients.  has_bias must be 0.  What a position holds that no
+ *   position of the sequence sees has no effect on others, NaN or infinity included; of one that some see and others do not, NaN may reach them.
+ *   In bf16 stages probabilities and their gradients are rounded to bf16 as operands of the next product; scores, sums and
+ *   the softmax stay in float. */
 typedef struct {
     int32_t kind;
     int32_t cin, cout;
@@ -238,6 +263,26 @@ int bapipe_stage_step(bapipe_stage_t *st, float lr);
  * mini-batches (after create or step). */
 int bapipe_stage_set_dropout(bapipe_stage_t *st, uint64_t seed, uint32_t mini_batch);
 
+/* Spans of the ATTENTION layers with BAPIPE_MASK_SPANS for micro-batch mb_id, the next to be forwarded (E_ORDER
+ * otherwise, and of a forward without): int32 [micro_batch][T][2] on the device, for every position the first key it sees and the
+ * end behind the last; first >= end: none.  Values are clamped to [0, T].  All such layers of a stage share them and have
+ * one T (else create returns E_SHAPE).  Read by kernels of the forward pass, which keep a copy for the backward pass:
+ * spans_dev stays untouched until forward has run.  E_INVALID: NULL, not aligned to 4 bytes, no such layer. */
+int bapipe_stage_set_spans(bapipe_stage_t *st, int mb_id, const int32_t *spans_dev);
+
+/* Angles of a ROTARY layer; after create base 10000, factor 1, original_length 0, magnitude 1, first_position 0.
+ * Frequency of pair j of r turning channels: f = base^(-2 j / r).  original_length 0: f / factor.  Else, for contexts longer than
+ * the original_length L that frequencies were made for, those that turn high_turns times or more over L (L f / 2 pi) stay, those
+ * that turn low_turns times or less become f / factor, and between f (s + (1 - s) / factor), s = (turns - low) / (high - low).
+ * Sines and cosines, of angles in double, are multiplied by magnitude.  The sequences' first position is
+ * first_position, 0 to 2^40.  Enqueues on opts->hip_stream.  E_INVALID: not a ROTARY, values out of range; E_ORDER unless
+ * between mini-batches. */
+typedef struct {
+    double base, factor, original_length, low_turns, high_turns, magnitude;
+    int64_t first_position;
+} bapipe_rotary_t;
+int bapipe_stage_set_rotary(bapipe_stage_t *st, int layer, const bapipe_rotary_t *angles);
+
 /* Per-layer profile (Sec. III-A "DNN profile"; Sec. III-B-2 asks for it per batch size, which
  * is the micro_batch the stage was created with).  Runs each layer's forward and backward
  * kernels in isolation on scratch data, `warmup` untimed then `iters` timed repetitions,
@@ -303,8 +348,9 @@ enum {
     BAPIPE_KC_CONV_DIRECT = 2,      /* vector-ALU convolution (fp32 stages, odd channels) */
     BAPIPE_KC_POOL = 3,
     BAPIPE_KC_BATCHNORM = 4,        /* and layer norm                                        */
-    BAPIPE_KC_ELEMENTWISE = 5,      /* ReLU, add, dropout, gradient copies, bias-gradient sums, gradients of GATED's projections */
-    BAPIPE_KC_COUNT = 6
+    BAPIPE_KC_ELEMENTWISE = 5,      /* ReLU, add, dropout, rotary positions, gradient copies, bias-gradient sums, gradients of GATED's projections */
+    BAPIPE_KC_ATTENTION = 6,        /* FLOP of scored pairs: all, or half of them with a causal mask; with spans as if all were */
+    BAPIPE_KC_COUNT = 7
 };
 int bapipe_stage_kernel_timing(bapipe_stage_t *st, int kernel_class);
 int bapipe_stage_kernel_timing_read(bapipe_stage_t *st, double *total_ms, uint64_t *launches,

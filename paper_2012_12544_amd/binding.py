@@ -15,8 +15,10 @@ LIB_PATH = os.path.join(_HERE, "libbapipe_stage.so")
 OK, E_INVALID, E_SHAPE, E_ORDER, E_OOM, E_DEVICE, E_UNSUPPORTED = range(7)
 STATUS_NAMES = ["OK", "E_INVALID", "E_SHAPE", "E_ORDER", "E_OOM", "E_DEVICE", "E_UNSUPPORTED"]
 (CONV2D, RELU, MAXPOOL2D, BATCHNORM2D, ADD, FLATTEN, LINEAR, SOFTMAX_XENT, AVGPOOL2D, LSTM, LAYERNORM, GATED,
- DROPOUT) = range(13)
+ DROPOUT, ROTARY, ATTENTION) = range(15)
 GATE_SIGMOID, GATE_SILU, GATE_GELU, GATE_RELU = range(4)
+ROTARY_HALVES, ROTARY_PAIRS = range(2)
+MASK_NONE, MASK_CAUSAL, MASK_SPANS = range(3)
 FP32, BF16 = 0, 1
 NCHW, NHWC = 0, 1
 SCHED_1F1B, SCHED_1F1B_SO = 0, 1
@@ -25,7 +27,7 @@ STATIC_SCRATCH_BYTES = 64 << 20
 EXPORTS = [
     "bapipe_stage_create", "bapipe_stage_forward", "bapipe_stage_backward", "bapipe_stage_backward_static",
     "bapipe_stage_set_streams",
-    "bapipe_stage_step", "bapipe_stage_set_dropout",
+    "bapipe_stage_step", "bapipe_stage_set_dropout", "bapipe_stage_set_spans", "bapipe_stage_set_rotary",
     "bapipe_profile_layers", "bapipe_profile_sweep", "bapipe_stage_set_params", "bapipe_stage_get_params",
     "bapipe_stage_get_grads", "bapipe_stage_get_pool_indices", "bapipe_stage_get_loss",
     "bapipe_stage_stash_bytes", "bapipe_last_error", "bapipe_stage_destroy",
@@ -33,7 +35,7 @@ EXPORTS = [
     "bapipe_schedule_cost", "bapipe_schedule_choose", "bapipe_partition",
 ]
 PLAN_1F1B_AS, PLAN_FBP_AS, PLAN_1F1B_SNO, PLAN_1F1B_SO = range(4)
-KC_CONV_GATHER_MFMA, KC_CONV_WGRAD_MFMA, KC_CONV_DIRECT, KC_POOL, KC_BATCHNORM, KC_ELEMENTWISE = range(6)
+KC_CONV_GATHER_MFMA, KC_CONV_WGRAD_MFMA, KC_CONV_DIRECT, KC_POOL, KC_BATCHNORM, KC_ELEMENTWISE, KC_ATTENTION = range(7)
 
 
 class LayerDesc(ct.Structure):
@@ -56,6 +58,11 @@ class StageOpts(ct.Structure):
                 ("io_layout", ct.c_int32), ("stage_index", ct.c_int32), ("n_stages", ct.c_int32),
                 ("schedule", ct.c_int32), ("need_input_grad", ct.c_int32), ("loss_scale", ct.c_float),
                 ("hip_stream", ct.c_void_p), ("mem", Allocator)]
+
+
+class Rotary(ct.Structure):
+    _fields_ = [("base", ct.c_double), ("factor", ct.c_double), ("original_length", ct.c_double), ("low_turns", ct.c_double),
+                ("high_turns", ct.c_double), ("magnitude", ct.c_double), ("first_position", ct.c_int64)]
 
 
 class LayerProfile(ct.Structure):
@@ -89,6 +96,8 @@ def load():
     lib.bapipe_stage_set_streams.argtypes = [vp, vp, vp]
     lib.bapipe_stage_step.argtypes = [vp, ct.c_float]
     lib.bapipe_stage_set_dropout.argtypes = [vp, ct.c_uint64, ct.c_uint32]
+    lib.bapipe_stage_set_spans.argtypes = [vp, i32, vp]
+    lib.bapipe_stage_set_rotary.argtypes = [vp, i32, ct.POINTER(Rotary)]
     lib.bapipe_profile_layers.argtypes = [vp, i32, i32, ct.POINTER(LayerProfile), i32, ct.POINTER(i32)]
     fp = ct.POINTER(ct.c_float)
     lib.bapipe_stage_set_params.argtypes = [vp, i32, fp, fp]
@@ -191,6 +200,15 @@ def bapipe_stage_step(h, lr):
 def bapipe_stage_set_dropout(h, seed, mini_batch=0):
     """Seed (taken modulo 2^64) of the DROPOUT layers' masks and number of the coming mini-batch (modulo 2^32)."""
     _check(load().bapipe_stage_set_dropout(h, seed % (1 << 64), mini_batch % (1 << 32)), h)
+
+
+def bapipe_stage_set_spans(h, mb_id, spans_ptr):
+    _check(load().bapipe_stage_set_spans(h, mb_id, spans_ptr), h)
+
+
+def bapipe_stage_set_rotary(h, layer, base=10000.0, factor=1.0, original_length=0.0, low_turns=0.0, high_turns=0.0, magnitude=1.0, first_position=0):
+    a = Rotary(base, factor, original_length, low_turns, high_turns, magnitude, first_position)
+    _check(load().bapipe_stage_set_rotary(h, layer, ct.byref(a)), h)
 
 
 def bapipe_profile_layers(h, warmup, iters, n_layers):

@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbapipe_stage.so")
 SOURCES = ["stage.cpp", "plan.cpp", "kernels_elementwise.hip", "kernels_conv_direct.hip", "kernels_conv_mfma.hip",
-           "kernels_conv_halo.hip", "kernels_lstm.hip", "kernels_layernorm.hip", "kernels_gated.hip", "kernels_dropout.hip", "probe_peaks.hip"]
+           "kernels_conv_halo.hip", "kernels_lstm.hip", "kernels_layernorm.hip", "kernels_gated.hip", "kernels_dropout.hip", "kernels_rotary.hip",
+           "kernels_attention_fwd.hip", "kernels_attention_dq.hip", "kernels_attention_dkv.hip", "probe_peaks.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]
@@ -29,7 +30,7 @@ def _compile(src):
 
 def build(verbose=False):
     os.makedirs(OBJ, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         objs = list(ex.map(_compile, SOURCES))
     cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objs
     subprocess.check_call(cmd)

@@ -1,0 +1,371 @@
+// Pieces shared by the attention kernels (kernels_attention_*.hip).
+//
+// One wave owns 32 rows of one axis (queries in the forward pass and for dq, keys for dk and dv), one to a lane of either half, whose
+// values stay in registers as the right operand of the 32x32 MFMAs; the other axis streams through LDS in tiles.  With streamed rows
+// as the left operand a product of both comes out with the owned row in the lane and streamed rows in the registers:
+//     register i of lane l: owned row l & 31, streamed row 8 (i / 4) + 4 (l / 32) + i % 4 of the tile's 32.
+// Sums over streamed rows are sums over registers, with one exchange between the halves.  And the next product, which sums over the
+// streamed rows, finds its right operand in those registers as they are: the order of a product's summands is free, so its left operand
+// is read with the same order of rows (bf16: transposing LDS reads of four rows each; float: single words).
+// Nothing of a score's size ever leaves the registers.
+#pragma once
+#include <type_traits>
+
+#include "kernels.h"
+#include "mfma_common.h"
+
+namespace bapipe {
+
+constexpr int AT_WAVES = 4, AT_TPB = 64 * AT_WAVES, AT_ROWS = 32 * AT_WAVES;      // rows that a block owns
+
+// A tile of rows of DP elements in LDS, in groups of 64 bytes of every row: group after group, each of all rows.  The four 16-byte chunks of a
+// row in a group change places with the row / 4, so that both kinds of reads meet each bank once - 16 rows at one chunk (row operands),
+// four rows at four chunks (transposing reads) - and everything but two lane addresses of either kind is an immediate offset.  (With whole
+// rows one after the other and a chunk's place XORed with the row every step and column tile took an address register of its own,
+// and the kernel for dk and dv spilled 106.)  Loads bring 64 bytes of 16 rows at a time.
+// R: rows, 0 for what two operands, twice, in 128 KB leave
+struct half_t {
+    uint16_t v;
+};
+template <class T, int DP, int R = 0> struct AtTile {
+    static constexpr int EPC = 16 / (int)sizeof(T);                   // elements of a chunk
+    static constexpr int CH = DP / EPC, RB = DP * (int)sizeof(T);     // chunks, bytes of a row
+    static constexpr int STEPS = CH / 2;                              // a step of a row product takes two chunks, one for each half
+    static constexpr int ROWS = R ? R : RB <= 512 ? 64 : 32;
+    static constexpr int BYTES = ROWS * RB;
+    static constexpr int ISSUES = ROWS * CH / AT_TPB;                 // 16-byte loads of a thread for a tile
+    static_assert(ROWS * CH % AT_TPB == 0, "");
+    static __device__ __forceinline__ int at(int group, int row, int chunk) { return (group * ROWS + row) * 64 + ((chunk ^ ((row >> 2) & 3)) << 4); }
+    // row and chunk of the i-th 16 bytes
+    static __device__ __forceinline__ int row_of(int i) { return i / 4 % ROWS; }
+    static __device__ __forceinline__ int chunk_of(int i) { return i / (4 * ROWS) * 4 + ((i & 3) ^ ((row_of(i) >> 2) & 3)); }
+};
+
+// acc += streamed rows x owned rows over one step of their elements
+template <class T> __device__ __forceinline__ void at_mma(f32x16_t &acc, chunk16 a, chunk16 b)
+{
+    typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+    if constexpr (std::is_same<T, half_t>::value)
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), acc, 0, 0, 0);
+    else if constexpr (sizeof(T) == 2) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_frag(a), as_frag(b), acc, 0, 0, 0);
+    else
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), acc, 0, 0, 0);
+}
+
+// acc = 32 streamed rows from row0 of the tile x owned rows
+template <class T, class Tile> __device__ __forceinline__ f32x16_t at_rows(const unsigned char *tile, int row0, const chunk16 *own, int lane)
+{
+    const int row = lane & 31, h = lane >> 5;
+    f32x16_t acc = {};
+#pragma unroll
+    for (int c = 0; c < Tile::STEPS; ++c)
+        at_mma<T>(acc, *(const chunk16 *)(tile + Tile::at(0, row, 2 * (c & 1) + h) + ((c >> 1) * Tile::ROWS + row0) * 64), own[c]);
+    return acc;
+}
+
+// The right operand of a product that sums over 32 streamed rows: the registers of at_rows, in the storage type
+template <class T> struct AtWeights {
+    float v[16];
+    __device__ __forceinline__ explicit AtWeights(const float (&x)[16])
+    {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = x[i];
+    }
+};
+template <> struct AtWeights<bf16_t> {
+    uint32_t v[8];
+    __device__ __forceinline__ explicit AtWeights(const float (&x)[16])
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+    }
+};
+
+// acc[t][element 32 (t0 + t) + register's row][owned row] += sum over the 32 streamed rows from row0 of their elements x weights
+template <class T, class Tile, int ND>
+__device__ __forceinline__ void at_columns(f32x16_t (&acc)[ND], const unsigned char *tile, int row0, int t0, const AtWeights<T> &w, int lane)
+{
+    const int h = lane >> 5;
+    if constexpr (sizeof(T) == 2) {
+        typedef __attribute__((address_space(3))) s16x4_t lds_v4;
+        typedef short s16x8_t __attribute__((ext_vector_type(8)));
+        const int sl = lane & 15, chunk = 2 * ((lane >> 4) & 1) + ((sl & 3) >> 1), row = 4 * h + (sl >> 2);
+        const unsigned char *from = tile + t0 * (Tile::ROWS * 64);
+        const int lo_at = Tile::at(0, row, chunk) + 8 * (sl & 1), hi_at = Tile::at(0, row + 8, chunk) + 8 * (sl & 1);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const chunk16 b = {w.v[4 * c], w.v[4 * c + 1], w.v[4 * c + 2], w.v[4 * c + 3]};
+#pragma unroll
+            for (int t = 0; t < ND; ++t) {
+                const int off = (t * Tile::ROWS + row0 + 16 * c) * 64;
+                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)(from + lo_at + off));
+                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)(from + hi_at + off));
+                const s16x8_t a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), as_frag(b), acc[t], 0, 0, 0);
+            }
+        }
+    } else {
+        const int e = lane & 31;
+        const unsigned char *from = tile + 2 * t0 * (Tile::ROWS * 64);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int at = Tile::at(e >> 4, 8 * ((i >> 2) & 1) + 4 * h, (e >> 2) & 3) + 4 * (e & 3);
+#pragma unroll
+            for (int t = 0; t < ND; ++t) {
+                const float a = *(const float *)(from + at + (2 * t * Tile::ROWS + row0 + 16 * (i >> 3) + (i & 3)) * 64);
+                acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.v[i], acc[t], 0, 0, 0);
+            }
+        }
+    }
+}
+
+// The chunks of an owned row, which lies at `row` (NULL: zeros) with d elements
+template <class T> __device__ __forceinline__ T at_zero()
+{
+    T z;
+    __builtin_memset(&z, 0, sizeof z);
+    return z;
+}
+template <class T, int DP, bool VEC> __device__ __forceinline__ void at_own(chunk16 *own, const T *row, int d, int lane)
+{
+    typedef AtTile<T, DP> Tile;
+    constexpr int EPC = Tile::EPC;
+#pragma unroll
+    for (int c = 0; c < Tile::STEPS; ++c) {
+        const int e0 = (2 * c + (lane >> 5)) * EPC;
+        own[c] = chunk16{0, 0, 0, 0};
+        if constexpr (VEC) {
+            if (row && e0 < d) own[c] = *(const chunk16 *)(row + e0);
+        } else {
+            vec_t<T, EPC> v;
+#pragma unroll
+            for (int j = 0; j < EPC; ++j) v.e[j] = row && e0 + j < d ? row[e0 + j] : at_zero<T>();
+            own[c] = __builtin_bit_cast(chunk16, v);
+        }
+    }
+}
+
+// dma16 of a resource that differs from tile to tile: it may have been written by a vector instruction (a lane read back from a spilled
+// scalar) just before, which a load has to be five states behind of, and the compiler counts none inside of assembly
+__device__ __forceinline__ void at_dma16(__amdgpu_buffer_rsrc_t rsrc, unsigned lds_addr, unsigned voffset)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_addr), "v"(voffset), "s"(rsrc));
+}
+
+// Fills tiles from rows of d elements, `stride` elements apart.  VEC: d a multiple of a chunk and 16-byte aligned rows; asynchronous,
+// complete after WAIT_VMCNT(0) and a barrier.  Rows that are not there, and what is behind d, are zeros: zero times zero is what the products
+// see of them, whatever memory holds.
+template <class T, int DP, bool VEC, int R = 0> struct AtStream {
+    typedef AtTile<T, DP, R> Tile;
+    static constexpr int STEP = AT_TPB / Tile::ROWS;      // chunks of a row that the block loads at once
+    unsigned voff = 0;       // of the lane's first chunk
+    int chunk = 0;
+    __device__ __forceinline__ AtStream(int stride, int tid)
+    {
+        if constexpr (VEC) {
+            static_assert(STEP % 4 == 0, "");
+            const int row = Tile::row_of(tid);
+            chunk = Tile::chunk_of(tid);
+            const long long at = (long long)row * stride * (int)sizeof(T) + chunk * 16;
+            voff = at < (1ll << 31) ? (unsigned)at : 0x80000000u;      // no row of a tensor lies behind 2 GiB
+        }
+    }
+    // from: the tile's first row; rows: how many there are from it on
+    __device__ __forceinline__ void fill(unsigned char *tile, const lds_addr_of &lds, const T *from, int rows, int stride, int d, int tid) const
+    {
+        if constexpr (VEC) {
+            const int n = rows < Tile::ROWS ? rows : Tile::ROWS;
+            const int bytes = n > 0 ? (int)(((long long)(n - 1) * stride + d) * (int)sizeof(T)) : 0;
+            const uint64_t place = (uint64_t)(uintptr_t)from;
+            const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)place), high = __builtin_amdgcn_readfirstlane((uint32_t)(place >> 32));
+            const __amdgpu_buffer_rsrc_t rsrc =
+                __builtin_amdgcn_make_buffer_rsrc((void *)(((uint64_t)high << 32) | low), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+            unsigned at = voff;
+            asm volatile("" : "+v"(at));        // else every load's address is kept in a register of its own
+#pragma unroll
+            for (int i = 0; i < Tile::ISSUES; ++i)
+                at_dma16(rsrc, lds(tile + (i * AT_TPB + (tid & ~63)) * 16), (chunk + i * STEP) * Tile::EPC < d ? at + i * STEP * 16 : 0x80000000u);
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < Tile::ISSUES; ++i) {
+                const int at = i * AT_TPB + tid, row = Tile::row_of(at), e0 = Tile::chunk_of(at) * Tile::EPC;
+                vec_t<T, Tile::EPC> v;
+#pragma unroll
+                for (int j = 0; j < Tile::EPC; ++j) v.e[j] = row < rows && e0 + j < d ? from[(size_t)row * stride + e0 + j] : at_zero<T>();
+                *(chunk16 *)(tile + at * 16) = __builtin_bit_cast(chunk16, v);
+            }
+        }
+    }
+};
+
+// the other half's value of an owned row, combined with this one's
+__device__ __forceinline__ float at_halves_max(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
+__device__ __forceinline__ float at_halves_sum(float v) { return v + __shfl_xor(v, 32, 64); }
+
+// What is done to a score on its way to the softmax, in units of log 2
+constexpr float kLog2e = 1.44269504088896341f;
+struct AtScore {
+    float scale;         // log2(e) / sqrt(d)
+    float cap, per_cap;  // log2(e) times the cap, and one over that; 0: none
+    float fall;          // log2(e) times the head's slope; 0: no bias
+};
+__device__ __forceinline__ AtScore at_score(const AttnShape &a, int head)
+{
+    AtScore s;
+    s.scale = a.scale * kLog2e;
+    s.cap = a.cap * kLog2e;
+    s.per_cap = a.cap > 0.0f ? 1.0f / s.cap : 0.0f;
+    s.fall = a.bias ? kLog2e * exp2f(-(float)a.bias * (float)(head + 1) / (float)a.heads) : 0.0f;
+    s.fall = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s.fall)));
+    s.cap = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s.cap)));
+    return s;
+}
+// tanh: near zero, where the difference would cancel, its series (off by less than 2^-21 of it at 1/4); float stages call the function
+template <class T> __device__ __forceinline__ float at_tanh(float x)
+{
+    if constexpr (sizeof(T) == 4) return tanhf(x);
+    const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.0f * kLog2e * x)), q = x * x;
+    const float near = x * (1.0f + q * (-1.0f / 3.0f + q * (2.0f / 15.0f - q * (17.0f / 315.0f))));
+    return fabsf(x) < 0.25f ? near : far;
+}
+// Scores of at_rows to logarithms base 2, register i of a key (or query) `off` + 8 (i / 4) + i % 4 further on than the first; slope receives the
+// derivative of the cap.  The registers are taken out of the product one by one first: with elements of the vector changed behind branches
+// the compiler has stored one of them over its neighbours where accumulators lie in AGPRs (float heads of 128, bf16 ones of 256 channels).
+template <class T, bool SLOPE>
+__device__ __forceinline__ void at_bend(float (&x)[16], const AtScore &p, float by, float distance, float (&slope)[16])
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] *= by;
+    if (SLOPE)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) slope[i] = 1.0f;
+    if (p.cap > 0.0f)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float th = at_tanh<T>(x[i] * p.per_cap);
+            x[i] = p.cap * th;
+            if (SLOPE) slope[i] = 1.0f - th * th;
+        }
+    if (p.fall != 0.0f)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] -= p.fall * fabsf(distance - (float)(8 * (i >> 2) + (i & 3)));
+}
+
+// keys that the query at t of sample n sees: [x, y), none where x >= y
+__device__ __forceinline__ int2 at_span(const AttnArgs &a, int n, int t)
+{
+    if (t >= a.s.T) return {a.s.T, 0};
+    if (a.s.mask == ATTN_NONE) return {0, a.s.T};
+    if (a.s.mask == ATTN_CAUSAL) return {0, t + 1};
+    const int2 v = a.spans[(size_t)n * a.s.T + t];
+    return v.x < v.y ? v : int2{a.s.T, 0};
+}
+
+// What the 32 queries of a wave see: some of them [any.x, any.y), all of them [all.x, all.y)
+struct AtRange {
+    int2 any, all;
+};
+__device__ __forceinline__ AtRange at_wave_range(int2 span)
+{
+    AtRange r{span, span};
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        r.any.x = min(r.any.x, __shfl_xor(r.any.x, o, 64));
+        r.any.y = max(r.any.y, __shfl_xor(r.any.y, o, 64));
+        r.all.x = max(r.all.x, __shfl_xor(r.all.x, o, 64));
+        r.all.y = min(r.all.y, __shfl_xor(r.all.y, o, 64));
+    }
+    auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    return {{uniform(r.any.x), uniform(r.any.y)}, {uniform(r.all.x), uniform(r.all.y)}};
+}
+
+// Block to (sample, key head) and the rest.  Samples and key heads change fastest: blocks go round the XCDs, so that where there are a
+// multiple of eight of them the blocks that read the same keys share an L2.
+struct AtBlock {
+    int n, g, rest;
+};
+__device__ __forceinline__ AtBlock at_block(const AttnShape &s)
+{
+    const int of = s.N * s.groups, ng = blockIdx.x % of;
+    return {ng / s.groups, ng % s.groups, (int)(blockIdx.x / of)};
+}
+
+__device__ __forceinline__ void at_barrier()
+{
+    WAIT_LGKMCNT(0);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// four neighbouring elements of a row of d, from element e0 on
+template <class T, bool VEC> __device__ __forceinline__ void at_store4(T *row, int e0, int d, float x0, float x1, float x2, float x3)
+{
+    vec_t<T, 4> v;
+    if constexpr (sizeof(T) == 2) {
+        const chunk8 c = {pack_bf16(x0, x1), pack_bf16(x2, x3)};
+        v = __builtin_bit_cast(vec_t<T, 4>, c);
+    } else {
+        const chunk16 c = {__float_as_uint(x0), __float_as_uint(x1), __float_as_uint(x2), __float_as_uint(x3)};
+        v = __builtin_bit_cast(vec_t<T, 4>, c);
+    }
+    if constexpr (VEC) {
+        if (e0 < d) *(vec_t<T, 4> *)(row + e0) = v;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (e0 + j < d) row[e0 + j] = v.e[j];
+    }
+}
+// all elements of an owned row from the accumulators of at_columns
+template <class T, bool VEC, int ND> __device__ __forceinline__ void at_store(T *row, int d, int t0, const f32x16_t (&acc)[ND], float by, int lane)
+{
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            at_store4<T, VEC>(row, 32 * (t0 + t) + 8 * g + 4 * (lane >> 5), d, acc[t][4 * g] * by, acc[t][4 * g + 1] * by, acc[t][4 * g + 2] * by,
+                              acc[t][4 * g + 3] * by);
+}
+
+// Calls F<T, DP, VEC, EXTRA, HALF> for a shape.  Heads of a width that is no multiple of 16 bytes are read element by element.
+// bf16 heads take the next multiple of 32 or 64; float and element-wise ones, of which fewer kernels are built, 64, 128 or 256.
+// HALF: scores are made of 16-bit floats (AttnArgs::half).
+template <template <class, int, bool, bool, bool> class F, class... A> hipError_t at_dispatch(int dt, const AttnArgs &p, const A &...a)
+{
+    const AttnShape &s = p.s;
+    const bool extra = s.cap > 0.0f || s.bias != 0, vec = s.d % (16 / (int)dt_size(dt)) == 0;
+    const int d = s.d;
+#define AT_GO(T, DP, VEC, EXTRA, HALF) return F<T, DP, VEC, EXTRA, HALF>::go(p, a...)
+    if (dt == DT_F32) {
+        if (vec) { if (d <= 64) AT_GO(float, 64, true, true, false); if (d <= 128) AT_GO(float, 128, true, true, false); AT_GO(float, 256, true, true, false); }
+        if (d <= 64) AT_GO(float, 64, false, true, false);
+        if (d <= 128) AT_GO(float, 128, false, true, false);
+        AT_GO(float, 256, false, true, false);
+    }
+#define AT_ODD(DP) if (d <= DP) { if (p.half) AT_GO(bf16_t, DP, false, true, true); AT_GO(bf16_t, DP, false, true, false); }
+#define AT_BF16(DP)                                                                                                \
+    if (d <= DP) {                                                                                                 \
+        if (p.half) { if (extra) AT_GO(bf16_t, DP, true, true, true); AT_GO(bf16_t, DP, true, false, true); }      \
+        if (extra) AT_GO(bf16_t, DP, true, true, false);                                                           \
+        AT_GO(bf16_t, DP, true, false, false);                                                                     \
+    }
+    if (!vec) { AT_ODD(64) AT_ODD(128) AT_ODD(256) return hipErrorInvalidValue; }
+    AT_BF16(32) AT_BF16(64) AT_BF16(96) AT_BF16(128) AT_BF16(192) AT_BF16(256)
+#undef AT_BF16
+#undef AT_ODD
+#undef AT_GO
+    return hipErrorInvalidValue;
+}
+
+template <class K> hipError_t at_launch(K kernel, int blocks, int smem, const AttnArgs &a, hipStream_t stream)
+{
+    if (smem > (48 << 10)) {
+        const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(AT_TPB), smem, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace bapipe

@@ -231,6 +231,70 @@ int gated_dgrad_parts(int rows, int C, int F);
 hipError_t gated_dgrad_direct(int dt, const void *D, const void *wt, void *dx, bool parts, GradEpi epi, int rows, int C, int F, void *workspace, hipStream_t s);
 hipError_t gated_wgrad_direct(int dt, const void *x, const void *D, float *dw, float *db, int rows, int C, int F, void *workspace, hipStream_t s);
 
+// ---- attention (kernels_attention_*.hip) of [N][T] positions whose channels hold `heads` query heads, `groups` key heads and as many value
+// heads, of d <= 256 each
+enum { ATTN_NONE = 0, ATTN_CAUSAL = 1, ATTN_SPANS = 2 };
+constexpr int kAttnHead = 256, kAttnTile = 64;
+struct AttnShape {
+    int N, T, heads, groups, d, mask;
+    float scale, cap;        // of the scores: 1 / sqrt(d); 0 or c for c tanh(score / c)
+    int bias;                // 0, or head h's scores fall by 2^(-bias (h + 1) / heads) per position of distance
+    __host__ __device__ int stride() const { return (heads + 2 * groups) * d; }      // elements from position to position of qk, v, dqk and dv
+};
+struct AttnArgs {
+    AttnShape s;
+    // qk: queries and keys, v: values; both point at a position's first query, and so do dqk and dv
+    const void *qk, *v;
+    // bf16, or NULL: queries and keys once more, [N][T][heads + groups][d] 16-bit floats that were divided by powers of two, and
+    // those, [heads + groups][N T]: what scores are made of, eight times as fine
+    const void *half;
+    const float *half_scale;
+    void *o;                 // [N][T][heads d]
+    float *lse;              // [N][heads][T]: log2 of a query's sum of exponentials, inf where it sees nothing
+    const int2 *spans;       // [N][T], ATTN_SPANS: first key and end; of attention_spans
+    const int4 *bounds;      // [N][tiles of kAttnTile queries]: smallest first, largest end of those that see something; largest first, smallest end of all
+    // backward
+    const void *dout;        // as o
+    float *dsum;             // [N][heads][T]: dout . o, of the first of its two kernels to the second
+    void *dqk, *dv;
+    float *dqk_float;        // NULL, or where dq and dk go instead, [N][T][heads + groups][d]
+    float *part;
+    int splits;              // of the second kernel's sums, which then go through part
+};
+// spans clamped to [0, T], and the tiles' bounds; given NULL: every position sees those up to itself
+hipError_t attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int N, int T, hipStream_t s);
+hipError_t attention_fwd(int dt, const AttnArgs &a, hipStream_t s);
+size_t attention_workspace(int dt, const AttnShape &a, int compute_units);          // of a backward pass
+hipError_t attention_bwd(int dt, AttnArgs a, void *workspace, int compute_units, hipStream_t s);
+hipError_t attention_dq(int dt, const AttnArgs &a, hipStream_t s);
+hipError_t attention_dkv(int dt, const AttnArgs &a, hipStream_t s);
+
+// ---- rotary positions of the query and key heads, with an RMS norm of each before (kernels_rotary.hip)
+struct RotaryShape {
+    int rows, T;             // N T positions; row r is at position r % T of its sequence
+    int heads, groups, d;
+    int rotated;             // channels of a head that turn, even
+    int pairs;               // neighbours turn together, else j and j + rotated / 2
+    int values;              // value heads are copied
+    float eps;               // of the norm, 0: none
+    __host__ __device__ int stride() const { return (heads + 2 * groups) * d; }
+};
+struct RotaryAngles {
+    double base, factor, original_length, low_turns, high_turns, magnitude;
+    long long first_position;
+};
+// cosine and sine [T][rotated / 2] times the magnitude
+hipError_t rotary_table(float2 *table, int T, int rotated, const RotaryAngles &a, hipStream_t s);
+// gains: [2][d], of query heads, of key heads; y may be x
+// half, half_scale: where an ATTENTION's AttnArgs find them (bf16), or NULL
+hipError_t rotary_fwd(int dt, const RotaryShape &r, const void *x, void *y, const float2 *table, const float *gains, hipStream_t s, void *half = nullptr,
+                      float *half_scale = nullptr);
+size_t rotary_workspace(int dt, const RotaryShape &r);
+// x, gains, dgains (added to) and the workspace only with a norm; dx may be dy or, where there is nothing to give it to, NULL
+// dy_float: NULL, or (bf16) where the gradients of query and key heads are instead, [rows][heads + groups][d]
+hipError_t rotary_bwd(int dt, const RotaryShape &r, const void *x, const void *dy, const float *dy_float, void *dx, const float2 *table, const float *gains,
+                      float *dgains, void *workspace, hipStream_t s);
+
 // ---- dropout (kernels_dropout.hip): y[e] = word(e) >= 2^32 p ? x[e] / (1-p) : 0, or with the gradient epilogue the same of dy
 // state: three device words (seed low, seed high, number of the mini-batch), which the kernel reads
 constexpr int kDropoutState = 3;

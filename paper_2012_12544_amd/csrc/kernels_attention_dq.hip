@@ -1,0 +1,137 @@
+// Attention, backward, the queries' gradients: scores and probabilities again from the stored logarithm of each query's sum.
+//   p = 2^(score - lse), ds = p (dout v^T - dout . o), dq = ds k / sqrt(d)
+#include "attention_common.h"
+
+namespace bapipe {
+namespace {
+
+template <class T, int DP, bool VEC, bool EXTRA, bool HALF>
+__global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void k_attention_dq(AttnArgs p)
+{
+    constexpr int R = HALF && DP >= 128 ? 32 : 0;        // three operands
+    typedef AtTile<T, DP, R> Tile;
+    typedef std::conditional_t<HALF, half_t, T> S;
+    typedef AtTile<S, DP, R> STile;
+    constexpr int ND = DP / 32, SUBS = Tile::ROWS / 32, STREAMS = HALF ? 3 : 2;
+    extern __shared__ __align__(256) unsigned char smem[];
+    __shared__ __align__(16) float row_scale[2][HALF ? Tile::ROWS : 4];
+    __shared__ int2 block_range[AT_WAVES];
+    const AttnShape &s = p.s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+    const int d = s.d, stride = s.stride(), per = s.heads / s.groups;
+    const AtBlock b = at_block(s);
+    const int blocks = (s.T + AT_ROWS - 1) / AT_ROWS, head = b.g * per + b.rest % per, q0 = (blocks - 1 - b.rest / per) * AT_ROWS;
+    const int q = q0 + 32 * wave + (lane & 31);
+    const int sstride = HALF ? (s.heads + s.groups) * d : stride;
+    const S *base = (const S *)(HALF ? p.half : p.qk) + (size_t)b.n * s.T * sstride, *score_keys = base + (size_t)(s.heads + b.g) * d;
+    const T *keys = (const T *)p.qk + (size_t)b.n * s.T * stride + (size_t)(s.heads + b.g) * d;
+    const T *values = (const T *)p.v + (size_t)b.n * s.T * stride + (size_t)(s.heads + s.groups + b.g) * d;
+    const float *key_scale = HALF ? p.half_scale + ((size_t)(s.heads + b.g) * s.N + b.n) * s.T : nullptr;
+    const size_t at_o = ((size_t)b.n * s.T + q) * s.heads * d + (size_t)head * d, at_row = ((size_t)b.n * s.heads + head) * s.T + q;
+
+    const int2 span = at_span(p, b.n, q);
+    const bool sees = span.x < span.y;
+    chunk16 query[Tile::STEPS], dout[Tile::STEPS];
+    at_own<S, DP, VEC>(query, sees ? base + (size_t)q * sstride + (size_t)head * d : nullptr, d, lane);
+    at_own<T, DP, VEC>(dout, sees ? (const T *)p.dout + at_o : nullptr, d, lane);
+    float dsum = 0.0f;
+    {
+        chunk16 o[Tile::STEPS];
+        at_own<T, DP, VEC>(o, sees ? (const T *)p.o + at_o : nullptr, d, lane);
+#pragma unroll
+        for (int c = 0; c < Tile::STEPS; ++c)
+#pragma unroll
+            for (int j = 0; j < Tile::EPC; ++j) dsum = fmaf(chunk_value<T>(dout[c], j), chunk_value<T>(o[c], j), dsum);
+        dsum = at_halves_sum(dsum);
+    }
+    const float lse = sees ? p.lse[at_row] : __builtin_inff();
+    if (q < s.T && h == 0) p.dsum[at_row] = dsum;
+
+    const AtRange range = at_wave_range(span);
+    if (lane == 0) block_range[wave] = range.any;
+    __syncthreads();
+    int first = s.T, end = 0;
+#pragma unroll
+    for (int w = 0; w < AT_WAVES; ++w) {
+        first = min(first, block_range[w].x);
+        end = max(end, block_range[w].y);
+    }
+    first = __builtin_amdgcn_readfirstlane(first);
+    end = __builtin_amdgcn_readfirstlane(end);
+
+    const AtScore score = at_score(s, head);
+    float by = score.scale;
+    if (HALF && sees) by *= p.half_scale[((size_t)head * s.N + b.n) * s.T + q];
+    const lds_addr_of lds(smem);
+    const AtStream<S, DP, VEC, R> score_stream(sstride, tid);
+    const AtStream<T, DP, VEC, R> stream(stride, tid);
+    float next_scale = 0.0f;
+    auto fill = [&](int it) {
+        const int k0 = first + it * Tile::ROWS;
+        unsigned char *to = smem + (it & 1) * STREAMS * Tile::BYTES;
+        if (HALF && tid < Tile::ROWS) next_scale = k0 + tid < end ? key_scale[k0 + tid] : 0.0f;
+        stream.fill(to, lds, keys + (size_t)k0 * stride, end - k0, stride, d, tid);
+        stream.fill(to + Tile::BYTES, lds, values + (size_t)k0 * stride, end - k0, stride, d, tid);
+        if (HALF) score_stream.fill(to + 2 * Tile::BYTES, lds, score_keys + (size_t)k0 * sstride, end - k0, sstride, d, tid);
+    };
+    f32x16_t dq[ND] = {};
+    const int tiles = (end - first + Tile::ROWS - 1) / Tile::ROWS;
+    if (tiles > 0) fill(0);
+    for (int it = 0; it < tiles; ++it) {
+        if (HALF && tid < Tile::ROWS) row_scale[it & 1][tid] = next_scale;
+        WAIT_VMCNT(0);
+        at_barrier();
+        if (it + 1 < tiles) fill(it + 1);
+        const int k0 = first + it * Tile::ROWS;
+        if (k0 >= range.any.y || k0 + Tile::ROWS <= range.any.x) continue;
+        const unsigned char *key = smem + (it & 1) * STREAMS * Tile::BYTES, *value = key + Tile::BYTES, *score_key = HALF ? value + Tile::BYTES : key;
+        const bool whole = k0 >= range.all.x && k0 + Tile::ROWS <= range.all.y;
+#pragma unroll 1
+        for (int u = 0; u < SUBS; ++u) {
+            const f32x16_t w = at_rows<S, STile>(score_key, 32 * u, query, lane), dw = at_rows<T, Tile>(value, 32 * u, dout, lane);
+            float x[16], ds[16], slope[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[i] = w[i];
+                ds[i] = dw[i] - dsum;
+            }
+            if (HALF)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 r = *(const float4 *)&row_scale[it & 1][32 * u + 8 * g + 4 * h];
+                    x[4 * g] *= r.x; x[4 * g + 1] *= r.y; x[4 * g + 2] *= r.z; x[4 * g + 3] *= r.w;
+                }
+            if (EXTRA) at_bend<T, true>(x, score, by, (float)(q - (k0 + 32 * u + 4 * h)), slope);
+            const float unit = EXTRA ? 1.0f : by;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], unit, -lse));
+            if (!whole)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int k = k0 + 32 * u + 8 * (i >> 2) + 4 * h + (i & 3);
+                    x[i] = k >= span.x && k < span.y ? x[i] : 0.0f;
+                }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ds[i] = EXTRA ? x[i] * ds[i] * slope[i] : x[i] * ds[i];
+            at_columns<T, Tile, ND>(dq, key, 32 * u, 0, AtWeights<T>(ds), lane);
+        }
+    }
+    if (q >= s.T) return;
+    const size_t row = (size_t)b.n * s.T + q;
+    if (p.dqk_float) at_store<float, VEC, ND>(p.dqk_float + row * (s.heads + s.groups) * d + (size_t)head * d, d, 0, dq, s.scale, lane);
+    else at_store<T, VEC, ND>((T *)p.dqk + row * stride + (size_t)head * d, d, 0, dq, s.scale, lane);
+}
+
+template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Queries {
+    static hipError_t go(const AttnArgs &a, hipStream_t stream)
+    {
+        constexpr int smem = HALF ? 6 * AtTile<T, DP, DP >= 128 ? 32 : 0>::BYTES : 4 * AtTile<T, DP>::BYTES;
+        return at_launch(k_attention_dq<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS - 1) / AT_ROWS), smem, a, stream);
+    }
+};
+
+}  // namespace
+
+hipError_t attention_dq(int dt, const AttnArgs &a, hipStream_t s) { return at_dispatch<Queries>(dt, a, s); }
+
+}  // namespace bapipe

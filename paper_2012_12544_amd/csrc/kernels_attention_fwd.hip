@@ -1,0 +1,176 @@
+// Attention, forward: o = softmax(scores) v in one pass over the keys, with a running maximum and sum per query.
+#include "attention_common.h"
+
+namespace bapipe {
+namespace {
+
+template <class T, int DP, bool VEC, bool EXTRA, bool HALF>
+__global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void k_attention_fwd(AttnArgs p)
+{
+    typedef AtTile<T, DP> Tile;
+    typedef std::conditional_t<HALF, half_t, T> S;       // what scores are made of
+    typedef AtTile<S, DP, 0> STile;
+    constexpr int ND = DP / 32, SUBS = Tile::ROWS / 32;
+    extern __shared__ __align__(256) unsigned char smem[];
+    __shared__ __align__(16) float row_scale[2][HALF ? Tile::ROWS : 4];
+    __shared__ int2 block_range[AT_WAVES];
+    const AttnShape &s = p.s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+    const int d = s.d, stride = s.stride(), per = s.heads / s.groups;
+    const AtBlock b = at_block(s);
+    // queries with the most keys first
+    const int blocks = (s.T + AT_ROWS - 1) / AT_ROWS, head = b.g * per + b.rest % per, q0 = (blocks - 1 - b.rest / per) * AT_ROWS;
+    const int q = q0 + 32 * wave + (lane & 31);
+    const int sstride = HALF ? (s.heads + s.groups) * d : stride;
+    const S *base = (const S *)(HALF ? p.half : p.qk) + (size_t)b.n * s.T * sstride, *keys = base + (size_t)(s.heads + b.g) * d;
+    const T *values = (const T *)p.v + (size_t)b.n * s.T * stride + (size_t)(s.heads + s.groups + b.g) * d;
+    const float *key_scale = HALF ? p.half_scale + ((size_t)(s.heads + b.g) * s.N + b.n) * s.T : nullptr;
+
+    chunk16 query[Tile::STEPS];
+    at_own<S, DP, VEC>(query, q < s.T ? base + (size_t)q * sstride + (size_t)head * d : nullptr, d, lane);
+    const int2 span = at_span(p, b.n, q);
+    const AtRange range = at_wave_range(span);
+    if (lane == 0) block_range[wave] = range.any;
+    __syncthreads();
+    int first = s.T, end = 0;
+#pragma unroll
+    for (int w = 0; w < AT_WAVES; ++w) {
+        first = min(first, block_range[w].x);
+        end = max(end, block_range[w].y);
+    }
+    first = __builtin_amdgcn_readfirstlane(first);
+    end = __builtin_amdgcn_readfirstlane(end);
+
+    const AtScore score = at_score(s, head);
+    float by = score.scale;
+    if (HALF && q < s.T) by *= p.half_scale[((size_t)head * s.N + b.n) * s.T + q];
+    const lds_addr_of lds(smem);
+    const AtStream<S, DP, VEC> key_stream(sstride, tid);
+    const AtStream<T, DP, VEC> value_stream(stride, tid);
+    float next_scale = 0.0f;
+    auto fill = [&](int it) {
+        const int k0 = first + it * Tile::ROWS;
+        unsigned char *to = smem + (it & 1) * 2 * Tile::BYTES;
+        if (HALF && tid < Tile::ROWS) next_scale = k0 + tid < end ? key_scale[k0 + tid] : 0.0f;
+        key_stream.fill(to, lds, keys + (size_t)k0 * sstride, end - k0, sstride, d, tid);
+        value_stream.fill(to + Tile::BYTES, lds, values + (size_t)k0 * stride, end - k0, stride, d, tid);
+    };
+    f32x16_t out[ND] = {};
+    float top = -__builtin_inff(), sum = 0.0f;            // sum: of this half's keys
+    const int tiles = (end - first + Tile::ROWS - 1) / Tile::ROWS;        // none where nobody sees anything
+    if (tiles > 0) fill(0);
+    for (int it = 0; it < tiles; ++it) {
+        if (HALF && tid < Tile::ROWS) row_scale[it & 1][tid] = next_scale;
+        WAIT_VMCNT(0);
+        at_barrier();                                      // the tile has arrived, the other one is read
+        if (it + 1 < tiles) fill(it + 1);
+        const int k0 = first + it * Tile::ROWS;
+        if (k0 >= range.any.y || k0 + Tile::ROWS <= range.any.x) continue;
+        const unsigned char *key = smem + (it & 1) * 2 * Tile::BYTES, *value = key + Tile::BYTES;
+        float x[SUBS][16];
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u) {
+            const f32x16_t w = at_rows<S, STile>(key, 32 * u, query, lane);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[u][i] = w[i];
+            if (HALF)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 r = *(const float4 *)&row_scale[it & 1][32 * u + 8 * g + 4 * h];
+                    x[u][4 * g] *= r.x; x[u][4 * g + 1] *= r.y; x[u][4 * g + 2] *= r.z; x[u][4 * g + 3] *= r.w;
+                }
+        }
+        if (EXTRA)
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u) {
+                float none[16];
+                at_bend<T, false>(x[u], score, by, (float)(q - (k0 + 32 * u + 4 * h)), none);
+            }
+        if (!(k0 >= range.all.x && k0 + Tile::ROWS <= range.all.y))
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int k = k0 + 32 * u + 8 * (i >> 2) + 4 * h + (i & 3);
+                    x[u][i] = k >= span.x && k < span.y ? x[u][i] : -__builtin_inff();
+                }
+        const float unit = EXTRA ? 1.0f : by;
+        float most = x[0][0];
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = fmaxf(most, x[u][i]);
+        most = at_halves_max(most) * unit;
+        // The maximum that scores are taken relative to follows the true one only where that is 2^8 above: the sums stay far inside a float's
+        // range, and most tiles leave the accumulators alone.
+        if (__any(most > top + 8.0f)) {
+            const float next = fmaxf(top, most), fade = next > -__builtin_inff() ? __builtin_amdgcn_exp2f(top - next) : 1.0f;
+            top = next;
+            sum *= fade;
+#pragma unroll
+            for (int t = 0; t < ND; ++t) out[t] *= fade;
+        }
+        const float less = top > -__builtin_inff() ? top : 0.0f;
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[u][i] = __builtin_amdgcn_exp2f(fmaf(x[u][i], unit, -less));
+                sum += x[u][i];
+            }
+            at_columns<T, Tile, ND>(out, value, 32 * u, 0, AtWeights<T>(x[u]), lane);
+        }
+    }
+    sum = at_halves_sum(sum);
+    if (q >= s.T) return;
+    const bool sees = span.x < span.y;
+    at_store<T, VEC, ND>((T *)p.o + ((size_t)b.n * s.T + q) * s.heads * d + (size_t)head * d, d, 0, out, sees ? 1.0f / sum : 0.0f, lane);
+    if (h == 0) p.lse[((size_t)b.n * s.heads + head) * s.T + q] = sees ? top + log2f(sum) : __builtin_inff();
+}
+
+template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Forward {
+    static hipError_t go(const AttnArgs &a, hipStream_t stream)
+    {
+        return at_launch(k_attention_fwd<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS - 1) / AT_ROWS), 4 * AtTile<T, DP>::BYTES, a, stream);
+    }
+};
+
+// One wave to a tile of kAttnTile positions
+__global__ __launch_bounds__(64) void k_attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int T)
+{
+    const int lane = threadIdx.x, n = blockIdx.y, t = blockIdx.x * kAttnTile + lane;
+    int4 b = {T, 0, 0, T};
+    if (t < T) {
+        const size_t at = (size_t)n * T + t;
+        int2 v = given ? int2{max(given[2 * at], 0), min(given[2 * at + 1], T)} : int2{0, t + 1};
+        if (v.x >= v.y) v = {0, 0};
+        spans[at] = v;
+        b = v.x < v.y ? int4{v.x, v.y, v.x, v.y} : int4{T, 0, T, 0};
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        b.x = min(b.x, __shfl_xor(b.x, o, 64));
+        b.y = max(b.y, __shfl_xor(b.y, o, 64));
+        b.z = max(b.z, __shfl_xor(b.z, o, 64));
+        b.w = min(b.w, __shfl_xor(b.w, o, 64));
+    }
+    if (lane == 0) bounds[(size_t)n * gridDim.x + blockIdx.x] = b;
+}
+
+}  // namespace
+
+hipError_t attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int N, int T, hipStream_t s)
+{
+    // a sample's tiles are a row of the grid, which takes 65535 of them at a time
+    const int tiles = (T + kAttnTile - 1) / kAttnTile;
+    for (int n = 0; n < N; n += 65535) {
+        const size_t at = (size_t)n * T;
+        hipLaunchKernelGGL(k_attention_spans, dim3((unsigned)tiles, (unsigned)(N - n < 65535 ? N - n : 65535)), dim3(64), 0, s, given ? given + 2 * at : nullptr,
+                           spans + at, bounds + (size_t)n * tiles, T);
+    }
+    return hipGetLastError();
+}
+
+hipError_t attention_fwd(int dt, const AttnArgs &a, hipStream_t s) { return at_dispatch<Forward>(dt, a, s); }
+
+}  // namespace bapipe

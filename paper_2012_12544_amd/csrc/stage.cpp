@@ -8,8 +8,8 @@
 //             w [K][R][S][C] for forward, flipped channel-transposed [C][R][S][K] for dgrad
 //   stash     depth x slot ; a slot holds, for one in-flight micro-batch, exactly the tensors
 //             backward reads again: layer inputs of conv/linear/BN, ReLU gates, pool indices,
-//             BN and layer norm statistics, both projections of a gated layer (float), softmax
-//             output.  depth = min(M, N-i+1) (x2 for 1F1B-SO).
+//             BN and layer norm statistics, both projections of a gated layer (float), queries, keys, values, output
+//             and each query's sum of an attention, softmax output.  depth = min(M, N-i+1) (x2 for 1F1B-SO).
 //   transient forward tensors nobody reads in backward (reused by every micro-batch)
 //   grads     one buffer per tensor that receives an activation gradient (reused), and the
 //             gradients of a gated layer's projections
@@ -17,6 +17,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
@@ -116,6 +117,20 @@ struct Layer {
     size_t off_gates = 0, off_cells = 0, off_hs = 0, off_pd = 0, off_dcn = 0;
     // GATED: the slot keeps both projections (off_pd, float); their gradients have a place among the gradients (off_d)
     size_t off_d = 0, off_d_rest = 0;    // off_d_rest: see Tensor::fine
+    // ROTARY: the cosines and sines of its angles; whether the value heads stay in its input, where the ATTENTION behind it reads them, and
+    // their gradients come to lie with that input's.  Without a norm nobody needs what it reads again: it turns a convolution's output where it
+    // lies (the tensors share their storage) and value heads stay by themselves.
+    float2 *table = nullptr;
+    bool values_stay = false, dvalues_stay = false;
+    // bf16 ROTARY that only an ATTENTION reads: the slot also keeps its queries and keys as 16-bit floats with a scale for each head and position
+    // (off_half, off_scale), which scores are made of, and their gradients come back as floats (off_float, among the gradients).  A score is a
+    // sum of products of two rounded factors: with scores of standard deviation 4, which a cap is for, bf16 factors make gradients 1.05e-2 wrong
+    // in the 2-norm, 16-bit floats and float gradients 4.3e-3; at 1, with norms, 4.6e-3 and 3.5e-3.
+    bool half = false;
+    size_t off_half = 0, off_scale = 0, off_float = 0;
+    // ATTENTION: logarithms of the sums (aux_off); where its input's gradient cannot be written at once (other readers, a ReLU in front), a place
+    // among the gradients: off_d, as for ROTARY
+    bool by_copy = false;
     bool mfma = false;                   // its products run on the bf16 MFMA kernels
     bool groups = false;                 // its weight gradient may share a launch with others
     // LINEAR, a 1x1 convolution of 1x1 maps, and products that stream their filter (streams_filter), on the MFMA kernels: the copies that forward
@@ -184,6 +199,11 @@ struct bapipe_stage {
     float *losses = nullptr;                 // and, behind them, the tickets of conv_gather_mfma: of the handle's stream, of the backward stream
     uint32_t *dropout_state = nullptr;       // behind those: seed and mini-batch number of the DROPOUT layers
     bool has_dropout = false;
+    // ATTENTION layers with spans: positions of a sequence, place in the slot of the clamped spans and their tiles' bounds, and what the caller
+    // has set for the coming micro-batch
+    int span_T = 0;
+    size_t off_spans = 0, off_bounds = 0;
+    const int32_t *spans_given = nullptr;
     bool dx_at_dy = false, dx_across_dy = false;      // see dx_may_lie_over_dy: at the same address, at any other
     unsigned *tickets = nullptr, *tickets_f = nullptr, *tickets_b = nullptr;      // as work: of the pass being enqueued, of either
     size_t params_bytes = 0, slot_bytes = 0, transient_bytes = 0, grads_bytes = 0, work_bytes = 0;
@@ -292,8 +312,9 @@ bool has_params(int kind)
     return kind == BAPIPE_CONV2D || kind == BAPIPE_LINEAR || kind == BAPIPE_BATCHNORM2D || kind == BAPIPE_LSTM || kind == BAPIPE_LAYERNORM ||
            kind == BAPIPE_GATED;
 }
+bool has_heads(int kind) { return kind == BAPIPE_ROTARY || kind == BAPIPE_ATTENTION; }
 bool has_matrix(int kind) { return kind == BAPIPE_CONV2D || kind == BAPIPE_LINEAR || kind == BAPIPE_LSTM || kind == BAPIPE_GATED; }
-bool is_norm(int kind) { return kind == BAPIPE_BATCHNORM2D || kind == BAPIPE_LAYERNORM; }
+bool is_norm(int kind) { return kind == BAPIPE_BATCHNORM2D || kind == BAPIPE_LAYERNORM || kind == BAPIPE_ROTARY; }      // parameters are gains
 
 GatherConv fwd_geom(const bapipe_stage *st, const Layer &L)
 {
@@ -665,6 +686,70 @@ void *out_ptr(bapipe_stage *st, const Layer &L, FwdCtx &c, size_t align)
     return c.y_direct;
 }
 
+RotaryShape rotary_shape(const bapipe_stage *st, const Layer &L, bool values)
+{
+    const Tensor &A = st->tensors[L.a];
+    RotaryShape r;
+    r.rows = rows_of(st, A); r.T = A.H;
+    r.heads = L.d.kh; r.groups = L.d.kw; r.d = A.C / (L.d.kh + 2 * L.d.kw);
+    r.rotated = L.d.pad;
+    r.pairs = L.d.stride == BAPIPE_ROTARY_PAIRS;
+    r.values = values;
+    r.eps = L.d.has_bias ? L.d.eps : 0.0f;
+    return r;
+}
+
+AttnShape attn_shape(const bapipe_stage *st, const Layer &L)
+{
+    const Tensor &A = st->tensors[L.a];
+    AttnShape a;
+    a.N = st->mb; a.T = A.H;
+    a.heads = L.d.kh; a.groups = L.d.kw; a.d = A.C / (L.d.kh + 2 * L.d.kw);
+    a.mask = L.d.stride;
+    a.scale = 1.0f / sqrtf((float)a.d);
+    a.cap = L.d.eps;
+    a.bias = L.d.pad;
+    return a;
+}
+
+// pairs of query and key, of all heads, that a forward pass scores where the mask is not the caller's
+double attn_pairs(const AttnShape &a)
+{
+    return (double)a.N * a.heads * a.T * (a.mask == ATTN_CAUSAL ? 0.5 * (a.T + 1.0) : (double)a.T);
+}
+
+// the ROTARY in front of an ATTENTION, or NULL
+const Layer *rotary_before(const bapipe_stage *st, const Layer &L)
+{
+    return L.a > 0 && st->layers[L.a - 1].d.kind == BAPIPE_ROTARY ? &st->layers[L.a - 1] : nullptr;
+}
+
+size_t turning_elems(const bapipe_stage *st, const Layer &L)
+{
+    const RotaryShape r = rotary_shape(st, L, false);
+    return (size_t)r.rows * (r.heads + r.groups) * r.d;
+}
+
+// what both passes of an ATTENTION are handed
+AttnArgs attn_args(bapipe_stage *st, const Layer &L, int mbid)
+{
+    char *slot = st->slot(mbid);
+    const Layer *R = rotary_before(st, L);
+    AttnArgs q = {};
+    q.s = attn_shape(st, L);
+    q.qk = st->tptr(L.a, mbid);
+    q.v = R && R->values_stay ? st->tptr(R->a, mbid) : q.qk;
+    if (R && R->half) {
+        q.half = slot + R->off_half;
+        q.half_scale = (const float *)(slot + R->off_scale);
+    }
+    q.o = st->tptr(L.o, mbid);
+    q.lse = (float *)(slot + L.aux_off);
+    q.spans = (const int2 *)(slot + st->off_spans);
+    q.bounds = (const int4 *)(slot + st->off_bounds);
+    return q;
+}
+
 int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
 {
     Layer &L = st->layers[li];
@@ -781,6 +866,21 @@ int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
                          rows_of(st, A), L.d.cin, L.d.cout, L.w_panels, st->work, s));
         // x and the weights read, h and both projections (float) written
         st->tap_end(tp, conv_flop(g, L.d.cin) * (A.rest ? 2.0 : 1.0), A.bytes() * (A.rest ? 2.0 : 1.0) + O.bytes() + 8.0 * O.elems + (double)L.w_elems * dt_size(dt));
+        break;
+    }
+    case BAPIPE_ROTARY: {
+        const RotaryShape r = rotary_shape(st, L, !L.values_stay && O.root == L.o);
+        const bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
+        HIPCHK(rotary_fwd(dt, r, a, O.root == L.o ? out_ptr(st, L, c, dt_size(dt)) : o, L.table, L.w, s, L.half ? st->slot(c.mbid) + L.off_half : nullptr,
+                          L.half ? (float *)(st->slot(c.mbid) + L.off_scale) : nullptr));
+        st->tap_end(tp, 0.0, 2.0 * O.bytes() * (L.d.kh + L.d.kw * (r.values ? 2.0 : 1.0)) / (L.d.kh + 2.0 * L.d.kw));
+        break;
+    }
+    case BAPIPE_ATTENTION: {
+        const AttnArgs q = attn_args(st, L, c.mbid);
+        const bool tp = st->tap_begin(BAPIPE_KC_ATTENTION);
+        HIPCHK(attention_fwd(dt, q, s));
+        st->tap_end(tp, 4.0 * q.s.d * attn_pairs(q.s), (double)st->tensors[L.a].bytes() + O.bytes() + L.aux_bytes);
         break;
     }
     case BAPIPE_DROPOUT: {
@@ -1102,6 +1202,39 @@ int layer_backward(bapipe_stage *st, int li, BwdCtx &c)
         }
         break;
     }
+    case BAPIPE_ROTARY: {
+        if (!a_grad && !L.w_elems) break;
+        const bool in_place = O.root != L.o;
+        const RotaryShape r = rotary_shape(st, L, !L.dvalues_stay && !in_place);
+        GradEpi e{nullptr, 0};
+        void *dx = nullptr;
+        if (a_grad && in_place) dx = grad_ptr(st, L.a, c);
+        else if (a_grad) {
+            e = epi_for(st, L.a, c);
+            dx = L.by_copy ? st->grads + L.off_d : grad_ptr(st, L.a, c);
+        }
+        const bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
+        HIPCHK(rotary_bwd(dt, r, L.w_elems ? st->tptr(L.a, c.mbid) : nullptr, grad_ptr(st, L.o, c),
+                          L.half ? (const float *)(st->grads + L.off_float) : nullptr, dx, L.table, L.w, L.dw, st->work, s));
+        if (dx && L.by_copy) HIPCHK(grad_copy(dt, dx, grad_ptr(st, L.a, c), e, A.elems, s));
+        st->tap_end(tp, 0.0, (double)O.bytes() * (L.w_elems ? 3.0 : 2.0) * (L.d.kh + L.d.kw * (r.values ? 2.0 : 1.0)) / (L.d.kh + 2.0 * L.d.kw));
+        break;
+    }
+    case BAPIPE_ATTENTION: {
+        if (!a_grad) break;
+        AttnArgs q = attn_args(st, L, c.mbid);
+        const Layer *R = rotary_before(st, L);
+        q.dout = grad_ptr(st, L.o, c);
+        const GradEpi e = epi_for(st, L.a, c);
+        q.dqk = L.by_copy ? st->grads + L.off_d : grad_ptr(st, L.a, c);
+        q.dv = R && R->dvalues_stay ? grad_ptr(st, R->a, c) : q.dqk;
+        if (R && R->half) q.dqk_float = (float *)(st->grads + R->off_float);
+        const bool tp = st->tap_begin(BAPIPE_KC_ATTENTION);
+        HIPCHK(attention_bwd(dt, q, st->work, st->compute_units, s));
+        if (L.by_copy) HIPCHK(grad_copy(dt, q.dqk, grad_ptr(st, L.a, c), e, A.elems, s));
+        st->tap_end(tp, 10.0 * q.s.d * attn_pairs(q.s), 2.0 * A.bytes() + 2.0 * O.bytes() + L.aux_bytes);
+        break;
+    }
     case BAPIPE_DROPOUT:
         if (a_grad) {
             GradEpi e = epi_for(st, L.a, c);
@@ -1193,6 +1326,8 @@ bool dx_may_lie_over_dy(const bapipe_stage *st, bool same)
         const Layer &L = st->layers[i];
         const int kind = L.d.kind;
         if (kind == BAPIPE_FLATTEN) continue;
+        // its second kernel reads what its first one has read, and the values' gradients may go past a ROTARY
+        if (kind == BAPIPE_ATTENTION && (root(L.a) == 0 || (st->layers[L.a - 1].dvalues_stay && root(st->layers[L.a - 1].a) == 0))) return false;
         const bool own = place(L.o) == dy, late = reads_late[i], reads = own || late;
         if (reads && changed) return false;
         for (int t : {L.a, L.b}) {
@@ -1207,7 +1342,8 @@ bool dx_may_lie_over_dy(const bapipe_stage *st, bool same)
                 stored = true;
                 continue;
             }
-            const bool by_element = kind == BAPIPE_ADD || kind == BAPIPE_RELU || kind == BAPIPE_DROPOUT || kind == BAPIPE_LAYERNORM;
+            // (ROTARY has read all of a head before it stores it)
+            const bool by_element = kind == BAPIPE_ADD || kind == BAPIPE_RELU || kind == BAPIPE_DROPOUT || kind == BAPIPE_LAYERNORM || kind == BAPIPE_ROTARY;
             // GATED has read all of its output's gradient before its input's is stored
             if (own && !(same && by_element) && kind != BAPIPE_GATED) return false;
             if (late && !same) return false;
@@ -1318,7 +1454,7 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         O.esize = es; O.root = L.o; O.producer = i;
         if (A.esize != es) return create_fail(BAPIPE_E_SHAPE, "layer %d: consumes the softmax output", i);
         // which of its readers only LINEAR knows of
-        if (A.map_order && (d.kind == BAPIPE_LAYERNORM || d.kind == BAPIPE_GATED || d.kind == BAPIPE_DROPOUT))
+        if (A.map_order && (d.kind == BAPIPE_LAYERNORM || d.kind == BAPIPE_GATED || d.kind == BAPIPE_DROPOUT || has_heads(d.kind)))
             return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: a flattened map as input; DROPOUT may stand in front of the FLATTEN", i);
         switch (d.kind) {
         case BAPIPE_CONV2D: {
@@ -1388,6 +1524,40 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
             O.C = A.C; O.H = A.H; O.W = A.W;
             st->has_dropout = true;
             break;
+        case BAPIPE_ROTARY:
+        case BAPIPE_ATTENTION: {
+            const bool rotary = d.kind == BAPIPE_ROTARY;
+            const char *what = rotary ? "rotary" : "attention";
+            if (d.kh <= 0 || d.kw <= 0 || d.kh > (1 << 20) || d.kw > (1 << 20))
+                return create_fail(BAPIPE_E_INVALID, "layer %d: %s over %d query and %d key heads", i, what, d.kh, d.kw);
+            if (d.kh % d.kw) return create_fail(BAPIPE_E_SHAPE, "layer %d: %d query heads do not share %d key heads evenly", i, d.kh, d.kw);
+            if (A.C != d.cin) return create_fail(BAPIPE_E_SHAPE, "layer %d: cin=%d but input has %d channels", i, d.cin, A.C);
+            if (A.W != 1) return create_fail(BAPIPE_E_SHAPE, "layer %d: %s input must be (cin, T, 1)", i, what);
+            if (A.Cp != A.C) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: %s input with padded channels", i, what);
+            const int all = d.kh + 2 * d.kw, width = A.C / all;
+            if (A.C % all) return create_fail(BAPIPE_E_SHAPE, "layer %d: %d channels are no %d heads", i, A.C, all);
+            if (width > kAttnHead) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: heads of %d channels, more than %d", i, width, kAttnHead);
+            if (d.cout != (rotary ? A.C : d.kh * width)) return create_fail(BAPIPE_E_SHAPE, "layer %d: cout=%d of %s with %d query heads of %d channels", i, d.cout, what, d.kh, width);
+            if (d.fuse_relu) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: %s has no fused ReLU", i, what);
+            if (rotary) {
+                if (d.stride != BAPIPE_ROTARY_HALVES && d.stride != BAPIPE_ROTARY_PAIRS) return create_fail(BAPIPE_E_INVALID, "layer %d: unknown layout %d", i, d.stride);
+                if (d.pad < 0 || d.pad % 2 || d.pad > width) return create_fail(BAPIPE_E_INVALID, "layer %d: %d turning channels of %d", i, d.pad, width);
+                if (d.has_bias ? !(d.eps > 0.f) || d.eps > FLT_MAX : d.eps != 0.f)
+                    return create_fail(BAPIPE_E_INVALID, "layer %d: eps must be positive with norms, else 0", i);
+                if (d.has_bias) L.w_elems = 2 * (size_t)width;
+            } else {
+                if (d.stride < BAPIPE_MASK_NONE || d.stride > BAPIPE_MASK_SPANS) return create_fail(BAPIPE_E_INVALID, "layer %d: unknown mask %d", i, d.stride);
+                if (d.pad < 0 || d.pad > 64) return create_fail(BAPIPE_E_INVALID, "layer %d: range %d of the slopes, must be 0 to 64", i, d.pad);
+                if (d.has_bias) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: attention has no parameters", i);
+                if (!(d.eps >= 0.f) || d.eps > FLT_MAX) return create_fail(BAPIPE_E_INVALID, "layer %d: cap must be positive, or 0 for none", i);
+                if (d.stride == BAPIPE_MASK_SPANS) {
+                    if (st->span_T && st->span_T != A.H) return create_fail(BAPIPE_E_SHAPE, "layer %d: spans of %d positions, another layer's of %d", i, A.H, st->span_T);
+                    st->span_T = A.H;
+                }
+            }
+            O.C = d.cout; O.H = A.H; O.W = 1;
+            break;
+        }
         case BAPIPE_RELU:
             O.C = A.C; O.H = A.H; O.W = A.W;
             break;
@@ -1458,6 +1628,22 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         if (st->tensors[t].consumers.empty())
             return create_fail(BAPIPE_E_SHAPE, "layer %d: output is never used", t - 1);
 
+    // ROTARY: what turns in place, and whose values stay where they are
+    for (int i = 0; i < n_layers; ++i) {
+        Layer &L = st->layers[i];
+        if (L.d.kind != BAPIPE_ROTARY) continue;
+        const Tensor &A = st->tensors[L.a];
+        Tensor &O = st->tensors[L.o];
+        const bool only_attention = L.o != last_t && O.consumers.size() == 1 && st->layers[O.consumers[0]].d.kind == BAPIPE_ATTENTION;
+        L.half = only_attention && st->dt == DT_BF16;
+        if (!L.w_elems) {
+            if (L.a == 0 || L.o == last_t || A.consumers.size() != 1) continue;
+            const bapipe_layer_desc_t &P = st->layers[L.a - 1].d;
+            if (P.kind == BAPIPE_CONV2D && !P.fuse_relu) O.root = L.a;
+        } else
+            L.values_stay = only_attention;
+    }
+
     // ---- what backward needs
     for (int t = 1; t < nt; ++t) {
         const Layer &P = st->layers[t - 1];
@@ -1471,7 +1657,7 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
     st->tensors[0].need_grad = opts->need_input_grad != 0;
     for (int t = 1; t < nt; ++t) {
         const Layer &P = st->layers[t - 1];
-        bool ng = has_params(P.d.kind) || st->tensors[st->tensors[P.a].root].need_grad;
+        bool ng = has_params(P.d.kind) || P.w_elems || st->tensors[st->tensors[P.a].root].need_grad;
         if (P.b >= 0) ng = ng || st->tensors[st->tensors[P.b].root].need_grad;
         st->tensors[t].need_grad = ng;
     }
@@ -1494,6 +1680,12 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
             break;
         case BAPIPE_RELU: case BAPIPE_SOFTMAX_XENT:
             st->tensors[L.o].stashed = true;
+            break;
+        case BAPIPE_ROTARY:
+            if (L.w_elems) RA.stashed = true;
+            break;
+        case BAPIPE_ATTENTION:
+            RA.stashed = st->tensors[L.o].stashed = true;
             break;
         case BAPIPE_MAXPOOL2D:
             if (RA.gated && RA.need_grad) st->tensors[L.o].stashed = true;   // pooled values gate the window
@@ -1535,6 +1727,20 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         if (T.fine) T.gparts *= 2;
     }
 
+    // gradients that ROTARY and ATTENTION write where they belong, others pass through a copy that adds or gates
+    for (int i = 0; i < n_layers; ++i) {
+        Layer &L = st->layers[i];
+        if (!has_heads(L.d.kind)) continue;
+        const Tensor &RA = st->tensors[root_of(L.a)];
+        size_t readers = 0;
+        for (int t = 0; t < nt; ++t)
+            if (root_of(t) == root_of(L.a)) readers += st->tensors[t].consumers.size();
+        for (int j = 0; j < n_layers; ++j)          // those whose output is the same storage do not count
+            if (st->tensors[j + 1].root != j + 1 && st->tensors[j + 1].root == root_of(L.a)) --readers;
+        L.by_copy = RA.need_grad && (RA.gated || readers > 1) && st->tensors[L.o].root == L.o;
+        if (L.d.kind == BAPIPE_ROTARY) L.dvalues_stay = L.values_stay && RA.need_grad && !L.by_copy;
+    }
+
     // ---- memory plan
     size_t slot = 0, trans = 0, gr = 0;
     for (int t = 0; t < nt; ++t) {
@@ -1548,6 +1754,11 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
     {   // gradient of the stage output (ingest target when the caller's dy cannot be used in place)
         Tensor &T = st->tensors[root_of(last_t)];
         if (st->layers[n_layers - 1].d.kind != BAPIPE_SOFTMAX_XENT && root_of(last_t) == last_t) { T.goff = gr; gr += align_up(T.bytes()); }
+    }
+    for (int i = 0; i < n_layers; ++i) {
+        Layer &L = st->layers[i];
+        if (L.half) { L.off_float = gr; gr += align_up(turning_elems(st, L) * sizeof(float)); }
+        if (L.by_copy) { L.off_d = gr; gr += align_up(st->tensors[L.a].bytes()); }
     }
     // conv -> max-pool fusion (bf16, halo kernel shapes): the conv output must be a transient tensor
     // read by that pool only
@@ -1625,6 +1836,26 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
                     grouped += align_up(w);
                 }
             }
+        }
+        if (L.d.kind == BAPIPE_ROTARY) {
+            if (L.half) {
+                const size_t n = turning_elems(st, L);
+                L.aux_off = L.off_half = slot; slot += align_up(n * sizeof(uint16_t));
+                L.off_scale = slot; slot += align_up(n / (A.C / (L.d.kh + 2 * L.d.kw)) * sizeof(float));
+                L.aux_bytes = slot - L.aux_off;
+            }
+            const size_t w = rotary_workspace(st->dt, rotary_shape(st, L, !L.dvalues_stay));
+            work = w > work ? w : work;
+        }
+        if (L.d.kind == BAPIPE_ATTENTION) {
+            const AttnShape q = attn_shape(st, L);
+            L.aux_off = slot; L.aux_bytes = (size_t)q.N * q.heads * q.T * sizeof(float); slot += align_up(L.aux_bytes);
+            if (q.mask == ATTN_SPANS && !st->off_bounds) {
+                st->off_spans = slot; slot += align_up((size_t)q.N * q.T * sizeof(int2));
+                st->off_bounds = slot; slot += align_up((size_t)q.N * ((q.T + kAttnTile - 1) / kAttnTile) * sizeof(int4));
+            }
+            const size_t w = attention_workspace(st->dt, q, st->compute_units);
+            work = w > work ? w : work;
         }
         if (L.d.kind == BAPIPE_LSTM) {
             const int N = micro_batch, T = A.H, In = A.Cp, H = L.d.cout, G = 4 * H;
@@ -1773,6 +2004,12 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         o_ww[i] = pb; pb += mat ? align_up(L.w_elems * es) : 0;
         o_wt[i] = pb; pb += mat ? align_up(L.w_elems * es) : 0;
     }
+    std::vector<size_t> o_table(n_layers);
+    for (int i = 0; i < n_layers; ++i) {
+        const Layer &L = st->layers[i];
+        o_table[i] = pb;
+        if (L.d.kind == BAPIPE_ROTARY) pb += align_up((size_t)st->tensors[L.a].H * (L.d.pad / 2) * sizeof(float2));
+    }
     st->params_bytes = pb;
 
     size_t defb = 0;
@@ -1823,6 +2060,12 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
     hipError_t e = fill_f32((float *)st->params, 0.f, st->params_bytes / 4, st->stream);
     for (int i = 0; i < n_layers && e == hipSuccess; ++i)
         if (is_norm(st->layers[i].d.kind)) e = fill_f32(st->layers[i].w, 1.f, st->layers[i].w_elems, st->stream);
+    for (int i = 0; i < n_layers && e == hipSuccess; ++i) {
+        Layer &L = st->layers[i];
+        if (L.d.kind != BAPIPE_ROTARY) continue;
+        L.table = (float2 *)(st->params + o_table[i]);
+        e = rotary_table(L.table, st->tensors[L.a].H, L.d.pad, {10000.0, 1.0, 0.0, 0.0, 0.0, 1.0, 0}, st->stream);
+    }
     if (e == hipSuccess) e = fill_f32(st->losses, 0.f, loss_words + 2 * kGatherTickets + kDropoutState, st->stream);
     if (e == hipSuccess) e = hipStreamSynchronize(st->stream);
     if (e != hipSuccess) return create_fail(BAPIPE_E_DEVICE, "initialisation: %s", hipGetErrorString(e));
@@ -1841,6 +2084,8 @@ int bapipe_stage_forward(bapipe_stage_t *st, int mb_id, const void *x_dev, void 
     const Tensor &In = st->tensors[0];
     const int dt = st->dt;
     hipStream_t s = st->stream;
+    if (st->span_T && !st->spans_given)
+        return st->fail(BAPIPE_E_ORDER, "forward: micro-batch %d has no spans (bapipe_stage_set_spans)", mb_id);
     if (mb_id == 0) st->loss_valid.assign(st->M, 0);       // a new mini-batch: the previous one's losses are gone
     if (st->stream_b && mb_id >= st->depth) HIPCHK(hipStreamWaitEvent(s, st->ev_bwd[mb_id - st->depth], 0));
     FwdCtx c{mb_id, nullptr};
@@ -1856,6 +2101,8 @@ int bapipe_stage_forward(bapipe_stage_t *st, int mb_id, const void *x_dev, void 
     } else {
         c.x_direct = x_dev;
     }
+    if (st->span_T)
+        HIPCHK(attention_spans(st->spans_given, (int2 *)(st->slot(mb_id) + st->off_spans), (int4 *)(st->slot(mb_id) + st->off_bounds), st->mb, st->span_T, s));
     const int last = (int)st->tensors.size() - 1;
     const Tensor &O = st->tensors[last];
     const Tensor &R = st->tensors[O.root];
@@ -1879,6 +2126,7 @@ int bapipe_stage_forward(bapipe_stage_t *st, int mb_id, const void *x_dev, void 
             HIPCHK(hipMemcpyAsync(y_dev, src, O.bytes(), hipMemcpyDeviceToDevice, s));
     }
     if (st->stream_b) HIPCHK(hipEventRecord(st->ev_fwd[mb_id], s));
+    st->spans_given = nullptr;
     st->n_fwd++;
     return BAPIPE_OK;
 }
@@ -1908,7 +2156,10 @@ int bapipe_stage_backward(bapipe_stage_t *st, int mb_id, const void *dy_dev_or_l
     c.pending.assign(st->tensors.size(), nullptr);
     const Tensor &In = st->tensors[0];
     const bool want_dx = In.need_grad && dx_dev != nullptr;
-    if (want_dx && (nhwc || In.H * In.W == 1) && In.Cp == In.C) c.dx_direct = dx_dev;
+    // ATTENTION reads and writes gradients in pieces of 16 bytes: a caller's that do not lie so pass through the stage's own
+    bool attends = false;
+    for (const Layer &L : st->layers) attends |= L.d.kind == BAPIPE_ATTENTION;
+    if (want_dx && (nhwc || In.H * In.W == 1) && In.Cp == In.C && !(attends && (uintptr_t)dx_dev % 16)) c.dx_direct = dx_dev;
     if (st->layers[nl - 1].d.kind == BAPIPE_SOFTMAX_XENT) {
         c.labels = (const int32_t *)dy_dev_or_labels;
     } else {
@@ -1928,7 +2179,7 @@ int bapipe_stage_backward(bapipe_stage_t *st, int mb_id, const void *dy_dev_or_l
             c.dy_nchw = dy_dev_or_labels;
         } else if ((!nhwc && R.H * R.W > 1) || flat_of_spatial) {
             HIPCHK(nchw_to_nhwc(dt, dy_dev_or_labels, st->gptr(last), e, st->mb, R.C, R.H, R.W, R.Cp, s));
-        } else if (e.gate || r == 0) {
+        } else if (e.gate || r == 0 || (attends && (uintptr_t)dy_dev_or_labels % 16)) {
             HIPCHK(grad_copy(dt, dy_dev_or_labels, st->gptr(last), e, O.elems, s));
         } else {
             c.dy_direct = dy_dev_or_labels;
@@ -2055,6 +2306,37 @@ int bapipe_stage_set_dropout(bapipe_stage_t *st, uint64_t seed, uint32_t mini_ba
     if (st->n_fwd != 0 || st->n_bwd != 0)
         return st->fail(BAPIPE_E_ORDER, "set_dropout: only between mini-batches (after create or step)");
     HIPCHK(dropout_set(st->dropout_state, seed, mini_batch, st->stream));
+    return BAPIPE_OK;
+}
+
+int bapipe_stage_set_spans(bapipe_stage_t *st, int mb_id, const int32_t *spans_dev)
+{
+    if (!st || !spans_dev) return st ? st->fail(BAPIPE_E_INVALID, "set_spans: NULL argument") : BAPIPE_E_INVALID;
+    if (!st->span_T) return st->fail(BAPIPE_E_INVALID, "set_spans: the stage has no ATTENTION layer with spans");
+    if (mb_id != st->n_fwd || mb_id >= st->M)
+        return st->fail(BAPIPE_E_ORDER, "set_spans: expected micro-batch %d of %d, got %d", st->n_fwd, st->M, mb_id);
+    if ((uintptr_t)spans_dev % sizeof(int32_t)) return st->fail(BAPIPE_E_INVALID, "set_spans: spans must be aligned to 4 bytes");
+    st->spans_given = spans_dev;
+    return BAPIPE_OK;
+}
+
+int bapipe_stage_set_rotary(bapipe_stage_t *st, int layer, const bapipe_rotary_t *angles)
+{
+    if (!st || !angles) return st ? st->fail(BAPIPE_E_INVALID, "set_rotary: NULL argument") : BAPIPE_E_INVALID;
+    if (layer < 0 || layer >= (int)st->layers.size() || st->layers[layer].d.kind != BAPIPE_ROTARY)
+        return st->fail(BAPIPE_E_INVALID, "set_rotary: layer %d is not a ROTARY", layer);
+    const bapipe_rotary_t &a = *angles;
+    const Layer &L = st->layers[layer];
+    const int T = st->tensors[L.a].H;
+    if (!(a.base > 0.0 && std::isfinite(a.base)) || !(a.factor > 0.0 && std::isfinite(a.factor)) || !(a.magnitude > 0.0 && a.magnitude <= FLT_MAX))
+        return st->fail(BAPIPE_E_INVALID, "set_rotary: base, factor and magnitude must be positive");
+    if (!(a.original_length >= 0.0 && std::isfinite(a.original_length)) ||
+        (a.original_length > 0.0 && !(a.low_turns < a.high_turns && std::isfinite(a.low_turns) && std::isfinite(a.high_turns))))
+        return st->fail(BAPIPE_E_INVALID, "set_rotary: original_length must not be negative, and with one low_turns must be below high_turns");
+    if (a.first_position < 0 || a.first_position > (1ll << 40)) return st->fail(BAPIPE_E_INVALID, "set_rotary: first_position must be 0 to 2^40");
+    if (st->n_fwd != 0 || st->n_bwd != 0)
+        return st->fail(BAPIPE_E_ORDER, "set_rotary: only between mini-batches (after create or step)");
+    HIPCHK(rotary_table(L.table, T, L.d.pad, {a.base, a.factor, a.original_length, a.low_turns, a.high_turns, a.magnitude, a.first_position}, st->stream));
     return BAPIPE_OK;
 }
 
@@ -2219,6 +2501,7 @@ int bapipe_profile_layers(bapipe_stage_t *st, int warmup, int iters, bapipe_laye
     HIPCHK(fill_f32((float *)st->slot(0), 0.f, st->slot_bytes / 4, s));
     HIPCHK(fill_f32((float *)st->transient, 0.f, st->transient_bytes / 4, s));
     HIPCHK(fill_f32((float *)st->grads, 0.f, st->grads_bytes / 4, s));
+    if (st->span_T) HIPCHK(attention_spans(nullptr, (int2 *)(st->slot(0) + st->off_spans), (int4 *)(st->slot(0) + st->off_bounds), st->mb, st->span_T, s));
     hipEvent_t e0, e1;
     HIPCHK(hipEventCreate(&e0));
     HIPCHK(hipEventCreate(&e1));
