@@ -33,8 +33,6 @@ template <class T, int DP, int R = 0> struct AtTile {
     static constexpr int STEPS = CH / 2;                              // a step of a row product takes two chunks, one for each half
     static constexpr int ROWS = R ? R : RB <= 512 ? 64 : 32;
     static constexpr int BYTES = ROWS * RB;
-    static constexpr int ISSUES = ROWS * CH / AT_TPB;                 // 16-byte loads of a thread for a tile
-    static_assert(ROWS * CH % AT_TPB == 0, "");
     static __device__ __forceinline__ int at(int group, int row, int chunk) { return (group * ROWS + row) * 64 + ((chunk ^ ((row >> 2) & 3)) << 4); }
     // row and chunk of the i-th 16 bytes
     static __device__ __forceinline__ int row_of(int i) { return i / 4 % ROWS; }
@@ -53,15 +51,28 @@ template <class T> __device__ __forceinline__ void at_mma(f32x16_t &acc, chunk16
         for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), acc, 0, 0, 0);
 }
 
+// The order of N LDS reads and as many matrix instructions: AHEAD reads first, then one for every instruction
+template <int N, int AHEAD> __device__ __forceinline__ void at_order()
+{
+    constexpr int first = AHEAD < N ? AHEAD : N;
+    __builtin_amdgcn_sched_group_barrier(0x100, first, 0);
+#pragma unroll
+    for (int i = 0; i < N - first; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, first, 0);
+}
+
 // acc = 32 streamed rows from row0 of the tile x owned rows
-template <class T, class Tile> __device__ __forceinline__ f32x16_t at_rows(const unsigned char *tile, int row0, const chunk16 *own, int lane)
+template <class T, class Tile>
+__device__ __forceinline__ void at_rows(f32x16_t &acc, const unsigned char *tile, int row0, const chunk16 (&own)[Tile::STEPS], int lane)
 {
     const int row = lane & 31, h = lane >> 5;
-    f32x16_t acc = {};
+    acc = f32x16_t{};
 #pragma unroll
     for (int c = 0; c < Tile::STEPS; ++c)
         at_mma<T>(acc, *(const chunk16 *)(tile + Tile::at(0, row, 2 * (c & 1) + h) + ((c >> 1) * Tile::ROWS + row0) * 64), own[c]);
-    return acc;
 }
 
 // The right operand of a product that sums over 32 streamed rows: the registers of at_rows, in the storage type
@@ -148,52 +159,88 @@ template <class T, int DP, bool VEC> __device__ __forceinline__ void at_own(chun
 
 // dma16 of a resource that differs from tile to tile: it may have been written by a vector instruction (a lane read back from a spilled
 // scalar) just before, which a load has to be five states behind of, and the compiler counts none inside of assembly
-__device__ __forceinline__ void at_dma16(__amdgpu_buffer_rsrc_t rsrc, unsigned lds_addr, unsigned voffset)
+// OFF: more bytes of the address in memory; the instruction adds them to that in LDS too, from which they are taken off
+template <int OFF> __device__ __forceinline__ void at_dma16(__amdgpu_buffer_rsrc_t rsrc, unsigned lds_addr, unsigned voffset)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_addr), "v"(voffset), "s"(rsrc));
+    static_assert(OFF >= 0 && OFF < 4096, "");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen offset:%3 lds" ::"s"(lds_addr - OFF), "v"(voffset), "s"(rsrc), "n"(OFF));
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t at_resource(const void *from, int bytes)
+{
+    const uint64_t address = (uint64_t)(uintptr_t)from;
+    const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)address), high = __builtin_amdgcn_readfirstlane((uint32_t)(address >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc((void *)(((uint64_t)high << 32) | low), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+
+// v, of which the compiler does not know that it is the same every time: what is made of it in a loop is made there again, in a few instructions,
+// and does not occupy registers all the while.  (A register that is spilled is read back behind all loads under way.)
+__device__ __forceinline__ int at_again(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// 4 bytes a lane, of rows of a tile's: lane l's word lands at lds_addr + 4 l, zero from word `words` on
+__device__ __forceinline__ void at_dma4(const void *from, int words, unsigned lds_addr, int tid)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds_addr), "v"((at_again(tid) & 63) * 4),
+                 "s"(at_resource(from, words > 0 ? words * 4 : 0)));
 }
 
 // Fills tiles from rows of d elements, `stride` elements apart.  VEC: d a multiple of a chunk and 16-byte aligned rows; asynchronous,
 // complete after WAIT_VMCNT(0) and a barrier.  Rows that are not there, and what is behind d, are zeros: zero times zero is what the products
 // see of them, whatever memory holds.
-template <class T, int DP, bool VEC, int R = 0> struct AtStream {
+// AGAIN: a lane's place is worked out again for every tile (see at_again), else it is kept.
+template <class T, int DP, bool VEC, int R = 0, bool AGAIN = true> struct AtStream {
     typedef AtTile<T, DP, R> Tile;
-    static constexpr int STEP = AT_TPB / Tile::ROWS;      // chunks of a row that the block loads at once
-    unsigned voff = 0;       // of the lane's first chunk
-    int chunk = 0;
+    static constexpr int TPB = AT_TPB, STEP = TPB / Tile::ROWS, ISSUES = Tile::ROWS * Tile::CH / TPB;      // chunks of a row that the block loads at once, and how often
+    static_assert(Tile::ROWS * Tile::CH % TPB == 0, "");
+    int row = 0, chunk = 0;
+    unsigned voff = 0;
     __device__ __forceinline__ AtStream(int stride, int tid)
     {
-        if constexpr (VEC) {
-            static_assert(STEP % 4 == 0, "");
-            const int row = Tile::row_of(tid);
-            chunk = Tile::chunk_of(tid);
-            const long long at = (long long)row * stride * (int)sizeof(T) + chunk * 16;
-            voff = at < (1ll << 31) ? (unsigned)at : 0x80000000u;      // no row of a tensor lies behind 2 GiB
+        static_assert(STEP % 4 == 0, "");
+        if (VEC && !AGAIN) place(stride, tid);
+    }
+    __device__ __forceinline__ void place(int stride, int tid)
+    {
+        row = Tile::row_of(tid);
+        chunk = Tile::chunk_of(tid);
+        voff = (unsigned)row * (unsigned)(stride * (int)sizeof(T)) + chunk * 16;
+    }
+    template <int I> static __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t rsrc, unsigned lds_addr, unsigned at, int chunk, int chunks)
+    {
+        if constexpr (I < ISSUES) {
+            at_dma16<I * STEP * 16>(rsrc, lds_addr + I * TPB * 16, chunk < chunks - I * STEP ? at : 0x80000000u);
+            issue<I + 1>(rsrc, lds_addr, at, chunk, chunks);
         }
     }
-    // from: the tile's first row; rows: how many there are from it on
-    __device__ __forceinline__ void fill(unsigned char *tile, const lds_addr_of &lds, const T *from, int rows, int stride, int d, int tid) const
+    // to: the tile's place in the block's LDS, which begins at `lds`; from: the tile's first row; rows: how many there are from it on
+    __device__ __forceinline__ void fill(unsigned char *smem, unsigned lds, int to, const T *from, int rows, int stride, int d, int tid)
     {
         if constexpr (VEC) {
             const int n = rows < Tile::ROWS ? rows : Tile::ROWS;
             const int bytes = n > 0 ? (int)(((long long)(n - 1) * stride + d) * (int)sizeof(T)) : 0;
-            const uint64_t place = (uint64_t)(uintptr_t)from;
-            const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)place), high = __builtin_amdgcn_readfirstlane((uint32_t)(place >> 32));
-            const __amdgpu_buffer_rsrc_t rsrc =
-                __builtin_amdgcn_make_buffer_rsrc((void *)(((uint64_t)high << 32) | low), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
-            unsigned at = voff;
-            asm volatile("" : "+v"(at));        // else every load's address is kept in a register of its own
-#pragma unroll
-            for (int i = 0; i < Tile::ISSUES; ++i)
-                at_dma16(rsrc, lds(tile + (i * AT_TPB + (tid & ~63)) * 16), (chunk + i * STEP) * Tile::EPC < d ? at + i * STEP * 16 : 0x80000000u);
+            const __amdgpu_buffer_rsrc_t rsrc = at_resource(from, bytes);
+            if (AGAIN) place(stride, at_again(tid));
+            const unsigned at = row < n ? voff : 0x80000000u;      // rows that are there lie within 2 GiB
+            const unsigned lds_addr = lds + to + (unsigned)__builtin_amdgcn_readfirstlane(tid >> 6) * 1024;
+            if (d == DP) issue<0>(rsrc, lds_addr, at, 0, 1 << 20);
+            else issue<0>(rsrc, lds_addr, at, chunk, d / Tile::EPC);
         } else {
+            constexpr int AT_ONCE = 32 / Tile::EPC < ISSUES ? 32 / Tile::EPC : ISSUES;      // 32 loads under way
+            static_assert(ISSUES % AT_ONCE == 0, "");
 #pragma unroll 1
-            for (int i = 0; i < Tile::ISSUES; ++i) {
-                const int at = i * AT_TPB + tid, row = Tile::row_of(at), e0 = Tile::chunk_of(at) * Tile::EPC;
-                vec_t<T, Tile::EPC> v;
+            for (int i0 = 0; i0 < ISSUES; i0 += AT_ONCE) {
+                vec_t<T, Tile::EPC> v[AT_ONCE];
 #pragma unroll
-                for (int j = 0; j < Tile::EPC; ++j) v.e[j] = row < rows && e0 + j < d ? from[(size_t)row * stride + e0 + j] : at_zero<T>();
-                *(chunk16 *)(tile + at * 16) = __builtin_bit_cast(chunk16, v);
+                for (int i = 0; i < AT_ONCE; ++i) {
+                    const int at = (i0 + i) * TPB + tid, row = Tile::row_of(at), e0 = Tile::chunk_of(at) * Tile::EPC;
+#pragma unroll
+                    for (int j = 0; j < Tile::EPC; ++j) v[i].e[j] = row < rows && e0 + j < d ? from[(size_t)row * stride + e0 + j] : at_zero<T>();
+                }
+#pragma unroll
+                for (int i = 0; i < AT_ONCE; ++i) *(chunk16 *)(smem + to + ((i0 + i) * TPB + tid) * 16) = __builtin_bit_cast(chunk16, v[i]);
             }
         }
     }
@@ -240,16 +287,18 @@ __device__ __forceinline__ void at_bend(float (&x)[16], const AtScore &p, float 
     if (SLOPE)
 #pragma unroll
         for (int i = 0; i < 16; ++i) slope[i] = 1.0f;
-    if (p.cap > 0.0f)
+    if (p.cap > 0.0f) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const float th = at_tanh<T>(x[i] * p.per_cap);
             x[i] = p.cap * th;
             if (SLOPE) slope[i] = 1.0f - th * th;
         }
-    if (p.fall != 0.0f)
+    }
+    if (p.fall != 0.0f) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] -= p.fall * fabsf(distance - (float)(8 * (i >> 2) + (i & 3)));
+    }
 }
 
 // keys that the query at t of sample n sees: [x, y), none where x >= y
@@ -290,6 +339,9 @@ __device__ __forceinline__ AtBlock at_block(const AttnShape &s)
     const int of = s.N * s.groups, ng = blockIdx.x % of;
     return {ng / s.groups, ng % s.groups, (int)(blockIdx.x / of)};
 }
+
+// address of the dynamic LDS
+__device__ __forceinline__ unsigned at_lds(const unsigned char *smem) { return __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void_t *)smem); }
 
 __device__ __forceinline__ void at_barrier()
 {

@@ -252,7 +252,9 @@ struct AttnArgs {
     void *o;                 // [N][T][heads d]
     float *lse;              // [N][heads][T]: log2 of a query's sum of exponentials, inf where it sees nothing
     const int2 *spans;       // [N][T], ATTN_SPANS: first key and end; of attention_spans
-    const int4 *bounds;      // [N][tiles of kAttnTile queries]: smallest first, largest end of those that see something; largest first, smallest end of all
+    // [N][tiles of kAttnTile queries][2]: smallest first, largest end of those that see something, largest first, smallest end of all (0 with one that
+    // sees nothing); how many there are up to the last that sees something
+    const int4 *bounds;
     // backward
     const void *dout;        // as o
     float *dsum;             // [N][heads][T]: dout . o, of the first of its two kernels to the second

@@ -14,10 +14,9 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
     typedef AtTile<S, DP, R> STile;
     constexpr int ND = DP / 32, SUBS = Tile::ROWS / 32, STREAMS = HALF ? 3 : 2;
     extern __shared__ __align__(256) unsigned char smem[];
-    __shared__ __align__(16) float row_scale[2][HALF ? Tile::ROWS : 4];
     __shared__ int2 block_range[AT_WAVES];
     const AttnShape &s = p.s;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int d = s.d, stride = s.stride(), per = s.heads / s.groups;
     const AtBlock b = at_block(s);
     const int blocks = (s.T + AT_ROWS - 1) / AT_ROWS, head = b.g * per + b.rest % per, q0 = (blocks - 1 - b.rest / per) * AT_ROWS;
@@ -38,6 +37,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
     {
         chunk16 o[Tile::STEPS];
         at_own<T, DP, VEC>(o, sees ? (const T *)p.o + at_o : nullptr, d, lane);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < Tile::STEPS; ++c)
 #pragma unroll
@@ -62,23 +62,22 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
     const AtScore score = at_score(s, head);
     float by = score.scale;
     if (HALF && sees) by *= p.half_scale[((size_t)head * s.N + b.n) * s.T + q];
-    const lds_addr_of lds(smem);
-    const AtStream<S, DP, VEC, R> score_stream(sstride, tid);
-    const AtStream<T, DP, VEC, R> stream(stride, tid);
-    float next_scale = 0.0f;
+    const unsigned lds = at_lds(smem);
+    AtStream<S, DP, VEC, R> score_stream(sstride, tid);
+    AtStream<T, DP, VEC, R> stream(stride, tid);
+    constexpr int SCALE_AT = 2 * STREAMS * Tile::BYTES;      // 64 words, twice
     auto fill = [&](int it) {
         const int k0 = first + it * Tile::ROWS;
-        unsigned char *to = smem + (it & 1) * STREAMS * Tile::BYTES;
-        if (HALF && tid < Tile::ROWS) next_scale = k0 + tid < end ? key_scale[k0 + tid] : 0.0f;
-        stream.fill(to, lds, keys + (size_t)k0 * stride, end - k0, stride, d, tid);
-        stream.fill(to + Tile::BYTES, lds, values + (size_t)k0 * stride, end - k0, stride, d, tid);
-        if (HALF) score_stream.fill(to + 2 * Tile::BYTES, lds, score_keys + (size_t)k0 * sstride, end - k0, sstride, d, tid);
+        const int to = (it & 1) * STREAMS * Tile::BYTES;
+        if (HALF && wave == 0) at_dma4(key_scale + k0, end - k0, lds + SCALE_AT + (it & 1) * 256, tid);
+        stream.fill(smem, lds, to, keys + (size_t)k0 * stride, end - k0, stride, d, tid);
+        stream.fill(smem, lds, to + Tile::BYTES, values + (size_t)k0 * stride, end - k0, stride, d, tid);
+        if (HALF) score_stream.fill(smem, lds, to + 2 * Tile::BYTES, score_keys + (size_t)k0 * sstride, end - k0, sstride, d, tid);
     };
     f32x16_t dq[ND] = {};
     const int tiles = (end - first + Tile::ROWS - 1) / Tile::ROWS;
     if (tiles > 0) fill(0);
     for (int it = 0; it < tiles; ++it) {
-        if (HALF && tid < Tile::ROWS) row_scale[it & 1][tid] = next_scale;
         WAIT_VMCNT(0);
         at_barrier();
         if (it + 1 < tiles) fill(it + 1);
@@ -88,7 +87,9 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
         const bool whole = k0 >= range.all.x && k0 + Tile::ROWS <= range.all.y;
 #pragma unroll 1
         for (int u = 0; u < SUBS; ++u) {
-            const f32x16_t w = at_rows<S, STile>(score_key, 32 * u, query, lane), dw = at_rows<T, Tile>(value, 32 * u, dout, lane);
+            f32x16_t w, dw;
+            at_rows<S, STile>(w, score_key, 32 * u, query, lane);
+            at_rows<T, Tile>(dw, value, 32 * u, dout, lane);
             float x[16], ds[16], slope[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -98,22 +99,23 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
             if (HALF)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const float4 r = *(const float4 *)&row_scale[it & 1][32 * u + 8 * g + 4 * h];
+                    const float4 r = *(const float4 *)(smem + SCALE_AT + (it & 1) * 256 + 4 * (32 * u + 8 * g + 4 * h));
                     x[4 * g] *= r.x; x[4 * g + 1] *= r.y; x[4 * g + 2] *= r.z; x[4 * g + 3] *= r.w;
                 }
             if (EXTRA) at_bend<T, true>(x, score, by, (float)(q - (k0 + 32 * u + 4 * h)), slope);
             const float unit = EXTRA ? 1.0f : by;
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], unit, -lse));
-            if (!whole)
+            if (!whole) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int k = k0 + 32 * u + 8 * (i >> 2) + 4 * h + (i & 3);
                     x[i] = k >= span.x && k < span.y ? x[i] : 0.0f;
                 }
+            }
 #pragma unroll
             for (int i = 0; i < 16; ++i) ds[i] = EXTRA ? x[i] * ds[i] * slope[i] : x[i] * ds[i];
-            at_columns<T, Tile, ND>(dq, key, 32 * u, 0, AtWeights<T>(ds), lane);
+            at_columns<T, Tile>(dq, key, 32 * u, 0, AtWeights<T>(ds), lane);
         }
     }
     if (q >= s.T) return;
@@ -125,7 +127,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Queries {
     static hipError_t go(const AttnArgs &a, hipStream_t stream)
     {
-        constexpr int smem = HALF ? 6 * AtTile<T, DP, DP >= 128 ? 32 : 0>::BYTES : 4 * AtTile<T, DP>::BYTES;
+        constexpr int smem = HALF ? 6 * AtTile<T, DP, DP >= 128 ? 32 : 0>::BYTES + 512 : 4 * AtTile<T, DP>::BYTES;
         return at_launch(k_attention_dq<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS - 1) / AT_ROWS), smem, a, stream);
     }
 };

@@ -1,21 +1,27 @@
 // Attention, forward: o = softmax(scores) v in one pass over the keys, with a running maximum and sum per query.
 #include "attention_common.h"
 
+#ifndef VR
+#define VR 32
+#endif
 namespace bapipe {
 namespace {
 
+// Rows of a tile.  bf16 heads of 192 and 256 channels: with 32 keys at a time registers and LDS hold two blocks a unit (TODO)
+template <class T, int DP> constexpr int kFwdRows = sizeof(T) == 2 && DP > 128 ? VR : 0;
+
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF>
-__global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void k_attention_fwd(AttnArgs p)
+__global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && (DP <= 128 || VR) ? 2 : DP * (int)sizeof(T) <= 256 ? 2 : 1)) void k_attention_fwd(AttnArgs p)
 {
-    typedef AtTile<T, DP> Tile;
+    constexpr int R = kFwdRows<T, DP>;
+    typedef AtTile<T, DP, R> Tile;
     typedef std::conditional_t<HALF, half_t, T> S;       // what scores are made of
-    typedef AtTile<S, DP, 0> STile;
+    typedef AtTile<S, DP, R> STile;
     constexpr int ND = DP / 32, SUBS = Tile::ROWS / 32;
     extern __shared__ __align__(256) unsigned char smem[];
-    __shared__ __align__(16) float row_scale[2][HALF ? Tile::ROWS : 4];
     __shared__ int2 block_range[AT_WAVES];
     const AttnShape &s = p.s;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int d = s.d, stride = s.stride(), per = s.heads / s.groups;
     const AtBlock b = at_block(s);
     // queries with the most keys first
@@ -44,23 +50,22 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
     const AtScore score = at_score(s, head);
     float by = score.scale;
     if (HALF && q < s.T) by *= p.half_scale[((size_t)head * s.N + b.n) * s.T + q];
-    const lds_addr_of lds(smem);
-    const AtStream<S, DP, VEC> key_stream(sstride, tid);
-    const AtStream<T, DP, VEC> value_stream(stride, tid);
-    float next_scale = 0.0f;
+    const unsigned lds = at_lds(smem);
+    AtStream<S, DP, VEC, R, (DP > 192)> key_stream(sstride, tid);
+    AtStream<T, DP, VEC, R, (DP > 192)> value_stream(stride, tid);
+    constexpr int SCALE_AT = 2 * 2 * Tile::BYTES;      // 64 words, twice
     auto fill = [&](int it) {
         const int k0 = first + it * Tile::ROWS;
-        unsigned char *to = smem + (it & 1) * 2 * Tile::BYTES;
-        if (HALF && tid < Tile::ROWS) next_scale = k0 + tid < end ? key_scale[k0 + tid] : 0.0f;
-        key_stream.fill(to, lds, keys + (size_t)k0 * sstride, end - k0, sstride, d, tid);
-        value_stream.fill(to + Tile::BYTES, lds, values + (size_t)k0 * stride, end - k0, stride, d, tid);
+        const int to = (it & 1) * 2 * Tile::BYTES;
+        if (HALF && wave == 0) at_dma4(key_scale + k0, end - k0, lds + SCALE_AT + (it & 1) * 256, tid);
+        key_stream.fill(smem, lds, to, keys + (size_t)k0 * sstride, end - k0, sstride, d, tid);
+        value_stream.fill(smem, lds, to + Tile::BYTES, values + (size_t)k0 * stride, end - k0, stride, d, tid);
     };
     f32x16_t out[ND] = {};
     float top = -__builtin_inff(), sum = 0.0f;            // sum: of this half's keys
     const int tiles = (end - first + Tile::ROWS - 1) / Tile::ROWS;        // none where nobody sees anything
     if (tiles > 0) fill(0);
     for (int it = 0; it < tiles; ++it) {
-        if (HALF && tid < Tile::ROWS) row_scale[it & 1][tid] = next_scale;
         WAIT_VMCNT(0);
         at_barrier();                                      // the tile has arrived, the other one is read
         if (it + 1 < tiles) fill(it + 1);
@@ -70,23 +75,25 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
         float x[SUBS][16];
 #pragma unroll
         for (int u = 0; u < SUBS; ++u) {
-            const f32x16_t w = at_rows<S, STile>(key, 32 * u, query, lane);
+            f32x16_t w;
+            at_rows<S, STile>(w, key, 32 * u, query, lane);
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[u][i] = w[i];
             if (HALF)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const float4 r = *(const float4 *)&row_scale[it & 1][32 * u + 8 * g + 4 * h];
+                    const float4 r = *(const float4 *)(smem + SCALE_AT + (it & 1) * 256 + 4 * (32 * u + 8 * g + 4 * h));
                     x[u][4 * g] *= r.x; x[u][4 * g + 1] *= r.y; x[u][4 * g + 2] *= r.z; x[u][4 * g + 3] *= r.w;
                 }
         }
+        if (sizeof(T) == 2) at_order<SUBS * Tile::STEPS, 4>();
         if (EXTRA)
 #pragma unroll
             for (int u = 0; u < SUBS; ++u) {
                 float none[16];
                 at_bend<T, false>(x[u], score, by, (float)(q - (k0 + 32 * u + 4 * h)), none);
             }
-        if (!(k0 >= range.all.x && k0 + Tile::ROWS <= range.all.y))
+        if (!(k0 >= range.all.x && k0 + Tile::ROWS <= range.all.y)) {
 #pragma unroll
             for (int u = 0; u < SUBS; ++u)
 #pragma unroll
@@ -94,6 +101,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
                     const int k = k0 + 32 * u + 8 * (i >> 2) + 4 * h + (i & 3);
                     x[u][i] = k >= span.x && k < span.y ? x[u][i] : -__builtin_inff();
                 }
+        }
         const float unit = EXTRA ? 1.0f : by;
         float most = x[0][0];
 #pragma unroll
@@ -118,7 +126,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
                 x[u][i] = __builtin_amdgcn_exp2f(fmaf(x[u][i], unit, -less));
                 sum += x[u][i];
             }
-            at_columns<T, Tile, ND>(out, value, 32 * u, 0, AtWeights<T>(x[u]), lane);
+            at_columns<T, Tile>(out, value, 32 * u, 0, AtWeights<T>(x[u]), lane);
         }
     }
     sum = at_halves_sum(sum);
@@ -131,7 +139,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Forward {
     static hipError_t go(const AttnArgs &a, hipStream_t stream)
     {
-        return at_launch(k_attention_fwd<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS - 1) / AT_ROWS), 4 * AtTile<T, DP>::BYTES, a, stream);
+        return at_launch(k_attention_fwd<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS - 1) / AT_ROWS), 4 * AtTile<T, DP, kFwdRows<T, DP>>::BYTES + (HALF ? 512 : 0), a, stream);
     }
 };
 
@@ -140,12 +148,14 @@ __global__ __launch_bounds__(64) void k_attention_spans(const int32_t *given, in
 {
     const int lane = threadIdx.x, n = blockIdx.y, t = blockIdx.x * kAttnTile + lane;
     int4 b = {T, 0, 0, T};
+    int count = 0;
     if (t < T) {
         const size_t at = (size_t)n * T + t;
         int2 v = given ? int2{max(given[2 * at], 0), min(given[2 * at + 1], T)} : int2{0, t + 1};
         if (v.x >= v.y) v = {0, 0};
         spans[at] = v;
         b = v.x < v.y ? int4{v.x, v.y, v.x, v.y} : int4{T, 0, T, 0};
+        count = v.x < v.y ? lane + 1 : 0;
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
@@ -153,8 +163,12 @@ __global__ __launch_bounds__(64) void k_attention_spans(const int32_t *given, in
         b.y = max(b.y, __shfl_xor(b.y, o, 64));
         b.z = max(b.z, __shfl_xor(b.z, o, 64));
         b.w = min(b.w, __shfl_xor(b.w, o, 64));
+        count = max(count, __shfl_xor(count, o, 64));
     }
-    if (lane == 0) bounds[(size_t)n * gridDim.x + blockIdx.x] = b;
+    if (lane == 0) {
+        bounds[2 * ((size_t)n * gridDim.x + blockIdx.x)] = b;
+        bounds[2 * ((size_t)n * gridDim.x + blockIdx.x) + 1] = {count, 0, 0, 0};
+    }
 }
 
 }  // namespace
@@ -166,7 +180,7 @@ hipError_t attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int 
     for (int n = 0; n < N; n += 65535) {
         const size_t at = (size_t)n * T;
         hipLaunchKernelGGL(k_attention_spans, dim3((unsigned)tiles, (unsigned)(N - n < 65535 ? N - n : 65535)), dim3(64), 0, s, given ? given + 2 * at : nullptr,
-                           spans + at, bounds + (size_t)n * tiles, T);
+                           spans + at, bounds + (size_t)n * 2 * tiles, T);
     }
     return hipGetLastError();
 }

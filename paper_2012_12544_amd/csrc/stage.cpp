@@ -1852,7 +1852,7 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
             L.aux_off = slot; L.aux_bytes = (size_t)q.N * q.heads * q.T * sizeof(float); slot += align_up(L.aux_bytes);
             if (q.mask == ATTN_SPANS && !st->off_bounds) {
                 st->off_spans = slot; slot += align_up((size_t)q.N * q.T * sizeof(int2));
-                st->off_bounds = slot; slot += align_up((size_t)q.N * ((q.T + kAttnTile - 1) / kAttnTile) * sizeof(int4));
+                st->off_bounds = slot; slot += align_up((size_t)q.N * ((q.T + kAttnTile - 1) / kAttnTile) * 2 * sizeof(int4));
             }
             const size_t w = attention_workspace(st->dt, q, st->compute_units);
             work = w > work ? w : work;
