@@ -259,46 +259,47 @@ struct AtScore {
 };
 __device__ __forceinline__ AtScore at_score(const AttnShape &a, int head)
 {
+    auto uniform = [](float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); };
     AtScore s;
     s.scale = a.scale * kLog2e;
-    s.cap = a.cap * kLog2e;
+    s.cap = uniform(a.cap * kLog2e);
     s.per_cap = a.cap > 0.0f ? 1.0f / s.cap : 0.0f;
-    s.fall = a.bias ? kLog2e * exp2f(-(float)a.bias * (float)(head + 1) / (float)a.heads) : 0.0f;
-    s.fall = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s.fall)));
-    s.cap = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s.cap)));
+    s.fall = uniform(a.bias ? kLog2e * exp2f(-(float)a.bias * (float)(head + 1) / (float)a.heads) : 0.0f);
     return s;
 }
-// tanh: near zero, where the difference would cancel, its series (off by less than 2^-21 of it at 1/4); float stages call the function
-template <class T> __device__ __forceinline__ float at_tanh(float x)
-{
-    if constexpr (sizeof(T) == 4) return tanhf(x);
-    const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.0f * kLog2e * x)), q = x * x;
-    const float near = x * (1.0f + q * (-1.0f / 3.0f + q * (2.0f / 15.0f - q * (17.0f / 315.0f))));
-    return fabsf(x) < 0.25f ? near : far;
-}
-// Scores of at_rows to logarithms base 2, register i of a key (or query) `off` + 8 (i / 4) + i % 4 further on than the first; slope receives the
-// derivative of the cap.  The registers are taken out of the product one by one first: with elements of the vector changed behind branches
-// the compiler has stored one of them over its neighbours where accumulators lie in AGPRs (float heads of 128, bf16 ones of 256 channels).
+// Scores of at_rows to logarithms base 2, register i of a key (or query) 8 (i / 4) + i % 4 further on than the first; slope receives the
+// derivative of the cap.  tanh x = 1 - 2 r with r = 1 / (1 + e^2x), whose derivative is 4 r (1 - r).  In a bf16 stage that is off by 2^-24 of the
+// cap, which caps of up to 4096 can afford; above them, and in float stages, the function is called.
+// The registers are taken out of the product one by one first: with elements of the vector changed behind branches the compiler has stored one
+// of them over its neighbours where accumulators lie in AGPRs (float heads of 128, bf16 ones of 256 channels).
 template <class T, bool SLOPE>
 __device__ __forceinline__ void at_bend(float (&x)[16], const AtScore &p, float by, float distance, float (&slope)[16])
 {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] *= by;
     if (SLOPE)
 #pragma unroll
         for (int i = 0; i < 16; ++i) slope[i] = 1.0f;
-    if (p.cap > 0.0f) {
+    if (sizeof(T) == 2 && p.cap > 0.0f && p.cap < 4096.0f * kLog2e) {
+        const float twice = by * p.per_cap * (2.0f * kLog2e);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const float th = at_tanh<T>(x[i] * p.per_cap);
-            x[i] = p.cap * th;
-            if (SLOPE) slope[i] = 1.0f - th * th;
+            const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[i] * twice));
+            x[i] = fmaf(-2.0f * p.cap, r, p.cap);
+            if (SLOPE) slope[i] = 4.0f * r * (1.0f - r);
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] *= by;
+        if (p.cap > 0.0f)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float th = tanhf(x[i] * p.per_cap);
+                x[i] = p.cap * th;
+                if (SLOPE) slope[i] = 1.0f - th * th;
+            }
     }
-    if (p.fall != 0.0f) {
+    if (p.fall != 0.0f)
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] -= p.fall * fabsf(distance - (float)(8 * (i >> 2) + (i & 3)));
-    }
 }
 
 // keys that the query at t of sample n sees: [x, y), none where x >= y

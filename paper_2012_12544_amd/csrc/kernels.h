@@ -250,6 +250,8 @@ struct AttnArgs {
     const void *half;
     const float *half_scale;
     void *o;                 // [N][T][heads d]
+    // forward, or NULL: a second place for o; for qk (and v, which is the same tensor then; d a multiple of 16 bytes, 16-byte aligned)
+    void *o2, *copy;
     float *lse;              // [N][heads][T]: log2 of a query's sum of exponentials, inf where it sees nothing
     const int2 *spans;       // [N][T], ATTN_SPANS: first key and end; of attention_spans
     // [N][tiles of kAttnTile queries][2]: smallest first, largest end of those that see something, largest first, smallest end of all (0 with one that
@@ -266,7 +268,7 @@ struct AttnArgs {
 // spans clamped to [0, T], and the tiles' bounds; given NULL: every position sees those up to itself
 hipError_t attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int N, int T, hipStream_t s);
 hipError_t attention_fwd(int dt, const AttnArgs &a, hipStream_t s);
-size_t attention_workspace(int dt, const AttnShape &a, int compute_units);          // of a backward pass
+size_t attention_workspace(int dt, const AttnShape &a, bool half, int compute_units);          // of a backward pass; half: with AttnArgs::half
 hipError_t attention_bwd(int dt, AttnArgs a, void *workspace, int compute_units, hipStream_t s);
 hipError_t attention_dq(int dt, const AttnArgs &a, hipStream_t s);
 hipError_t attention_dkv(int dt, const AttnArgs &a, hipStream_t s);
@@ -289,8 +291,9 @@ struct RotaryAngles {
 hipError_t rotary_table(float2 *table, int T, int rotated, const RotaryAngles &a, hipStream_t s);
 // gains: [2][d], of query heads, of key heads; y may be x
 // half, half_scale: where an ATTENTION's AttnArgs find them (bf16), or NULL
+// copy: a second place for x, or NULL
 hipError_t rotary_fwd(int dt, const RotaryShape &r, const void *x, void *y, const float2 *table, const float *gains, hipStream_t s, void *half = nullptr,
-                      float *half_scale = nullptr);
+                      float *half_scale = nullptr, void *copy = nullptr);
 size_t rotary_workspace(int dt, const RotaryShape &r);
 // x, gains, dgains (added to) and the workspace only with a norm; dx may be dy or, where there is nothing to give it to, NULL
 // dy_float: NULL, or (bf16) where the gradients of query and key heads are instead, [rows][heads + groups][d]

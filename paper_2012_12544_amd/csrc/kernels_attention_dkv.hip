@@ -237,16 +237,18 @@ template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Keys {
     }
 };
 
-// In how many parts the queries of the keys' sums are taken: a block owns 128 keys of a key head, for all query heads that share it, and few
-// of them leave units idle or, with a causal mask, waiting for the longest.
-int key_splits(int dt, const AttnShape &s, int compute_units)
+// In how many parts the queries of the keys' sums are taken.  A block owns 128 keys of a key head, for all query heads that share it: few of
+// them leave units idle or, where keys are seen by different numbers of queries, waiting for the longest.  Splits cost a pass over their sums:
+// 12 heads of 80, 3 x 1003 positions without a mask, 288 blocks of the 512 that fit, us: 69 in one part, 59 and 14 in three.
+int key_splits(int dt, const AttnShape &s, bool half, int compute_units)
 {
-    const int halves = dt == DT_F32 && s.d > 128 ? 2 : 1, units = compute_units > 0 ? compute_units : 256;
-    const long long blocks = (long long)s.N * s.groups * ((s.T + AT_ROWS - 1) / AT_ROWS) * halves;
-    const int per = s.heads / s.groups, tiles = (s.T + 63) / 64 * per;           // of queries
-    int splits = (int)(4 * units / blocks);
+    const bool wide = dt == DT_F32 ? s.d > 64 : half ? s.d > 96 : s.d > 128;
+    const long long fit = (long long)(compute_units > 0 ? compute_units : 256) * (wide ? 1 : 2);
+    const long long blocks = (long long)s.N * s.groups * ((s.T + AT_ROWS - 1) / AT_ROWS) * (dt == DT_F32 && s.d > 128 ? 2 : 1);
+    const long long tiles = (long long)((s.T + 63) / 64) * (s.heads / s.groups);           // of queries
+    long long splits = s.mask == ATTN_NONE ? fit / blocks : (2 * fit + blocks / 2) / blocks;
     if (splits > tiles / 4) splits = tiles / 4;
-    return splits > 16 ? 16 : splits > 1 ? splits : 1;
+    return splits > 16 ? 16 : splits > 1 ? (int)splits : 1;
 }
 
 }  // namespace
@@ -265,9 +267,9 @@ hipError_t attention_dkv(int dt, const AttnArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-size_t attention_workspace(int dt, const AttnShape &a, int compute_units)
+size_t attention_workspace(int dt, const AttnShape &a, bool half, int compute_units)
 {
-    const int splits = key_splits(dt, a, compute_units);
+    const int splits = key_splits(dt, a, half, compute_units);
     const size_t rows = ((size_t)a.N * a.heads * a.T * sizeof(float) + 255) / 256 * 256;
     return rows + (splits > 1 ? (size_t)splits * a.N * a.groups * a.T * 2 * a.d * sizeof(float) : 0);
 }
@@ -276,7 +278,7 @@ hipError_t attention_bwd(int dt, AttnArgs a, void *workspace, int compute_units,
 {
     a.dsum = (float *)workspace;
     a.part = (float *)((char *)workspace + ((size_t)a.s.N * a.s.heads * a.s.T * sizeof(float) + 255) / 256 * 256);
-    a.splits = key_splits(dt, a.s, compute_units);
+    a.splits = key_splits(dt, a.s, a.half != nullptr, compute_units);
     const hipError_t e = attention_dq(dt, a, s);
     return e == hipSuccess ? attention_dkv(dt, a, s) : e;
 }

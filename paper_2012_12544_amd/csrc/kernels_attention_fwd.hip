@@ -1,17 +1,14 @@
 // Attention, forward: o = softmax(scores) v in one pass over the keys, with a running maximum and sum per query.
 #include "attention_common.h"
 
-#ifndef VR
-#define VR 32
-#endif
 namespace bapipe {
 namespace {
 
-// Rows of a tile.  bf16 heads of 192 and 256 channels: with 32 keys at a time registers and LDS hold two blocks a unit (TODO)
-template <class T, int DP> constexpr int kFwdRows = sizeof(T) == 2 && DP > 128 ? VR : 0;
+// Rows of a tile.  bf16 heads of 192 channels: with 32 keys at a time registers and LDS hold two blocks a unit (of 256 that was as fast: 151 and 154 us)
+template <class T, int DP> constexpr int kFwdRows = sizeof(T) == 2 && DP == 192 ? 32 : 0;
 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF>
-__global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && (DP <= 128 || VR) ? 2 : DP * (int)sizeof(T) <= 256 ? 2 : 1)) void k_attention_fwd(AttnArgs p)
+__global__ __launch_bounds__(AT_TPB, (DP <= (sizeof(T) == 2 ? 192 : 64) ? 2 : 1)) void k_attention_fwd(AttnArgs p)
 {
     constexpr int R = kFwdRows<T, DP>;
     typedef AtTile<T, DP, R> Tile;
@@ -34,6 +31,22 @@ __global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && (DP <= 128 || VR) ? 2 : 
 
     chunk16 query[Tile::STEPS];
     at_own<S, DP, VEC>(query, q < s.T ? base + (size_t)q * sstride + (size_t)head * d : nullptr, d, lane);
+    if constexpr (VEC && !HALF) {
+        if (p.copy) {                                      // its own queries and, for the first of their heads, the keys and values at their positions
+            T *copy = (T *)p.copy + (size_t)b.n * s.T * stride;
+#pragma unroll
+            for (int c = 0; c < Tile::STEPS; ++c) {
+                const int e = (2 * c + h) * Tile::EPC;
+                if (q < s.T && e < d) *(chunk16 *)(copy + (size_t)q * stride + (size_t)head * d + e) = query[c];
+            }
+            const int chunks = d / Tile::EPC, rows = min(AT_ROWS, s.T - q0);
+            for (int i = tid; head % per == 0 && i < 2 * rows * chunks; i += AT_TPB) {
+                const int which = i / (rows * chunks), row = (i - which * rows * chunks) / chunks, chunk = i % chunks;
+                const size_t at = (size_t)(q0 + row) * stride + (size_t)(s.heads + which * s.groups + b.g) * d + chunk * Tile::EPC;
+                *(chunk16 *)(copy + at) = *(const chunk16 *)((const T *)p.qk + (size_t)b.n * s.T * stride + at);
+            }
+        }
+    }
     const int2 span = at_span(p, b.n, q);
     const AtRange range = at_wave_range(span);
     if (lane == 0) block_range[wave] = range.any;
@@ -51,8 +64,8 @@ __global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && (DP <= 128 || VR) ? 2 : 
     float by = score.scale;
     if (HALF && q < s.T) by *= p.half_scale[((size_t)head * s.N + b.n) * s.T + q];
     const unsigned lds = at_lds(smem);
-    AtStream<S, DP, VEC, R, (DP > 192)> key_stream(sstride, tid);
-    AtStream<T, DP, VEC, R, (DP > 192)> value_stream(stride, tid);
+    AtStream<S, DP, VEC, R, false> key_stream(sstride, tid);
+    AtStream<T, DP, VEC, R, false> value_stream(stride, tid);
     constexpr int SCALE_AT = 2 * 2 * Tile::BYTES;      // 64 words, twice
     auto fill = [&](int it) {
         const int k0 = first + it * Tile::ROWS;
@@ -132,7 +145,9 @@ __global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && (DP <= 128 || VR) ? 2 : 
     sum = at_halves_sum(sum);
     if (q >= s.T) return;
     const bool sees = span.x < span.y;
-    at_store<T, VEC, ND>((T *)p.o + ((size_t)b.n * s.T + q) * s.heads * d + (size_t)head * d, d, 0, out, sees ? 1.0f / sum : 0.0f, lane);
+    const size_t at_o = ((size_t)b.n * s.T + q) * s.heads * d + (size_t)head * d;
+    at_store<T, VEC, ND>((T *)p.o + at_o, d, 0, out, sees ? 1.0f / sum : 0.0f, lane);
+    if (p.o2) at_store<T, VEC, ND>((T *)p.o2 + at_o, d, 0, out, sees ? 1.0f / sum : 0.0f, lane);
     if (h == 0) p.lse[((size_t)b.n * s.heads + head) * s.T + q] = sees ? top + log2f(sum) : __builtin_inff();
 }
 

@@ -1,6 +1,7 @@
 // Rotary positions of query and key heads, and the RMS norm of each head in front of them, one pass forward and one backward.
 //   z = g x / sqrt(mean(x^2) + eps);   (a, b) -> (a cos - b sin, a sin + b cos)  for the pairs of a head's first `rotated` channels
 // The rotation by minus the angle is its transpose: dz = rotation of dy, dg = sum dz xhat, dx = rs (g dz - xhat mean(g dz xhat)).
+// HBM bounds both.
 #include "dev_common.h"
 #include "kernels.h"
 
@@ -10,12 +11,11 @@ namespace {
 constexpr int TPB = 256;
 constexpr int kGainBlocks = 1024;        // that leave sums of the gains' gradients
 
-// A head is taken by L lanes of a wave, a power of two, V neighbouring channels each (so L V >= d: one access a lane and tensor).
-// V = 16 bytes where every head, and in half layout each half of the turning part, is whole such pieces; else 1, with C channels a lane.
 template <class T> struct RotaryArgs {
     RotaryShape r;
     const T *x, *dy;
     T *y;                    // or dx
+    T *copy;                 // forward: a second place for x, or NULL
     const float2 *table;
     const float *gains;
     float *part;             // [blocks][2][d]
@@ -23,19 +23,9 @@ template <class T> struct RotaryArgs {
     uint16_t *half;
     float *half_scale;
     const float *dy_float;   // [rows][heads + groups][d]
-    int units;               // heads of all positions
+    int per_row, per_unit;   // heads of a row that are read, and how many of them a group of lanes takes
+    int units;
 };
-
-// turned value at channel e of its head from its own and its partner's value; sign: -1 turns back
-template <bool PAIRS> __device__ __forceinline__ int partner(int e, int rotated)
-{
-    if (PAIRS) return e ^ 1;
-    return e < rotated / 2 ? e + rotated / 2 : e - rotated / 2;
-}
-template <bool PAIRS> __device__ __forceinline__ float turn(float own, float other, float2 cs, bool second, float sign)
-{
-    return fmaf(own, cs.x, (second ? sign : -sign) * other * cs.y);
-}
 
 template <int L> __device__ __forceinline__ float group_sum(float v)
 {
@@ -43,9 +33,17 @@ template <int L> __device__ __forceinline__ float group_sum(float v)
     for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     return v;
 }
+template <int L> __device__ __forceinline__ float group_max(float v)
+{
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
 
-// V channels a lane, C accesses of them, L lanes to a head
-template <class T, int V, int C, int L, bool PAIRS, bool NORM, bool BACK, bool FLOATS>
+// A head is taken by L lanes of a wave, a power of two with L V C >= d: C times V neighbouring channels each, C = 1 where V is 16 bytes, which it is
+// where d and the turning part (in half layout each half of it) are whole such pieces; else V = 1, C = 8.  A group of L lanes takes K heads
+// of a position, all loaded before the first is worked on; their angles are the same.
+template <class T, int V, int C, int L, int K, bool PAIRS, bool NORM, bool BACK, bool FLOATS>
 __global__ __launch_bounds__(TPB) void k_rotary(RotaryArgs<T> p)
 {
     typedef vec_t<T, V> vec;
@@ -53,128 +51,166 @@ __global__ __launch_bounds__(TPB) void k_rotary(RotaryArgs<T> p)
     __shared__ float sums[BACK && NORM ? TPB * V * C : 1];
     const RotaryShape &r = p.r;
     const int lane = threadIdx.x % L, group = threadIdx.x / L, d = r.d, half = r.rotated / 2;
-    const int turning = r.heads + r.groups, per_row = turning + (r.values ? r.groups : 0);
+    const int turning = r.heads + r.groups;
+    auto mate_of = [&](int e) { return PAIRS ? e ^ 1 : e < half ? e + half : e - half; };      // of a channel that turns
     float dgain[2][C][V] = {};
     for (int unit = blockIdx.x * (TPB / L) + group; unit < p.units; unit += gridDim.x * (TPB / L)) {
-        const int row = unit / per_row, head = unit - row * per_row;
-        const size_t at = (size_t)row * r.stride() + (size_t)head * d;
-        const bool turns = head < turning;
+        const int row = unit / p.per_unit, head0 = unit - row * p.per_unit;      // heads head0 + k per_unit
         const float2 *cs = p.table + (size_t)(row % r.T) * half;
+        const size_t at_row = (size_t)row * r.stride();
         const T *from = BACK ? p.dy : p.x;
-        float v[C][V], w[C][V];                          // own, the partners' of a half layout
-        vec x[C];                                        // backward the norm's input
-        auto load = [&](float (&to)[V], int e) {
-            if (FLOATS && turns) {
-                const vecf f = *(const vecf *)(p.dy_float + ((size_t)row * turning + head) * d + e);
+        vec v[K][C], w[K][C], x[K][C];                   // own, the partners' of a half layout, backward the norm's input
+        vecf vf[K][C], wf[K][C];                         // FLOATS: instead of the first two
 #pragma unroll
-                for (int j = 0; j < V; ++j) to[j] = f.e[j];
-            } else {
-                const vec f = *(const vec *)(from + at + e);
+        for (int k = 0; k < K; ++k) {
+            const int head = head0 + k * p.per_unit;
 #pragma unroll
-                for (int j = 0; j < V; ++j) to[j] = to_f32(f.e[j]);
+            for (int c = 0; c < C; ++c) {
+                const int e = (c * L + lane) * V;
+                v[k][c] = w[k][c] = x[k][c] = vec{};
+                vf[k][c] = wf[k][c] = vecf{};
+                if (e >= d || head >= p.per_row) continue;
+                const bool turns = head < turning;
+                if (FLOATS && turns) {
+                    const float *at = p.dy_float + ((size_t)row * turning + head) * d;
+                    vf[k][c] = *(const vecf *)(at + e);
+                    if (e < r.rotated && (!PAIRS || V == 1)) wf[k][c] = *(const vecf *)(at + mate_of(e));
+                } else {
+                    const T *at = from + at_row + (size_t)head * d;
+                    v[k][c] = *(const vec *)(at + e);
+                    if (turns && e < r.rotated && (!PAIRS || V == 1)) w[k][c] = *(const vec *)(at + mate_of(e));
+                }
+                if (BACK && NORM && turns) x[k][c] = *(const vec *)(p.x + at_row + (size_t)head * d + e);
             }
-        };
+        }
+        float2 angle[C][V];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int e = (c * L + lane) * V;
+            const bool turns = e < r.rotated;
+            if (PAIRS) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[c][j] = w[c][j] = 0.0f;
-            x[c] = vec{};
-            if (e >= d) continue;
-            load(v[c], e);
-            if (turns && e < r.rotated) {
-                if (!PAIRS) load(w[c], partner<false>(e, r.rotated));
-                else if (V == 1) load(w[c], e ^ 1);
+                for (int j = 0; j < V; j += 2) {
+                    const float2 a = turns ? cs[(e + j) / 2] : float2{1.0f, 0.0f};
+                    angle[c][j] = a;
+                    if (V > 1) angle[c][j + (V > 1)] = a;
+                }
+            } else {
+                const float2 *a = cs + (e < half ? e : e - half);
+#pragma unroll
+                for (int j = 0; j < V; ++j) angle[c][j] = turns ? a[j] : float2{1.0f, 0.0f};
             }
-            if (BACK && NORM && turns) x[c] = *(const vec *)(p.x + at + e);
         }
-        float rs = 1.0f;
-        if (NORM && turns) {
-            float squares = 0.0f;
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+        for (int k = 0; k < K; ++k) {
+            const int head = head0 + k * p.per_unit;
+            if (head >= p.per_row) continue;
+            const bool turns = head < turning;
+            const size_t at = at_row + (size_t)head * d;
+            if (!BACK && p.copy) {
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+                    if ((c * L + lane) * V < d) *(vec *)(p.copy + at + (c * L + lane) * V) = v[k][c];
+            }
+            if (!turns) {
+                if (r.values && p.y)
+#pragma unroll
+                    for (int c = 0; c < C; ++c)
+                        if ((c * L + lane) * V < d) *(vec *)(p.y + at + (c * L + lane) * V) = v[k][c];
+                continue;
+            }
+            auto own = [&](int c, int j) { return FLOATS ? vf[k][c].e[j] : to_f32(v[k][c].e[j]); };
+            auto mate = [&](int c, int j) {
+                if (PAIRS && V > 1) return own(c, j ^ (V > 1 ? 1 : 0));
+                return FLOATS ? wf[k][c].e[j] : to_f32(w[k][c].e[j]);
+            };
+            float rs = 1.0f;
+            if (NORM) {
+                float squares = 0.0f;
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float f = BACK ? to_f32(x[k][c].e[j]) : own(c, j);
+                        squares = fmaf(f, f, squares);
+                    }
+                rs = rsqrtf(group_sum<L>(squares) / d + r.eps);
+            }
+            const float *gains = NORM ? p.gains + (head < r.heads ? 0 : d) : nullptr;
+            float z[C][V], dot = 0.0f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int e0 = (c * L + lane) * V;
+                if (e0 >= d) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) z[c][j] = 0.0f;
+                    continue;
+                }
+                const bool in = e0 < r.rotated;
+                vecf g = {}, gm = {};
+                if (NORM) g = *(const vecf *)(gains + e0);
+                if (NORM && !BACK && in && (!PAIRS || V == 1)) gm = *(const vecf *)(gains + mate_of(e0));
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float f = BACK ? to_f32(x[c].e[j]) : v[c][j];
-                    squares = fmaf(f, f, squares);
-                }
-            rs = rsqrtf(group_sum<L>(squares) / d + r.eps);
-        }
-        const float *gains = NORM && turns ? p.gains + (head < r.heads ? 0 : d) : nullptr;
-        float z[C][V], dot = 0.0f;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int e0 = (c * L + lane) * V;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int e = e0 + j;
-                float own = v[c][j];
-                if (!turns || e >= d) { z[c][j] = own; continue; }
-                float other = 0.0f;
-                float2 angle = {1.0f, 0.0f};
-                bool second = false;
-                const int mate = partner<PAIRS>(e, r.rotated);
-                if (e < r.rotated) {
-                    other = PAIRS && V > 1 ? v[c][j ^ (V > 1 ? 1 : 0)] : w[c][j];
-                    angle = cs[PAIRS ? e >> 1 : e < half ? e : e - half];
-                    second = PAIRS ? e & 1 : e >= half;
-                }
-                if (NORM && !BACK) {
-                    own *= rs * gains[e];
-                    if (e < r.rotated) other *= rs * gains[mate];
-                }
-                z[c][j] = turn<PAIRS>(own, other, angle, second, BACK ? -1.0f : 1.0f);
-                if (NORM && BACK) {
-                    const float xhat = to_f32(x[c].e[j]) * rs;
-                    if (head < r.heads) dgain[0][c][j] += z[c][j] * xhat;
-                    else dgain[1][c][j] += z[c][j] * xhat;
-                    z[c][j] *= gains[e];
-                    dot = fmaf(z[c][j], xhat, dot);
+                    float a = own(c, j), b = in ? mate(c, j) : 0.0f;
+                    if (NORM && !BACK) {
+                        a *= rs * g.e[j];
+                        b *= rs * (PAIRS && V > 1 ? g.e[j ^ (V > 1 ? 1 : 0)] : gm.e[j]);
+                    }
+                    const bool second = PAIRS ? (e0 + j) & 1 : e0 + j >= half;
+                    const float sine = second == BACK ? -angle[c][j].y : angle[c][j].y;
+                    z[c][j] = fmaf(a, angle[c][j].x, b * sine);
+                    if (NORM && BACK) {
+                        const float xhat = to_f32(x[k][c].e[j]) * rs;
+                        if (head < r.heads) dgain[0][c][j] += z[c][j] * xhat;
+                        else dgain[1][c][j] += z[c][j] * xhat;
+                        z[c][j] *= g.e[j];
+                        dot = fmaf(z[c][j], xhat, dot);
+                    }
                 }
             }
-        }
-        if (NORM && BACK && turns) {
-            const float mean = group_sum<L>(dot) / d;
+            if (NORM && BACK) {
+                const float mean = group_sum<L>(dot) / d;
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+                for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int j = 0; j < V; ++j) z[c][j] = rs * (z[c][j] - to_f32(x[c].e[j]) * rs * mean);
-        }
-        if (BACK && !p.y) continue;                      // only the gains want a gradient
-        if (!BACK && p.half && turns) {
-            // divided by the power of two that takes the head's largest magnitude to 2^14..2^15 of a format that holds 65504, so that what is
-            // 2^28 below it keeps all its digits; infinities and NaN stay what they are
-            float most = 0.0f;
+                    for (int j = 0; j < V; ++j) z[c][j] = rs * (z[c][j] - to_f32(x[k][c].e[j]) * rs * mean);
+            }
+            if (!BACK && p.half) {
+                // divided by the power of two that takes the head's largest magnitude to 2^14..2^15 of a format that holds 65504, so that what is
+                // 2^28 below it keeps all its digits; infinities and NaN stay what they are
+                float most = 0.0f;
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+                for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if ((c * L + lane) * V + j < d) most = fmaxf(most, fabsf(z[c][j]));
+                    for (int j = 0; j < V; ++j) most = fmaxf(most, fabsf(z[c][j]));
+                most = group_max<L>(most);
+                int up = 0;
+                if (most > 0.0f && most < __builtin_inff()) up = min(14 - ilogbf(most), 100);
+                if (lane == 0) p.half_scale[(size_t)head * r.rows + row] = ldexpf(1.0f, -up);
+                const float by = ldexpf(1.0f, up);
 #pragma unroll
-            for (int o = L / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
-            int up = 0;
-            if (most > 0.0f && most < __builtin_inff()) up = min(14 - ilogbf(most), 100);
-            if (lane == 0) p.half_scale[(size_t)head * r.rows + row] = ldexpf(1.0f, -up);
+                for (int c = 0; c < C; ++c) {
+                    const int e = (c * L + lane) * V;
+                    if (e >= d) continue;
+                    struct alignas(2 * V) {
+                        _Float16 e[V];
+                    } out;
+#pragma unroll
+                    for (int j = 0; j < V; ++j) out.e[j] = (_Float16)(z[c][j] * by);
+                    __builtin_memcpy(__builtin_assume_aligned(p.half + ((size_t)row * turning + head) * d + e, 2 * V), &out, sizeof out);
+                }
+            }
+            if (BACK && !p.y) continue;                  // only the gains want a gradient
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const int e = (c * L + lane) * V;
                 if (e >= d) continue;
-                struct alignas(2 * V) {
-                    _Float16 e[V];
-                } out;
+                vec out;
 #pragma unroll
-                for (int j = 0; j < V; ++j) out.e[j] = (_Float16)ldexpf(z[c][j], up);
-                __builtin_memcpy(__builtin_assume_aligned(p.half + ((size_t)row * turning + head) * d + e, 2 * V), &out, sizeof out);
+                for (int j = 0; j < V; ++j) out.e[j] = from_f32<T>(z[c][j]);
+                *(vec *)(p.y + at + e) = out;
             }
-        }
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int e = (c * L + lane) * V;
-            if (e >= d) continue;
-            vec out;
-#pragma unroll
-            for (int j = 0; j < V; ++j) out.e[j] = from_f32<T>(z[c][j]);
-            *(vec *)(p.y + at + e) = out;
         }
     }
     if constexpr (BACK && NORM) {
@@ -195,20 +231,21 @@ __global__ __launch_bounds__(TPB) void k_rotary(RotaryArgs<T> p)
     }
 }
 
-// dgains += the blocks' sums; 16 columns and 16 rows to a block
-__global__ __launch_bounds__(TPB) void k_rotary_gains(const float *part, int blocks, int n, float *dgains)
+// dgains += the blocks' sums; 16 columns and 64 rows to a block
+__global__ __launch_bounds__(1024) void k_rotary_gains(const float *part, int blocks, int n, float *dgains)
 {
-    __shared__ float sums[16][17];
+    __shared__ float sums[64][17];
     const int col = threadIdx.x % 16, row = threadIdx.x / 16, e = blockIdx.x * 16 + col;
     float sum = 0.0f;
-    for (int b = row; b < blocks && e < n; b += 16) sum += part[(size_t)b * n + e];
+    if (e < n)
+#pragma unroll 8
+        for (int b = row; b < blocks; b += 64) sum += part[(size_t)b * n + e];
     sums[row][col] = sum;
-    __syncthreads();
-    if (row == 0 && e < n) {
-        sum = 0.0f;
-        for (int i = 0; i < 16; ++i) sum += sums[i][col];
-        dgains[e] += sum;
+    for (int o = 32; o > 0; o /= 2) {
+        __syncthreads();
+        if (row < o) sums[row][col] += sums[row + o][col];
     }
+    if (row == 0 && e < n) dgains[e] += sums[0][col];
 }
 
 // Angles in double: a float holds position times frequency to 2^-24 of it, radians at position 10^7
@@ -229,19 +266,24 @@ __global__ __launch_bounds__(TPB) void k_rotary_table(float2 *table, size_t n, i
     table[i] = {(float)(a.magnitude * cosine), (float)(a.magnitude * sine)};
 }
 
+// K: a group of lanes takes four heads where there are enough of them for all units of the chip
+constexpr int kManyHeads = 32768;
 struct Plan {
-    int lanes, units, blocks;
+    int lanes, K, per_row, per_unit, units, blocks;
     bool vec;
 };
-Plan plan(int dt, const RotaryShape &r, bool sums, std::initializer_list<const void *> tensors)
+Plan plan(int dt, const RotaryShape &r, bool sums, bool all_heads, std::initializer_list<const void *> tensors)
 {
     Plan p;
     const int V = 16 / (int)dt_size(dt);
-    p.vec = r.d % V == 0 && (r.pairs || r.rotated / 2 % V == 0);
+    p.vec = r.d % V == 0 && (r.pairs ? r.rotated % V == 0 : r.rotated / 2 % V == 0);
     for (const void *t : tensors) p.vec = p.vec && (uintptr_t)t % 16 == 0;
     const int pieces = p.vec ? r.d / V : (r.d + 7) / 8;           // without vectors eight channels a lane
     for (p.lanes = 4; p.lanes < pieces;) p.lanes *= 2;
-    p.units = r.rows * (r.heads + r.groups + (r.values ? r.groups : 0));
+    p.per_row = r.heads + r.groups + (all_heads ? r.groups : 0);
+    p.K = p.vec && (long long)r.rows * p.per_row >= kManyHeads ? 4 : 1;
+    p.per_unit = (p.per_row + p.K - 1) / p.K;
+    p.units = r.rows * p.per_unit;
     const int per_block = TPB / p.lanes;
     p.blocks = (int)(((long long)p.units + per_block - 1) / per_block);
     if (sums && p.blocks > kGainBlocks) p.blocks = kGainBlocks;
@@ -252,15 +294,19 @@ template <class T, bool NORM, bool BACK, bool FLOATS = false> hipError_t launch(
 {
     constexpr int VEC = 16 / (int)sizeof(T);
     a.units = p.units;
-#define ROTARY(V, C, L)                                                                                                          \
-    if (p.vec == (V > 1) && p.lanes == L) {                                                                                      \
-        if (a.r.pairs) hipLaunchKernelGGL((k_rotary<T, V, C, L, true, NORM, BACK, FLOATS>), dim3(p.blocks), dim3(TPB), 0, s, a); \
-        else hipLaunchKernelGGL((k_rotary<T, V, C, L, false, NORM, BACK, FLOATS>), dim3(p.blocks), dim3(TPB), 0, s, a);          \
-        return hipGetLastError();                                                                                                \
+    a.per_row = p.per_row;
+    a.per_unit = p.per_unit;
+#define ROTARY(V, C, L, N)                                                                                                           \
+    if (p.vec == (V > 1) && p.lanes == L && p.K == N) {                                                                              \
+        if (a.r.pairs) hipLaunchKernelGGL((k_rotary<T, V, C, L, N, true, NORM, BACK, FLOATS>), dim3(p.blocks), dim3(TPB), 0, s, a);  \
+        else hipLaunchKernelGGL((k_rotary<T, V, C, L, N, false, NORM, BACK, FLOATS>), dim3(p.blocks), dim3(TPB), 0, s, a);           \
+        return hipGetLastError();                                                                                                    \
     }
-    ROTARY(VEC, 1, 4) ROTARY(VEC, 1, 8) ROTARY(VEC, 1, 16) ROTARY(VEC, 1, 32)
-    if constexpr (VEC == 4) { ROTARY(VEC, 1, 64) }
-    ROTARY(1, 8, 4) ROTARY(1, 8, 8) ROTARY(1, 8, 16) ROTARY(1, 8, 32)
+#define ROTARY_VEC(L) ROTARY(VEC, 1, L, 1) ROTARY(VEC, 1, L, 4)
+    ROTARY_VEC(4) ROTARY_VEC(8) ROTARY_VEC(16) ROTARY_VEC(32)
+    if constexpr (VEC == 4) { ROTARY_VEC(64) }
+    ROTARY(1, 8, 4, 1) ROTARY(1, 8, 8, 1) ROTARY(1, 8, 16, 1) ROTARY(1, 8, 32, 1)
+#undef ROTARY_VEC
 #undef ROTARY
     return hipErrorInvalidValue;
 }
@@ -275,43 +321,68 @@ hipError_t rotary_table(float2 *table, int T, int rotated, const RotaryAngles &a
     return hipGetLastError();
 }
 
-hipError_t rotary_fwd(int dt, const RotaryShape &r, const void *x, void *y, const float2 *table, const float *gains, hipStream_t s, void *half, float *half_scale)
+template <class T>
+static hipError_t forward(const RotaryShape &r, const void *x, void *y, const float2 *table, const float *gains, hipStream_t s, void *half, float *half_scale, void *copy)
 {
-    const Plan p = plan(dt, r, false, {x, y, half});
-    const bool norm = r.eps > 0.0f;
-    if (dt == DT_F32) {
-        const RotaryArgs<float> a{r, (const float *)x, nullptr, (float *)y, table, gains, nullptr, nullptr, nullptr, nullptr, 0};
-        return norm ? launch<float, true, false>(p, a, s) : launch<float, false, false>(p, a, s);
-    }
-    const RotaryArgs<bf16_t> a{r, (const bf16_t *)x, nullptr, (bf16_t *)y, table, gains, nullptr, (uint16_t *)half, half_scale, nullptr, 0};
-    return norm ? launch<bf16_t, true, false>(p, a, s) : launch<bf16_t, false, false>(p, a, s);
+    const Plan p = plan(sizeof(T) == 4 ? DT_F32 : DT_BF16, r, false, r.values || copy, {x, y, half, copy});
+    RotaryArgs<T> a = {};
+    a.r = r;
+    a.x = (const T *)x;
+    a.y = (T *)y;
+    a.copy = (T *)copy;
+    a.table = table;
+    a.gains = gains;
+    a.half = (uint16_t *)half;
+    a.half_scale = half_scale;
+    return r.eps > 0.0f ? launch<T, true, false>(p, a, s) : launch<T, false, false>(p, a, s);
+}
+
+hipError_t rotary_fwd(int dt, const RotaryShape &r, const void *x, void *y, const float2 *table, const float *gains, hipStream_t s, void *half, float *half_scale,
+                      void *copy)
+{
+    return dt == DT_F32 ? forward<float>(r, x, y, table, gains, s, half, half_scale, copy) : forward<bf16_t>(r, x, y, table, gains, s, half, half_scale, copy);
 }
 
 size_t rotary_workspace(int dt, const RotaryShape &r)
 {
-    // tensors at odd addresses are not read in vectors: no more lanes to a head, so no more blocks
-    return r.eps > 0.0f ? (size_t)plan(dt, r, true, {}).blocks * 2 * r.d * sizeof(float) : 0;
+    // tensors at odd addresses are not read in vectors: a head to a group of no more lanes, so as many blocks or kGainBlocks at most
+    if (!(r.eps > 0.0f)) return 0;
+    const Plan a = plan(dt, r, true, r.values, {}), b = plan(dt, r, true, r.values, {(const void *)1});
+    return (size_t)(a.blocks > b.blocks ? a.blocks : b.blocks) * 2 * r.d * sizeof(float);
+}
+
+template <class T>
+static hipError_t backward(const RotaryShape &r, const void *x, const void *dy, const float *dy_float, void *dx, const float2 *table, const float *gains, float *dgains,
+                           void *workspace, hipStream_t s)
+{
+    const bool norm = r.eps > 0.0f;
+    if (!norm && !dx) return hipSuccess;
+    const Plan p = plan(sizeof(T) == 4 ? DT_F32 : DT_BF16, r, norm, r.values, {x, dy, dx, dy_float});
+    RotaryArgs<T> a = {};
+    a.r = r;
+    a.x = (const T *)x;
+    a.dy = (const T *)dy;
+    a.y = (T *)dx;
+    a.table = table;
+    a.gains = gains;
+    a.part = (float *)workspace;
+    a.dy_float = dy_float;
+    hipError_t e;
+    if constexpr (sizeof(T) == 2) {
+        if (dy_float) e = norm ? launch<T, true, true, true>(p, a, s) : launch<T, false, true, true>(p, a, s);
+        else e = norm ? launch<T, true, true>(p, a, s) : launch<T, false, true>(p, a, s);
+    } else
+        e = norm ? launch<T, true, true>(p, a, s) : launch<T, false, true>(p, a, s);
+    if (e != hipSuccess || !norm) return e;
+    hipLaunchKernelGGL(k_rotary_gains, dim3((unsigned)((2 * r.d + 15) / 16)), dim3(1024), 0, s, (const float *)workspace, p.blocks, 2 * r.d, dgains);
+    return hipGetLastError();
 }
 
 hipError_t rotary_bwd(int dt, const RotaryShape &r, const void *x, const void *dy, const float *dy_float, void *dx, const float2 *table, const float *gains,
                       float *dgains, void *workspace, hipStream_t s)
 {
-    const bool norm = r.eps > 0.0f;
-    if (!norm && !dx) return hipSuccess;
-    const Plan p = plan(dt, r, norm, {x, dy, dx, dy_float});
-    float *part = (float *)workspace;
-    hipError_t e;
-    if (dt == DT_F32) {
-        const RotaryArgs<float> a{r, (const float *)x, (const float *)dy, (float *)dx, table, gains, part, nullptr, nullptr, nullptr, 0};
-        e = norm ? launch<float, true, true>(p, a, s) : launch<float, false, true>(p, a, s);
-    } else {
-        const RotaryArgs<bf16_t> a{r, (const bf16_t *)x, (const bf16_t *)dy, (bf16_t *)dx, table, gains, part, nullptr, nullptr, dy_float, 0};
-        if (dy_float) e = norm ? launch<bf16_t, true, true, true>(p, a, s) : launch<bf16_t, false, true, true>(p, a, s);
-        else e = norm ? launch<bf16_t, true, true>(p, a, s) : launch<bf16_t, false, true>(p, a, s);
-    }
-    if (e != hipSuccess || !norm) return e;
-    hipLaunchKernelGGL(k_rotary_gains, dim3((unsigned)((2 * r.d + 15) / 16)), dim3(TPB), 0, s, part, p.blocks, 2 * r.d, dgains);
-    return hipGetLastError();
+    return dt == DT_F32 ? backward<float>(r, x, dy, dy_float, dx, table, gains, dgains, workspace, s)
+                        : backward<bf16_t>(r, x, dy, dy_float, dx, table, gains, dgains, workspace, s);
 }
 
 }  // namespace bapipe

@@ -871,13 +871,23 @@ int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
     case BAPIPE_ROTARY: {
         const RotaryShape r = rotary_shape(st, L, !L.values_stay && O.root == L.o);
         const bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
-        HIPCHK(rotary_fwd(dt, r, a, O.root == L.o ? out_ptr(st, L, c, dt_size(dt)) : o, L.table, L.w, s, L.half ? st->slot(c.mbid) + L.off_half : nullptr,
-                          L.half ? (float *)(st->slot(c.mbid) + L.off_scale) : nullptr));
+        const void *x = li == 0 && c.x_copied ? c.x_copied : a;
+        HIPCHK(rotary_fwd(dt, r, x, O.root == L.o ? out_ptr(st, L, c, dt_size(dt)) : o, L.table, L.w, s, L.half ? st->slot(c.mbid) + L.off_half : nullptr,
+                          L.half ? (float *)(st->slot(c.mbid) + L.off_scale) : nullptr, x == a ? nullptr : const_cast<void *>(a)));
         st->tap_end(tp, 0.0, 2.0 * O.bytes() * (L.d.kh + L.d.kw * (r.values ? 2.0 : 1.0)) / (L.d.kh + 2.0 * L.d.kw));
         break;
     }
     case BAPIPE_ATTENTION: {
-        const AttnArgs q = attn_args(st, L, c.mbid);
+        AttnArgs q = attn_args(st, L, c.mbid);
+        if (li == 0 && c.x_copied) {
+            q.copy = const_cast<void *>(q.qk);
+            q.qk = q.v = c.x_copied;
+        }
+        // the stage's output goes to the caller in the pass that stores it
+        if (L.o + 1 == (int)st->tensors.size() && c.y_direct && (uintptr_t)c.y_direct % 16 == 0) {
+            q.o2 = c.y_direct;
+            c.y_stored = true;
+        }
         const bool tp = st->tap_begin(BAPIPE_KC_ATTENTION);
         HIPCHK(attention_fwd(dt, q, s));
         st->tap_end(tp, 4.0 * q.s.d * attn_pairs(q.s), (double)st->tensors[L.a].bytes() + O.bytes() + L.aux_bytes);
@@ -1854,7 +1864,7 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
                 st->off_spans = slot; slot += align_up((size_t)q.N * q.T * sizeof(int2));
                 st->off_bounds = slot; slot += align_up((size_t)q.N * ((q.T + kAttnTile - 1) / kAttnTile) * 2 * sizeof(int4));
             }
-            const size_t w = attention_workspace(st->dt, q, st->compute_units);
+            const size_t w = attention_workspace(st->dt, q, L.a > 0 && st->layers[L.a - 1].half, st->compute_units);
             work = w > work ? w : work;
         }
         if (L.d.kind == BAPIPE_LSTM) {
@@ -2094,6 +2104,9 @@ int bapipe_stage_forward(bapipe_stage_t *st, int mb_id, const void *x_dev, void 
         HIPCHK(nchw_to_nhwc(dt, x_dev, st->tptr(0, mb_id), none, st->mb, In.C, In.H, In.W, In.Cp, s));
     } else if (In.Cp != In.C) {
         HIPCHK(nhwc_repad(dt, x_dev, st->tptr(0, mb_id), (size_t)st->mb * In.H * In.W, In.C, In.Cp, s));
+    } else if (In.stashed && (st->layers[0].d.kind == BAPIPE_ROTARY || (st->layers[0].d.kind == BAPIPE_ATTENTION && (uintptr_t)x_dev % 16 == 0 &&
+                                                                                              attn_shape(st, st->layers[0]).d * dt_size(dt) % 16 == 0))) {
+        c.x_copied = x_dev;
     } else if (In.stashed && st->layers[0].d.kind == BAPIPE_LAYERNORM) {
         c.x_copied = x_dev;
     } else if (In.stashed) {
