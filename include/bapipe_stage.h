@@ -128,8 +128,9 @@ typedef enum { BAPIPE_MASK_NONE = 0, BAPIPE_MASK_CAUSAL = 1, BAPIPE_MASK_SPANS =
  *   has_bias = 0: eps must be 0, no parameters.  Value heads pass unchanged.
  * ATTENTION: cout = kh d.  Score of query i and key j: q_i k_j / sqrt(d); with eps > 0 capped to eps tanh(score / eps);
  *   with pad > 0 less 2^(-pad (h + 1) / kh) |i - j| in query head h (pad up to 64).  Softmax over the keys that stride
- *   lets the position see; one that sees none gets zeros and gives no gradients.  has_bias must be 0.  What a position holds that no
- *   position of the sequence sees has no effect on others, NaN or infinity included; of one that some see and others do not, NaN may reach them.
+ *   lets the position see; one that sees none gets zeros and gives no gradients.  has_bias must be 0.  What the
+ *   positions of a sequence hold behind the last that sees some, or is seen, has no effect on anything, NaN and infinity
+ *   included; at other positions that are not seen it has to be finite.
  *   In bf16 stages probabilities and their gradients are rounded to bf16 as operands of the next product; scores, sums and
  *   the softmax stay in float. */
 typedef struct {
@@ -236,8 +237,8 @@ int bapipe_stage_set_streams(bapipe_stage_t *st, void *hip_stream_backward, void
  * under HIP graph capture, tight serving loops, harnesses that forbid hipMalloc): same arguments,
  * same schedule rules, same results bit for bit, but the kernels' workspace (split-K partial
  * sums of the weight-gradient and linear-layer GEMMs, column-reduction partials of batch-norm and
- * bias gradients, what the blocks of an LSTM recurrence hand to each other) is a statically allocated
- * device array of BAPIPE_STATIC_SCRATCH_BYTES inside the library instead of the workspace the
+ * bias gradients, what the blocks of an LSTM recurrence hand to each other, partial sums of the
+ * gradients of ATTENTION and of ROTARY's gains) is a statically allocated device array of BAPIPE_STATIC_SCRATCH_BYTES inside the library instead of the workspace the
  * handle obtained from its allocator.  The call allocates and frees nothing on the device.  Every
  * GPU the library runs on holds one copy of the array until the process ends, and all handles on
  * a GPU share it: two calls that overlap in time on one GPU (different streams or threads) race

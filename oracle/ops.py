@@ -310,3 +310,123 @@ def xent_bwd(z, labels, scale):
 def sgd_step(w, g, lr):
     """In place: w <- w - lr*g."""
     lib().orc_sgd_step(_p(w), _p(_f64(g)), ct.c_double(lr), ct.c_size_t(w.size))
+
+
+# ------------------------------------------------------------------------------ rotary positions and attention
+def split_heads(x, heads):
+    """(N, C, T, 1) -> (N, heads, T, d) of as many heads in all."""
+    x = _f64(x)
+    N, Cn, T, _ = x.shape
+    return x[..., 0].reshape(N, heads, Cn // heads, T).transpose(0, 1, 3, 2)
+
+
+def join_heads(z):
+    N, heads, T, d = z.shape
+    return np.ascontiguousarray(z.transpose(0, 1, 3, 2)).reshape(N, heads * d, T, 1)
+
+
+ANGLES = dict(base=10000.0, factor=1.0, original_length=0.0, low_turns=1.0, high_turns=4.0, magnitude=1.0, first_position=0)
+
+
+def rotary_angles(T, turning, **changed):
+    """(T, turning / 2) complex numbers magnitude exp(i t f_j)"""
+    a = dict(ANGLES, **changed)
+    f = a["base"] ** (-2.0 * np.arange(turning // 2) / max(turning, 1))
+    if a["original_length"] == 0:
+        f = f / a["factor"]
+    else:
+        turns = a["original_length"] * f / (2 * math.pi)
+        s = np.clip((turns - a["low_turns"]) / (a["high_turns"] - a["low_turns"]), 0.0, 1.0)
+        f = f * (s + (1 - s) / a["factor"])
+    t = a["first_position"] + np.arange(T, dtype=np.float64)
+    return a["magnitude"] * np.exp(1j * t[:, None] * f)
+
+
+def _turn(z, by, pairs):
+    r = 2 * by.shape[1]
+    a, b = (z[..., 0:r:2], z[..., 1:r:2]) if pairs else (z[..., :r // 2], z[..., r // 2:r])
+    c = (a + 1j * b) * by
+    out = z.copy()
+    if pairs:
+        out[..., 0:r:2], out[..., 1:r:2] = c.real, c.imag
+    else:
+        out[..., :r // 2], out[..., r // 2:r] = c.real, c.imag
+    return out
+
+
+def _rms(z, eps):
+    return 1.0 / np.sqrt((z * z).mean(-1, keepdims=True) + eps)
+
+
+def rotary_fwd(x, heads, groups, by, pairs, gains=None, eps=0.0):
+    z = split_heads(x, heads + 2 * groups)
+    qk = z[:, :heads + groups]
+    if gains is not None:
+        gain = np.repeat(gains, [heads, groups], axis=0)[:, None]
+        qk = qk * _rms(qk, eps) * gain
+    return join_heads(np.concatenate([_turn(qk, by, pairs), z[:, heads + groups:]], 1))
+
+
+def rotary_bwd(x, dy, heads, groups, by, pairs, gains=None, eps=0.0, dgains=None):
+    """dx; accumulates into dgains [2][d]"""
+    z, g = split_heads(x, heads + 2 * groups), split_heads(dy, heads + 2 * groups)
+    qk, dqk = z[:, :heads + groups], _turn(g[:, :heads + groups], by.conj(), pairs)
+    if gains is not None:
+        gain, r = np.repeat(gains, [heads, groups], axis=0)[:, None], _rms(qk, eps)
+        xhat = qk * r
+        by_head = (dqk * xhat).sum((0, 2))
+        dgains += np.stack([by_head[:heads].sum(0), by_head[heads:].sum(0)])
+        dqk = dqk * gain
+        dqk = r * (dqk - xhat * (dqk * xhat).mean(-1, keepdims=True))
+    return join_heads(np.concatenate([dqk, g[:, heads + groups:]], 1))
+
+
+def attention_sees(mask, N, T, spans=None):
+    """(N or 1, 1, T, T) of booleans: whether a position (third axis) sees a key.  mask: 0 all, 1 up to itself, 2 spans (N, T, 2)."""
+    i = np.arange(T)
+    if mask == 0:
+        return np.ones((1, 1, T, T), bool)
+    if mask == 1:
+        return (i <= i[:, None])[None, None]
+    spans = np.asarray(spans).reshape(N, 1, T, 1, 2)
+    return (i >= spans[..., 0]) & (i < spans[..., 1])
+
+
+def attention_probabilities(x, heads, groups, sees, cap=0.0, bias=0):
+    """(N, heads, T, T) probabilities and the cap's slope there, of the queries and keys in x"""
+    z = split_heads(x, heads + 2 * groups)
+    d, T = z.shape[-1], z.shape[2]
+    q, k = z[:, :heads], np.repeat(z[:, heads:heads + groups], heads // groups, axis=1)
+    s = q @ k.transpose(0, 1, 3, 2) / math.sqrt(d)
+    slope = np.ones_like(s)
+    if cap:
+        t = np.tanh(s / cap)
+        s, slope = cap * t, 1 - t * t
+    if bias:
+        i = np.arange(T)
+        s = s - 2.0 ** (-bias * np.arange(1, heads + 1) / heads)[:, None, None] * np.abs(i[:, None] - i)
+    s = np.where(sees, s, -np.inf)
+    top = s.max(-1, keepdims=True)
+    p = np.exp(s - np.where(np.isneginf(top), 0.0, top))
+    total = p.sum(-1, keepdims=True)
+    return p / np.where(total == 0, 1.0, total), slope
+
+
+def attention_fwd(x, heads, groups, p):
+    v = np.repeat(split_heads(x, heads + 2 * groups)[:, heads + groups:], heads // groups, axis=1)
+    return join_heads(p @ v)
+
+
+def attention_bwd(x, dy, heads, groups, p, slope):
+    z, do = split_heads(x, heads + 2 * groups), split_heads(dy, heads)
+    N, _, T, d = z.shape
+    per = heads // groups
+    q = z[:, :heads]
+    k, v = (np.repeat(t, per, axis=1) for t in (z[:, heads:heads + groups], z[:, heads + groups:]))
+    dp = do @ v.transpose(0, 1, 3, 2)
+    ds = p * (dp - (p * dp).sum(-1, keepdims=True)) * slope / math.sqrt(d)
+
+    def shared(t):
+        return t.reshape(N, groups, per, T, d).sum(2)
+
+    return join_heads(np.concatenate([ds @ k, shared(ds.transpose(0, 1, 3, 2) @ q), shared(p.transpose(0, 1, 3, 2) @ do)], 1))

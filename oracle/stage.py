@@ -14,7 +14,9 @@ the working copy of conv/linear weight matrices.  Bias, gamma, beta, weight grad
 BN statistics, softmax and loss are never rounded.  Inside an LSTM layer the input projection
 of all steps and the pre-activation gradients are stored tensors too (rounded); the cell state
 and the recurrent sums are not.  A gated layer's projections are not rounded, their gradients
-are; the gradients that layer norm, gated layer and 1x1 convolution hand to each other are not.  storage="exact" rounds nothing.
+are; the gradients that layer norm, gated layer and 1x1 convolution hand to each other are not.  Of a ROTARY that only an ATTENTION
+reads, scores are made of what it computed, the other products of what it stored, and the gradient between the two is not rounded.
+storage="exact" rounds nothing.
 """
 import numpy as np
 
@@ -58,18 +60,28 @@ class OracleStage:
         self.trace = None          # set to {} to record, per (mb, layer), the masked output gradient and dx
         self.n_fwd = self.n_bwd = 0
         self.peak_in_flight = 0
+        self.spans = {}            # of ATTENTION layers with spans: micro-batch -> int [N][T][2], to be filled before its forward pass
+        self.angles = {}           # of ROTARY layers: layer -> what differs from ops.ANGLES
         self.dropout_seed = self.mini_batch = 0        # key and last counter word of the DROPOUT layers' masks
 
     def _float_grad(self, t):
         """Whether the gradient of layer t's output is not rounded: of a layer norm that only a gated layer reads, of a gated layer
-        that only a 1x1 convolution of widths that are multiples of 8 does."""
+        that only a 1x1 convolution of widths that are multiples of 8 does, of a ROTARY that only an ATTENTION does."""
         if len(self.readers.get(t, [])) != 1:
             return False
         P, N = self.layers[t], self.layers[self.readers[t][0]]
         if P["kind"] == C.LAYERNORM:
             return N["kind"] == C.GATED
+        if P["kind"] == C.ROTARY:
+            return N["kind"] == C.ATTENTION
         return (P["kind"] == C.GATED and N["kind"] == C.CONV2D and (N["kh"], N["stride"], N["pad"]) == (1, 1, 0) and
                 N["cin"] % 8 == 0 and N["cout"] % 8 == 0)
+
+    def _turned(self, i):
+        """Arguments of ops.rotary_*, from the heads on, of ROTARY layer i."""
+        L = self.layers[i]
+        by = ops.rotary_angles(self.shapes[i][1], L["pad"], **self.angles.get(i, {}))
+        return L["kh"], L["kw"], by, L["stride"] == C.ROTARY_PAIRS, self.w[i], L["eps"]
 
     # ---- schedule bookkeeping -------------------------------------------------------
     def _claim(self, mb):
@@ -143,6 +155,15 @@ class OracleStage:
                 extra = ops.dropout_factor(a.shape, L["eps"], self.dropout_seed, i + 65536 * (self.stage["stage_index"] - 1), mb,
                                            self.mini_batch)
                 y = q(a * extra)
+            elif k == C.ROTARY:
+                y = extra = ops.rotary_fwd(a, *self._turned(i))
+                y = q(y)
+            elif k == C.ATTENTION:
+                t = L["src0"]
+                fine = aux[t] if t in self.float_grads and self.layers[t]["kind"] == C.ROTARY else a
+                sees = ops.attention_sees(L["stride"], len(a), a.shape[2], self.spans.get(mb))
+                extra = ops.attention_probabilities(fine, L["kh"], L["kw"], sees, L["eps"], L["pad"])
+                y = q(ops.attention_fwd(a, L["kh"], L["kw"], extra[0]))
             elif k == C.SOFTMAX_XENT:
                 y = ops.softmax_fwd(a.reshape(a.shape[0], -1)).reshape(a.shape)
             else:
@@ -234,6 +255,13 @@ class OracleStage:
                     give(L["src0"], dx)
             elif k == C.DROPOUT:
                 give(L["src0"], g * aux[i])
+            elif k == C.ROTARY:
+                dx = ops.rotary_bwd(a, g, *self._turned(i), dgains=self.dw[i])
+                if wants:
+                    give(L["src0"], dx)
+            elif k == C.ATTENTION:
+                if wants:
+                    give(L["src0"], ops.attention_bwd(a, g, L["kh"], L["kw"], *aux[i]))
             elif k == C.LINEAR:
                 a2 = a.reshape(a.shape[0], -1)
                 g2 = g.reshape(g.shape[0], -1)

@@ -23,6 +23,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA || HALF ? 19
     static_assert(Tile::ROWS <= kAttnTile && kAttnTile % Tile::ROWS == 0, "");
     extern __shared__ __align__(256) unsigned char smem[];
     __shared__ int2 block_range[AT_WAVES];
+    __shared__ int block_seen[AT_WAVES];
     const AttnShape &s = p.s;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int d = s.d, stride = s.stride(), per = s.heads / s.groups, ostride = s.heads * d;
@@ -33,21 +34,18 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA || HALF ? 19
     const int sstride = HALF ? (s.heads + s.groups) * d : stride;
     const T *base = (const T *)p.qk + (size_t)b.n * s.T * stride;
     const S *score_base = (const S *)(HALF ? p.half : p.qk) + (size_t)b.n * s.T * sstride;
-    chunk16 key[Tile::STEPS], value[Tile::STEPS];
-    at_own<S, DP, VEC>(key, own < s.T ? score_base + (size_t)own * sstride + (size_t)(s.heads + b.g) * d : nullptr, d, lane);
-    at_own<T, DP, VEC>(value, own < s.T ? (const T *)p.v + ((size_t)b.n * s.T + own) * stride + (size_t)(s.heads + s.groups + b.g) * d : nullptr, d, lane);
-    const float own_scale = HALF && own < s.T ? p.half_scale[((size_t)(s.heads + b.g) * s.N + b.n) * s.T + own] : 1.0f;
 
     // tiles of queries, from the first that sees one of the block's keys to the last
     const int all_tiles = (s.T + Tile::ROWS - 1) / Tile::ROWS;
-    int first = 0, end = all_tiles;
+    int first = 0, end = all_tiles, seen = s.T;                    // seen: end of the keys that some position sees
     const int4 *bounds = p.bounds + (size_t)b.n * 2 * ((s.T + kAttnTile - 1) / kAttnTile);
     if (s.mask == ATTN_CAUSAL) first = key0 / Tile::ROWS;
     if (s.mask == ATTN_SPANS) {
         first = all_tiles;
-        end = 0;
+        end = seen = 0;
         for (int i = tid; i < all_tiles; i += AT_TPB) {
             const int4 v = bounds[i * Tile::ROWS / kAttnTile * 2];
+            seen = max(seen, v.y);
             if (v.x < key0 + AT_ROWS && v.y > key0) {
                 first = min(first, i);
                 end = i + 1;
@@ -57,17 +55,27 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA || HALF ? 19
         for (int o = 32; o > 0; o >>= 1) {
             first = min(first, __shfl_xor(first, o, 64));
             end = max(end, __shfl_xor(end, o, 64));
+            seen = max(seen, __shfl_xor(seen, o, 64));
         }
-        if (lane == 0) block_range[wave] = {first, end};
+        if (lane == 0) {
+            block_range[wave] = {first, end};
+            block_seen[wave] = seen;
+        }
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < AT_WAVES; ++w) {
             first = min(first, block_range[w].x);
             end = max(end, block_range[w].y);
+            seen = max(seen, block_seen[w]);
         }
     }
     first = __builtin_amdgcn_readfirstlane(first);
     end = __builtin_amdgcn_readfirstlane(end);
+    // as with the queries, what is behind the last key that is seen is not read
+    chunk16 key[Tile::STEPS], value[Tile::STEPS];
+    at_own<S, DP, VEC>(key, own < seen ? score_base + (size_t)own * sstride + (size_t)(s.heads + b.g) * d : nullptr, d, lane);
+    at_own<T, DP, VEC>(value, own < seen ? (const T *)p.v + ((size_t)b.n * s.T + own) * stride + (size_t)(s.heads + s.groups + b.g) * d : nullptr, d, lane);
+    const float own_scale = HALF && own < seen ? p.half_scale[((size_t)(s.heads + b.g) * s.N + b.n) * s.T + own] : 1.0f;
     const int of_head = end > first ? end - first : 0, total = of_head * per;
     const int begin = (int)((long long)total * split / p.splits), stop = (int)((long long)total * (split + 1) / p.splits);
 
@@ -77,9 +85,8 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA || HALF ? 19
     // of the rows of a tile, twice: 64 words each of lse, dout . o and scale, 128 of spans
     constexpr int ROW_BYTES = 5 * 256;
     constexpr int ROWS_AT = 2 * STREAMS * Tile::BYTES;
-    // Head and tile of the loads that are under way, counted, so that addresses stay scalar.  Last tile first: with a causal mask that is
-    // where blocks of different keys have something to read together (4 x 4096 positions, 32 / 8 heads of 128: 2190 us from the first one on, as
-    // no two of them ever found the other's rows in the L2; so TODO).
+    // Head and tile of the loads that are under way, counted, so that addresses stay scalar.  Last tile first: with a causal mask all blocks of
+    // a key head read the last ones.
     int next_head = 0, next_tile = 0;
     if (begin < stop) {
         next_head = __builtin_amdgcn_readfirstlane(b.g * per + begin / of_head);

@@ -12,10 +12,13 @@ A layer is a dict with the integer fields of the C descriptor:
 """
 
 (CONV2D, RELU, MAXPOOL2D, BATCHNORM2D, ADD, FLATTEN, LINEAR, SOFTMAX_XENT, AVGPOOL2D, LSTM, LAYERNORM, GATED,
- DROPOUT) = range(13)
+ DROPOUT, ROTARY, ATTENTION) = range(15)
 KIND_NAMES = ["conv2d", "relu", "maxpool2d", "batchnorm2d", "add", "flatten",
-              "linear", "softmax_xent", "avgpool2d", "lstm", "layernorm", "gated", "dropout"]
+              "linear", "softmax_xent", "avgpool2d", "lstm", "layernorm", "gated", "dropout",
+              "rotary", "attention"]
 GATE_SIGMOID, GATE_SILU, GATE_GELU, GATE_RELU = range(4)
+ROTARY_HALVES, ROTARY_PAIRS = range(2)
+MASK_NONE, MASK_CAUSAL, MASK_SPANS = range(3)
 
 FP32, BF16 = 0, 1
 SCHED_1F1B, SCHED_1F1B_SO = 0, 1
@@ -81,6 +84,21 @@ class _Builder:
 
     def dropout(self, p, src=None):
         return self.add(kind=DROPOUT, eps=p, src0=src)
+
+    def rotary(self, heads, groups, d, turning=None, layout=ROTARY_HALVES, norm=0, eps=1e-6, src=None):
+        """Rotary positions of heads query and groups key heads of d channels, RMS norms with gains w [2][d] before them with norm=1.
+        The descriptor's kh, kw, stride, pad are heads, groups, layout, turning channels."""
+        c = (heads + 2 * groups) * d
+        i = self.add(kind=ROTARY, cin=c, cout=c, stride=layout, pad=d // 2 * 2 if turning is None else turning, has_bias=norm,
+                     eps=eps if norm else 0.0, src0=src)
+        self.layers[i].update(kh=heads, kw=groups)
+        return i
+
+    def attention(self, heads, groups, d, mask=MASK_CAUSAL, cap=0.0, bias=0, src=None):
+        """The descriptor's kh, kw, stride, pad, eps are heads, groups, mask, bias, cap."""
+        i = self.add(kind=ATTENTION, cin=(heads + 2 * groups) * d, cout=heads * d, stride=mask, pad=bias, eps=cap, src0=src)
+        self.layers[i].update(kh=heads, kw=groups)
+        return i
 
     def xent(self, src=None):
         return self.add(kind=SOFTMAX_XENT, src0=src)
@@ -318,6 +336,9 @@ def infer_shapes(stage):
         elif k == GATED:
             assert s[0] == L["cin"], (idx, s, L)
             o = (L["cout"], s[1], s[2])
+        elif k in (ROTARY, ATTENTION):
+            assert s[0] == L["cin"] and s[2] == 1, (idx, s, L)
+            o = (L["cout"], s[1], 1)
         elif k == ADD:
             s1 = inp if L["src1"] < 0 else shapes[L["src1"]]
             assert s == s1, (idx, s, s1)

@@ -63,7 +63,7 @@ def layer_params(stage, idx, perturb=False):
     linear: Xavier-uniform bound sqrt(6/(fan_in+fan_out)) ('xavier' stages) ;
     lstm: w [4*hidden][cin+hidden] and (perturbed) bias uniform in +-1/sqrt(hidden) ;
     gated: w [2*cout][cin], as conv or linear ;
-    batchnorm, layernorm: w = gamma = 1, b = beta = 0 ; biases 0.
+    batchnorm, layernorm: w = gamma = 1, b = beta = 0 ; rotary with norms: w [2][d] = 1 ; biases 0.
     perturb=True draws biases/beta ~ 0.1*N(0,1) and gamma ~ 1 + 0.1*N(0,1) instead, so that
     tests can see a dropped bias or scale term."""
     L = stage["layers"][idx]
@@ -95,6 +95,11 @@ def layer_params(stage, idx, perturb=False):
             g = (1.0 + 0.1 * r.standard_normal(L["cout"])).astype(np.float32)
             b = (0.1 * rb.standard_normal(L["cout"])).astype(np.float32)
         return g, b
+    elif k == C.ROTARY and L["has_bias"]:
+        g = np.ones((2, L["cin"] // (L["kh"] + 2 * L["kw"])), np.float32)
+        if perturb:
+            g = (1.0 + 0.1 * r.standard_normal(g.shape)).astype(np.float32)
+        return g, None
     else:
         return None, None
     if stage["init"] == "xavier":
