@@ -350,7 +350,8 @@ enum {
     BAPIPE_KC_POOL = 3,
     BAPIPE_KC_BATCHNORM = 4,        /* and layer norm                                        */
     BAPIPE_KC_ELEMENTWISE = 5,      /* ReLU, add, dropout, rotary positions, gradient copies, bias-gradient sums, gradients of GATED's projections */
-    BAPIPE_KC_ATTENTION = 6,        /* FLOP of scored pairs: all, or half of them with a causal mask; with spans as if all were */
+    BAPIPE_KC_ATTENTION = 6,        /* FLOP of two products forward, five backward, over all pairs, with a causal mask
+                                     * those up to the diagonal; with spans as if all were seen */
     BAPIPE_KC_COUNT = 7
 };
 int bapipe_stage_kernel_timing(bapipe_stage_t *st, int kernel_class);

@@ -872,7 +872,7 @@ int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
         const RotaryShape r = rotary_shape(st, L, !L.values_stay && O.root == L.o);
         const bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
         const void *x = li == 0 && c.x_copied ? c.x_copied : a;
-        HIPCHK(rotary_fwd(dt, r, x, O.root == L.o ? out_ptr(st, L, c, dt_size(dt)) : o, L.table, L.w, s, L.half ? st->slot(c.mbid) + L.off_half : nullptr,
+        HIPCHK(rotary_fwd(dt, r, x, O.root == L.o ? out_ptr(st, L, c, 16) : o, L.table, L.w, s, L.half ? st->slot(c.mbid) + L.off_half : nullptr,
                           L.half ? (float *)(st->slot(c.mbid) + L.off_scale) : nullptr, x == a ? nullptr : const_cast<void *>(a)));
         st->tap_end(tp, 0.0, 2.0 * O.bytes() * (L.d.kh + L.d.kw * (r.values ? 2.0 : 1.0)) / (L.d.kh + 2.0 * L.d.kw));
         break;
@@ -2104,7 +2104,7 @@ int bapipe_stage_forward(bapipe_stage_t *st, int mb_id, const void *x_dev, void 
         HIPCHK(nchw_to_nhwc(dt, x_dev, st->tptr(0, mb_id), none, st->mb, In.C, In.H, In.W, In.Cp, s));
     } else if (In.Cp != In.C) {
         HIPCHK(nhwc_repad(dt, x_dev, st->tptr(0, mb_id), (size_t)st->mb * In.H * In.W, In.C, In.Cp, s));
-    } else if (In.stashed && (st->layers[0].d.kind == BAPIPE_ROTARY || (st->layers[0].d.kind == BAPIPE_ATTENTION && (uintptr_t)x_dev % 16 == 0 &&
+    } else if (In.stashed && (uintptr_t)x_dev % 16 == 0 && (st->layers[0].d.kind == BAPIPE_ROTARY || (st->layers[0].d.kind == BAPIPE_ATTENTION &&
                                                                                               attn_shape(st, st->layers[0]).d * dt_size(dt) % 16 == 0))) {
         c.x_copied = x_dev;
     } else if (In.stashed && st->layers[0].d.kind == BAPIPE_LAYERNORM) {
@@ -2169,9 +2169,10 @@ int bapipe_stage_backward(bapipe_stage_t *st, int mb_id, const void *dy_dev_or_l
     c.pending.assign(st->tensors.size(), nullptr);
     const Tensor &In = st->tensors[0];
     const bool want_dx = In.need_grad && dx_dev != nullptr;
-    // ATTENTION reads and writes gradients in pieces of 16 bytes: a caller's that do not lie so pass through the stage's own
+    // ATTENTION reads and writes gradients in pieces of 16 bytes, and ROTARY's norms would be summed in another order without: a caller's
+    // that do not lie so pass through the stage's own
     bool attends = false;
-    for (const Layer &L : st->layers) attends |= L.d.kind == BAPIPE_ATTENTION;
+    for (const Layer &L : st->layers) attends |= has_heads(L.d.kind);
     if (want_dx && (nhwc || In.H * In.W == 1) && In.Cp == In.C && !(attends && (uintptr_t)dx_dev % 16)) c.dx_direct = dx_dev;
     if (st->layers[nl - 1].d.kind == BAPIPE_SOFTMAX_XENT) {
         c.labels = (const int32_t *)dy_dev_or_labels;
