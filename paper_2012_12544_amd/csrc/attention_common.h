@@ -341,6 +341,18 @@ __device__ __forceinline__ AtBlock at_block(const AttnShape &s)
     return {ng / s.groups, ng % s.groups, (int)(blockIdx.x / of)};
 }
 
+// Which block of rows is the i-th to be started: those with the most to do first, with a causal mask the last queries and the first keys
+__device__ __forceinline__ int at_query_block(const AttnArgs &a, int n, int i)
+{
+    const int blocks = (a.s.T + AT_ROWS - 1) / AT_ROWS;
+    return a.order ? __builtin_amdgcn_readfirstlane(a.order[(size_t)n * 2 * blocks + i]) : blocks - 1 - i;
+}
+__device__ __forceinline__ int at_key_block(const AttnArgs &a, int n, int i)
+{
+    const int blocks = (a.s.T + AT_ROWS - 1) / AT_ROWS;
+    return a.order ? __builtin_amdgcn_readfirstlane(a.order[((size_t)n * 2 + 1) * blocks + i]) : i;
+}
+
 // address of the dynamic LDS
 __device__ __forceinline__ unsigned at_lds(const unsigned char *smem) { return __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void_t *)smem); }
 

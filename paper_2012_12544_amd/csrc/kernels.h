@@ -257,6 +257,8 @@ struct AttnArgs {
     // [N][tiles of kAttnTile queries][2]: smallest first, largest end of those that see something, largest first, smallest end of all (0 with one that
     // sees nothing); how many there are up to the last that sees something
     const int4 *bounds;
+    // ATTN_SPANS, or NULL: [N][2][blocks of rows] blocks in the order in which they are started: of queries, of keys
+    const int *order;
     // backward
     const void *dout;        // as o
     float *dsum;             // [N][heads][T]: dout . o, of the first of its two kernels to the second
@@ -266,7 +268,9 @@ struct AttnArgs {
     int splits;              // of the second kernel's sums, which then go through part
 };
 // spans clamped to [0, T], and the tiles' bounds; given NULL: every position sees those up to itself
-hipError_t attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int N, int T, hipStream_t s);
+// order: attention_order_size elements, or NULL where that is 0
+hipError_t attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int *order, int N, int T, hipStream_t s);
+size_t attention_order_size(int N, int T);
 hipError_t attention_fwd(int dt, const AttnArgs &a, hipStream_t s);
 size_t attention_workspace(int dt, const AttnShape &a, bool half, int compute_units);          // of a backward pass; half: with AttnArgs::half
 hipError_t attention_bwd(int dt, AttnArgs a, void *workspace, int compute_units, hipStream_t s);

@@ -28,8 +28,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA || HALF ? 19
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int d = s.d, stride = s.stride(), per = s.heads / s.groups, ostride = s.heads * d;
     const AtBlock b = at_block(s);
-    // with a causal mask the first keys have the most queries
-    const int half = b.rest % HALVES, split = b.rest / HALVES % p.splits, key0 = b.rest / HALVES / p.splits * AT_ROWS;
+    const int half = b.rest % HALVES, split = b.rest / HALVES % p.splits, key0 = at_key_block(p, b.n, b.rest / HALVES / p.splits) * AT_ROWS;
     const int wave0 = key0 + 32 * wave, own = wave0 + (lane & 31);
     const int sstride = HALF ? (s.heads + s.groups) * d : stride;
     const T *base = (const T *)p.qk + (size_t)b.n * s.T * stride;

@@ -19,7 +19,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int d = s.d, stride = s.stride(), per = s.heads / s.groups;
     const AtBlock b = at_block(s);
-    const int blocks = (s.T + AT_ROWS - 1) / AT_ROWS, head = b.g * per + b.rest % per, q0 = (blocks - 1 - b.rest / per) * AT_ROWS;
+    const int head = b.g * per + b.rest % per, q0 = at_query_block(p, b.n, b.rest / per) * AT_ROWS;
     const int q = q0 + 32 * wave + (lane & 31);
     const int sstride = HALF ? (s.heads + s.groups) * d : stride;
     const S *base = (const S *)(HALF ? p.half : p.qk) + (size_t)b.n * s.T * sstride, *score_keys = base + (size_t)(s.heads + b.g) * d;

@@ -21,8 +21,7 @@ __global__ __launch_bounds__(AT_TPB, (DP <= (sizeof(T) == 2 ? 192 : 64) ? 2 : 1)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int d = s.d, stride = s.stride(), per = s.heads / s.groups;
     const AtBlock b = at_block(s);
-    // queries with the most keys first
-    const int blocks = (s.T + AT_ROWS - 1) / AT_ROWS, head = b.g * per + b.rest % per, q0 = (blocks - 1 - b.rest / per) * AT_ROWS;
+    const int head = b.g * per + b.rest % per, q0 = at_query_block(p, b.n, b.rest / per) * AT_ROWS;
     const int q = q0 + 32 * wave + (lane & 31);
     const int sstride = HALF ? (s.heads + s.groups) * d : stride;
     const S *base = (const S *)(HALF ? p.half : p.qk) + (size_t)b.n * s.T * sstride, *keys = base + (size_t)(s.heads + b.g) * d;
@@ -186,9 +185,65 @@ __global__ __launch_bounds__(64) void k_attention_spans(const int32_t *given, in
     }
 }
 
+// The blocks of a sample with the most to do first: the last ones to be started are what others wait for.  Documents of 1500 to 4500 in 16384
+// positions, 8 heads of 128 that share one key head, 1024 blocks of which 512 fit, us for the three kernels: 206, 243 and 354 from the last
+// position to the first, 170, 188 and 302 so, and 6 for this.
+// Blocks of queries by the tiles from the first to the last key that one of them sees, blocks of keys by the tiles of queries that see one of them;
+// a block's place is the number of those in front of it.
+constexpr int kOrderBlocks = 1024;      // of more the others' work is long enough
+__global__ __launch_bounds__(1024) void k_attention_order(const int4 *bounds, int *order, int T)
+{
+    constexpr int L = 8, SPT = 1024 / L;      // lanes to a block, which share its sums
+    __shared__ int2 range[kOrderBlocks * AT_ROWS / kAttnTile];
+    __shared__ int work[kOrderBlocks];
+    const int tiles = (T + kAttnTile - 1) / kAttnTile, blocks = (T + AT_ROWS - 1) / AT_ROWS, part = threadIdx.x % L, which = blockIdx.y;
+    bounds += (size_t)blockIdx.x * 2 * tiles;
+    order += ((size_t)blockIdx.x * 2 + which) * blocks;
+    for (int i = threadIdx.x; i < tiles; i += 1024) range[i] = *(const int2 *)&bounds[2 * i];
+    __syncthreads();
+    auto sum = [&](int n) {
+#pragma unroll
+        for (int o = L / 2; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+        return n;
+    };
+    for (int b0 = 0; b0 < blocks; b0 += SPT) {
+        const int b = b0 + threadIdx.x / L;
+        int n = 0;
+        if (which == 0) {
+            int first = T, end = 0;
+            for (int i = b * (AT_ROWS / kAttnTile); i < (b + 1) * (AT_ROWS / kAttnTile) && i < tiles; ++i) {
+                first = min(first, range[i].x);
+                end = max(end, range[i].y);
+            }
+            n = max(end - first, 0) / kAttnTile;
+        } else {
+#pragma unroll 4
+            for (int i = part; i < tiles; i += L) n += range[i].x < (b + 1) * AT_ROWS && range[i].y > b * AT_ROWS;
+            n = sum(n);
+        }
+        if (part == 0 && b < blocks) work[b] = n;
+    }
+    __syncthreads();
+    for (int b0 = 0; b0 < blocks; b0 += SPT) {
+        const int b = b0 + threadIdx.x / L, mine = b < blocks ? work[b] : 0;
+        int place = 0;
+#pragma unroll 4
+        for (int i = part; i < blocks; i += L) place += work[i] > mine || (work[i] == mine && i < b);
+        place = sum(place);
+        if (part == 0 && b < blocks) order[place] = b;
+    }
+}
+
 }  // namespace
 
-hipError_t attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int N, int T, hipStream_t s)
+// Sequences of less than eight blocks are over too soon
+size_t attention_order_size(int N, int T)
+{
+    const int blocks = (T + AT_ROWS - 1) / AT_ROWS;
+    return blocks >= 8 && blocks <= kOrderBlocks ? (size_t)N * 2 * blocks : 0;
+}
+
+hipError_t attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int *order, int N, int T, hipStream_t s)
 {
     // a sample's tiles are a row of the grid, which takes 65535 of them at a time
     const int tiles = (T + kAttnTile - 1) / kAttnTile;
@@ -197,6 +252,7 @@ hipError_t attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int 
         hipLaunchKernelGGL(k_attention_spans, dim3((unsigned)tiles, (unsigned)(N - n < 65535 ? N - n : 65535)), dim3(64), 0, s, given ? given + 2 * at : nullptr,
                            spans + at, bounds + (size_t)n * 2 * tiles, T);
     }
+    if (order) hipLaunchKernelGGL(k_attention_order, dim3((unsigned)N, 2), dim3(1024), 0, s, (const int4 *)bounds, order, T);
     return hipGetLastError();
 }
 

@@ -202,7 +202,7 @@ struct bapipe_stage {
     // ATTENTION layers with spans: positions of a sequence, place in the slot of the clamped spans and their tiles' bounds, and what the caller
     // has set for the coming micro-batch
     int span_T = 0;
-    size_t off_spans = 0, off_bounds = 0;
+    size_t off_spans = 0, off_bounds = 0, off_order = 0;
     const int32_t *spans_given = nullptr;
     bool dx_at_dy = false, dx_across_dy = false;      // see dx_may_lie_over_dy: at the same address, at any other
     unsigned *tickets = nullptr, *tickets_f = nullptr, *tickets_b = nullptr;      // as work: of the pass being enqueued, of either
@@ -747,7 +747,16 @@ AttnArgs attn_args(bapipe_stage *st, const Layer &L, int mbid)
     q.lse = (float *)(slot + L.aux_off);
     q.spans = (const int2 *)(slot + st->off_spans);
     q.bounds = (const int4 *)(slot + st->off_bounds);
+    if (q.s.mask == ATTN_SPANS && st->off_order) q.order = (const int *)(slot + st->off_order);
     return q;
+}
+
+// given spans, or (NULL) those of a causal mask, to the slot
+hipError_t spans_of(bapipe_stage *st, const int32_t *given, int mbid)
+{
+    char *slot = st->slot(mbid);
+    return attention_spans(given, (int2 *)(slot + st->off_spans), (int4 *)(slot + st->off_bounds), st->off_order ? (int *)(slot + st->off_order) : nullptr,
+                           st->mb, st->span_T, st->stream);
 }
 
 int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
@@ -1863,6 +1872,7 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
             if (q.mask == ATTN_SPANS && !st->off_bounds) {
                 st->off_spans = slot; slot += align_up((size_t)q.N * q.T * sizeof(int2));
                 st->off_bounds = slot; slot += align_up((size_t)q.N * ((q.T + kAttnTile - 1) / kAttnTile) * 2 * sizeof(int4));
+                if (const size_t n = attention_order_size(q.N, q.T)) { st->off_order = slot; slot += align_up(n * sizeof(int)); }
             }
             const size_t w = attention_workspace(st->dt, q, L.a > 0 && st->layers[L.a - 1].half, st->compute_units);
             work = w > work ? w : work;
@@ -2115,7 +2125,7 @@ int bapipe_stage_forward(bapipe_stage_t *st, int mb_id, const void *x_dev, void 
         c.x_direct = x_dev;
     }
     if (st->span_T)
-        HIPCHK(attention_spans(st->spans_given, (int2 *)(st->slot(mb_id) + st->off_spans), (int4 *)(st->slot(mb_id) + st->off_bounds), st->mb, st->span_T, s));
+        HIPCHK(spans_of(st, st->spans_given, mb_id));
     const int last = (int)st->tensors.size() - 1;
     const Tensor &O = st->tensors[last];
     const Tensor &R = st->tensors[O.root];
@@ -2515,7 +2525,7 @@ int bapipe_profile_layers(bapipe_stage_t *st, int warmup, int iters, bapipe_laye
     HIPCHK(fill_f32((float *)st->slot(0), 0.f, st->slot_bytes / 4, s));
     HIPCHK(fill_f32((float *)st->transient, 0.f, st->transient_bytes / 4, s));
     HIPCHK(fill_f32((float *)st->grads, 0.f, st->grads_bytes / 4, s));
-    if (st->span_T) HIPCHK(attention_spans(nullptr, (int2 *)(st->slot(0) + st->off_spans), (int4 *)(st->slot(0) + st->off_bounds), st->mb, st->span_T, s));
+    if (st->span_T) HIPCHK(spans_of(st, nullptr, 0));
     hipEvent_t e0, e1;
     HIPCHK(hipEventCreate(&e0));
     HIPCHK(hipEventCreate(&e1));
