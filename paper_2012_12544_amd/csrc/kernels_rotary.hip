@@ -44,7 +44,7 @@ template <int L> __device__ __forceinline__ float group_max(float v)
 // where d and the turning part (in half layout each half of it) are whole such pieces; else V = 1, C = 8.  A group of L lanes takes K heads
 // of a position, all loaded before the first is worked on; their angles are the same.
 template <class T, int V, int C, int L, int K, bool PAIRS, bool NORM, bool BACK, bool FLOATS>
-__global__ __launch_bounds__(TPB) void k_rotary(RotaryArgs<T> p)
+__global__ __launch_bounds__(TPB, (BACK && NORM && !FLOATS ? 4 : 1)) void k_rotary(RotaryArgs<T> p)
 {
     typedef vec_t<T, V> vec;
     typedef vec_t<float, V> vecf;
@@ -266,13 +266,17 @@ __global__ __launch_bounds__(TPB) void k_rotary_table(float2 *table, size_t n, i
     table[i] = {(float)(a.magnitude * cosine), (float)(a.magnitude * sine)};
 }
 
-// K: a group of lanes takes four heads where there are enough of them for all units of the chip
+// K: a group of lanes takes two or three heads where there are enough of them for all units of the chip.  More share their angles' loads and
+// leave less room for other waves; 8192 positions of 32 / 8 heads of 128 with norms, us forward and backward: one head 98 and -, two 85 and 84,
+// three 77 and 80 (3.9 and 3.8 TB/s), four 85 and 93; 32768 of 16 / 16 heads of 128 without: 134, 136, 141, 144 either way; with norms, from float
+// gradients, 8192 of 16 / 2 heads: two 38, four 53.
+constexpr int rotary_heads(bool norm, bool floats) { return norm && !floats ? 3 : 2; }
 constexpr int kManyHeads = 32768;
 struct Plan {
     int lanes, K, per_row, per_unit, units, blocks;
     bool vec;
 };
-Plan plan(int dt, const RotaryShape &r, bool sums, bool all_heads, std::initializer_list<const void *> tensors)
+Plan plan(int dt, const RotaryShape &r, bool sums, bool all_heads, std::initializer_list<const void *> tensors, int many)
 {
     Plan p;
     const int V = 16 / (int)dt_size(dt);
@@ -281,7 +285,7 @@ Plan plan(int dt, const RotaryShape &r, bool sums, bool all_heads, std::initiali
     const int pieces = p.vec ? r.d / V : (r.d + 7) / 8;           // without vectors eight channels a lane
     for (p.lanes = 4; p.lanes < pieces;) p.lanes *= 2;
     p.per_row = r.heads + r.groups + (all_heads ? r.groups : 0);
-    p.K = p.vec && (long long)r.rows * p.per_row >= kManyHeads ? 4 : 1;
+    p.K = p.vec && (long long)r.rows * p.per_row >= kManyHeads ? many : 1;
     p.per_unit = (p.per_row + p.K - 1) / p.K;
     p.units = r.rows * p.per_unit;
     const int per_block = TPB / p.lanes;
@@ -302,7 +306,7 @@ template <class T, bool NORM, bool BACK, bool FLOATS = false> hipError_t launch(
         else hipLaunchKernelGGL((k_rotary<T, V, C, L, N, false, NORM, BACK, FLOATS>), dim3(p.blocks), dim3(TPB), 0, s, a);           \
         return hipGetLastError();                                                                                                    \
     }
-#define ROTARY_VEC(L) ROTARY(VEC, 1, L, 1) ROTARY(VEC, 1, L, 4)
+#define ROTARY_VEC(L) ROTARY(VEC, 1, L, 1) ROTARY(VEC, 1, L, (rotary_heads(NORM, FLOATS)))
     ROTARY_VEC(4) ROTARY_VEC(8) ROTARY_VEC(16) ROTARY_VEC(32)
     if constexpr (VEC == 4) { ROTARY_VEC(64) }
     ROTARY(1, 8, 4, 1) ROTARY(1, 8, 8, 1) ROTARY(1, 8, 16, 1) ROTARY(1, 8, 32, 1)
@@ -324,7 +328,7 @@ hipError_t rotary_table(float2 *table, int T, int rotated, const RotaryAngles &a
 template <class T>
 static hipError_t forward(const RotaryShape &r, const void *x, void *y, const float2 *table, const float *gains, hipStream_t s, void *half, float *half_scale, void *copy)
 {
-    const Plan p = plan(sizeof(T) == 4 ? DT_F32 : DT_BF16, r, false, r.values || copy, {x, y, half, copy});
+    const Plan p = plan(sizeof(T) == 4 ? DT_F32 : DT_BF16, r, false, r.values || copy, {x, y, half, copy}, rotary_heads(r.eps > 0.0f, false));
     RotaryArgs<T> a = {};
     a.r = r;
     a.x = (const T *)x;
@@ -347,7 +351,7 @@ size_t rotary_workspace(int dt, const RotaryShape &r)
 {
     // tensors at odd addresses are not read in vectors: a head to a group of no more lanes, so as many blocks or kGainBlocks at most
     if (!(r.eps > 0.0f)) return 0;
-    const Plan a = plan(dt, r, true, r.values, {}), b = plan(dt, r, true, r.values, {(const void *)1});
+    const Plan a = plan(dt, r, true, r.values, {}, 1), b = plan(dt, r, true, r.values, {(const void *)1}, 1);
     return (size_t)(a.blocks > b.blocks ? a.blocks : b.blocks) * 2 * r.d * sizeof(float);
 }
 
@@ -357,7 +361,7 @@ static hipError_t backward(const RotaryShape &r, const void *x, const void *dy, 
 {
     const bool norm = r.eps > 0.0f;
     if (!norm && !dx) return hipSuccess;
-    const Plan p = plan(sizeof(T) == 4 ? DT_F32 : DT_BF16, r, norm, r.values, {x, dy, dx, dy_float});
+    const Plan p = plan(sizeof(T) == 4 ? DT_F32 : DT_BF16, r, norm, r.values, {x, dy, dx, dy_float}, rotary_heads(norm, dy_float));
     RotaryArgs<T> a = {};
     a.r = r;
     a.x = (const T *)x;
