@@ -4,11 +4,13 @@
 namespace bapipe {
 namespace {
 
-// Rows of a tile.  bf16 heads of 192 channels: with 32 keys at a time registers and LDS hold two blocks a unit (of 256 that was as fast: 151 and 154 us)
-template <class T, int DP> constexpr int kFwdRows = sizeof(T) == 2 && DP == 192 ? 32 : 0;
+// Rows of a tile.  With 32 keys at a time registers and LDS hold three blocks of heads of 128 channels a unit instead of two, and two of 192 instead
+// of one (of 256 that was as fast: 151 and 154 us).  4 x 4096 positions, causal, 32 / 8 heads of 128, us: 705 with 64, 674; packed documents 173, 178;
+// 4 x 2048, causal, 16 / 2 heads of 16-bit floats: 112, 101.
+template <class T, int DP> constexpr int kFwdRows = sizeof(T) == 2 && (DP == 128 || DP == 192) ? 32 : 0;
 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF>
-__global__ __launch_bounds__(AT_TPB, (DP <= (sizeof(T) == 2 ? 192 : 64) ? 2 : 1)) void k_attention_fwd(AttnArgs p)
+__global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && DP == 128 && !EXTRA && !HALF ? 3 : DP <= (sizeof(T) == 2 ? 192 : 64) ? 2 : 1)) void k_attention_fwd(AttnArgs p)
 {
     constexpr int R = kFwdRows<T, DP>;
     typedef AtTile<T, DP, R> Tile;
