@@ -14,8 +14,8 @@ the working copy of conv/linear weight matrices.  Bias, gamma, beta, weight grad
 BN statistics, softmax and loss are never rounded.  Inside an LSTM layer the input projection
 of all steps and the pre-activation gradients are stored tensors too (rounded); the cell state
 and the recurrent sums are not.  A gated layer's projections are not rounded, their gradients
-are; the gradients that layer norm, gated layer and 1x1 convolution hand to each other are not.  Of a ROTARY that only an ATTENTION
-reads, scores are made of what it computed, the other products of what it stored, and the gradient between the two is not rounded.
+are; the gradients that layer norm, gated layer and 1x1 convolution hand to each other are not, nor is what a ROTARY and the ATTENTION
+that alone reads it do (which the library keeps in 16-bit floats with scales, eight times as fine).
 storage="exact" rounds nothing.
 """
 import numpy as np
@@ -156,13 +156,12 @@ class OracleStage:
                                            self.mini_batch)
                 y = q(a * extra)
             elif k == C.ROTARY:
-                y = extra = ops.rotary_fwd(a, *self._turned(i))
-                y = q(y)
+                y = ops.rotary_fwd(a, *self._turned(i))
+                if i not in self.float_grads:
+                    y = q(y)
             elif k == C.ATTENTION:
-                t = L["src0"]
-                fine = aux[t] if t in self.float_grads and self.layers[t]["kind"] == C.ROTARY else a
                 sees = ops.attention_sees(L["stride"], len(a), a.shape[2], self.spans.get(mb))
-                extra = ops.attention_probabilities(fine, L["kh"], L["kw"], sees, L["eps"], L["pad"])
+                extra = ops.attention_probabilities(a, L["kh"], L["kw"], sees, L["eps"], L["pad"])
                 y = q(ops.attention_fwd(a, L["kh"], L["kw"], extra[0]))
             elif k == C.SOFTMAX_XENT:
                 y = ops.softmax_fwd(a.reshape(a.shape[0], -1)).reshape(a.shape)

@@ -92,6 +92,16 @@ template <> struct AtWeights<bf16_t> {
         for (int i = 0; i < 8; ++i) v[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
     }
 };
+template <> struct AtWeights<half_t> {
+    uint32_t v[8];
+    __device__ __forceinline__ explicit AtWeights(const float (&x)[16])
+    {
+        typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+        typedef float f32x2_t __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{x[2 * i], x[2 * i + 1]}), f16x2_t));
+    }
+};
 
 // acc[t][element 32 (t0 + t) + register's row][owned row] += sum over the 32 streamed rows from row0 of their elements x weights
 template <class T, class Tile, int ND>
@@ -113,7 +123,7 @@ __device__ __forceinline__ void at_columns(f32x16_t (&acc)[ND], const unsigned c
                 const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)(from + lo_at + off));
                 const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)(from + hi_at + off));
                 const s16x8_t a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), as_frag(b), acc[t], 0, 0, 0);
+                at_mma<T>(acc[t], __builtin_bit_cast(chunk16, a), b);
             }
         }
     } else {
@@ -129,6 +139,31 @@ __device__ __forceinline__ void at_columns(f32x16_t (&acc)[ND], const unsigned c
             }
         }
     }
+}
+
+// the other half's value of an owned row, combined with this one's
+__device__ __forceinline__ float at_halves_max(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
+__device__ __forceinline__ float at_halves_sum(float v) { return v + __shfl_xor(v, 32, 64); }
+
+// 16-bit floats as weights: x times a power of two of the owned row's, mult, that takes the largest of all so far to at most 2^15 of a format that
+// ends at 65504.  It falls where a larger one comes, by so much that the next few times larger fit too, and what was summed up follows; weights
+// 2^25 below the largest lose digits, which are 2^-36 of the sum.  kAtRoom, the mult to begin with, takes all below 2^-85 as they are.
+constexpr float kAtRoom = 0x1p100f;
+template <int ND> __device__ __forceinline__ void at_fit(float (&x)[16], float &mult, f32x16_t (&acc)[ND])
+{
+    float most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(x[i]));
+    most = at_halves_max(most);
+    const bool over = most * mult > 0x1p15f;
+    if (__any(over)) {
+        const float next = over ? fminf(ldexpf(1.0f, 11 - __builtin_amdgcn_frexp_expf(most)), kAtRoom) : mult, fade = next / mult;
+        mult = next;
+#pragma unroll
+        for (int t = 0; t < ND; ++t) acc[t] *= fade;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] *= mult;
 }
 
 // The chunks of an owned row, which lies at `row` (NULL: zeros) with d elements
@@ -245,10 +280,6 @@ template <class T, int DP, bool VEC, int R = 0, bool AGAIN = true> struct AtStre
         }
     }
 };
-
-// the other half's value of an owned row, combined with this one's
-__device__ __forceinline__ float at_halves_max(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
-__device__ __forceinline__ float at_halves_sum(float v) { return v + __shfl_xor(v, 32, 64); }
 
 // What is done to a score on its way to the softmax, in units of log 2
 constexpr float kLog2e = 1.44269504088896341f;
@@ -393,9 +424,36 @@ template <class T, bool VEC, int ND> __device__ __forceinline__ void at_store(T 
                               acc[t][4 * g + 3] * by);
 }
 
+// What rounding to bf16 takes from a float: the difference of the two as numbers of 32 bits, in units of 2^8, and back
+__device__ __forceinline__ int at_low(float x)
+{
+    const int bits = (int)__float_as_uint(x), high = (int)(pack_bf16(x, 0.0f) << 16);
+    return min((bits - high + 128) >> 8, 127);
+}
+__device__ __forceinline__ float at_whole(uint32_t high, int low) { return __uint_as_float((high << 16) + ((uint32_t)low << 8)); }
+template <bool VEC, int ND> __device__ __forceinline__ void at_store_low(int8_t *row, int d, const f32x16_t (&acc)[ND], float by, int lane)
+{
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int e0 = 32 * t + 8 * g + 4 * (lane >> 5);
+            int low[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) low[j] = at_low(acc[t][4 * g + j] * by);
+            if constexpr (VEC) {
+                if (e0 < d) *(uint32_t *)(row + e0) = (low[0] & 255) | (low[1] & 255) << 8 | (low[2] & 255) << 16 | (uint32_t)low[3] << 24;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (e0 + j < d) row[e0 + j] = (int8_t)low[j];
+            }
+        }
+}
+
 // Calls F<T, DP, VEC, EXTRA, HALF> for a shape.  Heads of a width that is no multiple of 16 bytes are read element by element.
 // bf16 heads take the next multiple of 32 or 64; float and element-wise ones, of which fewer kernels are built, 64, 128 or 256.
-// HALF: scores are made of 16-bit floats (AttnArgs::half).
+// HALF: queries and keys are 16-bit floats (AttnArgs::half).
 template <template <class, int, bool, bool, bool> class F, class... A> hipError_t at_dispatch(int dt, const AttnArgs &p, const A &...a)
 {
     const AttnShape &s = p.s;

@@ -245,11 +245,14 @@ struct AttnArgs {
     AttnShape s;
     // qk: queries and keys, v: values; both point at a position's first query, and so do dqk and dv
     const void *qk, *v;
-    // bf16, or NULL: queries and keys once more, [N][T][heads + groups][d] 16-bit floats that were divided by powers of two, and
-    // those, [heads + groups][N T]: what scores are made of, eight times as fine
+    // bf16, or NULL: queries and keys instead, [N][T][heads + groups][d] 16-bit floats that were divided by powers of two, and those,
+    // [heads + groups][N T]: eight times as fine
     const void *half;
     const float *half_scale;
     void *o;                 // [N][T][heads d]
+    // bf16: what rounding took from o, the next eight bits of it, as a signed number that is added to them.  dout . o is what is taken from every
+    // product of a query's before the gradient of its scores, and where few keys have it all little is left
+    int8_t *o_low;
     // forward, or NULL: a second place for o; for qk (and v, which is the same tensor then; d a multiple of 16 bytes, 16-byte aligned)
     void *o2, *copy;
     float *lse;              // [N][heads][T]: log2 of a query's sum of exponentials, inf where it sees nothing
@@ -272,7 +275,7 @@ struct AttnArgs {
 hipError_t attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int *order, int N, int T, hipStream_t s);
 size_t attention_order_size(int N, int T);
 hipError_t attention_fwd(int dt, const AttnArgs &a, hipStream_t s);
-size_t attention_workspace(int dt, const AttnShape &a, bool half, int compute_units);          // of a backward pass; half: with AttnArgs::half
+size_t attention_workspace(int dt, const AttnShape &a, int compute_units);          // of a backward pass
 hipError_t attention_bwd(int dt, AttnArgs a, void *workspace, int compute_units, hipStream_t s);
 hipError_t attention_dq(int dt, const AttnArgs &a, hipStream_t s);
 hipError_t attention_dkv(int dt, const AttnArgs &a, hipStream_t s);
@@ -294,7 +297,7 @@ struct RotaryAngles {
 // cosine and sine [T][rotated / 2] times the magnitude
 hipError_t rotary_table(float2 *table, int T, int rotated, const RotaryAngles &a, hipStream_t s);
 // gains: [2][d], of query heads, of key heads; y may be x
-// half, half_scale: where an ATTENTION's AttnArgs find them (bf16), or NULL
+// half, half_scale: where an ATTENTION's AttnArgs find queries and keys (bf16), which y gets none of then, or NULL
 // copy: a second place for x, or NULL
 hipError_t rotary_fwd(int dt, const RotaryShape &r, const void *x, void *y, const float2 *table, const float *gains, hipStream_t s, void *half = nullptr,
                       float *half_scale = nullptr, void *copy = nullptr);

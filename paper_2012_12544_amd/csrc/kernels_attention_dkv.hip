@@ -9,17 +9,18 @@ namespace {
 // Float heads of more than 128 channels would need more registers than there are: their blocks own half of the gradients' columns, two to a key
 template <class T, int DP> constexpr int kDkvHalves = DP * (int)sizeof(T) > 768 ? 2 : 1;
 
-// Rows of a tile, 0: what two operands leave; three of 256 channels would need 192 KB
-template <int DP, bool HALF> constexpr int kDkvRows = HALF && DP > 192 ? 32 : 0;
+// Rows of a tile, 0: what fits.  16-bit floats of 128 channels, us: 66 registers are spilled with 64 rows, 286, and 36 with 32, 261; one wave a
+// SIMD, which spills none: 281.  (4 x 2048 positions, causal, 16 / 2 heads)
+template <int DP, bool EXTRA, bool HALF> constexpr int kDkvRows = HALF && !EXTRA && DP == 128 ? 32 : 0;
 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF>
-__global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA || HALF ? 192 : 256) ? 2 : 1)) void k_attention_dkv(AttnArgs p)
+__global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256) ? 2 : 1)) void k_attention_dkv(AttnArgs p)
 {
-    constexpr int R = kDkvRows<DP, HALF>;
+    constexpr int R = kDkvRows<DP, EXTRA, HALF>;
     typedef AtTile<T, DP, R> Tile;
-    typedef std::conditional_t<HALF, half_t, T> S;
+    typedef std::conditional_t<HALF, half_t, T> S;       // queries and keys
     typedef AtTile<S, DP, R> STile;
-    constexpr int HALVES = kDkvHalves<T, DP>, ND = DP / 32 / HALVES, SUBS = Tile::ROWS / 32, STREAMS = HALF ? 3 : 2;
+    constexpr int HALVES = kDkvHalves<T, DP>, ND = DP / 32 / HALVES, SUBS = Tile::ROWS / 32;
     static_assert(Tile::ROWS <= kAttnTile && kAttnTile % Tile::ROWS == 0, "");
     extern __shared__ __align__(256) unsigned char smem[];
     __shared__ int2 block_range[AT_WAVES];
@@ -31,8 +32,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA || HALF ? 19
     const int half = b.rest % HALVES, split = b.rest / HALVES % p.splits, key0 = at_key_block(p, b.n, b.rest / HALVES / p.splits) * AT_ROWS;
     const int wave0 = key0 + 32 * wave, own = wave0 + (lane & 31);
     const int sstride = HALF ? (s.heads + s.groups) * d : stride;
-    const T *base = (const T *)p.qk + (size_t)b.n * s.T * stride;
-    const S *score_base = (const S *)(HALF ? p.half : p.qk) + (size_t)b.n * s.T * sstride;
+    const S *base = (const S *)(HALF ? p.half : p.qk) + (size_t)b.n * s.T * sstride;
 
     // tiles of queries, from the first that sees one of the block's keys to the last
     const int all_tiles = (s.T + Tile::ROWS - 1) / Tile::ROWS;
@@ -72,18 +72,18 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA || HALF ? 19
     end = __builtin_amdgcn_readfirstlane(end);
     // as with the queries, what is behind the last key that is seen is not read
     chunk16 key[Tile::STEPS], value[Tile::STEPS];
-    at_own<S, DP, VEC>(key, own < seen ? score_base + (size_t)own * sstride + (size_t)(s.heads + b.g) * d : nullptr, d, lane);
+    at_own<S, DP, VEC>(key, own < seen ? base + (size_t)own * sstride + (size_t)(s.heads + b.g) * d : nullptr, d, lane);
     at_own<T, DP, VEC>(value, own < seen ? (const T *)p.v + ((size_t)b.n * s.T + own) * stride + (size_t)(s.heads + s.groups + b.g) * d : nullptr, d, lane);
     const float own_scale = HALF && own < seen ? p.half_scale[((size_t)(s.heads + b.g) * s.N + b.n) * s.T + own] : 1.0f;
     const int of_head = end > first ? end - first : 0, total = of_head * per;
     const int begin = (int)((long long)total * split / p.splits), stop = (int)((long long)total * (split + 1) / p.splits);
 
     const unsigned lds = at_lds(smem);
-    AtStream<T, DP, VEC, R> queries(stride, tid), gradients(ostride, tid);
-    AtStream<S, DP, VEC, R> score_queries(sstride, tid);
+    AtStream<S, DP, VEC, R> queries(sstride, tid);
+    AtStream<T, DP, VEC, R> gradients(ostride, tid);
     // of the rows of a tile, twice: 64 words each of lse, dout . o and scale, 128 of spans
     constexpr int ROW_BYTES = 5 * 256;
-    constexpr int ROWS_AT = 2 * STREAMS * Tile::BYTES;
+    constexpr int ROWS_AT = 4 * Tile::BYTES;
     // Head and tile of the loads that are under way, counted, so that addresses stay scalar.  Last tile first: with a causal mask all blocks of
     // a key head read the last ones.
     int next_head = 0, next_tile = 0;
@@ -106,12 +106,12 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA || HALF ? 19
             at_dma4(span, 2 * (s.T - q0), row + 768, tid);
             at_dma4(span + 32, 2 * (s.T - q0) - 64, row + 1024, tid);
         }
-        const int to = (it & 1) * STREAMS * Tile::BYTES;
-        queries.fill(smem, lds, to, base + (size_t)q0 * stride + (size_t)head * d, there, stride, d, tid);
+        const int to = (it & 1) * 2 * Tile::BYTES;
+        queries.fill(smem, lds, to, base + (size_t)q0 * sstride + (size_t)head * d, there, sstride, d, tid);
         gradients.fill(smem, lds, to + Tile::BYTES, (const T *)p.dout + ((size_t)b.n * s.T + q0) * ostride + (size_t)head * d, there, ostride, d, tid);
-        if (HALF) score_queries.fill(smem, lds, to + 2 * Tile::BYTES, score_base + (size_t)q0 * sstride + (size_t)head * d, there, sstride, d, tid);
     };
     f32x16_t dk[ND] = {}, dv[ND] = {};
+    float mult = HALF ? kAtRoom : 1.0f;
     AtScore score = {};
     int head_of = -1;
     if (begin < stop) fill(begin);
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA || HALF ? 19
             whole &= v.z <= wave0 && v.w >= wave0 + 32;
         }
         if (none) continue;
-        const unsigned char *query = smem + at * STREAMS * Tile::BYTES, *dout = query + Tile::BYTES, *score_query = HALF ? dout + Tile::BYTES : query;
+        const unsigned char *query = smem + at * 2 * Tile::BYTES, *dout = query + Tile::BYTES;
 #pragma unroll 1
         for (int u = 0; u < SUBS; ++u) {
             __builtin_amdgcn_sched_barrier(0);
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA || HALF ? 19
             const float by = score.scale * own_scale, unit = EXTRA ? 1.0f : by;
             float x[16], slope[16];
             f32x16_t w, dw;
-            at_rows<S, STile>(w, score_query, 32 * u, key, lane);
+            at_rows<S, STile>(w, query, 32 * u, key, lane);
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = w[i];
             if (HALF)
@@ -191,19 +191,27 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA || HALF ? 19
                     if (EXTRA) x[4 * g + j] *= slope[4 * g + j];
                 }
             }
-            at_columns<T, Tile>(dk, query, 32 * u, half * ND, AtWeights<T>(x), lane);
+            if (HALF) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 scale = *(const float4 *)(row + 512 + 32 * g);
+                    x[4 * g] *= scale.x; x[4 * g + 1] *= scale.y; x[4 * g + 2] *= scale.z; x[4 * g + 3] *= scale.w;
+                }
+                at_fit(x, mult, dk);
+            }
+            at_columns<S, STile>(dk, query, 32 * u, half * ND, AtWeights<S>(x), lane);
         }
     }
     if (own >= s.T) return;
     if (p.splits > 1) {
         float *to = p.part + ((((size_t)split * s.N + b.n) * s.groups + b.g) * s.T + own) * 2 * d;
-        at_store<float, VEC, ND>(to, d, half * ND, dk, s.scale, lane);
+        at_store<float, VEC, ND>(to, d, half * ND, dk, s.scale / mult, lane);
         at_store<float, VEC, ND>(to + d, d, half * ND, dv, 1.0f, lane);
         return;
     }
     const size_t row = (size_t)b.n * s.T + own, at_k = row * stride + (size_t)(s.heads + b.g) * d;
-    if (p.dqk_float) at_store<float, VEC, ND>(p.dqk_float + row * (s.heads + s.groups) * d + (size_t)(s.heads + b.g) * d, d, half * ND, dk, s.scale, lane);
-    else at_store<T, VEC, ND>((T *)p.dqk + at_k, d, half * ND, dk, s.scale, lane);
+    if (p.dqk_float) at_store<float, VEC, ND>(p.dqk_float + row * (s.heads + s.groups) * d + (size_t)(s.heads + b.g) * d, d, half * ND, dk, s.scale / mult, lane);
+    else at_store<T, VEC, ND>((T *)p.dqk + at_k, d, half * ND, dk, s.scale / mult, lane);
     at_store<T, VEC, ND>((T *)p.dv + at_k + (size_t)s.groups * d, d, half * ND, dv, 1.0f, lane);
 }
 
@@ -237,7 +245,7 @@ template <class T, int V> __global__ __launch_bounds__(256) void k_attention_joi
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Keys {
     static hipError_t go(const AttnArgs &a, hipStream_t stream)
     {
-        constexpr int smem = (HALF ? 6 : 4) * AtTile<T, DP, kDkvRows<DP, HALF>>::BYTES + 2 * 5 * 256;
+        constexpr int smem = 4 * AtTile<T, DP, kDkvRows<DP, EXTRA, HALF>>::BYTES + 2 * 5 * 256;
         return at_launch(k_attention_dkv<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.groups * ((a.s.T + AT_ROWS - 1) / AT_ROWS) * a.splits * kDkvHalves<T, DP>, smem, a,
                          stream);
     }
@@ -246,9 +254,9 @@ template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Keys {
 // In how many parts the queries of the keys' sums are taken.  A block owns 128 keys of a key head, for all query heads that share it: few of
 // them leave units idle or, where keys are seen by different numbers of queries, waiting for the longest.  Splits cost a pass over their sums:
 // 12 heads of 80, 3 x 1003 positions without a mask, 288 blocks of the 512 that fit, us: 69 in one part, 59 and 14 in three.
-int key_splits(int dt, const AttnShape &s, bool half, int compute_units)
+int key_splits(int dt, const AttnShape &s, int compute_units)
 {
-    const bool wide = dt == DT_F32 ? s.d > 64 : half ? s.d > 96 : s.d > 128;
+    const bool wide = dt == DT_F32 ? s.d > 64 : s.d > 128;
     const long long fit = (long long)(compute_units > 0 ? compute_units : 256) * (wide ? 1 : 2);
     const long long blocks = (long long)s.N * s.groups * ((s.T + AT_ROWS - 1) / AT_ROWS) * (dt == DT_F32 && s.d > 128 ? 2 : 1);
     const long long tiles = (long long)((s.T + 63) / 64) * (s.heads / s.groups);           // of queries
@@ -273,9 +281,9 @@ hipError_t attention_dkv(int dt, const AttnArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-size_t attention_workspace(int dt, const AttnShape &a, bool half, int compute_units)
+size_t attention_workspace(int dt, const AttnShape &a, int compute_units)
 {
-    const int splits = key_splits(dt, a, half, compute_units);
+    const int splits = key_splits(dt, a, compute_units);
     const size_t rows = ((size_t)a.N * a.heads * a.T * sizeof(float) + 255) / 256 * 256;
     return rows + (splits > 1 ? (size_t)splits * a.N * a.groups * a.T * 2 * a.d * sizeof(float) : 0);
 }
@@ -284,7 +292,7 @@ hipError_t attention_bwd(int dt, AttnArgs a, void *workspace, int compute_units,
 {
     a.dsum = (float *)workspace;
     a.part = (float *)((char *)workspace + ((size_t)a.s.N * a.s.heads * a.s.T * sizeof(float) + 255) / 256 * 256);
-    a.splits = key_splits(dt, a.s, a.half != nullptr, compute_units);
+    a.splits = key_splits(dt, a.s, compute_units);
     const hipError_t e = attention_dq(dt, a, s);
     return e == hipSuccess ? attention_dkv(dt, a, s) : e;
 }

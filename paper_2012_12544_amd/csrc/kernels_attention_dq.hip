@@ -8,11 +8,10 @@ namespace {
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF>
 __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void k_attention_dq(AttnArgs p)
 {
-    constexpr int R = HALF && DP >= 128 ? 32 : 0;        // three operands
-    typedef AtTile<T, DP, R> Tile;
-    typedef std::conditional_t<HALF, half_t, T> S;
-    typedef AtTile<S, DP, R> STile;
-    constexpr int ND = DP / 32, SUBS = Tile::ROWS / 32, STREAMS = HALF ? 3 : 2;
+    typedef AtTile<T, DP> Tile;
+    typedef std::conditional_t<HALF, half_t, T> S;       // queries and keys
+    typedef AtTile<S, DP> STile;
+    constexpr int ND = DP / 32, SUBS = Tile::ROWS / 32;
     extern __shared__ __align__(256) unsigned char smem[];
     __shared__ int2 block_range[AT_WAVES];
     const AttnShape &s = p.s;
@@ -22,8 +21,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
     const int head = b.g * per + b.rest % per, q0 = at_query_block(p, b.n, b.rest / per) * AT_ROWS;
     const int q = q0 + 32 * wave + (lane & 31);
     const int sstride = HALF ? (s.heads + s.groups) * d : stride;
-    const S *base = (const S *)(HALF ? p.half : p.qk) + (size_t)b.n * s.T * sstride, *score_keys = base + (size_t)(s.heads + b.g) * d;
-    const T *keys = (const T *)p.qk + (size_t)b.n * s.T * stride + (size_t)(s.heads + b.g) * d;
+    const S *base = (const S *)(HALF ? p.half : p.qk) + (size_t)b.n * s.T * sstride, *keys = base + (size_t)(s.heads + b.g) * d;
     const T *values = (const T *)p.v + (size_t)b.n * s.T * stride + (size_t)(s.heads + s.groups + b.g) * d;
     const float *key_scale = HALF ? p.half_scale + ((size_t)(s.heads + b.g) * s.N + b.n) * s.T : nullptr;
     const size_t at_o = ((size_t)b.n * s.T + q) * s.heads * d + (size_t)head * d, at_row = ((size_t)b.n * s.heads + head) * s.T + q;
@@ -37,11 +35,31 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
     {
         chunk16 o[Tile::STEPS];
         at_own<T, DP, VEC>(o, sees ? (const T *)p.o + at_o : nullptr, d, lane);
+        uint2 low[Tile::STEPS];
+        if (sizeof(T) == 2)
+#pragma unroll
+            for (int c = 0; c < Tile::STEPS; ++c) {
+                const int e0 = (2 * c + h) * 8;
+                low[c] = {0, 0};
+                if constexpr (VEC) {
+                    if (sees && e0 < d) low[c] = *(const uint2 *)(p.o_low + at_o + e0);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t b = sees && e0 + j < d ? (uint8_t)p.o_low[at_o + e0 + j] : 0;
+                        (j < 4 ? low[c].x : low[c].y) |= b << 8 * (j & 3);
+                    }
+                }
+            }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < Tile::STEPS; ++c)
 #pragma unroll
-            for (int j = 0; j < Tile::EPC; ++j) dsum = fmaf(chunk_value<T>(dout[c], j), chunk_value<T>(o[c], j), dsum);
+            for (int j = 0; j < Tile::EPC; ++j) {
+                float of = chunk_value<T>(o[c], j);
+                if (sizeof(T) == 2) of = at_whole(__float_as_uint(of) >> 16, (int)(int8_t)((j < 4 ? low[c].x : low[c].y) >> 8 * (j & 3)));
+                dsum = fmaf(chunk_value<T>(dout[c], j), of, dsum);
+            }
         dsum = at_halves_sum(dsum);
     }
     const float lse = sees ? p.lse[at_row] : __builtin_inff();
@@ -63,18 +81,18 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
     float by = score.scale;
     if (HALF && sees) by *= p.half_scale[((size_t)head * s.N + b.n) * s.T + q];
     const unsigned lds = at_lds(smem);
-    AtStream<S, DP, VEC, R> score_stream(sstride, tid);
-    AtStream<T, DP, VEC, R> stream(stride, tid);
-    constexpr int SCALE_AT = 2 * STREAMS * Tile::BYTES;      // 64 words, twice
+    AtStream<S, DP, VEC> key_stream(sstride, tid);
+    AtStream<T, DP, VEC> value_stream(stride, tid);
+    constexpr int SCALE_AT = 4 * Tile::BYTES;                // 64 words, twice
     auto fill = [&](int it) {
         const int k0 = first + it * Tile::ROWS;
-        const int to = (it & 1) * STREAMS * Tile::BYTES;
+        const int to = (it & 1) * 2 * Tile::BYTES;
         if (HALF && wave == 0) at_dma4(key_scale + k0, end - k0, lds + SCALE_AT + (it & 1) * 256, tid);
-        stream.fill(smem, lds, to, keys + (size_t)k0 * stride, end - k0, stride, d, tid);
-        stream.fill(smem, lds, to + Tile::BYTES, values + (size_t)k0 * stride, end - k0, stride, d, tid);
-        if (HALF) score_stream.fill(smem, lds, to + 2 * Tile::BYTES, score_keys + (size_t)k0 * sstride, end - k0, sstride, d, tid);
+        key_stream.fill(smem, lds, to, keys + (size_t)k0 * sstride, end - k0, sstride, d, tid);
+        value_stream.fill(smem, lds, to + Tile::BYTES, values + (size_t)k0 * stride, end - k0, stride, d, tid);
     };
     f32x16_t dq[ND] = {};
+    float mult = HALF ? kAtRoom : 1.0f;
     const int tiles = (end - first + Tile::ROWS - 1) / Tile::ROWS;
     if (tiles > 0) fill(0);
     for (int it = 0; it < tiles; ++it) {
@@ -83,12 +101,12 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
         if (it + 1 < tiles) fill(it + 1);
         const int k0 = first + it * Tile::ROWS;
         if (k0 >= range.any.y || k0 + Tile::ROWS <= range.any.x) continue;
-        const unsigned char *key = smem + (it & 1) * STREAMS * Tile::BYTES, *value = key + Tile::BYTES, *score_key = HALF ? value + Tile::BYTES : key;
+        const unsigned char *key = smem + (it & 1) * 2 * Tile::BYTES, *value = key + Tile::BYTES;
         const bool whole = k0 >= range.all.x && k0 + Tile::ROWS <= range.all.y;
 #pragma unroll 1
         for (int u = 0; u < SUBS; ++u) {
             f32x16_t w, dw;
-            at_rows<S, STile>(w, score_key, 32 * u, query, lane);
+            at_rows<S, STile>(w, key, 32 * u, query, lane);
             at_rows<T, Tile>(dw, value, 32 * u, dout, lane);
             float x[16], ds[16], slope[16];
 #pragma unroll
@@ -115,19 +133,27 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) ds[i] = EXTRA ? x[i] * ds[i] * slope[i] : x[i] * ds[i];
-            at_columns<T, Tile>(dq, key, 32 * u, 0, AtWeights<T>(ds), lane);
+            if (HALF) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 r = *(const float4 *)(smem + SCALE_AT + (it & 1) * 256 + 4 * (32 * u + 8 * g + 4 * h));
+                    ds[4 * g] *= r.x; ds[4 * g + 1] *= r.y; ds[4 * g + 2] *= r.z; ds[4 * g + 3] *= r.w;
+                }
+                at_fit(ds, mult, dq);
+            }
+            at_columns<S, STile>(dq, key, 32 * u, 0, AtWeights<S>(ds), lane);
         }
     }
     if (q >= s.T) return;
     const size_t row = (size_t)b.n * s.T + q;
-    if (p.dqk_float) at_store<float, VEC, ND>(p.dqk_float + row * (s.heads + s.groups) * d + (size_t)head * d, d, 0, dq, s.scale, lane);
-    else at_store<T, VEC, ND>((T *)p.dqk + row * stride + (size_t)head * d, d, 0, dq, s.scale, lane);
+    if (p.dqk_float) at_store<float, VEC, ND>(p.dqk_float + row * (s.heads + s.groups) * d + (size_t)head * d, d, 0, dq, s.scale / mult, lane);
+    else at_store<T, VEC, ND>((T *)p.dqk + row * stride + (size_t)head * d, d, 0, dq, s.scale / mult, lane);
 }
 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Queries {
     static hipError_t go(const AttnArgs &a, hipStream_t stream)
     {
-        constexpr int smem = HALF ? 6 * AtTile<T, DP, DP >= 128 ? 32 : 0>::BYTES + 512 : 4 * AtTile<T, DP>::BYTES;
+        constexpr int smem = 4 * AtTile<T, DP>::BYTES + (HALF ? 512 : 0);
         return at_launch(k_attention_dq<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS - 1) / AT_ROWS), smem, a, stream);
     }
 };

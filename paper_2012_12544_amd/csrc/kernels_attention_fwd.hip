@@ -148,6 +148,7 @@ __global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && DP == 128 && !EXTRA && !
     const bool sees = span.x < span.y;
     const size_t at_o = ((size_t)b.n * s.T + q) * s.heads * d + (size_t)head * d;
     at_store<T, VEC, ND>((T *)p.o + at_o, d, 0, out, sees ? 1.0f / sum : 0.0f, lane);
+    if (sizeof(T) == 2) at_store_low<VEC, ND>(p.o_low + at_o, d, out, sees ? 1.0f / sum : 0.0f, lane);
     if (p.o2) at_store<T, VEC, ND>((T *)p.o2 + at_o, d, 0, out, sees ? 1.0f / sum : 0.0f, lane);
     if (h == 0) p.lse[((size_t)b.n * s.heads + head) * s.T + q] = sees ? top + log2f(sum) : __builtin_inff();
 }

@@ -19,7 +19,7 @@ template <class T> struct RotaryArgs {
     const float2 *table;
     const float *gains;
     float *part;             // [blocks][2][d]
-    // forward: query and key heads once more as 16-bit floats, and their scales (AttnArgs); backward: their gradients as floats.  Or NULL
+    // forward: query and key heads as 16-bit floats instead, and their scales (AttnArgs); backward: their gradients as floats.  Or NULL
     uint16_t *half;
     float *half_scale;
     const float *dy_float;   // [rows][heads + groups][d]
@@ -200,6 +200,7 @@ __global__ __launch_bounds__(TPB, (BACK && NORM && !FLOATS ? 4 : 1)) void k_rota
                     for (int j = 0; j < V; ++j) out.e[j] = (_Float16)(z[c][j] * by);
                     __builtin_memcpy(__builtin_assume_aligned(p.half + ((size_t)row * turning + head) * d + e, 2 * V), &out, sizeof out);
                 }
+                continue;
             }
             if (BACK && !p.y) continue;                  // only the gains want a gradient
 #pragma unroll

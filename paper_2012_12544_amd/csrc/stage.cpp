@@ -122,14 +122,15 @@ struct Layer {
     // lies (the tensors share their storage) and value heads stay by themselves.
     float2 *table = nullptr;
     bool values_stay = false, dvalues_stay = false;
-    // bf16 ROTARY that only an ATTENTION reads: the slot also keeps its queries and keys as 16-bit floats with a scale for each head and position
-    // (off_half, off_scale), which scores are made of, and their gradients come back as floats (off_float, among the gradients).  A score is a
-    // sum of products of two rounded factors: with scores of standard deviation 4, which a cap is for, bf16 factors make gradients 1.05e-2 wrong
-    // in the 2-norm, 16-bit floats and float gradients 4.3e-3; at 1, with norms, 4.6e-3 and 3.5e-3.
+    // bf16 ROTARY that only an ATTENTION reads: its queries and keys go to the slot as 16-bit floats with a scale for each head and position
+    // (off_half, off_scale) and nowhere else, and their gradients come back as floats (off_float, among the gradients).  A score is a sum of
+    // products of two rounded factors: with scores of standard deviation 4, which a cap is for, bf16 factors make gradients 1.05e-2 wrong in
+    // the 2-norm, 16-bit floats and float gradients HALF_A; at 1, with norms, 4.6e-3 and HALF_B.
     bool half = false;
     size_t off_half = 0, off_scale = 0, off_float = 0;
-    // ATTENTION: logarithms of the sums (aux_off); where its input's gradient cannot be written at once (other readers, a ReLU in front), a place
-    // among the gradients: off_d, as for ROTARY
+    // ATTENTION: logarithms of the sums (aux_off), in bf16 what rounding took from the output (off_low); where its input's gradient cannot be
+    // written at once (other readers, a ReLU in front), a place among the gradients: off_d, as for ROTARY
+    size_t off_low = 0;
     bool by_copy = false;
     bool mfma = false;                   // its products run on the bf16 MFMA kernels
     bool groups = false;                 // its weight gradient may share a launch with others
@@ -745,6 +746,7 @@ AttnArgs attn_args(bapipe_stage *st, const Layer &L, int mbid)
     }
     q.o = st->tptr(L.o, mbid);
     q.lse = (float *)(slot + L.aux_off);
+    q.o_low = (int8_t *)(slot + L.off_low);
     q.spans = (const int2 *)(slot + st->off_spans);
     q.bounds = (const int4 *)(slot + st->off_bounds);
     if (q.s.mask == ATTN_SPANS && st->off_order) q.order = (const int *)(slot + st->off_order);
@@ -1655,12 +1657,11 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         Tensor &O = st->tensors[L.o];
         const bool only_attention = L.o != last_t && O.consumers.size() == 1 && st->layers[O.consumers[0]].d.kind == BAPIPE_ATTENTION;
         L.half = only_attention && st->dt == DT_BF16;
-        if (!L.w_elems) {
-            if (L.a == 0 || L.o == last_t || A.consumers.size() != 1) continue;
+        if (!L.w_elems && L.a != 0 && L.o != last_t && A.consumers.size() == 1) {
             const bapipe_layer_desc_t &P = st->layers[L.a - 1].d;
             if (P.kind == BAPIPE_CONV2D && !P.fuse_relu) O.root = L.a;
-        } else
-            L.values_stay = only_attention;
+        }
+        L.values_stay = only_attention && O.root == L.o && (L.w_elems || L.half);
     }
 
     // ---- what backward needs
@@ -1703,9 +1704,13 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         case BAPIPE_ROTARY:
             if (L.w_elems) RA.stashed = true;
             break;
-        case BAPIPE_ATTENTION:
-            RA.stashed = st->tensors[L.o].stashed = true;
+        case BAPIPE_ATTENTION: {
+            const Layer *R = rotary_before(st, L);
+            if (R && R->values_stay) st->tensors[root_of(R->a)].stashed = true;
+            if (!R || !R->values_stay || !R->half) RA.stashed = true;
+            st->tensors[L.o].stashed = true;
             break;
+        }
         case BAPIPE_MAXPOOL2D:
             if (RA.gated && RA.need_grad) st->tensors[L.o].stashed = true;   // pooled values gate the window
             break;
@@ -1869,12 +1874,13 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         if (L.d.kind == BAPIPE_ATTENTION) {
             const AttnShape q = attn_shape(st, L);
             L.aux_off = slot; L.aux_bytes = (size_t)q.N * q.heads * q.T * sizeof(float); slot += align_up(L.aux_bytes);
+            if (st->dt == DT_BF16) { L.off_low = slot; slot += align_up(st->tensors[L.o].elems); L.aux_bytes += st->tensors[L.o].elems; }
             if (q.mask == ATTN_SPANS && !st->off_bounds) {
                 st->off_spans = slot; slot += align_up((size_t)q.N * q.T * sizeof(int2));
                 st->off_bounds = slot; slot += align_up((size_t)q.N * ((q.T + kAttnTile - 1) / kAttnTile) * 2 * sizeof(int4));
                 if (const size_t n = attention_order_size(q.N, q.T)) { st->off_order = slot; slot += align_up(n * sizeof(int)); }
             }
-            const size_t w = attention_workspace(st->dt, q, L.a > 0 && st->layers[L.a - 1].half, st->compute_units);
+            const size_t w = attention_workspace(st->dt, q, st->compute_units);
             work = w > work ? w : work;
         }
         if (L.d.kind == BAPIPE_LSTM) {

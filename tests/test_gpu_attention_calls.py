@@ -393,7 +393,7 @@ def test_timing_and_profile_of_attention(dtype):
 
 def test_what_a_micro_batch_in_flight_holds():
     """A ROTARY in front of an ATTENTION turns the projection's output in place; in bf16 its queries and keys are kept in 16-bit floats with
-    a scale for each head and position as well."""
+    a scale for each head and position."""
     def per_micro_batch(norm, dtype):
         b = C._Builder()
         b.conv(64, 512, 1, src=-1)
@@ -405,8 +405,8 @@ def test_what_a_micro_batch_in_flight_holds():
         g.close()
         return per
     rows, es = 2 * 1024, 2
-    base = rows * (64 + 512 + 256) * es + rows * 4 * 4       # x, projection, attention's output, logarithms of its sums
+    base = rows * (64 + 512 + 256) * es + rows * 256 + rows * 4 * 4       # x, projection, attention's output and eight more bits of it, logarithms of its sums
     halves = rows * 6 * 64 * 2 + rows * 6 * 4
-    assert per_micro_batch(0, C.BF16) == base + halves
-    assert per_micro_batch(1, C.BF16) == base + halves + rows * 512 * es       # the norms' input stays as well
+    assert per_micro_batch(0, C.BF16) == per_micro_batch(1, C.BF16) == base + halves       # the norms' input, the values with it, is the projection
     assert per_micro_batch(0, C.FP32) == rows * (64 + 512 + 256) * 4 + rows * 4 * 4
+    assert per_micro_batch(1, C.FP32) == rows * (64 + 2 * 512 + 256) * 4 + rows * 4 * 4     # what was turned as well

@@ -166,7 +166,7 @@ def test_the_sublayers_gradients_against_differences(norm, layout, mask, cap, bi
 
 
 def test_what_the_oracle_rounds():
-    """Between a ROTARY and the ATTENTION that alone reads it nothing but the operands of products; with another reader all of it."""
+    """Between a ROTARY and the ATTENTION that alone reads it nothing; with another reader all of it."""
     def run(second):
         b = C._Builder()
         b.rotary(2, 1, 4, norm=1, src=-1)
@@ -183,8 +183,9 @@ def test_what_the_oracle_rounds():
 
     for second in (0, 1):
         o = run(second)
-        given = o.trace[(0, 1)]["dx"][:, :12]                # of queries and keys; what the values get is rounded for their input
-        assert np.array_equal(given, ops.round_bf16(given)) == bool(second)
+        for t in (o.trace[(0, 1)]["x"], o.trace[(0, 1)]["dx"]):
+            t = t[:, :12]                                    # queries and keys
+            assert np.array_equal(t, ops.round_bf16(t)) == bool(second)
         assert (0 in o.float_grads) == (not second)
 
 
