@@ -9,6 +9,7 @@
 // is read with the same order of rows (bf16: transposing LDS reads of four rows each; float: single words).
 // Nothing of a score's size ever leaves the registers.
 #pragma once
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
@@ -431,24 +432,63 @@ __device__ __forceinline__ int at_low(float x)
     return min((bits - high + 128) >> 8, 127);
 }
 __device__ __forceinline__ float at_whole(uint32_t high, int low) { return __uint_as_float((high << 16) + ((uint32_t)low << 8)); }
-template <bool VEC, int ND> __device__ __forceinline__ void at_store_low(int8_t *row, int d, const f32x16_t (&acc)[ND], float by, int lane)
+template <int ND> __device__ __forceinline__ void at_store_low(int8_t *row, int d, const f32x16_t (&acc)[ND], float by, int lane)
 {
 #pragma unroll
     for (int t = 0; t < ND; ++t)
 #pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int e = 32 * t + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
+            if (e < d) row[e] = (int8_t)at_low(acc[t][i] * by);
+        }
+}
+
+// The rows of a wave, through LDS, so that lanes next to each other write what is next to each other (a lane has four neighbouring elements of its
+// row at a time; forward, 4 x 4096 positions, causal, 32 / 8 heads of 128, two places for the output: 705 us from the registers, 645 so).  own: kAtOwn<DP> bytes of LDS that are this wave's alone; to: its first row, rows: how many there are; d a multiple of 8.
+template <int DP> constexpr int kAtOwn = 32 * (2 * DP + 16);
+template <int DP, int ND>
+__device__ __forceinline__ void at_store_rows(unsigned char *own, bf16_t *to, bf16_t *to2, size_t stride, int rows, int d, const f32x16_t (&acc)[ND], float by,
+                                              int lane)
+{
+    constexpr int CH = DP / 8, RB = 2 * DP + 16;
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const int e0 = 32 * t + 8 * g + 4 * (lane >> 5);
+            const chunk8 c = {pack_bf16(acc[t][4 * g] * by, acc[t][4 * g + 1] * by), pack_bf16(acc[t][4 * g + 2] * by, acc[t][4 * g + 3] * by)};
+            *(chunk8 *)(own + (lane & 31) * RB + 2 * (32 * t + 8 * g + 4 * (lane >> 5))) = c;
+        }
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i0 = 0; i0 < 32 * CH; i0 += 64) {
+        const int i = i0 + lane, row = i / CH, c = i % CH;
+        if (row >= rows || 8 * c >= d) continue;
+        const chunk16 v = *(const chunk16 *)(own + row * RB + 16 * c);
+        *(chunk16 *)(to + row * stride + 8 * c) = v;
+        if (to2) *(chunk16 *)(to2 + row * stride + 8 * c) = v;
+    }
+}
+template <int DP, int ND>
+__device__ __forceinline__ void at_store_low_rows(unsigned char *own, int8_t *to, size_t stride, int rows, int d, const f32x16_t (&acc)[ND], float by, int lane)
+{
+    constexpr int CH = DP / 8, RB = DP + 8;
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
             int low[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) low[j] = at_low(acc[t][4 * g + j] * by);
-            if constexpr (VEC) {
-                if (e0 < d) *(uint32_t *)(row + e0) = (low[0] & 255) | (low[1] & 255) << 8 | (low[2] & 255) << 16 | (uint32_t)low[3] << 24;
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (e0 + j < d) row[e0 + j] = (int8_t)low[j];
-            }
+            *(uint32_t *)(own + (lane & 31) * RB + 32 * t + 8 * g + 4 * (lane >> 5)) = (low[0] & 255) | (low[1] & 255) << 8 | (low[2] & 255) << 16 | (uint32_t)low[3] << 24;
         }
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i0 = 0; i0 < 32 * CH; i0 += 64) {
+        const int i = i0 + lane, row = i / CH, c = i % CH;
+        if (row < rows && 8 * c < d) *(chunk8 *)(to + row * stride + 8 * c) = *(const chunk8 *)(own + row * RB + 8 * c);
+    }
 }
 
 // Calls F<T, DP, VEC, EXTRA, HALF> for a shape.  Heads of a width that is no multiple of 16 bytes are read element by element.

@@ -202,6 +202,18 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256)
             at_columns<S, STile>(dk, query, 32 * u, half * ND, AtWeights<S>(x), lane);
         }
     }
+    if constexpr (VEC && sizeof(T) == 2) {
+        if (p.splits == 1) {
+            at_barrier();                                  // the tiles are read
+            unsigned char *mine = smem + wave * kAtOwn<DP>;
+            const size_t at_k = ((size_t)b.n * s.T + wave0) * stride + (size_t)(s.heads + b.g) * d;
+            if (!p.dqk_float) at_store_rows<DP, ND>(mine, (T *)p.dqk + at_k, nullptr, stride, s.T - wave0, d, dk, s.scale / mult, lane);
+            else if (own < s.T)
+                at_store<float, VEC, ND>(p.dqk_float + (((size_t)b.n * s.T + own) * (s.heads + s.groups) + s.heads + b.g) * d, d, 0, dk, s.scale / mult, lane);
+            at_store_rows<DP, ND>(mine, (T *)p.dv + at_k + (size_t)s.groups * d, nullptr, stride, s.T - wave0, d, dv, 1.0f, lane);
+            return;
+        }
+    }
     if (own >= s.T) return;
     if (p.splits > 1) {
         float *to = p.part + ((((size_t)split * s.N + b.n) * s.groups + b.g) * s.T + own) * 2 * d;
@@ -245,7 +257,7 @@ template <class T, int V> __global__ __launch_bounds__(256) void k_attention_joi
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Keys {
     static hipError_t go(const AttnArgs &a, hipStream_t stream)
     {
-        constexpr int smem = 4 * AtTile<T, DP, kDkvRows<DP, EXTRA, HALF>>::BYTES + 2 * 5 * 256;
+        constexpr int smem = std::max(4 * AtTile<T, DP, kDkvRows<DP, EXTRA, HALF>>::BYTES + 2 * 5 * 256, sizeof(T) == 2 ? AT_WAVES * kAtOwn<DP> : 0);
         return at_launch(k_attention_dkv<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.groups * ((a.s.T + AT_ROWS - 1) / AT_ROWS) * a.splits * kDkvHalves<T, DP>, smem, a,
                          stream);
     }

@@ -144,6 +144,14 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
             at_columns<S, STile>(dq, key, 32 * u, 0, AtWeights<S>(ds), lane);
         }
     }
+    if (VEC && sizeof(T) == 2 && !p.dqk_float) {
+        at_barrier();                                      // the tiles are read
+        const int row0 = q0 + 32 * wave;
+        if constexpr (VEC && sizeof(T) == 2)
+            at_store_rows<DP, ND>(smem + wave * kAtOwn<DP>, (T *)p.dqk + ((size_t)b.n * s.T + row0) * stride + (size_t)head * d, nullptr, stride, s.T - row0, d, dq,
+                                  s.scale / mult, lane);
+        return;
+    }
     if (q >= s.T) return;
     const size_t row = (size_t)b.n * s.T + q;
     if (p.dqk_float) at_store<float, VEC, ND>(p.dqk_float + row * (s.heads + s.groups) * d + (size_t)head * d, d, 0, dq, s.scale / mult, lane);
@@ -153,7 +161,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Queries {
     static hipError_t go(const AttnArgs &a, hipStream_t stream)
     {
-        constexpr int smem = 4 * AtTile<T, DP>::BYTES + (HALF ? 512 : 0);
+        constexpr int smem = std::max(4 * AtTile<T, DP>::BYTES + (HALF ? 512 : 0), sizeof(T) == 2 ? AT_WAVES * kAtOwn<DP> : 0);
         return at_launch(k_attention_dq<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS - 1) / AT_ROWS), smem, a, stream);
     }
 };

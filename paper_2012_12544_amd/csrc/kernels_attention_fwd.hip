@@ -10,7 +10,7 @@ namespace {
 template <class T, int DP> constexpr int kFwdRows = sizeof(T) == 2 && (DP == 128 || DP == 192) ? 32 : 0;
 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF>
-__global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && DP == 128 && !EXTRA && !HALF ? 3 : DP <= (sizeof(T) == 2 ? 192 : 64) ? 2 : 1)) void k_attention_fwd(AttnArgs p)
+__global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && DP == 128 && !EXTRA ? 3 : DP <= (sizeof(T) == 2 ? 192 : 64) ? 2 : 1)) void k_attention_fwd(AttnArgs p)
 {
     constexpr int R = kFwdRows<T, DP>;
     typedef AtTile<T, DP, R> Tile;
@@ -144,19 +144,29 @@ __global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && DP == 128 && !EXTRA && !
         }
     }
     sum = at_halves_sum(sum);
-    if (q >= s.T) return;
     const bool sees = span.x < span.y;
-    const size_t at_o = ((size_t)b.n * s.T + q) * s.heads * d + (size_t)head * d;
-    at_store<T, VEC, ND>((T *)p.o + at_o, d, 0, out, sees ? 1.0f / sum : 0.0f, lane);
-    if (sizeof(T) == 2) at_store_low<VEC, ND>(p.o_low + at_o, d, out, sees ? 1.0f / sum : 0.0f, lane);
-    if (p.o2) at_store<T, VEC, ND>((T *)p.o2 + at_o, d, 0, out, sees ? 1.0f / sum : 0.0f, lane);
+    const float by_sum = sees ? 1.0f / sum : 0.0f;
+    if constexpr (VEC && sizeof(T) == 2) {
+        at_barrier();                                      // the tiles are read
+        const int row0 = q0 + 32 * wave, rows = s.T - row0;
+        const size_t at_o = ((size_t)b.n * s.T + row0) * s.heads * d + (size_t)head * d, ostride = (size_t)s.heads * d;
+        unsigned char *own = smem + wave * kAtOwn<DP>;
+        at_store_rows<DP, ND>(own, (T *)p.o + at_o, p.o2 ? (T *)p.o2 + at_o : nullptr, ostride, rows, d, out, by_sum, lane);
+        at_store_low_rows<DP, ND>(own, p.o_low + at_o, ostride, rows, d, out, by_sum, lane);
+    } else if (q < s.T) {
+        const size_t at_o = ((size_t)b.n * s.T + q) * s.heads * d + (size_t)head * d;
+        at_store<T, VEC, ND>((T *)p.o + at_o, d, 0, out, by_sum, lane);
+        if (p.o2) at_store<T, VEC, ND>((T *)p.o2 + at_o, d, 0, out, by_sum, lane);
+        if (sizeof(T) == 2) at_store_low<ND>(p.o_low + at_o, d, out, by_sum, lane);
+    }
+    if (q >= s.T) return;
     if (h == 0) p.lse[((size_t)b.n * s.heads + head) * s.T + q] = sees ? top + log2f(sum) : __builtin_inff();
 }
 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Forward {
     static hipError_t go(const AttnArgs &a, hipStream_t stream)
     {
-        return at_launch(k_attention_fwd<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS - 1) / AT_ROWS), 4 * AtTile<T, DP, kFwdRows<T, DP>>::BYTES + (HALF ? 512 : 0), a, stream);
+        return at_launch(k_attention_fwd<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS - 1) / AT_ROWS), std::max(4 * AtTile<T, DP, kFwdRows<T, DP>>::BYTES + (HALF ? 512 : 0), sizeof(T) == 2 ? AT_WAVES * kAtOwn<DP> : 0), a, stream);
     }
 };
 
