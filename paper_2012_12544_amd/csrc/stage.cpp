@@ -1659,7 +1659,9 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         L.half = only_attention && st->dt == DT_BF16;
         if (!L.w_elems && L.a != 0 && L.o != last_t && A.consumers.size() == 1) {
             const bapipe_layer_desc_t &P = st->layers[L.a - 1].d;
-            if (P.kind == BAPIPE_CONV2D && !P.fuse_relu) O.root = L.a;
+            bool flattened = false;                   // a view that was made of the output's storage before
+            for (int j : O.consumers) flattened |= st->layers[j].d.kind == BAPIPE_FLATTEN;
+            if (P.kind == BAPIPE_CONV2D && !P.fuse_relu && !flattened) O.root = L.a;
         }
         L.values_stay = only_attention && O.root == L.o && (L.w_elems || L.half);
     }

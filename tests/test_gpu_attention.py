@@ -565,9 +565,45 @@ def _graphs():
         b.rotary(H, G, d, norm=1)
         b.attention(H, G, d)
 
+    def turned_in_place_for_two(b):
+        b.conv(wide, wide, 1, src=-1)
+        b.rotary(H, G, d)
+        b.attention(H, G, d, src=1)
+        b.conv(wide, H * d, 1, src=1)
+        b.addl(2, 3, relu=0)
+
+    def turned_in_place_for_a_sum(b):
+        b.conv(wide, wide, 1, src=-1)
+        b.rotary(H, G, d, layout=1)
+        b.addl(1, -1, relu=0)
+        b.attention(H, G, d)
+
+    def two_rotaries_of_one(b):
+        b.conv(wide, wide, 1, src=-1)
+        b.rotary(H, G, d, norm=1, src=0)
+        b.rotary(H, G, d, src=0)
+        b.attention(H, G, d, src=1)
+        b.attention(H, G, d, C.MASK_NONE, src=2)
+        b.addl(3, 4, relu=0)
+
+    def a_recurrence_and_a_loss_behind(b):
+        b.bn(wide, src=-1)
+        b.attention(H, G, d)
+        b.lstm(H * d, 16)
+        b.flatten()
+        b.linear(16 * 37, 10)
+        b.xent()
+
+    def rotary_before_a_linear_layer(b):
+        b.conv(wide, wide, 1, src=-1)
+        b.rotary(H, G, d)
+        b.flatten()
+        b.linear(wide * 37, 10)
+
     return {f.__name__: f for f in (two_readers_of_the_input, rotary_with_two_readers, projection_with_two_readers, behind_a_relu,
                                     attention_behind_a_relu, rotary_of_a_relu_layer, two_in_a_row, attention_twice,
-                                    two_attentions_of_a_rotary, rotary_last, gated_behind, sum_in_front)}
+                                    two_attentions_of_a_rotary, rotary_last, gated_behind, sum_in_front, turned_in_place_for_two,
+                                    turned_in_place_for_a_sum, two_rotaries_of_one, a_recurrence_and_a_loss_behind, rotary_before_a_linear_layer)}
 
 
 @BOTH

@@ -370,6 +370,20 @@ def test_a_window_over_a_long_sequence(dtype, T, window):
             assert e <= limit * np.linalg.norm(b[:, :, lo:lo + T // 10]), (name, lo)
 
 
+def test_sums_that_the_static_workspace_does_not_hold():
+    """Few key heads of many positions: the parts of their sums take more than the array.  The call is refused and the other one works."""
+    st = _attention(C.BF16, 8, 1, 128, 16384, C.MASK_CAUSAL, micro_batch=1)
+    xs, gs = stage_io(st)
+    g = GpuStage(st, [(None, None)])
+    g.forward(0, xs[0])
+    with pytest.raises(B.BapipeError) as e:
+        g.backward(0, gs[0], static=True)
+    assert e.value.status == B.E_UNSUPPORTED
+    dx = g.backward(0, gs[0])
+    assert np.all(np.isfinite(dx)) and np.linalg.norm(dx) > 0
+    g.close()
+
+
 # ------------------------------------------------------------------------------ profile and timing
 @BOTH
 def test_timing_and_profile_of_attention(dtype):
