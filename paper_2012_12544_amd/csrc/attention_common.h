@@ -65,15 +65,17 @@ template <int N, int AHEAD> __device__ __forceinline__ void at_order()
     __builtin_amdgcn_sched_group_barrier(0x008, first, 0);
 }
 
-// acc = 32 streamed rows from row0 of the tile x owned rows
+// acc = 32 streamed rows from row0 of the tile x owned rows.  Floats leave out what is behind their d elements: their tiles are built for 64, 128
+// and 256, and a step takes four instructions of 64 cycles.
 template <class T, class Tile>
-__device__ __forceinline__ void at_rows(f32x16_t &acc, const unsigned char *tile, int row0, const chunk16 (&own)[Tile::STEPS], int lane)
+__device__ __forceinline__ void at_rows(f32x16_t &acc, const unsigned char *tile, int row0, const chunk16 (&own)[Tile::STEPS], int d, int lane)
 {
     const int row = lane & 31, h = lane >> 5;
     acc = f32x16_t{};
 #pragma unroll
     for (int c = 0; c < Tile::STEPS; ++c)
-        at_mma<T>(acc, *(const chunk16 *)(tile + Tile::at(0, row, 2 * (c & 1) + h) + ((c >> 1) * Tile::ROWS + row0) * 64), own[c]);
+        if (sizeof(T) == 2 || 2 * c * Tile::EPC < d)
+            at_mma<T>(acc, *(const chunk16 *)(tile + Tile::at(0, row, 2 * (c & 1) + h) + ((c >> 1) * Tile::ROWS + row0) * 64), own[c]);
 }
 
 // The right operand of a product that sums over 32 streamed rows: the registers of at_rows, in the storage type
@@ -106,7 +108,7 @@ template <> struct AtWeights<half_t> {
 
 // acc[t][element 32 (t0 + t) + register's row][owned row] += sum over the 32 streamed rows from row0 of their elements x weights
 template <class T, class Tile, int ND>
-__device__ __forceinline__ void at_columns(f32x16_t (&acc)[ND], const unsigned char *tile, int row0, int t0, const AtWeights<T> &w, int lane)
+__device__ __forceinline__ void at_columns(f32x16_t (&acc)[ND], const unsigned char *tile, int row0, int t0, const AtWeights<T> &w, int d, int lane)
 {
     const int h = lane >> 5;
     if constexpr (sizeof(T) == 2) {
@@ -131,10 +133,11 @@ __device__ __forceinline__ void at_columns(f32x16_t (&acc)[ND], const unsigned c
         const int e = lane & 31;
         const unsigned char *from = tile + 2 * t0 * (Tile::ROWS * 64);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int at = Tile::at(e >> 4, 8 * ((i >> 2) & 1) + 4 * h, (e >> 2) & 3) + 4 * (e & 3);
+        for (int t = 0; t < ND; ++t) {
+            if (32 * (t0 + t) >= d) break;
 #pragma unroll
-            for (int t = 0; t < ND; ++t) {
+            for (int i = 0; i < 16; ++i) {
+                const int at = Tile::at(e >> 4, 8 * ((i >> 2) & 1) + 4 * h, (e >> 2) & 3) + 4 * (e & 3);
                 const float a = *(const float *)(from + at + (2 * t * Tile::ROWS + row0 + 16 * (i >> 3) + (i & 3)) * 64);
                 acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.v[i], acc[t], 0, 0, 0);
             }
@@ -223,8 +226,16 @@ __device__ __forceinline__ void at_dma4(const void *from, int words, unsigned ld
                  "s"(at_resource(from, words > 0 ? words * 4 : 0)));
 }
 
-// Fills tiles from rows of d elements, `stride` elements apart.  VEC: d a multiple of a chunk and 16-byte aligned rows; asynchronous,
-// complete after WAIT_VMCNT(0) and a barrier.  Rows that are not there, and what is behind d, are zeros: zero times zero is what the products
+template <int OFF> __device__ __forceinline__ void at_dma4(__amdgpu_buffer_rsrc_t rsrc, unsigned lds_addr, unsigned voffset)
+{
+    static_assert(OFF >= 0 && OFF < 4096, "");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen offset:%3 lds" ::"s"(lds_addr - OFF), "v"(voffset), "s"(rsrc), "n"(OFF));
+}
+
+// Fills tiles from rows of d elements, `stride` elements apart.  VEC: d a multiple of a chunk and 16-byte aligned rows.  These and all floats, which
+// come word by word, are asynchronous: complete after WAIT_VMCNT(0) and a barrier.
+// (Causal float heads of 45 channels, 4 x 1024 positions, 8 of them, a mini-batch: 431 us element by element through registers, 356.)
+// Rows that are not there, and what is behind d, are zeros: zero times zero is what the products
 // see of them, whatever memory holds.
 // AGAIN: a lane's place is worked out again for every tile (see at_again), else it is kept.
 template <class T, int DP, bool VEC, int R = 0, bool AGAIN = true> struct AtStream {
@@ -251,6 +262,14 @@ template <class T, int DP, bool VEC, int R = 0, bool AGAIN = true> struct AtStre
             issue<I + 1>(rsrc, lds_addr, at, chunk, chunks);
         }
     }
+    // words of a group of 64 bytes: 16 rows at once
+    template <int G> static __device__ __forceinline__ void words(__amdgpu_buffer_rsrc_t rsrc, unsigned lds_addr, unsigned at, int left)
+    {
+        if constexpr (G < DP / 16) {
+            at_dma4<G * 64>(rsrc, lds_addr + G * Tile::ROWS * 64, 16 * G < left ? at : 0x80000000u);
+            words<G + 1>(rsrc, lds_addr, at, left);
+        }
+    }
     // to: the tile's place in the block's LDS, which begins at `lds`; from: the tile's first row; rows: how many there are from it on
     __device__ __forceinline__ void fill(unsigned char *smem, unsigned lds, int to, const T *from, int rows, int stride, int d, int tid)
     {
@@ -263,6 +282,17 @@ template <class T, int DP, bool VEC, int R = 0, bool AGAIN = true> struct AtStre
             const unsigned lds_addr = lds + to + (unsigned)__builtin_amdgcn_readfirstlane(tid >> 6) * 1024;
             if (d == DP) issue<0>(rsrc, lds_addr, at, 0, 1 << 20);
             else issue<0>(rsrc, lds_addr, at, chunk, d / Tile::EPC);
+        } else if constexpr (sizeof(T) == 4) {
+            const int n = rows < Tile::ROWS ? rows : Tile::ROWS;
+            const int bytes = n > 0 ? (int)(((long long)(n - 1) * stride + d) * 4) : 0;
+            const __amdgpu_buffer_rsrc_t rsrc = at_resource(from, bytes);
+            const int t = at_again(tid), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+            const int e = 4 * (((t >> 2) & 3) ^ wave) + (t & 3);                  // row / 4 of a lane's rows is the wave, modulo 4
+#pragma unroll
+            for (int q = 0; q < Tile::ROWS / 16; ++q) {
+                const int r = 16 * q + (t >> 4);
+                words<0>(rsrc, lds + to + q * 1024 + wave * 256, r < n ? (unsigned)r * (unsigned)(stride * 4) + 4 * e : 0x80000000u, d - e);
+            }
         } else {
             constexpr int AT_ONCE = 32 / Tile::EPC < ISSUES ? 32 / Tile::EPC : ISSUES;      // 32 loads under way
             static_assert(ISSUES % AT_ONCE == 0, "");

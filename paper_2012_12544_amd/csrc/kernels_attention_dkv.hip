@@ -147,7 +147,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256)
             const float by = score.scale * own_scale, unit = EXTRA ? 1.0f : by;
             float x[16], slope[16];
             f32x16_t w, dw;
-            at_rows<S, STile>(w, query, 32 * u, key, lane);
+            at_rows<S, STile>(w, query, 32 * u, key, d, lane);
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = w[i];
             if (HALF)
@@ -179,8 +179,8 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256)
                     for (int j = 0; j < 4; ++j) x[4 * g + j] = k >= f[j] && k < e[j] ? x[4 * g + j] : 0.0f;
                 }
             }
-            at_columns<T, Tile>(dv, dout, 32 * u, half * ND, AtWeights<T>(x), lane);
-            at_rows<T, Tile>(dw, dout, 32 * u, value, lane);
+            at_columns<T, Tile>(dv, dout, 32 * u, half * ND, AtWeights<T>(x), d, lane);
+            at_rows<T, Tile>(dw, dout, 32 * u, value, d, lane);
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const float4 dsum = *(const float4 *)(row + 256 + 32 * g);
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256)
                 }
                 at_fit(x, mult, dk);
             }
-            at_columns<S, STile>(dk, query, 32 * u, half * ND, AtWeights<S>(x), lane);
+            at_columns<S, STile>(dk, query, 32 * u, half * ND, AtWeights<S>(x), d, lane);
         }
     }
     if constexpr (VEC && sizeof(T) == 2) {

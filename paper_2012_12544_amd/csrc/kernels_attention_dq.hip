@@ -106,8 +106,8 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
 #pragma unroll 1
         for (int u = 0; u < SUBS; ++u) {
             f32x16_t w, dw;
-            at_rows<S, STile>(w, key, 32 * u, query, lane);
-            at_rows<T, Tile>(dw, value, 32 * u, dout, lane);
+            at_rows<S, STile>(w, key, 32 * u, query, d, lane);
+            at_rows<T, Tile>(dw, value, 32 * u, dout, d, lane);
             float x[16], ds[16], slope[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
                 }
                 at_fit(ds, mult, dq);
             }
-            at_columns<S, STile>(dq, key, 32 * u, 0, AtWeights<S>(ds), lane);
+            at_columns<S, STile>(dq, key, 32 * u, 0, AtWeights<S>(ds), d, lane);
         }
     }
     if (VEC && sizeof(T) == 2 && !p.dqk_float) {

@@ -90,7 +90,7 @@ __global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && DP == 128 && !EXTRA ? 3 
 #pragma unroll
         for (int u = 0; u < SUBS; ++u) {
             f32x16_t w;
-            at_rows<S, STile>(w, key, 32 * u, query, lane);
+            at_rows<S, STile>(w, key, 32 * u, query, d, lane);
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[u][i] = w[i];
             if (HALF)
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && DP == 128 && !EXTRA ? 3 
                 x[u][i] = __builtin_amdgcn_exp2f(fmaf(x[u][i], unit, -less));
                 sum += x[u][i];
             }
-            at_columns<T, Tile>(out, value, 32 * u, 0, AtWeights<T>(x[u]), lane);
+            at_columns<T, Tile>(out, value, 32 * u, 0, AtWeights<T>(x[u]), d, lane);
         }
     }
     sum = at_halves_sum(sum);
