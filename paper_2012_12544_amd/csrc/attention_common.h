@@ -403,16 +403,41 @@ __device__ __forceinline__ AtBlock at_block(const AttnShape &s)
     return {ng / s.groups, ng % s.groups, (int)(blockIdx.x / of)};
 }
 
+// KS waves of a block share 32 rows, each for its part of every tile's 32-row pieces, and add up what they have in LDS at the end: where rows are
+// few that makes twice as many blocks, or keeps waves busy that have no rows of their own.  Tiles of 64 rows.  us for the forward pass, dq and dkv
+// with KS 1 and 2: 4 x 333 positions of 6 / 2 float heads of 45, 72 blocks of 128 rows: 40, 52, 67 and 28, 34, 43; 64 x 50 of 16 / 4 heads of 64:
+// 14.2, 15.2, 14.6 and 13.9, 14.9, 12.2; but 3 x 1003 of 12 heads of 80, 288 blocks for 256 units: 49, 55, 66 and 45, 58, 73.
+template <class T, int DP> constexpr bool kAtShares = AtTile<T, DP>::ROWS == 64;
+inline bool at_shares(const AttnArgs &a, long long blocks) { return a.s.T <= 64 || blocks <= a.units; }
+
 // Which block of rows is the i-th to be started: those with the most to do first, with a causal mask the last queries and the first keys
-__device__ __forceinline__ int at_query_block(const AttnArgs &a, int n, int i)
+template <int KS> __device__ __forceinline__ int at_query_block(const AttnArgs &a, int n, int i)
 {
-    const int blocks = (a.s.T + AT_ROWS - 1) / AT_ROWS;
-    return a.order ? __builtin_amdgcn_readfirstlane(a.order[(size_t)n * 2 * blocks + i]) : blocks - 1 - i;
+    const int blocks = (a.s.T + AT_ROWS / KS - 1) / (AT_ROWS / KS);
+    return KS == 1 && a.order ? __builtin_amdgcn_readfirstlane(a.order[(size_t)n * 2 * blocks + i]) : blocks - 1 - i;
 }
-__device__ __forceinline__ int at_key_block(const AttnArgs &a, int n, int i)
+template <int KS> __device__ __forceinline__ int at_key_block(const AttnArgs &a, int n, int i)
 {
-    const int blocks = (a.s.T + AT_ROWS - 1) / AT_ROWS;
-    return a.order ? __builtin_amdgcn_readfirstlane(a.order[((size_t)n * 2 + 1) * blocks + i]) : i;
+    const int blocks = (a.s.T + AT_ROWS / KS - 1) / (AT_ROWS / KS);
+    return KS == 1 && a.order ? __builtin_amdgcn_readfirstlane(a.order[((size_t)n * 2 + 1) * blocks + i]) : i;
+}
+// accumulators of a lane to its wave's partner and back, a float at a time in a row of all lanes
+template <int ND> __device__ __forceinline__ void at_give(float *to, const f32x16_t (&acc)[ND], float by, int lane)
+{
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) to[(16 * t + i) * 64 + lane] = acc[t][i] * by;
+}
+template <int ND> __device__ __forceinline__ void at_take(const float *from, f32x16_t (&acc)[ND], float mine, float theirs, int lane)
+{
+#pragma unroll
+    for (int t = 0; t < ND; ++t) {
+        f32x16_t v;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = from[(16 * t + i) * 64 + lane];
+        acc[t] = acc[t] * mine + v * theirs;
+    }
 }
 
 // address of the dynamic LDS

@@ -262,6 +262,7 @@ struct AttnArgs {
     const int4 *bounds;
     // ATTN_SPANS, or NULL: [N][2][blocks of rows] blocks in the order in which they are started: of queries, of keys
     const int *order;
+    int units;               // of the chip
     // backward
     const void *dout;        // as o
     float *dsum;             // [N][heads][T]: dout . o, of the first of its two kernels to the second

@@ -11,12 +11,12 @@ template <class T, int DP> constexpr int kDkvHalves = DP * (int)sizeof(T) > 768 
 
 // Rows of a tile, 0: what fits.  16-bit floats of 128 channels, us: 66 registers are spilled with 64 rows, 286, and 36 with 32, 261; one wave a
 // SIMD, which spills none: 281.  (4 x 2048 positions, causal, 16 / 2 heads)
-template <int DP, bool EXTRA, bool HALF> constexpr int kDkvRows = HALF && !EXTRA && DP == 128 ? 32 : 0;
+template <int DP, bool EXTRA, bool HALF, int KS> constexpr int kDkvRows = KS == 1 && HALF && !EXTRA && DP == 128 ? 32 : 0;
 
-template <class T, int DP, bool VEC, bool EXTRA, bool HALF>
+template <class T, int DP, bool VEC, bool EXTRA, bool HALF, int KS>
 __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256) ? 2 : 1)) void k_attention_dkv(AttnArgs p)
 {
-    constexpr int R = kDkvRows<DP, EXTRA, HALF>;
+    constexpr int R = kDkvRows<DP, EXTRA, HALF, KS>, ROWS = AT_ROWS / KS;
     typedef AtTile<T, DP, R> Tile;
     typedef std::conditional_t<HALF, half_t, T> S;       // queries and keys
     typedef AtTile<S, DP, R> STile;
@@ -26,11 +26,11 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256)
     __shared__ int2 block_range[AT_WAVES];
     __shared__ int block_seen[AT_WAVES];
     const AttnShape &s = p.s;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ks = wave % KS;
     const int d = s.d, stride = s.stride(), per = s.heads / s.groups, ostride = s.heads * d;
     const AtBlock b = at_block(s);
-    const int half = b.rest % HALVES, split = b.rest / HALVES % p.splits, key0 = at_key_block(p, b.n, b.rest / HALVES / p.splits) * AT_ROWS;
-    const int wave0 = key0 + 32 * wave, own = wave0 + (lane & 31);
+    const int half = b.rest % HALVES, split = b.rest / HALVES % p.splits, key0 = at_key_block<KS>(p, b.n, b.rest / HALVES / p.splits) * ROWS;
+    const int wave0 = key0 + 32 * (wave / KS), own = wave0 + (lane & 31);
     const int sstride = HALF ? (s.heads + s.groups) * d : stride;
     const S *base = (const S *)(HALF ? p.half : p.qk) + (size_t)b.n * s.T * sstride;
 
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256)
         for (int i = tid; i < all_tiles; i += AT_TPB) {
             const int4 v = bounds[i * Tile::ROWS / kAttnTile * 2];
             seen = max(seen, v.y);
-            if (v.x < key0 + AT_ROWS && v.y > key0) {
+            if (v.x < key0 + ROWS && v.y > key0) {
                 first = min(first, i);
                 end = i + 1;
             }
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256)
         if (none) continue;
         const unsigned char *query = smem + at * 2 * Tile::BYTES, *dout = query + Tile::BYTES;
 #pragma unroll 1
-        for (int u = 0; u < SUBS; ++u) {
+        for (int u = ks; u < SUBS; u += KS) {
             __builtin_amdgcn_sched_barrier(0);
             const int lane = at_again(tid) & 63, h = lane >> 5, k = wave0 + (lane & 31);
             const int r = 32 * u + 4 * h;                                // rows of a register's four: r + 8 g
@@ -202,14 +202,29 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256)
             at_columns<S, STile>(dk, query, 32 * u, half * ND, AtWeights<S>(x), d, lane);
         }
     }
+    unsigned char *mine = smem + wave * kAtOwn<DP>;
+    float by_mult = s.scale / mult;
+    if constexpr (KS == 2) {
+        float *theirs = (float *)(smem + wave / 2 * (64 * 32 * ND * 4));
+        mine = (unsigned char *)theirs;
+        at_barrier();                                      // the tiles are read
+        if (ks) {
+            at_give(theirs, dk, by_mult, lane);
+            at_give(theirs + 64 * 16 * ND, dv, 1.0f, lane);
+        }
+        at_barrier();
+        if (ks) return;
+        at_take(theirs, dk, by_mult, 1.0f, lane);
+        at_take(theirs + 64 * 16 * ND, dv, 1.0f, 1.0f, lane);
+        by_mult = 1.0f;
+    }
     if constexpr (VEC && sizeof(T) == 2) {
         if (p.splits == 1) {
-            at_barrier();                                  // the tiles are read
-            unsigned char *mine = smem + wave * kAtOwn<DP>;
+            if (KS == 1) at_barrier();                     // the tiles are read
             const size_t at_k = ((size_t)b.n * s.T + wave0) * stride + (size_t)(s.heads + b.g) * d;
-            if (!p.dqk_float) at_store_rows<DP, ND>(mine, (T *)p.dqk + at_k, nullptr, stride, s.T - wave0, d, dk, s.scale / mult, lane);
+            if (!p.dqk_float) at_store_rows<DP, ND>(mine, (T *)p.dqk + at_k, nullptr, stride, s.T - wave0, d, dk, by_mult, lane);
             else if (own < s.T)
-                at_store<float, VEC, ND>(p.dqk_float + (((size_t)b.n * s.T + own) * (s.heads + s.groups) + s.heads + b.g) * d, d, 0, dk, s.scale / mult, lane);
+                at_store<float, VEC, ND>(p.dqk_float + (((size_t)b.n * s.T + own) * (s.heads + s.groups) + s.heads + b.g) * d, d, 0, dk, by_mult, lane);
             at_store_rows<DP, ND>(mine, (T *)p.dv + at_k + (size_t)s.groups * d, nullptr, stride, s.T - wave0, d, dv, 1.0f, lane);
             return;
         }
@@ -217,13 +232,13 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256)
     if (own >= s.T) return;
     if (p.splits > 1) {
         float *to = p.part + ((((size_t)split * s.N + b.n) * s.groups + b.g) * s.T + own) * 2 * d;
-        at_store<float, VEC, ND>(to, d, half * ND, dk, s.scale / mult, lane);
+        at_store<float, VEC, ND>(to, d, half * ND, dk, by_mult, lane);
         at_store<float, VEC, ND>(to + d, d, half * ND, dv, 1.0f, lane);
         return;
     }
     const size_t row = (size_t)b.n * s.T + own, at_k = row * stride + (size_t)(s.heads + b.g) * d;
-    if (p.dqk_float) at_store<float, VEC, ND>(p.dqk_float + row * (s.heads + s.groups) * d + (size_t)(s.heads + b.g) * d, d, half * ND, dk, s.scale / mult, lane);
-    else at_store<T, VEC, ND>((T *)p.dqk + at_k, d, half * ND, dk, s.scale / mult, lane);
+    if (p.dqk_float) at_store<float, VEC, ND>(p.dqk_float + row * (s.heads + s.groups) * d + (size_t)(s.heads + b.g) * d, d, half * ND, dk, by_mult, lane);
+    else at_store<T, VEC, ND>((T *)p.dqk + at_k, d, half * ND, dk, by_mult, lane);
     at_store<T, VEC, ND>((T *)p.dv + at_k + (size_t)s.groups * d, d, half * ND, dv, 1.0f, lane);
 }
 
@@ -255,11 +270,17 @@ template <class T, int V> __global__ __launch_bounds__(256) void k_attention_joi
 }
 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Keys {
+    template <int KS> static hipError_t launch(const AttnArgs &a, hipStream_t stream)
+    {
+        constexpr int smem = std::max(4 * AtTile<T, DP, kDkvRows<DP, EXTRA, HALF, KS>>::BYTES + 2 * 5 * 256, sizeof(T) == 2 ? AT_WAVES * kAtOwn<DP> : 0);
+        return at_launch(k_attention_dkv<T, DP, VEC, EXTRA, HALF, KS>,
+                         a.s.N * a.s.groups * ((a.s.T + AT_ROWS / KS - 1) / (AT_ROWS / KS)) * a.splits * kDkvHalves<T, DP>, smem, a, stream);
+    }
     static hipError_t go(const AttnArgs &a, hipStream_t stream)
     {
-        constexpr int smem = std::max(4 * AtTile<T, DP, kDkvRows<DP, EXTRA, HALF>>::BYTES + 2 * 5 * 256, sizeof(T) == 2 ? AT_WAVES * kAtOwn<DP> : 0);
-        return at_launch(k_attention_dkv<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.groups * ((a.s.T + AT_ROWS - 1) / AT_ROWS) * a.splits * kDkvHalves<T, DP>, smem, a,
-                         stream);
+        if constexpr (kAtShares<T, DP>)
+            if (at_shares(a, (long long)a.s.N * a.s.groups * ((a.s.T + AT_ROWS - 1) / AT_ROWS) * a.splits)) return launch<2>(a, stream);
+        return launch<1>(a, stream);
     }
 };
 

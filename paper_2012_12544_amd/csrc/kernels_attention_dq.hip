@@ -5,7 +5,7 @@
 namespace bapipe {
 namespace {
 
-template <class T, int DP, bool VEC, bool EXTRA, bool HALF>
+template <class T, int DP, bool VEC, bool EXTRA, bool HALF, int KS>
 __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void k_attention_dq(AttnArgs p)
 {
     typedef AtTile<T, DP> Tile;
@@ -15,11 +15,11 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
     extern __shared__ __align__(256) unsigned char smem[];
     __shared__ int2 block_range[AT_WAVES];
     const AttnShape &s = p.s;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, ks = wave % KS;
     const int d = s.d, stride = s.stride(), per = s.heads / s.groups;
     const AtBlock b = at_block(s);
-    const int head = b.g * per + b.rest % per, q0 = at_query_block(p, b.n, b.rest / per) * AT_ROWS;
-    const int q = q0 + 32 * wave + (lane & 31);
+    const int head = b.g * per + b.rest % per, q0 = at_query_block<KS>(p, b.n, b.rest / per) * (AT_ROWS / KS);
+    const int q = q0 + 32 * (wave / KS) + (lane & 31);
     const int sstride = HALF ? (s.heads + s.groups) * d : stride;
     const S *base = (const S *)(HALF ? p.half : p.qk) + (size_t)b.n * s.T * sstride, *keys = base + (size_t)(s.heads + b.g) * d;
     const T *values = (const T *)p.v + (size_t)b.n * s.T * stride + (size_t)(s.heads + s.groups + b.g) * d;
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
         dsum = at_halves_sum(dsum);
     }
     const float lse = sees ? p.lse[at_row] : __builtin_inff();
-    if (q < s.T && h == 0) p.dsum[at_row] = dsum;
+    if (ks == 0 && q < s.T && h == 0) p.dsum[at_row] = dsum;
 
     const AtRange range = at_wave_range(span);
     if (lane == 0) block_range[wave] = range.any;
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
         const unsigned char *key = smem + (it & 1) * 2 * Tile::BYTES, *value = key + Tile::BYTES;
         const bool whole = k0 >= range.all.x && k0 + Tile::ROWS <= range.all.y;
 #pragma unroll 1
-        for (int u = 0; u < SUBS; ++u) {
+        for (int u = ks; u < SUBS; u += KS) {
             f32x16_t w, dw;
             at_rows<S, STile>(w, key, 32 * u, query, d, lane);
             at_rows<T, Tile>(dw, value, 32 * u, dout, d, lane);
@@ -144,25 +144,43 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) void 
             at_columns<S, STile>(dq, key, 32 * u, 0, AtWeights<S>(ds), d, lane);
         }
     }
-    if (VEC && sizeof(T) == 2 && !p.dqk_float) {
+    unsigned char *own = smem + wave * kAtOwn<DP>;
+    float by_mult = s.scale / mult;
+    if constexpr (KS == 2) {
+        float *theirs = (float *)(smem + wave / 2 * (64 * 16 * ND * 4));
+        own = (unsigned char *)theirs;
         at_barrier();                                      // the tiles are read
-        const int row0 = q0 + 32 * wave;
+        if (ks) at_give(theirs, dq, by_mult, lane);
+        at_barrier();
+        if (ks) return;
+        at_take(theirs, dq, by_mult, 1.0f, lane);
+        by_mult = 1.0f;
+    }
+    if (VEC && sizeof(T) == 2 && !p.dqk_float) {
+        if (KS == 1) at_barrier();                         // the tiles are read
+        const int row0 = q0 + 32 * (wave / KS);
         if constexpr (VEC && sizeof(T) == 2)
-            at_store_rows<DP, ND>(smem + wave * kAtOwn<DP>, (T *)p.dqk + ((size_t)b.n * s.T + row0) * stride + (size_t)head * d, nullptr, stride, s.T - row0, d, dq,
-                                  s.scale / mult, lane);
+            at_store_rows<DP, ND>(own, (T *)p.dqk + ((size_t)b.n * s.T + row0) * stride + (size_t)head * d, nullptr, stride, s.T - row0, d, dq,
+                                  by_mult, lane);
         return;
     }
     if (q >= s.T) return;
     const size_t row = (size_t)b.n * s.T + q;
-    if (p.dqk_float) at_store<float, VEC, ND>(p.dqk_float + row * (s.heads + s.groups) * d + (size_t)head * d, d, 0, dq, s.scale / mult, lane);
-    else at_store<T, VEC, ND>((T *)p.dqk + row * stride + (size_t)head * d, d, 0, dq, s.scale / mult, lane);
+    if (p.dqk_float) at_store<float, VEC, ND>(p.dqk_float + row * (s.heads + s.groups) * d + (size_t)head * d, d, 0, dq, by_mult, lane);
+    else at_store<T, VEC, ND>((T *)p.dqk + row * stride + (size_t)head * d, d, 0, dq, by_mult, lane);
 }
 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Queries {
-    static hipError_t go(const AttnArgs &a, hipStream_t stream)
+    template <int KS> static hipError_t launch(const AttnArgs &a, hipStream_t stream)
     {
         constexpr int smem = std::max(4 * AtTile<T, DP>::BYTES + (HALF ? 512 : 0), sizeof(T) == 2 ? AT_WAVES * kAtOwn<DP> : 0);
-        return at_launch(k_attention_dq<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS - 1) / AT_ROWS), smem, a, stream);
+        return at_launch(k_attention_dq<T, DP, VEC, EXTRA, HALF, KS>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS / KS - 1) / (AT_ROWS / KS)), smem, a, stream);
+    }
+    static hipError_t go(const AttnArgs &a, hipStream_t stream)
+    {
+        if constexpr (kAtShares<T, DP>)
+            if (at_shares(a, (long long)a.s.N * a.s.heads * ((a.s.T + AT_ROWS - 1) / AT_ROWS))) return launch<2>(a, stream);
+        return launch<1>(a, stream);
     }
 };
 

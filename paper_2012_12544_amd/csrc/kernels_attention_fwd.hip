@@ -7,24 +7,24 @@ namespace {
 // Rows of a tile.  With 32 keys at a time registers and LDS hold three blocks of heads of 128 channels a unit instead of two, and two of 192 instead
 // of one (of 256 that was as fast: 151 and 154 us).  4 x 4096 positions, causal, 32 / 8 heads of 128, us: 705 with 64, 674; packed documents 173, 178;
 // 4 x 2048, causal, 16 / 2 heads of 16-bit floats: 112, 101.
-template <class T, int DP> constexpr int kFwdRows = sizeof(T) == 2 && (DP == 128 || DP == 192) ? 32 : 0;
+template <class T, int DP, int KS> constexpr int kFwdRows = KS == 1 && sizeof(T) == 2 && (DP == 128 || DP == 192) ? 32 : 0;
 
-template <class T, int DP, bool VEC, bool EXTRA, bool HALF>
-__global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && DP == 128 && !EXTRA ? 3 : DP <= (sizeof(T) == 2 ? 192 : 64) ? 2 : 1)) void k_attention_fwd(AttnArgs p)
+template <class T, int DP, bool VEC, bool EXTRA, bool HALF, int KS>
+__global__ __launch_bounds__(AT_TPB, (KS == 1 && sizeof(T) == 2 && DP == 128 && !EXTRA ? 3 : DP <= (sizeof(T) == 2 ? 192 : 64) ? 2 : 1)) void k_attention_fwd(AttnArgs p)
 {
-    constexpr int R = kFwdRows<T, DP>;
+    constexpr int R = kFwdRows<T, DP, KS>, ROWS = AT_ROWS / KS;
     typedef AtTile<T, DP, R> Tile;
     typedef std::conditional_t<HALF, half_t, T> S;       // what scores are made of
     typedef AtTile<S, DP, R> STile;
-    constexpr int ND = DP / 32, SUBS = Tile::ROWS / 32;
+    constexpr int ND = DP / 32, SUBS = Tile::ROWS / 32 / KS;      // a wave's pieces of a tile: the KS u + ks-th
     extern __shared__ __align__(256) unsigned char smem[];
     __shared__ int2 block_range[AT_WAVES];
     const AttnShape &s = p.s;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, ks = wave % KS;
     const int d = s.d, stride = s.stride(), per = s.heads / s.groups;
     const AtBlock b = at_block(s);
-    const int head = b.g * per + b.rest % per, q0 = at_query_block(p, b.n, b.rest / per) * AT_ROWS;
-    const int q = q0 + 32 * wave + (lane & 31);
+    const int head = b.g * per + b.rest % per, q0 = at_query_block<KS>(p, b.n, b.rest / per) * ROWS;
+    const int q = q0 + 32 * (wave / KS) + (lane & 31);
     const int sstride = HALF ? (s.heads + s.groups) * d : stride;
     const S *base = (const S *)(HALF ? p.half : p.qk) + (size_t)b.n * s.T * sstride, *keys = base + (size_t)(s.heads + b.g) * d;
     const T *values = (const T *)p.v + (size_t)b.n * s.T * stride + (size_t)(s.heads + s.groups + b.g) * d;
@@ -38,9 +38,9 @@ __global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && DP == 128 && !EXTRA ? 3 
 #pragma unroll
             for (int c = 0; c < Tile::STEPS; ++c) {
                 const int e = (2 * c + h) * Tile::EPC;
-                if (q < s.T && e < d) *(chunk16 *)(copy + (size_t)q * stride + (size_t)head * d + e) = query[c];
+                if (ks == 0 && q < s.T && e < d) *(chunk16 *)(copy + (size_t)q * stride + (size_t)head * d + e) = query[c];
             }
-            const int chunks = d / Tile::EPC, rows = min(AT_ROWS, s.T - q0);
+            const int chunks = d / Tile::EPC, rows = min(ROWS, s.T - q0);
             for (int i = tid; head % per == 0 && i < 2 * rows * chunks; i += AT_TPB) {
                 const int which = i / (rows * chunks), row = (i - which * rows * chunks) / chunks, chunk = i % chunks;
                 const size_t at = (size_t)(q0 + row) * stride + (size_t)(s.heads + which * s.groups + b.g) * d + chunk * Tile::EPC;
@@ -90,13 +90,13 @@ __global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && DP == 128 && !EXTRA ? 3 
 #pragma unroll
         for (int u = 0; u < SUBS; ++u) {
             f32x16_t w;
-            at_rows<S, STile>(w, key, 32 * u, query, d, lane);
+            at_rows<S, STile>(w, key, 32 * (KS * u + ks), query, d, lane);
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[u][i] = w[i];
             if (HALF)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const float4 r = *(const float4 *)(smem + SCALE_AT + (it & 1) * 256 + 4 * (32 * u + 8 * g + 4 * h));
+                    const float4 r = *(const float4 *)(smem + SCALE_AT + (it & 1) * 256 + 4 * (32 * (KS * u + ks) + 8 * g + 4 * h));
                     x[u][4 * g] *= r.x; x[u][4 * g + 1] *= r.y; x[u][4 * g + 2] *= r.z; x[u][4 * g + 3] *= r.w;
                 }
         }
@@ -105,14 +105,14 @@ __global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && DP == 128 && !EXTRA ? 3 
 #pragma unroll
             for (int u = 0; u < SUBS; ++u) {
                 float none[16];
-                at_bend<T, false>(x[u], score, by, (float)(q - (k0 + 32 * u + 4 * h)), none);
+                at_bend<T, false>(x[u], score, by, (float)(q - (k0 + 32 * (KS * u + ks) + 4 * h)), none);
             }
         if (!(k0 >= range.all.x && k0 + Tile::ROWS <= range.all.y)) {
 #pragma unroll
             for (int u = 0; u < SUBS; ++u)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int k = k0 + 32 * u + 8 * (i >> 2) + 4 * h + (i & 3);
+                    const int k = k0 + 32 * (KS * u + ks) + 8 * (i >> 2) + 4 * h + (i & 3);
                     x[u][i] = k >= span.x && k < span.y ? x[u][i] : -__builtin_inff();
                 }
         }
@@ -140,17 +140,36 @@ __global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && DP == 128 && !EXTRA ? 3 
                 x[u][i] = __builtin_amdgcn_exp2f(fmaf(x[u][i], unit, -less));
                 sum += x[u][i];
             }
-            at_columns<T, Tile>(out, value, 32 * u, 0, AtWeights<T>(x[u]), d, lane);
+            at_columns<T, Tile>(out, value, 32 * (KS * u + ks), 0, AtWeights<T>(x[u]), d, lane);
         }
     }
-    sum = at_halves_sum(sum);
+    if (KS == 1) sum = at_halves_sum(sum);
+    unsigned char *own = smem + wave * kAtOwn<DP>;
+    if constexpr (KS == 2) {
+        float *theirs = (float *)(smem + wave / 2 * (64 * (16 * ND + 2) * 4));
+        own = (unsigned char *)theirs;
+        at_barrier();                                      // the tiles are read
+        if (ks) {
+            at_give(theirs, out, 1.0f, lane);
+            theirs[16 * ND * 64 + lane] = top;
+            theirs[(16 * ND + 1) * 64 + lane] = sum;
+        }
+        at_barrier();
+        if (ks) return;
+        const float their_top = theirs[16 * ND * 64 + lane], both = fmaxf(top, their_top);
+        const float mine = top > -__builtin_inff() ? __builtin_amdgcn_exp2f(top - both) : 0.0f;
+        const float other = their_top > -__builtin_inff() ? __builtin_amdgcn_exp2f(their_top - both) : 0.0f;
+        at_take(theirs, out, mine, other, lane);
+        sum = sum * mine + theirs[(16 * ND + 1) * 64 + lane] * other;
+        top = both;
+        sum = at_halves_sum(sum);
+    }
     const bool sees = span.x < span.y;
     const float by_sum = sees ? 1.0f / sum : 0.0f;
     if constexpr (VEC && sizeof(T) == 2) {
-        at_barrier();                                      // the tiles are read
-        const int row0 = q0 + 32 * wave, rows = s.T - row0;
+        if (KS == 1) at_barrier();                         // the tiles are read
+        const int row0 = q0 + 32 * (wave / KS), rows = s.T - row0;
         const size_t at_o = ((size_t)b.n * s.T + row0) * s.heads * d + (size_t)head * d, ostride = (size_t)s.heads * d;
-        unsigned char *own = smem + wave * kAtOwn<DP>;
         at_store_rows<DP, ND>(own, (T *)p.o + at_o, p.o2 ? (T *)p.o2 + at_o : nullptr, ostride, rows, d, out, by_sum, lane);
         at_store_low_rows<DP, ND>(own, p.o_low + at_o, ostride, rows, d, out, by_sum, lane);
     } else if (q < s.T) {
@@ -164,9 +183,16 @@ __global__ __launch_bounds__(AT_TPB, (sizeof(T) == 2 && DP == 128 && !EXTRA ? 3 
 }
 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Forward {
+    template <int KS> static hipError_t launch(const AttnArgs &a, hipStream_t stream)
+    {
+        constexpr int smem = std::max(4 * AtTile<T, DP, kFwdRows<T, DP, KS>>::BYTES + (HALF ? 512 : 0), sizeof(T) == 2 ? AT_WAVES * kAtOwn<DP> : 0);
+        return at_launch(k_attention_fwd<T, DP, VEC, EXTRA, HALF, KS>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS / KS - 1) / (AT_ROWS / KS)), smem, a, stream);
+    }
     static hipError_t go(const AttnArgs &a, hipStream_t stream)
     {
-        return at_launch(k_attention_fwd<T, DP, VEC, EXTRA, HALF>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS - 1) / AT_ROWS), std::max(4 * AtTile<T, DP, kFwdRows<T, DP>>::BYTES + (HALF ? 512 : 0), sizeof(T) == 2 ? AT_WAVES * kAtOwn<DP> : 0), a, stream);
+        if constexpr (kAtShares<T, DP>)
+            if (at_shares(a, (long long)a.s.N * a.s.heads * ((a.s.T + AT_ROWS - 1) / AT_ROWS))) return launch<2>(a, stream);
+        return launch<1>(a, stream);
     }
 };
 

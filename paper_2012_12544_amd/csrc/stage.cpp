@@ -738,6 +738,7 @@ AttnArgs attn_args(bapipe_stage *st, const Layer &L, int mbid)
     const Layer *R = rotary_before(st, L);
     AttnArgs q = {};
     q.s = attn_shape(st, L);
+    q.units = st->compute_units > 0 ? st->compute_units : 256;
     q.qk = st->tptr(L.a, mbid);
     q.v = R && R->values_stay ? st->tptr(R->a, mbid) : q.qk;
     if (R && R->half) {
