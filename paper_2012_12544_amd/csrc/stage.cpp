@@ -713,6 +713,14 @@ AttnShape attn_shape(const bapipe_stage *st, const Layer &L)
     return a;
 }
 
+// Whether a caller's tensor that a ROTARY or ATTENTION meets has to lie at 16 bytes: ATTENTION reads and writes whole heads in such pieces where
+// their width allows it, and ROTARY's norms would be summed in another order without
+size_t heads_align(const bapipe_stage *st, const Layer &L)
+{
+    const size_t es = dt_size(st->dt), head = st->tensors[L.a].C / (L.d.kh + 2 * L.d.kw) * es;
+    return has_heads(L.d.kind) && head % 16 == 0 && (L.d.kind == BAPIPE_ATTENTION || L.w_elems) ? 16 : es;
+}
+
 // pairs of query and key, of all heads, that a forward pass scores where the mask is not the caller's
 double attn_pairs(const AttnShape &a)
 {
@@ -884,7 +892,7 @@ int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
         const RotaryShape r = rotary_shape(st, L, !L.values_stay && O.root == L.o);
         const bool tp = st->tap_begin(BAPIPE_KC_ELEMENTWISE);
         const void *x = li == 0 && c.x_copied ? c.x_copied : a;
-        HIPCHK(rotary_fwd(dt, r, x, O.root == L.o ? out_ptr(st, L, c, 16) : o, L.table, L.w, s, L.half ? st->slot(c.mbid) + L.off_half : nullptr,
+        HIPCHK(rotary_fwd(dt, r, x, O.root == L.o ? out_ptr(st, L, c, heads_align(st, L)) : o, L.table, L.w, s, L.half ? st->slot(c.mbid) + L.off_half : nullptr,
                           L.half ? (float *)(st->slot(c.mbid) + L.off_scale) : nullptr, x == a ? nullptr : const_cast<void *>(a)));
         st->tap_end(tp, 0.0, 2.0 * O.bytes() * (L.d.kh + L.d.kw * (r.values ? 2.0 : 1.0)) / (L.d.kh + 2.0 * L.d.kw));
         break;
@@ -896,7 +904,7 @@ int layer_forward(bapipe_stage *st, int li, FwdCtx &c)
             q.qk = q.v = c.x_copied;
         }
         // the stage's output goes to the caller in the pass that stores it
-        if (L.o + 1 == (int)st->tensors.size() && c.y_direct && (uintptr_t)c.y_direct % 16 == 0) {
+        if (L.o + 1 == (int)st->tensors.size() && c.y_direct && (uintptr_t)c.y_direct % heads_align(st, L) == 0) {
             q.o2 = c.y_direct;
             c.y_stored = true;
         }
@@ -2123,8 +2131,8 @@ int bapipe_stage_forward(bapipe_stage_t *st, int mb_id, const void *x_dev, void 
         HIPCHK(nchw_to_nhwc(dt, x_dev, st->tptr(0, mb_id), none, st->mb, In.C, In.H, In.W, In.Cp, s));
     } else if (In.Cp != In.C) {
         HIPCHK(nhwc_repad(dt, x_dev, st->tptr(0, mb_id), (size_t)st->mb * In.H * In.W, In.C, In.Cp, s));
-    } else if (In.stashed && (uintptr_t)x_dev % 16 == 0 && (st->layers[0].d.kind == BAPIPE_ROTARY || (st->layers[0].d.kind == BAPIPE_ATTENTION &&
-                                                                                              attn_shape(st, st->layers[0]).d * dt_size(dt) % 16 == 0))) {
+    } else if (In.stashed && has_heads(st->layers[0].d.kind) && (uintptr_t)x_dev % heads_align(st, st->layers[0]) == 0 &&
+               (st->layers[0].d.kind == BAPIPE_ROTARY || heads_align(st, st->layers[0]) == 16)) {
         c.x_copied = x_dev;
     } else if (In.stashed && st->layers[0].d.kind == BAPIPE_LAYERNORM) {
         c.x_copied = x_dev;
@@ -2188,11 +2196,11 @@ int bapipe_stage_backward(bapipe_stage_t *st, int mb_id, const void *dy_dev_or_l
     c.pending.assign(st->tensors.size(), nullptr);
     const Tensor &In = st->tensors[0];
     const bool want_dx = In.need_grad && dx_dev != nullptr;
-    // ATTENTION reads and writes gradients in pieces of 16 bytes, and ROTARY's norms would be summed in another order without: a caller's
-    // that do not lie so pass through the stage's own
-    bool attends = false;
-    for (const Layer &L : st->layers) attends |= has_heads(L.d.kind);
-    if (want_dx && (nhwc || In.H * In.W == 1) && In.Cp == In.C && !(attends && (uintptr_t)dx_dev % 16)) c.dx_direct = dx_dev;
+    // gradients that do not lie as the layers need it pass through the stage's own
+    size_t align = 1;
+    for (const Layer &L : st->layers)
+        if (has_heads(L.d.kind)) align = std::max(align, heads_align(st, L));
+    if (want_dx && (nhwc || In.H * In.W == 1) && In.Cp == In.C && (uintptr_t)dx_dev % align == 0) c.dx_direct = dx_dev;
     if (st->layers[nl - 1].d.kind == BAPIPE_SOFTMAX_XENT) {
         c.labels = (const int32_t *)dy_dev_or_labels;
     } else {
@@ -2212,7 +2220,7 @@ int bapipe_stage_backward(bapipe_stage_t *st, int mb_id, const void *dy_dev_or_l
             c.dy_nchw = dy_dev_or_labels;
         } else if ((!nhwc && R.H * R.W > 1) || flat_of_spatial) {
             HIPCHK(nchw_to_nhwc(dt, dy_dev_or_labels, st->gptr(last), e, st->mb, R.C, R.H, R.W, R.Cp, s));
-        } else if (e.gate || r == 0 || (attends && (uintptr_t)dy_dev_or_labels % 16)) {
+        } else if (e.gate || r == 0 || (uintptr_t)dy_dev_or_labels % align) {
             HIPCHK(grad_copy(dt, dy_dev_or_labels, st->gptr(last), e, O.elems, s));
         } else {
             c.dy_direct = dy_dev_or_labels;
