@@ -131,8 +131,8 @@ typedef enum { BAPIPE_MASK_NONE = 0, BAPIPE_MASK_CAUSAL = 1, BAPIPE_MASK_SPANS =
  *   lets the position see; one that sees none gets zeros and gives no gradients.  has_bias must be 0.  What the
  *   positions of a sequence hold behind the last that sees some, or is seen, has no effect on anything, NaN and infinity
  *   included; at other positions that are not seen it has to be finite.
- *   In bf16 stages probabilities and their gradients are rounded to bf16 as operands of the next product; scores, sums and
- *   the softmax stay in float. */
+ *   In bf16 stages probabilities and the gradients of scores are rounded to 16 bits as operands of the next product, and what a
+ *   ROTARY hands to an ATTENTION that alone reads it is 16-bit floats; scores, sums and the softmax stay in float. */
 typedef struct {
     int32_t kind;
     int32_t cin, cout;

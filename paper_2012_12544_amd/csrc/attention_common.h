@@ -19,15 +19,17 @@ namespace bapipe {
 
 constexpr int AT_WAVES = 4, AT_TPB = 64 * AT_WAVES, AT_ROWS = 32 * AT_WAVES;      // rows that a block owns
 
+// 16-bit floats, where bf16_t is the other type of that size
+struct half_t {
+    uint16_t v;
+};
+
 // A tile of rows of DP elements in LDS, in groups of 64 bytes of every row: group after group, each of all rows.  The four 16-byte chunks of a
 // row in a group change places with the row / 4, so that both kinds of reads meet each bank once - 16 rows at one chunk (row operands),
 // four rows at four chunks (transposing reads) - and everything but two lane addresses of either kind is an immediate offset.  (With whole
 // rows one after the other and a chunk's place XORed with the row every step and column tile took an address register of its own,
 // and the kernel for dk and dv spilled 106.)  Loads bring 64 bytes of 16 rows at a time.
 // R: rows, 0 for what two operands, twice, in 128 KB leave
-struct half_t {
-    uint16_t v;
-};
 template <class T, int DP, int R = 0> struct AtTile {
     static constexpr int EPC = 16 / (int)sizeof(T);                   // elements of a chunk
     static constexpr int CH = DP / EPC, RB = DP * (int)sizeof(T);     // chunks, bytes of a row
@@ -235,8 +237,7 @@ template <int OFF> __device__ __forceinline__ void at_dma4(__amdgpu_buffer_rsrc_
 // Fills tiles from rows of d elements, `stride` elements apart.  VEC: d a multiple of a chunk and 16-byte aligned rows.  These and all floats, which
 // come word by word, are asynchronous: complete after WAIT_VMCNT(0) and a barrier.
 // (Causal float heads of 45 channels, 4 x 1024 positions, 8 of them, a mini-batch: 431 us element by element through registers, 356.)
-// Rows that are not there, and what is behind d, are zeros: zero times zero is what the products
-// see of them, whatever memory holds.
+// Rows that are not there, and what is behind d, are zeros: zero times zero is what the products see of them, whatever memory holds.
 // AGAIN: a lane's place is worked out again for every tile (see at_again), else it is kept.
 template <class T, int DP, bool VEC, int R = 0, bool AGAIN = true> struct AtStream {
     typedef AtTile<T, DP, R> Tile;

@@ -1,6 +1,8 @@
 // Attention, backward, the gradients of keys and values: a block owns keys and streams the queries that see them, of every query head
 // that shares the key head.  No atomics: sums have one order.
 //   dv = p^T dout, dk = ds^T q / sqrt(d)
+// 4 x 4096 positions, causal, 32 / 8 heads of 128, bf16: 1190 us, 924 TFLOP/s of its four products, 59 % of the cycles.  Two waves a SIMD hold both sums, key and value of 32
+// rows in 256 registers each; 64 rows a wave, at one wave, halve the LDS reads and were slower (1842 and 1515 us).
 #include "attention_common.h"
 
 namespace bapipe {
