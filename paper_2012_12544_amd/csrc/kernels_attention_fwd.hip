@@ -1,6 +1,6 @@
 // Attention, forward: o = softmax(scores) v in one pass over the keys, with a running maximum and sum per query.
 // 4 x 4096 positions, causal, 32 / 8 heads of 128, bf16: 650 us, 845 TFLOP/s of the two products, of which 75 us are the second places for input
-// and output.  The card runs at 1.83 GHz there; matrix instructions take 45 % of the cycles, and 64 keys of a wave 32 of them (1024 cycles), 140 vector
+// and output.  The card runs at 1.7 to 1.8 GHz there; matrix instructions take 51 % of the cycles, and 64 keys of a wave 32 of them (1024 cycles), 140 vector
 // instructions and 32 exponentials.  No one of these bounds it: without the exponentials it takes 5 % less, without LDS reads 6, without loads of tiles
 // 15, without all three 27.
 #include "attention_common.h"
