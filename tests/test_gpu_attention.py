@@ -223,6 +223,25 @@ def test_attention_over_many_tiles(dtype, heads, groups, d, T, mask, micro_batch
     _check_attention(_attention(dtype, heads, groups, d, T, mask, micro_batch=micro_batch), "documents")
 
 
+# Up to here blocks of rows are fewer than the chip has units, and two waves share 32 rows.  Below, 264 and more of them, a wave to 32 rows.
+@BOTH
+@pytest.mark.parametrize("d", [1, 8, 24, 33, 64, 75, 96, 128, 136, 192, 250, 256])
+def test_attention_of_many_sequences(dtype, d):
+    _check_attention(_attention(dtype, 4, 4, d, 66, micro_batch=66))
+
+
+@BOTH
+@pytest.mark.parametrize("mask,cap,bias", [(C.MASK_NONE, 0.0, 8), (C.MASK_CAUSAL, 3.0, 0), (C.MASK_SPANS, 0.0, 0), (C.MASK_SPANS, 5000.0, 2)])
+@pytest.mark.parametrize("d", [30, 32, 80, 128, 200])
+def test_attention_of_many_sequences_with_masks_caps_and_slopes(dtype, mask, cap, bias, d):
+    _check_attention(_attention(dtype, 8, 4, d, 130, mask, cap, bias, micro_batch=33), "random" if cap else "documents")
+
+
+@pytest.mark.parametrize("dtype,kind", [(C.FP32, "documents"), (C.BF16, "documents"), (C.BF16, "random")])
+def test_blocks_in_the_order_of_their_work(dtype, kind):
+    _check_attention(_attention(dtype, 36, 36, 8, 900, C.MASK_SPANS, micro_batch=1), kind)
+
+
 @BOTH
 def test_attention_over_micro_batches_in_flight(dtype):
     _check_attention(_attention(dtype, 4, 2, 32, 70, C.MASK_SPANS, n_micro=4, stage_index=1, n_stages=3), "documents")
@@ -267,14 +286,25 @@ def test_positions_that_see_nothing_and_keys_that_nobody_sees(dtype):
 @pytest.mark.parametrize("rotary", [0, 1])
 @pytest.mark.parametrize("cap", [0.0, 3.0])
 def test_what_padding_holds_has_no_effect(dtype, d, used, poison, rotary, cap):
+    _padding(dtype, d, used, poison, rotary, cap, 2, 2)
+
+
+@BOTH
+@pytest.mark.parametrize("d", [45, 64, 128])
+@pytest.mark.parametrize("rotary", [0, 1])
+def test_what_padding_of_many_sequences_holds_has_no_effect(dtype, d, rotary):
+    _padding(dtype, d, 70, math.nan, rotary, 0.0, 40, 4)
+
+
+def _padding(dtype, d, used, poison, rotary, cap, micro_batch, groups):
     b = C._Builder()
     if rotary:
-        b.rotary(4, 2, d, src=-1)
-    b.attention(4, 2, d, C.MASK_SPANS, cap, src=-1 if not rotary else 0)
-    st = _stage(b.layers, dtype, (8 * d, 130, 1))
+        b.rotary(4, groups, d, src=-1)
+    b.attention(4, groups, d, C.MASK_SPANS, cap, src=-1 if not rotary else 0)
+    st = _stage(b.layers, dtype, ((4 + 2 * groups) * d, 130, 1), micro_batch)
     params = gen.all_params(st)
     xs, gs = stage_io(st)
-    spans = np.zeros((2, 130, 2), np.int32)
+    spans = np.zeros((micro_batch, 130, 2), np.int32)
     spans[:, :used, 0], spans[:, :used, 1] = 0, np.arange(1, used + 1)
     spans[1, 20:40] = 0                                      # the other sample also has positions in between that see nothing
     clean = run(st, params, xs, gs, [spans])
@@ -489,6 +519,17 @@ def test_rotary_and_attention(dtype, norm, d, heads, groups, T, mask):
     b.attention(heads, groups, d, mask)
     st = _stage(b.layers, dtype, ((heads + 2 * groups) * d, T, 1), n_micro=2)
     _compare(st, _spans(st, "window") if _has_spans(st) else None, {0: dict(base=1000.0, first_position=7)}, roundings=8)
+
+
+@BOTH
+@pytest.mark.parametrize("d,norm,mask,cap", [(24, 1, C.MASK_CAUSAL, 0.0), (33, 0, C.MASK_NONE, 0.0), (64, 1, C.MASK_SPANS, 0.0), (64, 0, C.MASK_CAUSAL, 4.0), (96, 1, C.MASK_CAUSAL, 0.0),
+                                             (128, 1, C.MASK_CAUSAL, 0.0), (128, 0, C.MASK_SPANS, 4.0), (192, 0, C.MASK_CAUSAL, 0.0), (256, 1, C.MASK_SPANS, 0.0)])
+def test_rotary_and_attention_of_many_sequences(dtype, d, norm, mask, cap):
+    b = C._Builder()
+    b.rotary(4, 4, d, norm=norm, src=-1)
+    b.attention(4, 4, d, mask, cap)
+    st = _stage(b.layers, dtype, (12 * d, 66, 1), micro_batch=66)
+    _compare(st, _spans(st, "documents") if _has_spans(st) else None, roundings=8)
 
 
 def _graphs():
