@@ -8,8 +8,10 @@
 namespace bapipe {
 namespace {
 
-// Float heads of more than 128 channels would need more registers than there are: their blocks own half of the gradients' columns, two to a key
-template <class T, int DP> constexpr int kDkvHalves = DP * (int)sizeof(T) > 768 ? 2 : 1;
+// Float heads of more than 128 channels, and 16-bit floats of 256, would need more registers than there are: their blocks own half of the gradients'
+// columns, two to a key, and make the scores twice.  A mini-batch of 2 x 4 x 2048 positions of 16 / 8 heads of 256 behind a ROTARY, us:
+// 4485 whole, with 245 registers spilled, 3022 so.
+template <class T, int DP, bool HALF> constexpr int kDkvHalves = DP * (int)sizeof(T) > 768 || (HALF && DP > 192) ? 2 : 1;
 
 // Rows of a tile, 0: what fits.  16-bit floats of 128 channels, us: 66 registers are spilled with 64 rows, 286, and 36 with 32, 261; one wave a
 // SIMD, which spills none: 281.  (4 x 2048 positions, causal, 16 / 2 heads)
@@ -22,7 +24,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256)
     typedef AtTile<T, DP, R> Tile;
     typedef std::conditional_t<HALF, half_t, T> S;       // queries and keys
     typedef AtTile<S, DP, R> STile;
-    constexpr int HALVES = kDkvHalves<T, DP>, ND = DP / 32 / HALVES, SUBS = Tile::ROWS / 32;
+    constexpr int HALVES = kDkvHalves<T, DP, HALF>, ND = DP / 32 / HALVES, SUBS = Tile::ROWS / 32;
     static_assert(Tile::ROWS <= kAttnTile && kAttnTile % Tile::ROWS == 0, "");
     extern __shared__ __align__(256) unsigned char smem[];
     __shared__ int2 block_range[AT_WAVES];
@@ -220,7 +222,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256)
         at_take(theirs + 64 * 16 * ND, dv, 1.0f, 1.0f, lane);
         by_mult = 1.0f;
     }
-    if constexpr (VEC && sizeof(T) == 2) {
+    if constexpr (VEC && sizeof(T) == 2 && HALVES == 1) {
         if (p.splits == 1) {
             if (KS == 1) at_barrier();                     // the tiles are read
             const size_t at_k = ((size_t)b.n * s.T + wave0) * stride + (size_t)(s.heads + b.g) * d;
@@ -276,7 +278,7 @@ template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Keys {
     {
         constexpr int smem = std::max(4 * AtTile<T, DP, kDkvRows<DP, EXTRA, HALF, KS>>::BYTES + 2 * 5 * 256, sizeof(T) == 2 ? AT_WAVES * kAtOwn<DP> : 0);
         return at_launch(k_attention_dkv<T, DP, VEC, EXTRA, HALF, KS>,
-                         a.s.N * a.s.groups * ((a.s.T + AT_ROWS / KS - 1) / (AT_ROWS / KS)) * a.splits * kDkvHalves<T, DP>, smem, a, stream);
+                         a.s.N * a.s.groups * ((a.s.T + AT_ROWS / KS - 1) / (AT_ROWS / KS)) * a.splits * kDkvHalves<T, DP, HALF>, smem, a, stream);
     }
     static hipError_t go(const AttnArgs &a, hipStream_t stream)
     {

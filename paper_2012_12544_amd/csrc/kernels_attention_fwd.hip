@@ -8,15 +8,18 @@
 namespace bapipe {
 namespace {
 
-// Rows of a tile.  With 32 keys at a time registers and LDS hold three blocks of heads of 128 channels a unit instead of two, and two of 192 instead
-// of one (of 256 that was as fast: 151 and 154 us).  4 x 4096 positions, causal, 32 / 8 heads of 128, us: 705 with 64, 674; packed documents 173, 178;
-// 4 x 2048, causal, 16 / 2 heads of 16-bit floats: 112, 101.
-template <class T, int DP, int KS> constexpr int kFwdRows = KS == 1 && sizeof(T) == 2 && (DP == 128 || DP == 192) ? 32 : 0;
+// Rows of a tile.  With 32 keys at a time registers and LDS hold three blocks of heads of 128 channels a unit instead of two, and two of 192 and 256
+// instead of one.  us with 64 and 32: 4 x 4096 positions, causal, 32 / 8 heads of 128: 705, 674; packed documents 173, 178; 4 x 2048, causal, 16 / 2
+// heads of 16-bit floats: 112, 101; 16 / 8 heads of 256: 295, 217, but with capped scores, which leave no registers for two, 192, 198.
+template <class T, int DP, bool EXTRA, int KS>
+constexpr int kFwdRows = KS == 1 && sizeof(T) == 2 && (DP == 128 || DP == 192 || (DP == 256 && !EXTRA)) ? 32 : 0;
+template <class T, int DP, bool EXTRA, int KS>
+constexpr int kFwdBlocks = sizeof(T) == 4 ? DP <= 64 ? 2 : 1 : KS == 1 && DP == 128 && !EXTRA ? 3 : DP <= 192 || kFwdRows<T, DP, EXTRA, KS> ? 2 : 1;
 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF, int KS>
-__global__ __launch_bounds__(AT_TPB, (KS == 1 && sizeof(T) == 2 && DP == 128 && !EXTRA ? 3 : DP <= (sizeof(T) == 2 ? 192 : 64) ? 2 : 1)) void k_attention_fwd(AttnArgs p)
+__global__ __launch_bounds__(AT_TPB, (kFwdBlocks<T, DP, EXTRA, KS>)) void k_attention_fwd(AttnArgs p)
 {
-    constexpr int R = kFwdRows<T, DP, KS>, ROWS = AT_ROWS / KS;
+    constexpr int R = kFwdRows<T, DP, EXTRA, KS>, ROWS = AT_ROWS / KS;
     typedef AtTile<T, DP, R> Tile;
     typedef std::conditional_t<HALF, half_t, T> S;       // what scores are made of
     typedef AtTile<S, DP, R> STile;
@@ -189,7 +192,7 @@ __global__ __launch_bounds__(AT_TPB, (KS == 1 && sizeof(T) == 2 && DP == 128 && 
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Forward {
     template <int KS> static hipError_t launch(const AttnArgs &a, hipStream_t stream)
     {
-        constexpr int smem = std::max(4 * AtTile<T, DP, kFwdRows<T, DP, KS>>::BYTES + (HALF ? 512 : 0), sizeof(T) == 2 ? AT_WAVES * kAtOwn<DP> : 0);
+        constexpr int smem = std::max(4 * AtTile<T, DP, kFwdRows<T, DP, EXTRA, KS>>::BYTES + (HALF ? 512 : 0), sizeof(T) == 2 ? AT_WAVES * kAtOwn<DP> : 0);
         return at_launch(k_attention_fwd<T, DP, VEC, EXTRA, HALF, KS>, a.s.N * a.s.heads * ((a.s.T + AT_ROWS / KS - 1) / (AT_ROWS / KS)), smem, a, stream);
     }
     static hipError_t go(const AttnArgs &a, hipStream_t stream)
