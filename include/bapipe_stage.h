@@ -132,7 +132,8 @@ typedef enum { BAPIPE_MASK_NONE = 0, BAPIPE_MASK_CAUSAL = 1, BAPIPE_MASK_SPANS =
  *   positions of a sequence hold behind the last that sees some, or is seen, has no effect on anything, NaN and infinity
  *   included; at other positions that are not seen it has to be finite.
  *   In bf16 stages probabilities and the gradients of scores are rounded to 16 bits as operands of the next product, and what a
- *   ROTARY hands to an ATTENTION that alone reads it is 16-bit floats; scores, sums and the softmax stay in float. */
+ *   ROTARY hands to an ATTENTION of the same kh and kw that alone reads it is 16-bit floats; scores, sums and the softmax stay in float.
+ * An ATTENTION may divide the channels of a ROTARY into other heads: it then reads what the ROTARY stores as any layer would. */
 typedef struct {
     int32_t kind;
     int32_t cin, cout;

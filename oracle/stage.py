@@ -15,7 +15,7 @@ BN statistics, softmax and loss are never rounded.  Inside an LSTM layer the inp
 of all steps and the pre-activation gradients are stored tensors too (rounded); the cell state
 and the recurrent sums are not.  A gated layer's projections are not rounded, their gradients
 are; the gradients that layer norm, gated layer and 1x1 convolution hand to each other are not, nor is what a ROTARY and the ATTENTION
-that alone reads it do (which the library keeps in 16-bit floats with scales, eight times as fine).
+of the same heads that alone reads it do (which the library keeps in 16-bit floats with scales, eight times as fine).
 storage="exact" rounds nothing.
 """
 import numpy as np
@@ -66,14 +66,14 @@ class OracleStage:
 
     def _float_grad(self, t):
         """Whether the gradient of layer t's output is not rounded: of a layer norm that only a gated layer reads, of a gated layer
-        that only a 1x1 convolution of widths that are multiples of 8 does, of a ROTARY that only an ATTENTION does."""
+        that only a 1x1 convolution of widths that are multiples of 8 does, of a ROTARY that only an ATTENTION of the same heads does."""
         if len(self.readers.get(t, [])) != 1:
             return False
         P, N = self.layers[t], self.layers[self.readers[t][0]]
         if P["kind"] == C.LAYERNORM:
             return N["kind"] == C.GATED
         if P["kind"] == C.ROTARY:
-            return N["kind"] == C.ATTENTION
+            return N["kind"] == C.ATTENTION and (N["kh"], N["kw"]) == (P["kh"], P["kw"])
         return (P["kind"] == C.GATED and N["kind"] == C.CONV2D and (N["kh"], N["stride"], N["pad"]) == (1, 1, 0) and
                 N["cin"] % 8 == 0 and N["cout"] % 8 == 0)
 

@@ -122,7 +122,7 @@ struct Layer {
     // lies (the tensors share their storage) and value heads stay by themselves.
     float2 *table = nullptr;
     bool values_stay = false, dvalues_stay = false;
-    // bf16 ROTARY that only an ATTENTION reads: its queries and keys go to the slot as 16-bit floats with a scale for each head and position
+    // bf16 ROTARY that only an ATTENTION of the same heads reads: its queries and keys go to the slot as 16-bit floats with a scale for each head and position
     // (off_half, off_scale) and nowhere else, and their gradients come back as floats (off_float, among the gradients).  A score is a sum of
     // products of two rounded factors: with scores of standard deviation 4, which a cap is for, bf16 factors make gradients 1.05e-2 wrong in
     // the 2-norm and 16-bit floats 2.3e-3; at 1, with norms, 4.6e-3 and 1.9e-3, of which the rounding of the result is 1.7e-3.
@@ -1664,7 +1664,9 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
         if (L.d.kind != BAPIPE_ROTARY) continue;
         const Tensor &A = st->tensors[L.a];
         Tensor &O = st->tensors[L.o];
-        const bool only_attention = L.o != last_t && O.consumers.size() == 1 && st->layers[O.consumers[0]].d.kind == BAPIPE_ATTENTION;
+        // (one that divides the channels into other heads takes them as it takes any layer's: what the two hand each other lies by heads)
+        const bapipe_layer_desc_t *N = L.o != last_t && O.consumers.size() == 1 ? &st->layers[O.consumers[0]].d : nullptr;
+        const bool only_attention = N && N->kind == BAPIPE_ATTENTION && N->kh == L.d.kh && N->kw == L.d.kw;
         L.half = only_attention && st->dt == DT_BF16;
         if (!L.w_elems && L.a != 0 && L.o != last_t && A.consumers.size() == 1) {
             const bapipe_layer_desc_t &P = st->layers[L.a - 1].d;

@@ -522,6 +522,23 @@ def test_rotary_and_attention(dtype, norm, d, heads, groups, T, mask):
 
 
 @BOTH
+@pytest.mark.parametrize("norm,conv", [(0, 0), (1, 0), (0, 1), (1, 1)])
+@pytest.mark.parametrize("turned,read", [((8, 4, 64), (12, 2, 64)), ((8, 4, 64), (4, 2, 128)), ((2, 1, 12), (6, 3, 4)), ((5, 1, 9), (1, 1, 21)), ((4, 4, 30), (8, 1, 36))])
+def test_an_attention_of_other_heads_than_the_rotary_in_front(dtype, turned, read, norm, conv):
+    """Channels that one layer turns as keys are queries of the other, and so on.  Both sides round what the ROTARY stores, so what differs is a
+    gradient's roundings: a probability, the output in dout . o, its own, the gradient of a score, itself, and once more behind the ROTARY; with a
+    convolution in front the product's.  Eight."""
+    c = (turned[0] + 2 * turned[1]) * turned[2]
+    assert c == (read[0] + 2 * read[1]) * read[2]
+    b = C._Builder()
+    if conv:
+        b.conv(c, c, 1, src=-1)
+    b.rotary(*turned, norm=norm, src=None if conv else -1)
+    b.attention(*read)
+    _compare(_stage(b.layers, dtype, (c, 70, 1), n_micro=3, stage_index=1, n_stages=2), roundings=8)
+
+
+@BOTH
 @pytest.mark.parametrize("d,norm,mask,cap", [(24, 1, C.MASK_CAUSAL, 0.0), (33, 0, C.MASK_NONE, 0.0), (64, 1, C.MASK_SPANS, 0.0), (64, 0, C.MASK_CAUSAL, 4.0), (96, 1, C.MASK_CAUSAL, 0.0),
                                              (128, 1, C.MASK_CAUSAL, 0.0), (128, 0, C.MASK_SPANS, 4.0), (192, 0, C.MASK_CAUSAL, 0.0), (256, 1, C.MASK_SPANS, 0.0)])
 def test_rotary_and_attention_of_many_sequences(dtype, d, norm, mask, cap):

@@ -1,0 +1,122 @@
+"""What rotary positions and attention launch and keep, asked without a GPU: tests/launch_recorder.c takes the place of the runtime."""
+import ctypes as ct
+import json
+import os
+import re
+import shutil
+import subprocess
+import sys
+
+import pytest
+
+from oracle.stage import one_f_one_b_order
+from paper_2012_12544_amd import binding as B
+from stage_inputs import configs as C
+from test_launches import SOMEWHERE, STREAMS
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+def _record(recorder, library, cases):
+    """In a process of its own, for each case: bytes of a micro-batch in flight, the blocks that the stage asked its allocator for, the status
+    of the pass that refused, and (kernel, integers among its template arguments, blocks) of every launch of a mini-batch."""
+    rec = ct.CDLL(recorder, mode=ct.RTLD_GLOBAL)
+    rec.recorder_launch.restype = ct.c_char_p
+    B.LIB_PATH = library
+    out = []
+    for case in cases:
+        blocks = []
+
+        def alloc(nbytes, ctx):
+            blocks.append((SOMEWHERE + (sum(n for _, n in blocks) + 4095) // 4096 * 4096 + 4096 * len(blocks), nbytes))
+            return blocks[-1][0]
+
+        b = C._Builder()
+        for kind, args, kw in case["layers"]:
+            getattr(b, kind)(*args, **kw)
+        st = C._stage("recorded", b.layers, case["dtype"], tuple(case["input"]), case["micro_batch"], 1, 1, 1, 1, 0, "xavier")
+        o = B.make_opts(st, io_layout=B.NHWC, stream=STREAMS["own"])
+        o.mem.alloc, o.mem.free = B.ALLOC_FN(alloc), B.FREE_FN(lambda ptr, ctx: None)
+        h = B.bapipe_stage_create(b.layers, case["micro_batch"], 1, o)
+        rec.recorder_clear()
+        status = 0
+        backward = B.bapipe_stage_backward_static if case.get("static") else B.bapipe_stage_backward
+        try:
+            for what, m in one_f_one_b_order(1, 1):
+                if what == "F":
+                    if any(L["kind"] == C.ATTENTION and L["stride"] == C.MASK_SPANS for L in b.layers):
+                        B.bapipe_stage_set_spans(h, m, SOMEWHERE >> 5)
+                    B.bapipe_stage_forward(h, m, SOMEWHERE >> 1, SOMEWHERE >> 2)
+                else:
+                    backward(h, m, SOMEWHERE >> 3, SOMEWHERE >> 4)
+        except B.BapipeError as e:
+            status = e.status
+        launches = []
+        for i in range(rec.recorder_launches()):
+            grid, stream, tickets, lds = (ct.c_uint * 3)(), ct.c_size_t(), ct.c_size_t(), ct.c_size_t()
+            name = rec.recorder_launch(i, grid, ct.byref(stream), ct.byref(tickets), ct.byref(lds)).decode()
+            m = re.search(r"\d(k_attention_[a-z]+|k_rotary(?:_[a-z]+)?)", name)
+            if m:
+                launches.append((m.group(1), [int(a) for a in re.findall(r"L[ib](\d+)E", name[m.end():])], list(grid)))
+        out.append(dict(per_micro_batch=B.bapipe_stage_stash_bytes(h)[0], blocks=blocks, status=status, launches=launches))
+        B.bapipe_stage_destroy(h)
+    return out
+
+
+@pytest.fixture(scope="module")
+def record(tmp_path_factory):
+    if shutil.which("gcc") is None:
+        pytest.skip("needs gcc")
+    B.load()
+    so = str(tmp_path_factory.mktemp("recorder") / "recorder.so")
+    subprocess.check_call(["gcc", "-O1", "-std=c11", "-shared", "-fPIC", "-Wall", "-o", so, os.path.join(HERE, "launch_recorder.c")])
+
+    def run(cases):
+        r = subprocess.run([sys.executable, os.path.abspath(__file__), so, B.LIB_PATH], input=json.dumps(cases), capture_output=True, text=True, timeout=120,
+                           env=dict(os.environ, PYTHONPATH=os.pathsep.join([os.path.dirname(HERE), HERE])))
+        assert r.returncode == 0, r.stderr[-2000:]
+        return json.loads(r.stdout)
+    return run
+
+
+def _case(layers, dtype, c, seq, micro_batch=1, static=False):
+    layers = [(layers[0][0], layers[0][1], dict(layers[0][2], src=-1))] + layers[1:]
+    return dict(layers=layers, dtype=dtype, input=[c, seq, 1], micro_batch=micro_batch, static=static)
+
+
+# Integers among the template arguments: of the attention kernels DP, VEC, EXTRA, HALF, KS, of k_rotary V, C, L, K, PAIRS, NORM, BACK, FLOATS
+ATTENTION = ("k_attention_fwd", "k_attention_dq", "k_attention_dkv")
+HALF, ROTARY_LANES, ROTARY_HEADS, ROTARY_FLOATS = 3, 2, 3, 7
+
+
+def _up(n):
+    return (n + 255) // 256 * 256
+
+
+@pytest.mark.parametrize("norm", [0, 1])
+@pytest.mark.parametrize("dtype", [C.FP32, C.BF16])
+@pytest.mark.parametrize("heads,groups,d", [(12, 2, 64), (4, 2, 128), (2, 1, 256), (14, 1, 64)])
+def test_an_attention_of_other_heads_than_the_rotary_in_front(record, dtype, norm, heads, groups, d):
+    """Both divide 1024 channels, the ROTARY into 8 / 4 heads of 64.  Nothing of one's layout is handed to the other: all channels are stored in
+    the storage type, and the gradients come back in it."""
+    rows, es = 2 * 40, 4 if dtype == C.FP32 else 2
+
+    def case(h, g, w):
+        return _case([("rotary", [8, 4, 64], dict(norm=norm)), ("attention", [h, g, w], {})], dtype, 1024, 40, micro_batch=2)
+
+    same, other = record([case(8, 4, 64), case(heads, groups, d)])
+    at = {name: (args, grid) for name, args, grid in other["launches"]}
+    assert all(at[name][0][HALF] == 0 for name in ATTENTION), other["launches"]
+    turns = [(args, grid) for name, args, grid in other["launches"] if name == "k_rotary"]
+    assert len(turns) == 2 and turns[0][0][ROTARY_FLOATS] == turns[1][0][ROTARY_FLOATS] == 0
+    for args, grid in turns:                                 # value heads too, a head to a group of lanes (few rows)
+        assert args[ROTARY_HEADS] == 1 and grid[0] == -(-rows * 16 // (256 // args[ROTARY_LANES])), turns
+    out = rows * heads * d
+    kept = _up(rows * 1024 * es) * (1 + norm) + _up(out * es) + _up(2 * heads * 40 * 4) + (_up(out) if dtype == C.BF16 else 0)
+    assert other["per_micro_batch"] == kept
+    # of the same heads: 16-bit floats in a bf16 stage
+    assert all(args[HALF] == (dtype == C.BF16) for name, args, _ in same["launches"] if name in ATTENTION)
+
+
+if __name__ == "__main__":
+    print(json.dumps(_record(sys.argv[1], sys.argv[2], json.load(sys.stdin))))
