@@ -246,7 +246,7 @@ __global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256)
     at_store<T, VEC, ND>((T *)p.dv + at_k + (size_t)s.groups * d, d, half * ND, dv, 1.0f, lane);
 }
 
-// The sums of all splits, V channels a thread (d a multiple of V)
+// The sums of all splits, V channels a thread (d a multiple of V, dqk and dv aligned to V elements)
 template <class T, int V> __global__ __launch_bounds__(256) void k_attention_join(AttnArgs p)
 {
     typedef vec_t<float, V> vecf;
@@ -308,7 +308,8 @@ hipError_t attention_dkv(int dt, const AttnArgs &a, hipStream_t s)
 {
     const hipError_t e = at_dispatch<Keys>(dt, a, s);
     if (e != hipSuccess || a.splits == 1) return e;
-    const bool vec = a.s.d % 4 == 0;
+    // bf16 heads that are read element by element may be stored to a caller's dx that is aligned to one of them
+    const bool vec = a.s.d % 4 == 0 && ((uintptr_t)a.dqk | (uintptr_t)a.dv) % (4 * dt_size(dt)) == 0;
     const size_t n = (size_t)a.s.N * a.s.groups * a.s.T * 2 * a.s.d / (vec ? 4 : 1);
     const dim3 grid((unsigned)((n + 255) / 256));
     if (dt == DT_F32 && vec) hipLaunchKernelGGL((k_attention_join<float, 4>), grid, dim3(256), 0, s, a);

@@ -231,6 +231,29 @@ def test_buffers_at_odd_addresses_and_over_one_another(dtype, name):
 
 
 @BOTH
+@pytest.mark.parametrize("d", [12, 20])
+def test_sums_in_parts_for_a_dx_at_an_odd_address(dtype, d):
+    """Keys' sums in parts, joined four channels at a time where dx allows it: the same bits at every address, nothing beside dx touched."""
+    st = _attention(dtype, 4, 1, d, 700, micro_batch=1)
+    (x0,), (g0,) = stage_io(st)
+    host = lambda a: torch.from_numpy(a).permute(0, 2, 3, 1).reshape(-1).to(DEV, tdtype(st))  # noqa: E731
+    x, dy = host(x0), host(g0)
+    ref = None
+    for offset in (0, 1, 2, 3, 4):
+        g = GpuStage(st, [(None, None)])
+        y, buf = torch.zeros_like(dy), torch.full((len(x) + 128,), 7.0, dtype=x.dtype, device=DEV)
+        dx = buf[64 + offset:64 + offset + len(x)]
+        torch.cuda.synchronize()
+        B.bapipe_stage_forward(g.h, 0, x.data_ptr(), y.data_ptr())
+        B.bapipe_stage_backward(g.h, 0, dy.data_ptr(), dx.data_ptr())
+        torch.cuda.synchronize()
+        ref = dx.clone() if ref is None else ref
+        assert torch.equal(dx, ref) and torch.any(dx != 0) and torch.all(torch.isfinite(dx)), offset
+        assert torch.all(buf[:64 + offset] == 7) and torch.all(buf[64 + offset + len(x):] == 7), offset
+        g.close()
+
+
+@BOTH
 @pytest.mark.parametrize("name", list(_address_stages(C.FP32)))
 def test_a_stage_that_hands_no_gradient_on(dtype, name):
     st = _address_stages(dtype)[name]

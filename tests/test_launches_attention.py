@@ -48,7 +48,7 @@ def _record(recorder, library, cases):
                         B.bapipe_stage_set_spans(h, m, SOMEWHERE >> 5)
                     B.bapipe_stage_forward(h, m, SOMEWHERE >> 1, SOMEWHERE >> 2)
                 else:
-                    backward(h, m, SOMEWHERE >> 3, SOMEWHERE >> 4)
+                    backward(h, m, SOMEWHERE >> 3, (SOMEWHERE >> 4) + case.get("dx", 0))
         except B.BapipeError as e:
             status = e.status
         launches = []
@@ -116,6 +116,17 @@ def test_an_attention_of_other_heads_than_the_rotary_in_front(record, dtype, nor
     assert other["per_micro_batch"] == kept
     # of the same heads: 16-bit floats in a bf16 stage
     assert all(args[HALF] == (dtype == C.BF16) for name, args, _ in same["launches"] if name in ATTENTION)
+
+
+@pytest.mark.parametrize("d", [12, 20, 100, 8, 64])
+@pytest.mark.parametrize("dx", [0, 2, 4, 8])
+def test_the_sums_of_all_splits_are_stored_in_no_wider_pieces_than_dx_allows(record, d, dx):
+    """Heads of 12, 20 or 100 bf16 are no whole number of 16 bytes, so dx may lie at any element: four of them at once only where that is a
+    multiple of 8 bytes.  (dx of the others passes through the stage's own tensor.)"""
+    case = _case([("attention", [4, 1, d], {})], C.BF16, 6 * d, 1100)
+    got, = record([dict(case, dx=dx)])
+    join, = [args for name, args, _ in got["launches"] if name == "k_attention_join"]
+    assert join == [1 if d % 8 and dx % 8 else 4]
 
 
 if __name__ == "__main__":
