@@ -409,7 +409,10 @@ __device__ __forceinline__ AtBlock at_block(const AttnShape &s)
 // with KS 1 and 2: 4 x 333 positions of 6 / 2 float heads of 45, 72 blocks of 128 rows: 40, 52, 67 and 28, 34, 43; 64 x 50 of 16 / 4 heads of 64:
 // 14.2, 15.2, 14.6 and 13.9, 14.9, 12.2; but 3 x 1003 of 12 heads of 80, 288 blocks for 256 units: 49, 55, 66 and 45, 58, 73.
 template <class T, int DP> constexpr bool kAtShares = AtTile<T, DP>::ROWS == 64;
-inline bool at_shares(const AttnArgs &a, long long blocks) { return a.s.T <= 64 || blocks <= a.units; }
+// per_unit: so many of the blocks, which are twice as many then, a unit holds at once; more than that take a second round.  dkv of wide heads,
+// one block a unit, a mini-batch of 1003 positions without a mask, us: 12 heads of 192 172 in 384 blocks of KS 2, 130 in 192 of KS 1, the
+// sums in two parts in both; 12 of 256 306 and 166 (KS 2 spills 264 registers there).
+inline bool at_shares(const AttnArgs &a, long long blocks, int per_unit = 2) { return a.s.T <= 64 || 2 * blocks <= (long long)a.units * per_unit; }
 
 // Which block of rows is the i-th to be started: those with the most to do first, with a causal mask the last queries and the first keys
 template <int KS> __device__ __forceinline__ int at_query_block(const AttnArgs &a, int n, int i)

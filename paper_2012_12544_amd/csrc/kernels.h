@@ -276,7 +276,8 @@ struct AttnArgs {
 hipError_t attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int *order, int N, int T, hipStream_t s);
 size_t attention_order_size(int N, int T);
 hipError_t attention_fwd(int dt, const AttnArgs &a, hipStream_t s);
-size_t attention_workspace(int dt, const AttnShape &a, int compute_units);          // of a backward pass
+// of a backward pass; half: queries and keys are 16-bit floats
+size_t attention_workspace(int dt, const AttnShape &a, bool half, int compute_units);
 hipError_t attention_bwd(int dt, AttnArgs a, void *workspace, int compute_units, hipStream_t s);
 hipError_t attention_dq(int dt, const AttnArgs &a, hipStream_t s);
 hipError_t attention_dkv(int dt, const AttnArgs &a, hipStream_t s);

@@ -17,8 +17,12 @@ template <class T, int DP, bool HALF> constexpr int kDkvHalves = DP * (int)sizeo
 // SIMD, which spills none: 281.  (4 x 2048 positions, causal, 16 / 2 heads)
 template <int DP, bool EXTRA, bool HALF, int KS> constexpr int kDkvRows = KS == 1 && HALF && !EXTRA && DP == 128 ? 32 : 0;
 
+// Blocks that the launch bounds let a unit hold, and those that fit: float heads of up to 64 channels take 251 registers
+template <class T, int DP, bool EXTRA> constexpr int kDkvBlocks = DP * (int)sizeof(T) <= (EXTRA ? 192 : 256) ? 2 : 1;
+template <class T, int DP, bool EXTRA> constexpr int kDkvFit = sizeof(T) == 4 && DP == 64 ? 2 : kDkvBlocks<T, DP, EXTRA>;
+
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF, int KS>
-__global__ __launch_bounds__(AT_TPB, (DP * (int)sizeof(T) <= (EXTRA ? 192 : 256) ? 2 : 1)) void k_attention_dkv(AttnArgs p)
+__global__ __launch_bounds__(AT_TPB, (kDkvBlocks<T, DP, EXTRA>)) void k_attention_dkv(AttnArgs p)
 {
     constexpr int R = kDkvRows<DP, EXTRA, HALF, KS>, ROWS = AT_ROWS / KS;
     typedef AtTile<T, DP, R> Tile;
@@ -273,6 +277,8 @@ template <class T, int V> __global__ __launch_bounds__(256) void k_attention_joi
     *(vec_t<T, V> *)(half_row & 1 ? (T *)p.dv + at + (size_t)s.groups * s.d : (T *)p.dqk + at) = out;
 }
 
+long long key_blocks(const AttnShape &s) { return (long long)s.N * s.groups * ((s.T + AT_ROWS - 1) / AT_ROWS); }
+
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Keys {
     template <int KS> static hipError_t launch(const AttnArgs &a, hipStream_t stream)
     {
@@ -283,7 +289,7 @@ template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Keys {
     static hipError_t go(const AttnArgs &a, hipStream_t stream)
     {
         if constexpr (kAtShares<T, DP>)
-            if (at_shares(a, (long long)a.s.N * a.s.groups * ((a.s.T + AT_ROWS - 1) / AT_ROWS) * a.splits)) return launch<2>(a, stream);
+            if (at_shares(a, key_blocks(a.s) * a.splits * kDkvHalves<T, DP, HALF>, kDkvFit<T, DP, EXTRA>)) return launch<2>(a, stream);
         return launch<1>(a, stream);
     }
 };
@@ -291,15 +297,26 @@ template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Keys {
 // In how many parts the queries of the keys' sums are taken.  A block owns 128 keys of a key head, for all query heads that share it: few of
 // them leave units idle or, where keys are seen by different numbers of queries, waiting for the longest.  Splits cost a pass over their sums:
 // 12 heads of 80, 3 x 1003 positions without a mask, 288 blocks of the 512 that fit, us: 69 in one part, 59 and 14 in three.
-int key_splits(int dt, const AttnShape &s, int compute_units)
+// What fits is by the kernel that runs.  With two blocks a unit for all of up to 128 channels, a column's halves not counted, 16 / 4 heads of 128 with
+// slopes over 2048 positions, causal, took 214 us a mini-batch, 184 so; 8 / 4 of 256 behind a ROTARY over 2 x 2048, causal, 482 and 454.
+template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Splits {
+    static hipError_t go(const AttnArgs &a, int *out)
+    {
+        const AttnShape &s = a.s;
+        const long long fit = (long long)a.units * kDkvFit<T, DP, EXTRA>, blocks = key_blocks(s) * kDkvHalves<T, DP, HALF>;
+        const long long tiles = (long long)((s.T + 63) / 64) * (s.heads / s.groups);           // of queries
+        long long splits = s.mask == ATTN_NONE ? fit / blocks : (2 * fit + blocks / 2) / blocks;
+        if (splits > tiles / 4) splits = tiles / 4;
+        *out = splits > 16 ? 16 : splits > 1 ? (int)splits : 1;
+        return hipSuccess;
+    }
+};
+int key_splits(int dt, AttnArgs a, int compute_units)
 {
-    const bool wide = dt == DT_F32 ? s.d > 64 : s.d > 128;
-    const long long fit = (long long)(compute_units > 0 ? compute_units : 256) * (wide ? 1 : 2);
-    const long long blocks = (long long)s.N * s.groups * ((s.T + AT_ROWS - 1) / AT_ROWS) * (dt == DT_F32 && s.d > 128 ? 2 : 1);
-    const long long tiles = (long long)((s.T + 63) / 64) * (s.heads / s.groups);           // of queries
-    long long splits = s.mask == ATTN_NONE ? fit / blocks : (2 * fit + blocks / 2) / blocks;
-    if (splits > tiles / 4) splits = tiles / 4;
-    return splits > 16 ? 16 : splits > 1 ? (int)splits : 1;
+    a.units = compute_units > 0 ? compute_units : 256;
+    int splits = 1;
+    (void)at_dispatch<Splits>(dt, a, &splits);
+    return splits;
 }
 
 }  // namespace
@@ -319,9 +336,12 @@ hipError_t attention_dkv(int dt, const AttnArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-size_t attention_workspace(int dt, const AttnShape &a, int compute_units)
+size_t attention_workspace(int dt, const AttnShape &a, bool half, int compute_units)
 {
-    const int splits = key_splits(dt, a, compute_units);
+    AttnArgs q = {};
+    q.s = a;
+    if (half) q.half = &q;                                   // not read
+    const int splits = key_splits(dt, q, compute_units);
     const size_t rows = ((size_t)a.N * a.heads * a.T * sizeof(float) + 255) / 256 * 256;
     return rows + (splits > 1 ? (size_t)splits * a.N * a.groups * a.T * 2 * a.d * sizeof(float) : 0);
 }
@@ -330,7 +350,7 @@ hipError_t attention_bwd(int dt, AttnArgs a, void *workspace, int compute_units,
 {
     a.dsum = (float *)workspace;
     a.part = (float *)((char *)workspace + ((size_t)a.s.N * a.s.heads * a.s.T * sizeof(float) + 255) / 256 * 256);
-    a.splits = key_splits(dt, a.s, compute_units);
+    a.splits = key_splits(dt, a, compute_units);
     const hipError_t e = attention_dq(dt, a, s);
     return e == hipSuccess ? attention_dkv(dt, a, s) : e;
 }

@@ -1893,7 +1893,8 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
                 st->off_bounds = slot; slot += align_up((size_t)q.N * ((q.T + kAttnTile - 1) / kAttnTile) * 2 * sizeof(int4));
                 if (const size_t n = attention_order_size(q.N, q.T)) { st->off_order = slot; slot += align_up(n * sizeof(int)); }
             }
-            const size_t w = attention_workspace(st->dt, q, st->compute_units);
+            const Layer *R = rotary_before(st, L);
+            const size_t w = attention_workspace(st->dt, q, R && R->half, st->compute_units);
             work = w > work ? w : work;
         }
         if (L.d.kind == BAPIPE_LSTM) {

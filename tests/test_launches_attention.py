@@ -129,5 +129,42 @@ def test_the_sums_of_all_splits_are_stored_in_no_wider_pieces_than_dx_allows(rec
     assert join == [1 if d % 8 and dx % 8 else 4]
 
 
+def _blocks_a_unit(bf16, d, extra):
+    """Of k_attention_dkv, by its launch bounds; float heads of up to 64 channels fit twice by their registers."""
+    if not bf16:
+        return 2 if d <= 64 else 1
+    extra = extra or d % 8 != 0                              # element by element there is one kernel, which knows caps and slopes
+    width = next(w for w in ((64, 128, 256) if d % 8 else (32, 64, 96, 128, 192, 256)) if d <= w)
+    return 2 if 2 * width <= (192 if extra else 256) else 1
+
+
+@pytest.mark.parametrize("dtype", [C.FP32, C.BF16])
+@pytest.mark.parametrize("rotary", [0, 1])
+@pytest.mark.parametrize("bias", [0, 8])
+def test_parts_of_the_keys_sums_are_no_more_than_fit_beside_each_other(record, dtype, rotary, bias):
+    """Without a mask all blocks take the same time: those that start in a second round leave the units idle behind it.  The blocks of heads that
+    are taken in two halves of their columns count twice, and so do those of two waves to 32 rows."""
+    cases = []
+    for d in (30, 64, 80, 96, 100, 104, 128, 160, 192, 200, 208, 256):
+        for heads, groups, seq, micro_batch in ((8, 1, 2048, 1), (4, 2, 1024, 2), (12, 12, 700, 1), (16, 2, 520, 3)):
+            layers = [("rotary", [heads, groups, d], {})] * rotary + [("attention", [heads, groups, d, C.MASK_NONE, 0.0, bias], {})]
+            cases.append((d, _case(layers, dtype, (heads + 2 * groups) * d, seq, micro_batch)))
+    parts = 0
+    for (d, case), got in zip(cases, record([c for _, c in cases])):
+        (args, grid), = [(args, grid) for name, args, grid in got["launches"] if name == "k_attention_dkv"]
+        if not any(name == "k_attention_join" for name, *_ in got["launches"]):
+            continue
+        parts += 1
+        assert grid[0] <= 256 * _blocks_a_unit(dtype == C.BF16, d, bias), (case, args, grid)
+    assert parts >= 20
+
+
+def test_wide_heads_behind_a_rotary_run_on_the_static_workspace(record):
+    """Their columns are taken in halves, so eight parts of the keys' sums fill the units: 32 MiB."""
+    case = _case([("rotary", [8, 1, 256], {}), ("attention", [8, 1, 256, C.MASK_NONE], {})], C.BF16, 2560, 2048, static=True)
+    got, = record([case])
+    assert got["status"] == 0 and 32 << 20 <= got["blocks"][4][1] < 33 << 20
+
+
 if __name__ == "__main__":
     print(json.dumps(_record(sys.argv[1], sys.argv[2], json.load(sys.stdin))))
