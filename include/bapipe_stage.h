@@ -128,7 +128,8 @@ typedef enum { BAPIPE_MASK_NONE = 0, BAPIPE_MASK_CAUSAL = 1, BAPIPE_MASK_SPANS =
  *   has_bias = 0: eps must be 0, no parameters.  Value heads pass unchanged.
  * ATTENTION: cout = kh d.  Score of query i and key j: q_i k_j / sqrt(d); with eps > 0 capped to eps tanh(score / eps);
  *   with pad > 0 less 2^(-pad (h + 1) / kh) |i - j| in query head h (pad up to 64).  Softmax over the keys that stride
- *   lets the position see; one that sees none gets zeros and gives no gradients.  has_bias must be 0.  What the
+ *   lets the position see; one that sees none gets zeros and gives no gradients.  has_bias must be 0.  micro_batch times kh times the
+ *   number of 128 positions (rounded up) must be below 2^24 (E_UNSUPPORTED).  What the
  *   positions of a sequence hold behind the last that sees some, or is seen, has no effect on anything, NaN and infinity
  *   included; at other positions that are not seen it has to be finite.
  *   In bf16 stages probabilities and the gradients of scores are rounded to 16 bits as operands of the next product, and what a

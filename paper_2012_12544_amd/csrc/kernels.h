@@ -275,6 +275,8 @@ struct AttnArgs {
 // order: attention_order_size elements, or NULL where that is 0
 hipError_t attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int *order, int N, int T, hipStream_t s);
 size_t attention_order_size(int N, int T);
+// whether its blocks are few enough for a launch
+bool attention_launches(int N, int heads, int T);
 hipError_t attention_fwd(int dt, const AttnArgs &a, hipStream_t s);
 // of a backward pass; half: queries and keys are 16-bit floats
 size_t attention_workspace(int dt, const AttnShape &a, bool half, int compute_units);

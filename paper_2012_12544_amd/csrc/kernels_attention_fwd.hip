@@ -302,6 +302,10 @@ hipError_t attention_spans(const int32_t *given, int2 *spans, int4 *bounds, int 
     return hipGetLastError();
 }
 
+// A launch holds less than 2^32 threads.  Where blocks are many nothing makes more of them: two waves share 32 rows, and sums are split, where blocks
+// are no more than a few times the units, and heads whose columns are taken in halves (of keys) are too wide for 2^23 of them in 2 GiB.
+bool attention_launches(int N, int heads, int T) { return (long long)N * heads * ((T + AT_ROWS - 1) / AT_ROWS) < (1ll << 32) / AT_TPB; }
+
 hipError_t attention_fwd(int dt, const AttnArgs &a, hipStream_t s) { return at_dispatch<Forward>(dt, a, s); }
 
 }  // namespace bapipe

@@ -3,6 +3,8 @@
 // The rotation by minus the angle is its transpose: dz = rotation of dy, dg = sum dz xhat, dx = rs (g dz - xhat mean(g dz xhat)).
 // HBM bounds both: 8192 positions of 32 / 8 heads of 128 with norms, forward with a second place for x, 77 us, 3.9 TB/s; backward 80 us, 3.8 TB/s;
 // 32768 of 16 / 16 heads without norms, 137 us either way, 5.9 TB/s.
+#include <algorithm>
+
 #include "dev_common.h"
 #include "kernels.h"
 
@@ -11,6 +13,7 @@ namespace {
 
 constexpr int TPB = 256;
 constexpr int kGainBlocks = 1024;        // that leave sums of the gains' gradients
+constexpr int kMostBlocks = 1 << 22;     // a launch holds less than 2^32 threads; the groups of lanes take what is left in further rounds
 
 template <class T> struct RotaryArgs {
     RotaryShape r;
@@ -291,7 +294,7 @@ Plan plan(int dt, const RotaryShape &r, bool sums, bool all_heads, std::initiali
     p.per_unit = (p.per_row + p.K - 1) / p.K;
     p.units = r.rows * p.per_unit;
     const int per_block = TPB / p.lanes;
-    p.blocks = (int)(((long long)p.units + per_block - 1) / per_block);
+    p.blocks = (int)std::min(((long long)p.units + per_block - 1) / per_block, (long long)kMostBlocks);
     if (sums && p.blocks > kGainBlocks) p.blocks = kGainBlocks;
     return p;
 }

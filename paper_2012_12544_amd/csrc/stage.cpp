@@ -1580,6 +1580,7 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
                 if (d.pad < 0 || d.pad > 64) return create_fail(BAPIPE_E_INVALID, "layer %d: range %d of the slopes, must be 0 to 64", i, d.pad);
                 if (d.has_bias) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: attention has no parameters", i);
                 if (!(d.eps >= 0.f) || d.eps > FLT_MAX) return create_fail(BAPIPE_E_INVALID, "layer %d: cap must be positive, or 0 for none", i);
+                if (!attention_launches(micro_batch, d.kh, A.H)) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: attention of 2^24 blocks or more", i);
                 if (d.stride == BAPIPE_MASK_SPANS) {
                     if (st->span_T && st->span_T != A.H) return create_fail(BAPIPE_E_SHAPE, "layer %d: spans of %d positions, another layer's of %d", i, A.H, st->span_T);
                     st->span_T = A.H;

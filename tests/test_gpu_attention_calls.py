@@ -393,6 +393,26 @@ def test_a_window_over_a_long_sequence(dtype, T, window):
             assert e <= limit * np.linalg.norm(b[:, :, lo:lo + T // 10]), (name, lo)
 
 
+def test_more_heads_than_a_launch_has_groups_of_lanes_for():
+    """2^28 heads of a channel in one round, 256 thousand more in the next.  Nothing turns, so y is x and dx is dy."""
+    st = _rotary(C.BF16, 32767, 1, 1, 1, micro_batch=8200)
+    n = 8200 * 32769
+    assert n > 2 ** 28
+    g = GpuStage(st, [(None, None)])
+    gen_ = torch.Generator(DEV)
+    gen_.manual_seed(3)
+    x, dy = (torch.randint(-32768, 32768, (n,), dtype=torch.int16, device=DEV, generator=gen_) & ~0x4000 for _ in range(2))      # no infinity, no NaN
+    y, dx = torch.zeros_like(x), torch.zeros_like(x)
+    torch.cuda.synchronize()
+    B.bapipe_stage_forward(g.h, 0, x.data_ptr(), y.data_ptr())
+    B.bapipe_stage_backward(g.h, 0, dy.data_ptr(), dx.data_ptr())
+    torch.cuda.synchronize()
+    # as numbers: -0 cos + 0 sin is +0, the sum of two zeros of different signs
+    assert all(torch.equal(a.view(torch.bfloat16), b.view(torch.bfloat16)) for a, b in ((x, y), (dy, dx)))
+    assert bool(((x == y) | (x == -32768)).all()) and bool(((dy == dx) | (dy == -32768)).all())
+    g.close()
+
+
 def test_sums_that_the_static_workspace_does_not_hold():
     """Few key heads of many positions: the parts of their sums take more than the array.  The call is refused and the other one works."""
     st = _attention(C.BF16, 8, 1, 128, 16384, C.MASK_CAUSAL, micro_batch=1)

@@ -166,5 +166,14 @@ def test_wide_heads_behind_a_rotary_run_on_the_static_workspace(record):
     assert got["status"] == 0 and 32 << 20 <= got["blocks"][4][1] < 33 << 20
 
 
+def test_launches_stay_below_two_to_the_32_threads(record):
+    """The most heads of one channel that 2 GiB hold, each for itself; many short sequences, as many blocks as an attention is taken with."""
+    cases = [_case([("rotary", [32767, 1, 1], {})], C.BF16, 32769, 1, micro_batch=32767),
+             _case([("attention", [256, 1, 4], {})], C.BF16, 1032, 1, micro_batch=65535)]
+    for case, got in zip(cases, record(cases)):
+        assert got["status"] == 0 and len(got["launches"]) >= 2
+        assert all(256 * grid[0] < 1 << 32 for _, _, grid in got["launches"]), got["launches"]
+
+
 if __name__ == "__main__":
     print(json.dumps(_record(sys.argv[1], sys.argv[2], json.load(sys.stdin))))

@@ -249,6 +249,15 @@ def test_what_create_refuses_of_an_attention():
     assert _status(two(4), shape=(32, 8, 1)) == B.E_SHAPE
 
 
+def test_what_create_refuses_of_many_blocks():
+    """A launch holds less than 2^24 blocks of 256 threads; a block is 128 positions of a head, or what there are of them."""
+    for heads, micro_batch, seq, want in ((256, 65535, 1, B.E_OOM), (256, 65536, 1, B.E_UNSUPPORTED), (256, 65536, 60, B.E_UNSUPPORTED), (4096, 4095, 1, B.E_OOM),
+                                          (4096, 4096, 1, B.E_UNSUPPORTED), (2 ** 20, 16, 1, B.E_UNSUPPORTED), (2 ** 20, 15, 8, B.E_OOM)):
+        d = 1 if heads * micro_batch * seq > 2 ** 26 else 4
+        for mask in (C.MASK_NONE, C.MASK_SPANS):
+            assert _status(_layer("attention", heads, 1, d, mask), shape=((heads + 2) * d, seq, 1), micro_batch=micro_batch) == want, (heads, micro_batch, seq)
+
+
 @pytest.mark.parametrize("method", ["rotary", "attention"])
 def test_a_flattened_sequence_is_refused(method):
     b = C._Builder()
