@@ -427,6 +427,44 @@ def test_sums_that_the_static_workspace_does_not_hold():
     g.close()
 
 
+def test_sums_of_many_parts_and_tiles():
+    """16384 positions of 8 query heads on one key head: y and dq of some positions, dk and dv of some keys, in 64 bits.
+
+    In the 2-norm of a head's channels: y has been through two roundings (a probability, itself), gradients through at most five (a probability,
+    the output in dout . o, its own, the gradient of a score, itself), each of root mean square up to HALF / sqrt(3) and independent from
+    summand to summand; twice that.  One of the eight parts that the keys' sums are taken in is a third of them, in the 2-norm."""
+    H, d, T = 8, 128, 16384
+    st = _attention(C.BF16, H, 1, d, T, C.MASK_CAUSAL, micro_batch=1)
+    xs, gs = stage_io(st)
+    got = run(st, [(None, None)], xs, gs)
+    r = np.random.default_rng(4)
+    some = np.unique(np.concatenate([[0, 1, 63, 64, 127, 128, 129, 8191, 8192, T - 64, T - 2, T - 1], r.integers(0, T, 24)]))
+    dev = lambda a, n: torch.from_numpy(ops.split_heads(a, n)[0]).to(DEV)  # noqa: E731
+    x, dy, at = dev(xs[0], H + 2), dev(gs[0], H), torch.from_numpy(some).to(DEV)
+    k, v = x[H], x[H + 1]
+    seen = torch.ones((T, T), dtype=torch.bool, device=DEV).tril()
+    y, dq, dk, dv = [], [], torch.zeros((len(some), d), dtype=torch.float64, device=DEV), torch.zeros((len(some), d), dtype=torch.float64, device=DEV)
+    for h in range(H):
+        q, do = x[h], dy[h]
+        p = torch.softmax((q @ k.T / math.sqrt(d)).masked_fill_(~seen, -math.inf), -1)
+        o = p @ v
+        less = (do * o).sum(-1, keepdim=True)
+        y.append(o[at])
+        dq.append((p[at] * (do[at] @ v.T - less[at])) @ k / math.sqrt(d))
+        p = p[:, at].contiguous()
+        dk += (p * (do @ v[at].T - less)).T @ q / math.sqrt(d)
+        dv += p.T @ do
+    loose = 4 * (math.sqrt(d) + math.sqrt(T) + 8) * 2 * U
+    dx = ops.split_heads(got["dx0"], H + 2)[0][:, some]
+    for name, a, b, n in (("y", ops.split_heads(got["y0"], H)[0][:, some], torch.stack(y), 2), ("dq", dx[:H], torch.stack(dq), 5), ("dk", dx[H], dk, 5), ("dv", dx[H + 1], dv, 5)):
+        b = b.cpu().numpy()
+        size = np.linalg.norm(b, axis=-1)
+        if name == "dq":                                     # position 0 sees one key: nothing of its gradient is left
+            a, b, size = a[:, 1:], b[:, 1:], size[:, 1:]
+        off = np.linalg.norm(a - b, axis=-1) / size
+        assert np.all(off <= 2 * math.sqrt(n / 3) * HALF[C.BF16] + loose), (name, float(off.max()))
+
+
 # ------------------------------------------------------------------------------ profile and timing
 @BOTH
 def test_timing_and_profile_of_attention(dtype):
