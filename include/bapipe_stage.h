@@ -126,7 +126,7 @@ typedef enum { BAPIPE_MASK_NONE = 0, BAPIPE_MASK_CAUSAL = 1, BAPIPE_MASK_SPANS =
  *   t base^(-2 j / pad); see bapipe_stage_set_rotary.  has_bias = 1: each query and key head is first divided by its root mean
  *   square, sqrt(mean(x^2) + eps), and multiplied by gains, w [2][d]: of query heads, of key heads, one at create.
  *   has_bias = 0: eps must be 0, no parameters.  Value heads pass unchanged.
- * ATTENTION: cout = kh d.  Score of query i and key j: q_i k_j / sqrt(d); with eps > 0 capped to eps tanh(score / eps);
+ * ATTENTION: cout = kh d.  Score of query i and key j: q_i k_j / sqrt(d); with eps > 0 (2^-100 or more) capped to eps tanh(score / eps);
  *   with pad > 0 less 2^(-pad (h + 1) / kh) |i - j| in query head h (pad up to 64).  Softmax over the keys that stride
  *   lets the position see; one that sees none gets zeros and gives no gradients.  has_bias must be 0.  micro_batch times kh times the
  *   number of 128 positions (rounded up) must be below 2^24 (E_UNSUPPORTED).  What the

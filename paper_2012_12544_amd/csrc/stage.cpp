@@ -708,7 +708,7 @@ AttnShape attn_shape(const bapipe_stage *st, const Layer &L)
     a.heads = L.d.kh; a.groups = L.d.kw; a.d = A.C / (L.d.kh + 2 * L.d.kw);
     a.mask = L.d.stride;
     a.scale = 1.0f / sqrtf((float)a.d);
-    a.cap = L.d.eps;
+    a.cap = L.d.eps < 0x1p100f ? L.d.eps : 0.0f;             // c tanh(s / c) is s to 2^-26 for s up to 2^87, and c log2(e) may be infinite
     a.bias = L.d.pad;
     return a;
 }
@@ -1579,7 +1579,9 @@ int bapipe_stage_create(const bapipe_layer_desc_t *layers, int n_layers, int mic
                 if (d.stride < BAPIPE_MASK_NONE || d.stride > BAPIPE_MASK_SPANS) return create_fail(BAPIPE_E_INVALID, "layer %d: unknown mask %d", i, d.stride);
                 if (d.pad < 0 || d.pad > 64) return create_fail(BAPIPE_E_INVALID, "layer %d: range %d of the slopes, must be 0 to 64", i, d.pad);
                 if (d.has_bias) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: attention has no parameters", i);
-                if (!(d.eps >= 0.f) || d.eps > FLT_MAX) return create_fail(BAPIPE_E_INVALID, "layer %d: cap must be positive, or 0 for none", i);
+                // of smaller ones the reciprocal may be infinite
+                if (!(d.eps >= 0.f) || d.eps > FLT_MAX || (d.eps > 0.f && d.eps < 0x1p-100f))
+                    return create_fail(BAPIPE_E_INVALID, "layer %d: cap must be 2^-100 or more, or 0 for none", i);
                 if (!attention_launches(micro_batch, d.kh, A.H)) return create_fail(BAPIPE_E_UNSUPPORTED, "layer %d: attention of 2^24 blocks or more", i);
                 if (d.stride == BAPIPE_MASK_SPANS) {
                     if (st->span_T && st->span_T != A.H) return create_fail(BAPIPE_E_SHAPE, "layer %d: spans of %d positions, another layer's of %d", i, A.H, st->span_T);

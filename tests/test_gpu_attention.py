@@ -213,6 +213,32 @@ def test_attention_with_caps_and_slopes(dtype, cap, bias, scale, mask, d):
 
 
 @BOTH
+@pytest.mark.parametrize("bias", [0, 6])
+@pytest.mark.parametrize("rotary", [0, 1])
+def test_caps_that_no_score_comes_near(dtype, rotary, bias):
+    """c tanh(s / c) is s - s^3 / 3 c^2 ..: for c of 2^100 and more a float's s up to 2^87.  The same bits as without a cap, up to the largest float."""
+    def stage(cap):
+        b = C._Builder()
+        if rotary:
+            b.rotary(4, 2, 40, norm=1, src=-1)
+        b.attention(4, 2, 40, C.MASK_CAUSAL, cap, bias, src=0 if rotary else -1)
+        return _stage(b.layers, dtype, (320, 90, 1))
+
+    params = gen.all_params(stage(0.0), perturb=True)
+    xs, gs = stage_io(stage(0.0))
+    ref = run(stage(0.0), params, xs, gs)
+    for cap in (2.0 ** 100, 2.0 ** 127, float(np.finfo(np.float32).max)):
+        got = run(stage(cap), params, xs, gs)
+        assert all(np.array_equal(got[k], ref[k]) for k in ref), cap
+
+
+@BOTH
+@pytest.mark.parametrize("cap", [2.0 ** -100, 2.0 ** 99])
+def test_the_smallest_cap_and_a_large_one(dtype, cap):
+    _check_attention(_attention(dtype, 4, 2, 40, 90, C.MASK_CAUSAL, cap))
+
+
+@BOTH
 @pytest.mark.parametrize("heads,groups,d,T,mask,micro_batch", [
     (4, 1, 64, 1100, C.MASK_CAUSAL, 1),                      # one key head for all: the queries of a key's sums in parts
     (4, 2, 75, 700, C.MASK_NONE, 1),

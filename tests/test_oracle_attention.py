@@ -249,6 +249,14 @@ def test_what_create_refuses_of_an_attention():
     assert _status(two(4), shape=(32, 8, 1)) == B.E_SHAPE
 
 
+def test_what_create_takes_and_refuses_of_caps():
+    """Of one below 2^-100 the reciprocal, times the score's factors, may be infinite, and a score of 0 times that is none."""
+    for cap in (2.0 ** -100, 1.0, 2.0 ** 100, float(np.finfo(np.float32).max)):
+        assert _status(_layer("attention", 4, 2, 4, eps=cap), shape=(32, 4, 1)) == B.E_OOM, cap
+    for cap in (2.0 ** -101, 2.0 ** -126, 1e-40, 2.0 ** -149):
+        assert _status(_layer("attention", 4, 2, 4, eps=cap), shape=(32, 4, 1)) == B.E_INVALID, cap
+
+
 def test_what_create_refuses_of_many_blocks():
     """A launch holds less than 2^24 blocks of 256 threads; a block is 128 positions of a head, or what there are of them."""
     for heads, micro_batch, seq, want in ((256, 65535, 1, B.E_OOM), (256, 65536, 1, B.E_UNSUPPORTED), (256, 65536, 60, B.E_UNSUPPORTED), (4096, 4095, 1, B.E_OOM),
