@@ -241,7 +241,8 @@ template <int OFF> __device__ __forceinline__ void at_dma4(__amdgpu_buffer_rsrc_
 // AGAIN: a lane's place is worked out again for every tile (see at_again), else it is kept.
 template <class T, int DP, bool VEC, int R = 0, bool AGAIN = true> struct AtStream {
     typedef AtTile<T, DP, R> Tile;
-    static constexpr int TPB = AT_TPB, STEP = TPB / Tile::ROWS, ISSUES = Tile::ROWS * Tile::CH / TPB;      // chunks of a row that the block loads at once, and how often
+    // chunks of a row that the block loads at once, and how often
+    static constexpr int TPB = AT_TPB, STEP = TPB / Tile::ROWS, ISSUES = Tile::ROWS * Tile::CH / TPB;
     static_assert(Tile::ROWS * Tile::CH % TPB == 0, "");
     int row = 0, chunk = 0;
     unsigned voff = 0;
@@ -407,7 +408,8 @@ __device__ __forceinline__ AtBlock at_block(const AttnShape &s)
 // KS waves of a block share 32 rows, each for its part of every tile's 32-row pieces, and add up what they have in LDS at the end: where rows are
 // few that makes twice as many blocks, or keeps waves busy that have no rows of their own.  Tiles of 64 rows.  us for the forward pass, dq and dkv
 // with KS 1 and 2: 4 x 333 positions of 6 / 2 float heads of 45, 72 blocks of 128 rows: 40, 52, 67 and 28, 34, 43; 64 x 50 of 16 / 4 heads of 64:
-// 14.2, 15.2, 14.6 and 13.9, 14.9, 12.2; but 3 x 1003 of 12 heads of 80, 288 blocks for 256 units: 49, 55, 66 and 45, 58, 73.
+// 14.2, 15.2, 14.6 and 13.9, 14.9, 12.2; but 3 x 1003 of 12 heads of 80, 288 blocks for 256 units: 49, 55, 66 and 45, 58, 73.  (One rule for all
+// three: the forward pass by itself would share a little beyond it.)
 template <class T, int DP> constexpr bool kAtShares = AtTile<T, DP>::ROWS == 64;
 // per_unit: so many of the blocks, which are twice as many then, a unit holds at once; more than that take a second round.  dkv of wide heads,
 // one block a unit, a mini-batch of 1003 positions without a mask, us: 12 heads of 192 172 in 384 blocks of KS 2, 130 in 192 of KS 1, the
@@ -503,7 +505,8 @@ template <int ND> __device__ __forceinline__ void at_store_low(int8_t *row, int 
 }
 
 // The rows of a wave, through LDS, so that lanes next to each other write what is next to each other (a lane has four neighbouring elements of its
-// row at a time; forward, 4 x 4096 positions, causal, 32 / 8 heads of 128, two places for the output: 705 us from the registers, 645 so).  own: kAtOwn<DP> bytes of LDS that are this wave's alone; to: its first row, rows: how many there are; d a multiple of 8.
+// row at a time; forward, 4 x 4096 positions, causal, 32 / 8 heads of 128, two places for the output: 674 us from the registers, 645 so).
+// own: kAtOwn<DP> bytes of LDS that are this wave's alone; to: its first row, rows: how many there are; d a multiple of 8.
 template <int DP> constexpr int kAtOwn = 32 * (2 * DP + 16);
 template <int DP, int ND>
 __device__ __forceinline__ void at_store_rows(unsigned char *own, bf16_t *to, bf16_t *to2, size_t stride, int rows, int d, const f32x16_t (&acc)[ND], float by,

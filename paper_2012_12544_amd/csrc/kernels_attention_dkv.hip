@@ -1,8 +1,9 @@
 // Attention, backward, the gradients of keys and values: a block owns keys and streams the queries that see them, of every query head
 // that shares the key head.  No atomics: sums have one order.
 //   dv = p^T dout, dk = ds^T q / sqrt(d)
-// 4 x 4096 positions, causal, 32 / 8 heads of 128, bf16: 1190 us, 924 TFLOP/s of its four products, 59 % of the cycles.  Two waves a SIMD hold both sums, key and value of 32
-// rows in 256 registers each; 64 rows a wave, at one wave, halve the LDS reads and were slower (1842 and 1515 us).
+// 4 x 4096 positions, causal, 32 / 8 heads of 128, bf16: 1173 us, 938 TFLOP/s of its four products, 59 % of the cycles.  Two waves a SIMD hold
+// both sums, key and value of 32 rows in 256 registers each; 64 rows a wave, at one wave, halve the LDS reads and were slower (1842 us where this
+// form took 1515).
 #include "attention_common.h"
 
 namespace bapipe {
@@ -13,8 +14,8 @@ namespace {
 // 4485 whole, with 245 registers spilled, 3022 so.
 template <class T, int DP, bool HALF> constexpr int kDkvHalves = DP * (int)sizeof(T) > 768 || (HALF && DP > 192) ? 2 : 1;
 
-// Rows of a tile, 0: what fits.  16-bit floats of 128 channels, us: 66 registers are spilled with 64 rows, 286, and 36 with 32, 261; one wave a
-// SIMD, which spills none: 281.  (4 x 2048 positions, causal, 16 / 2 heads)
+// Rows of a tile, 0: what fits.  16-bit floats of 128 channels (4 x 2048 positions, causal, 16 / 2 heads), us: with 64 rows, 66 registers spilled,
+// 286, with 32 and 36 of them 261; one wave a SIMD, which spills none, 281.  Now, with 32, 29 are spilled: 246.
 template <int DP, bool EXTRA, bool HALF, int KS> constexpr int kDkvRows = KS == 1 && HALF && !EXTRA && DP == 128 ? 32 : 0;
 
 // Blocks that the launch bounds let a unit hold, and those that fit: float heads of up to 64 channels take 251 registers
@@ -297,8 +298,8 @@ template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Keys {
 // In how many parts the queries of the keys' sums are taken.  A block owns 128 keys of a key head, for all query heads that share it: few of
 // them leave units idle or, where keys are seen by different numbers of queries, waiting for the longest.  Splits cost a pass over their sums:
 // 12 heads of 80, 3 x 1003 positions without a mask, 288 blocks of the 512 that fit, us: 69 in one part, 59 and 14 in three.
-// What fits is by the kernel that runs.  With two blocks a unit for all of up to 128 channels, a column's halves not counted, 16 / 4 heads of 128 with
-// slopes over 2048 positions, causal, took 214 us a mini-batch, 184 so; 8 / 4 of 256 behind a ROTARY over 2 x 2048, causal, 482 and 454.
+// What fits is by the kernel that runs.  With two blocks a unit for all of up to 128 channels, a column's halves not counted, 16 / 4 heads of
+// 128 with slopes over 2048 positions, causal, took 214 us a mini-batch, 184 so; 8 / 4 of 256 behind a ROTARY over 2 x 2048, causal, 482 and 454.
 template <class T, int DP, bool VEC, bool EXTRA, bool HALF> struct Splits {
     static hipError_t go(const AttnArgs &a, int *out)
     {

@@ -1,6 +1,6 @@
 // Attention, backward, the queries' gradients: scores and probabilities again from the stored logarithm of each query's sum.
 //   p = 2^(score - lse), ds = p (dout v^T - dout . o), dq = ds k / sqrt(d)
-// 4 x 4096 positions, causal, 32 / 8 heads of 128, bf16: 880 us, 938 TFLOP/s of its three products, 58 % of the cycles.  One of them
+// 4 x 4096 positions, causal, 32 / 8 heads of 128, bf16: 872 us, 946 TFLOP/s of its three products, 57 % of the cycles.  One of them
 // is the forward pass's again: to keep it would be to write and read 2 bytes for each of 1.1e9 pairs.
 #include "attention_common.h"
 

@@ -1,16 +1,17 @@
 // Attention, forward: o = softmax(scores) v in one pass over the keys, with a running maximum and sum per query.
-// 4 x 4096 positions, causal, 32 / 8 heads of 128, bf16: 650 us, 845 TFLOP/s of the two products, of which 75 us are the second places for input
-// and output.  The card runs at 1.7 to 1.8 GHz there; matrix instructions take 51 % of the cycles, and 64 keys of a wave 32 of them (1024 cycles), 140 vector
-// instructions and 32 exponentials.  No one of these bounds it: without the exponentials it takes 5 % less, without LDS reads 6, without loads of tiles
-// 15, without all three 27.
+// 4 x 4096 positions, causal, 32 / 8 heads of 128, bf16: 645 us, 852 TFLOP/s of the two products, of which 75 us are the second places for input
+// and output.  The card runs at 1.7 to 1.8 GHz there; matrix instructions take 51 % of the cycles, and 64 keys of a wave 32 of them (1024
+// cycles), 140 vector instructions and 32 exponentials.  No one of these bounds it: in an earlier form that took 711 us, leaving out the
+// exponentials saved 5 %, LDS reads 6, loads of tiles and LDS reads 20, all three 27.
 #include "attention_common.h"
 
 namespace bapipe {
 namespace {
 
 // Rows of a tile.  With 32 keys at a time registers and LDS hold three blocks of heads of 128 channels a unit instead of two, and two of 192 and 256
-// instead of one.  us with 64 and 32: 4 x 4096 positions, causal, 32 / 8 heads of 128: 705, 674; packed documents 173, 178; 4 x 2048, causal, 16 / 2
-// heads of 16-bit floats: 112, 101; 16 / 8 heads of 256: 295, 217, but with capped scores, which leave no registers for two, 192, 198.
+// instead of one.  us with 64 and 32, while rows were still stored from the registers: 4 x 4096 positions, causal, 32 / 8 heads of 128: 705, 674;
+// packed documents 173, 178; 4 x 2048, causal, 16 / 2 heads of 16-bit floats: 112, 101; 16 / 8 heads of 256: 295, 217, but with capped scores,
+// which leave no registers for two, 192, 198.
 template <class T, int DP, bool EXTRA, int KS>
 constexpr int kFwdRows = KS == 1 && sizeof(T) == 2 && (DP == 128 || DP == 192 || (DP == 256 && !EXTRA)) ? 32 : 0;
 template <class T, int DP, bool EXTRA, int KS>

@@ -9,7 +9,8 @@
 //   stash     depth x slot ; a slot holds, for one in-flight micro-batch, exactly the tensors
 //             backward reads again: layer inputs of conv/linear/BN, ReLU gates, pool indices,
 //             BN and layer norm statistics, both projections of a gated layer (float), queries, keys, values, output
-//             and each query's sum of an attention, softmax output.  depth = min(M, N-i+1) (x2 for 1F1B-SO).
+//             and each query's sum of an attention, softmax output.  (Of a bf16 ROTARY without norms in front of an
+//             ATTENTION only the values are read again; its input is kept whole.)  depth = min(M, N-i+1) (x2 for 1F1B-SO).
 //   transient forward tensors nobody reads in backward (reused by every micro-batch)
 //   grads     one buffer per tensor that receives an activation gradient (reused), and the
 //             gradients of a gated layer's projections
@@ -122,9 +123,9 @@ struct Layer {
     // lies (the tensors share their storage) and value heads stay by themselves.
     float2 *table = nullptr;
     bool values_stay = false, dvalues_stay = false;
-    // bf16 ROTARY that only an ATTENTION of the same heads reads: its queries and keys go to the slot as 16-bit floats with a scale for each head and position
-    // (off_half, off_scale) and nowhere else, and their gradients come back as floats (off_float, among the gradients).  A score is a sum of
-    // products of two rounded factors: with scores of standard deviation 4, which a cap is for, bf16 factors make gradients 1.05e-2 wrong in
+    // bf16 ROTARY that only an ATTENTION of the same heads reads: its queries and keys go to the slot as 16-bit floats with a scale for each
+    // head and position (off_half, off_scale) and nowhere else, and their gradients come back as floats (off_float, among the gradients).  A score
+    // is a sum of products of two rounded factors: with scores of standard deviation 4, which a cap is for, bf16 factors make gradients 1.05e-2 wrong in
     // the 2-norm and 16-bit floats 2.3e-3; at 1, with norms, 4.6e-3 and 1.9e-3, of which the rounding of the result is 1.7e-3.
     bool half = false;
     size_t off_half = 0, off_scale = 0, off_float = 0;
